@@ -28,8 +28,9 @@
 extern "C" {
 #endif
 
-/* Element types of the row kernels' and epilogues' activation operands. */
-enum { FL_DT_BF16 = 0, FL_DT_F32 = 1 };
+/* Element types of the row kernels' and epilogues' activation operands (FL_DT_F16: the rotary
+ * and key / value cache calls only). */
+enum { FL_DT_BF16 = 0, FL_DT_F32 = 1, FL_DT_F16 = 2 };
 
 /* GEMM epilogues.  acc = sum_k A(m,k) B(n,k) in fp32 (tcgen05, TMEM accumulator). */
 enum {
@@ -243,6 +244,110 @@ int fl_k_pack_clients(int32_t K, void* const* clients_host, const int64_t* bytes
 
 /* out[n] += sum_t x[t, n] for bf16 x [T, N] (bias gradients), fp32 out. */
 int fl_k_colsum(int32_t T, int32_t N, const void* x, float* out, void* stream);
+
+/* ---------------------------------------------------------------- answering with a model
+ * A model answers token by token: the keys and values of the tokens before stay in a paged cache, and a
+ * block is given a chunk of new tokens (a whole prompt, a part of one, or the one token chosen last).
+ * For each block: the QKV projection (fl_k_gemm, FL_EPI_STORE), fl_k_kv_append, fl_k_kv_attention.
+ * The lengths and the page table are read on the device when the kernels run: no call copies or synchronises,
+ * and a captured graph may be replayed after they changed.
+ *
+ * Bits that the kernels set in *status (device int, required): what is wrong is left out as each call says,
+ * and nothing outside of the buffers is touched. */
+enum {
+  FL_KV_BAD_POSITION = 1, /* a position outside [0, max_pos) */
+  FL_KV_BAD_PAGE = 2,     /* a page table entry outside [0, n_pages), or a token with no place in its table row */
+  FL_KV_TIMEOUT = 8       /* a bounded wait inside the kernel gave up: outputs and workspace are not valid */
+};
+
+/* Pairs that a rotation by position p turns, i < rotary_dim / 2, and the table's entry of each. */
+enum {
+  FL_ROPE_HALF = 0,       /* dims (i, i + rotary_dim / 2) */
+  FL_ROPE_INTERLEAVED = 1 /* dims (2 i, 2 i + 1) */
+};
+
+/* Rotary table [max_pos][rotary_dim / 2] of (size cos(p f_i), size sin(p f_i)), computed in double.  With
+ * b_i = base^(-2 i / rotary_dim), d = rotary_dim and the factor by which the context is longer than the
+ * original_max_pos positions of the training:
+ *   NONE      f = b, size = 1 (the server's table)
+ *   LINEAR    f = b / factor                      (position interpolation, Chen et al. 2023)
+ *   NTK       b with base factor^(d / (d - 2))    (the base enlarged so that the slowest pair is interpolated)
+ *   BY_PARTS  f = (1 - g) b / factor + g b, g = clamp((original_max_pos b / (2 pi) - 1) / 31, 0, 1),
+ *             size = 0.1 ln(factor) + 1           (YaRN, Peng et al. 2023: alpha 1, beta 32)
+ * table: fp32, 16-byte aligned; rotary_dim even (NTK: > 2); factor >= 1 (ignored with NONE);
+ * original_max_pos >= 1 with BY_PARTS. */
+enum { FL_ROPE_SCALE_NONE = 0, FL_ROPE_SCALE_LINEAR = 1, FL_ROPE_SCALE_NTK = 2, FL_ROPE_SCALE_BY_PARTS = 3 };
+int fl_k_rotary_table(int32_t max_pos, int32_t rotary_dim, float base, int32_t scaling, float factor,
+                      int32_t original_max_pos, float* table, void* stream);
+
+/* y = x [T, n_heads, head_dim] with dims [0, rotary_dim) of every head turned by positions[t] and, when
+ * block_positions is not NULL, dims [rotary_dim, 2 rotary_dim) by block_positions[t] (the two streams of
+ * GLM); the other dims are copied.  Pair (a, b) with the table's (c, s): (a c - b s, a s + b c) in fp32,
+ * rounded once.  backward = 1 applies the transpose, (a c + b s, b c - a s): x is then the gradient of the
+ * turned rows, y that of the rows before.  dtype FL_DT_BF16, FL_DT_F16 or FL_DT_F32.  Row t, head h starts at
+ * x + t ldx + h x_head_stride elements; y may be x with the same strides, else they do not overlap.
+ * A position outside [0, max_pos) gives a row of zeros and sets FL_KV_BAD_POSITION.
+ * Requirements (UNSUPPORTED): head_dim a multiple of 16 up to 256, rotary_dim a multiple of 16, the turned dims
+ * within head_dim; strides multiples of 16 bytes; pointers 16-byte aligned (positions and status 4).
+ * T = 0 does nothing.  A table row is [rotary_dim / 2] pairs. */
+int fl_k_rotary(int32_t T, int32_t n_heads, int32_t head_dim, int32_t rotary_dim, int32_t layout, int32_t backward,
+                int32_t dtype, const void* x, int64_t ldx, int64_t x_head_stride, void* y, int64_t ldy,
+                int64_t y_head_stride, const int32_t* positions, const int32_t* block_positions,
+                const float* rope_tab, int32_t max_pos, int* status, void* stream);
+
+/* One block's cache.  Token slot i of page p holds key head h at
+ *   k + p page_stride + h head_stride + i token_stride  (elements; head_dim consecutive ones),
+ * the value likewise at v.  Head-major pages ([n_pages, kv_heads, page_size, head_dim]) read fastest.
+ * dtype FL_DT_BF16 or FL_DT_F16; head_dim 64 or 128; page_size a power of two, 16 to 256; strides multiples
+ * of 8 elements, page_stride a multiple of head_stride (UNSUPPORTED otherwise); k, v 16-byte aligned. */
+typedef struct {
+  int32_t dtype, kv_heads, head_dim, page_size, n_pages;
+  void *k, *v;
+  int64_t page_stride, head_stride, token_stride;
+} fl_kv_cache;
+
+/* The sequences of a call.  Sequence s brings new tokens cu_new[s] .. cu_new[s + 1) of the n_tokens packed rows
+ * (cu_new ascending from 0 to n_tokens); with them its cache holds lens[s] tokens, so its new token i is
+ * token lens[s] - n_s + i.  Token u lies in slot u % page_size of page page_table[s * table_stride +
+ * u / page_size].  cu_new [n_seqs + 1], lens [n_seqs], page_table [n_seqs, table_stride]: device int32.
+ * max_new: at least the largest n_s (it chooses the kernel; a larger n_s is still computed). */
+typedef struct {
+  int32_t n_seqs, n_tokens, max_new, table_stride;
+  const int32_t *cu_new, *lens, *page_table;
+} fl_kv_batch;
+
+/* Writes the new tokens' keys and values into the cache and turns queries and keys on the way, as
+ * fl_k_rotary (forward).  q [n_tokens, n_heads, head_dim], k and v [n_tokens, kv_heads, head_dim] of the cache's
+ * dtype: row t at q + t ldq and so on, heads at head_dim consecutive elements each (in a fused projection
+ * k = q + n_heads head_dim, ldq = ldk = ldv); q_out likewise with ldqo, and may be q (ldqo = ldq).  positions
+ * [n_tokens] (NULL: the token's index in its sequence) and block_positions as in fl_k_rotary;
+ * rotary_dim = 0: nothing is turned and rope_tab may be NULL (P-tuning prefixes, which are not rotated).
+ * q = NULL: only the cache is written.  Where a position is out of range the turned rows are zeros
+ * (FL_KV_BAD_POSITION); a token that has no slot (before the first token, past its table row, no page) is
+ * not written (FL_KV_BAD_PAGE).  n_heads a multiple of kv_heads; strides multiples of 8 elements, pointers
+ * 16-byte aligned (index arrays and status 4); rotary_dim as in fl_k_rotary. */
+int fl_k_kv_append(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n_heads, const void* q, int64_t ldq,
+                   const void* k, int64_t ldk, const void* v, int64_t ldv, void* q_out, int64_t ldqo,
+                   int32_t rotary_dim, int32_t layout, const int32_t* positions, const int32_t* block_positions,
+                   const float* rope_tab, int32_t max_pos, int* status, void* stream);
+
+/* Attention of the new tokens over their sequences' cached keys and values (their own included: append
+ * first).  Query head h reads key / value head h / (n_heads / kv_heads).  Token p of a sequence of L tokens sees
+ * tokens u < min(L, max(p + 1, c)), c = context_lens[s] (device int32, the GLM context; NULL: 0, causal).
+ * o [n_tokens, n_heads, head_dim] = sum_u softmax_u(scale q k_u) v_u, of the cache's dtype, row t at o + t ldo;
+ * lse (or NULL): fp32 [n_heads, n_tokens], the log-sum-exp of the scaled scores.  scale = 0: 1 / sqrt(head_dim).
+ * A token that sees nothing (lens[s] = 0, or p < 0) gives zeros and lse = -infinity.  What a page holds past a
+ * sequence's last token is not used, NaN included.  Tokens of a page that the table does not name
+ * (FL_KV_BAD_PAGE) count as zero keys and values.
+ * workspace: fl_k_kv_attention_workspace bytes, 16-byte aligned, ZERO before its first use (and after
+ * FL_KV_TIMEOUT); a call leaves what it needs of it at zero, so calls one after another on a stream may share
+ * it, of any shapes for which it is large enough; calls that may overlap need one each.  Results do not depend on
+ * the order in which CTAs run.  q: row t at q + t ldq.  n_heads / kv_heads at most 16; ldq, ldo multiples of 8
+ * elements; pointers 16-byte aligned (index arrays, lse and status 4). */
+size_t fl_k_kv_attention_workspace(int32_t n_heads, const fl_kv_cache* cache, const fl_kv_batch* batch);
+int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n_heads, const void* q, int64_t ldq,
+                      float scale, const int32_t* context_lens, void* o, int64_t ldo, float* lse, void* workspace,
+                      int* status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,37 @@
+// What the kernels of the attention over a paged cache share.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "kv_plan.cuh"
+
+constexpr int KV_COUNTERS = 1024;  // at the start of a workspace: parts done of a unit, by the CTA it starts in
+
+struct KvAttnArgs {
+  KvBatchDev b;
+  const void *q, *k, *v;
+  void* o;
+  int64_t ldq, ldo, page_stride, head_stride, token_stride;
+  int group, kvh;  // query heads per key / value head, key / value heads
+  float* lse;
+  float scale_log2;
+  unsigned* counters;
+  float* parts;
+  int* status;
+};
+
+template <class T>
+struct KvIo;
+template <>
+struct KvIo<__nv_bfloat16> {
+  FL_DEV static uint32_t pack(float lo, float hi) { return pack_bf16x2(lo, hi); }
+  FL_DEV static bool finite(uint32_t x) { return (x & 0x7f80u) != 0x7f80u && (x & 0x7f800000u) != 0x7f800000u; }  // both halves
+};
+template <>
+struct KvIo<__half> {
+  FL_DEV static uint32_t pack(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  FL_DEV static bool finite(uint32_t x) { return (x & 0x7c00u) != 0x7c00u && (x & 0x7c000000u) != 0x7c000000u; }
+};

@@ -1,0 +1,151 @@
+// How the attention over a paged cache (kv_attention.cu, kv_attention_tc.cu) divides a call among its
+// CTAs, computed by each CTA from the batch's device arrays: no list is built on the host, so a call needs
+// no copy, no synchronisation and can be captured in a graph while the lengths change.
+//
+// A unit is (sequence, key / value head, tile of its new tokens); its work is its key blocks.  The units lie
+// one after another on a line, each as long as its cost (its blocks' and a constant for its ends), and CTA i
+// of G takes [i W / G, (i + 1) W / G) of the line's W: equal work whatever the lengths are.  A unit that lies
+// in several CTAs' ranges is computed in parts, which the CTA that finishes last joins in their order, so
+// the result does not depend on which CTA that is.
+#pragma once
+#include "../../include/flglm_kernels.h"
+#include "common.cuh"
+
+struct KvBatchDev {
+  const int32_t *cu, *lens, *table, *ctx;
+  int S, T, table_stride, ps_log2, n_pages;
+};
+
+struct KvSeq {
+  int q0, n, L, ctx;  // first row of the new tokens, their number, tokens in the cache, context length
+};
+// The arrays' values are brought into their ranges, so that no index leaves a buffer.
+FL_DEV KvSeq kv_seq(const KvBatchDev& b, int s) {
+  KvSeq q;
+  const int a = min(max(b.cu[s], 0), b.T), e = min(max(b.cu[s + 1], 0), b.T);
+  const int64_t cap = (int64_t)b.table_stride << b.ps_log2;
+  q.q0 = a;
+  q.n = max(e - a, 0);
+  q.L = (int)min((int64_t)max(b.lens[s], 0), cap);
+  q.ctx = b.ctx ? b.ctx[s] : 0;
+  return q;
+}
+// Number of keys that new token i sees (they are the first ones): its own and those before it, the
+// context's if it is shorter; none if the token lies before the cache's first one.
+FL_DEV int kv_sees(const KvSeq& q, int i) { return max(0, min(q.L, max(q.L - q.n + i + 1, q.ctx))); }
+
+// The page of block-table entry i of sequence s, or -1 (recorded) where the table holds no page of the cache.
+FL_DEV int kv_page(const KvBatchDev& b, int s, int i, int* status) {
+  const int p = __ldg(b.table + (int64_t)s * b.table_stride + i);
+  if ((unsigned)p < (unsigned)b.n_pages) return p;
+  atomicOr(status, FL_KV_BAD_PAGE);
+  return -1;
+}
+
+// Units of a sequence: U::units(q) tiles, U::cost(q, r) of tile r, for each of the kv heads.
+template <class U>
+struct KvWalk {
+  int s, h, r;         // the current unit
+  KvSeq q;
+  int64_t start;       // its place on the line
+  int units, cost;
+
+  FL_DEV void set(const KvBatchDev& b, const U& u, int s_, int64_t seq_start, int64_t at, int kvh) {
+    s = s_;
+    q = kv_seq(b, s);
+    units = u.units(q);
+    int64_t head = 0;
+    for (int i = 0; i < units; ++i) head += u.cost(q, i);
+    h = (int)((at - seq_start) / head);
+    start = seq_start + h * head;
+    r = 0;
+    cost = u.cost(q, 0);
+    while (r + 1 < units && start + cost <= at) {
+      start += cost;
+      cost = u.cost(q, ++r);
+    }
+  }
+  FL_DEV bool next(const KvBatchDev& b, const U& u, int kvh) {  // false behind the last unit
+    start += cost;
+    if (++r == units) {
+      r = 0;
+      if (++h == kvh) {
+        h = 0;
+        do {
+          if (++s >= b.S) return false;
+          q = kv_seq(b, s);
+        } while (q.n == 0);
+        units = u.units(q);
+      }
+    }
+    cost = u.cost(q, r);
+    return true;
+  }
+};
+
+struct KvRange {
+  int64_t lo, hi, W;
+  int G;               // CTAs with work
+  int s;               // sequence that holds lo, and where it starts
+  int64_t seq_start;
+  FL_DEV int cta_of(int64_t x) const { return (int)(((x + 1) * G - 1) / W); }  // whose range holds x
+  FL_DEV int64_t lo_of(int i) const { return i * W / G; }
+};
+
+// The calling CTA's range; every thread of the CTA takes part.  At most `ctas` CTAs get work, and each
+// that does at least about min_cost.  sh: THREADS / 32 + 3 int64 of shared memory, free after the CTA's next barrier.
+template <int THREADS, class U>
+FL_DEV KvRange kv_plan(const KvBatchDev& b, const U& u, int kvh, int cta, int ctas, int min_cost, int64_t* sh) {
+  constexpr int WARPS = THREADS / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (b.S + THREADS - 1) / THREADS;
+  const int s0 = tid * per, s1 = min(b.S, s0 + per);
+  auto seq_cost = [&](int s) {
+    const KvSeq q = kv_seq(b, s);
+    int64_t c = 0;
+    if (q.n > 0)
+      for (int r = 0, n = u.units(q); r < n; ++r) c += u.cost(q, r);
+    return c * kvh;
+  };
+  int64_t mine = 0, one = 0;
+  for (int s = s0; s < s1; ++s) mine += one = seq_cost(s);
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) sh[warp] = incl;
+  if (tid == 0) sh[WARPS] = -1;
+  __syncthreads();
+  int64_t before = 0, W = 0;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) {
+    if (w < warp) before += sh[w];
+    W += sh[w];
+  }
+  KvRange g;
+  g.W = W;
+  g.G = (int)max((int64_t)1, min((int64_t)ctas, W / min_cost));
+  g.lo = g.hi = 0;
+  g.s = -1;
+  g.seq_start = 0;
+  if (W == 0 || cta >= g.G) return g;  // the whole CTA
+  g.lo = g.lo_of(cta);
+  g.hi = g.lo_of(cta + 1);
+  int64_t at = before + incl - mine;
+  if (g.lo >= at && g.lo < at + mine) {
+    int s = s0;
+    if (per > 1)
+      for (one = seq_cost(s); g.lo >= at + one; one = seq_cost(++s)) at += one;
+    sh[WARPS] = s;
+    sh[WARPS + 1] = at;
+  }
+  __syncthreads();
+  g.s = (int)sh[WARPS];
+  g.seq_start = sh[WARPS + 1];
+  return g;
+}
+
+// Checks of a cache and a batch that the calls share (kv_cache.cu); fills *out but for ctx.
+int fl_kv_check(const char* who, const fl_kv_cache* c, const fl_kv_batch* b, int n_heads, KvBatchDev* out);

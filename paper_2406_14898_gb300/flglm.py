@@ -29,7 +29,10 @@ FL_T_COUNT = 14
 FL_TILE_AUTO, FL_TILE_128x128, FL_TILE_128x256, FL_TILE_256x256_PAIR = range(4)
 FL_GEMM_MAX_BATCH = 4
 PROF_CLASSES = ("gemm", "attention", "layernorm", "adamw", "other")
-FL_DT_BF16, FL_DT_F32 = 0, 1
+FL_DT_BF16, FL_DT_F32, FL_DT_F16 = 0, 1, 2
+FL_KV_BAD_POSITION, FL_KV_BAD_PAGE, FL_KV_TIMEOUT = 1, 2, 8
+FL_ROPE_HALF, FL_ROPE_INTERLEAVED = 0, 1
+FL_ROPE_SCALE_NONE, FL_ROPE_SCALE_LINEAR, FL_ROPE_SCALE_NTK, FL_ROPE_SCALE_BY_PARTS = range(4)
 
 
 class FlError(RuntimeError):
@@ -74,6 +77,17 @@ class fl_gemm_args(C.Structure):
                 ("d_bstride", C.c_int64), ("aux_bstride", C.c_int64), ("aux_out_bstride", C.c_int64),
                 ("bias_bstride", C.c_int64), ("row_bstride", C.c_int64), ("lnp_bstride", C.c_int64),
                 ("adam_bstride", C.c_int64)]
+
+
+class fl_kv_cache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+                ("n_pages", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class fl_kv_batch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32), ("table_stride", C.c_int32),
+                ("cu_new", C.c_void_p), ("lens", C.c_void_p), ("page_table", C.c_void_p)]
 
 
 _P = C.c_void_p
@@ -122,6 +136,14 @@ _SIGS = {
     "fl_k_embedding_gather": (C.c_int, [_I32, _I32, _P, _P, _I32, _P, _P, _P]),
     "fl_k_embedding_scatter_add": (C.c_int, [_I32, _I32, _P, _I32, _P, _P, _P]),
     "fl_k_cross_entropy": (C.c_int, [_I32, _I32, _I64, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "fl_k_rotary_table": (C.c_int, [_I32, _I32, _F, _I32, _F, _I32, _P, _P]),
+    "fl_k_rotary": (C.c_int, [_I32, _I32, _I32, _I32, _I32, _I32, _I32, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P,
+                              _I32, _P, _P]),
+    "fl_k_kv_append": (C.c_int, [C.POINTER(fl_kv_cache), C.POINTER(fl_kv_batch), _I32, _P, _I64, _P, _I64, _P, _I64,
+                                 _P, _I64, _I32, _I32, _P, _P, _P, _I32, _P, _P]),
+    "fl_k_kv_attention_workspace": (C.c_size_t, [_I32, C.POINTER(fl_kv_cache), C.POINTER(fl_kv_batch)]),
+    "fl_k_kv_attention": (C.c_int, [C.POINTER(fl_kv_cache), C.POINTER(fl_kv_batch), _I32, _P, _I64, _F, _P, _P, _I64,
+                                    _P, _P, _P, _P]),
     "fl_client_cfg_default": (None, [C.POINTER(fl_client_cfg)]),
     "fl_client_create": (C.c_int, [C.POINTER(fl_client_cfg), C.c_uint64, C.POINTER(_P)]),
     "fl_client_destroy": (C.c_int, [_P]),
@@ -543,3 +565,63 @@ def fl_k_pack_clients(clients: Sequence, nbytes: Sequence[int], packed, scatter:
     K = len(clients)
     b = (C.c_int64 * K)(*nbytes)
     check(lib().fl_k_pack_clients(K, _parr(clients), b, ptr(packed), 1 if scatter else 0, stream_ptr(stream)))
+
+
+def fl_k_rotary_table(max_pos, rotary_dim, base, table, scaling=FL_ROPE_SCALE_NONE, factor=1.0, original_max_pos=0,
+                      stream=None):
+    check(lib().fl_k_rotary_table(max_pos, rotary_dim, base, scaling, factor, original_max_pos, ptr(table),
+                                  stream_ptr(stream)))
+
+
+def fl_k_rotary(T, n_heads, head_dim, rotary_dim, x, y, rope_tab, max_pos, positions, status, block_positions=None,
+                dtype=FL_DT_BF16, layout=FL_ROPE_HALF, backward=False, ldx=None, x_head_stride=None, ldy=None,
+                y_head_stride=None, stream=None):
+    """Strides default to contiguous [T, n_heads, head_dim] rows."""
+    row = n_heads * head_dim
+    check(lib().fl_k_rotary(T, n_heads, head_dim, rotary_dim, layout, 1 if backward else 0, dtype, ptr(x),
+                            row if ldx is None else ldx, head_dim if x_head_stride is None else x_head_stride, ptr(y),
+                            row if ldy is None else ldy, head_dim if y_head_stride is None else y_head_stride,
+                            ptr(positions), ptr(block_positions), ptr(rope_tab), max_pos, ptr(status),
+                            stream_ptr(stream)))
+
+
+def kv_cache(k, v, n_pages, page_size, kv_heads, head_dim, dtype=FL_DT_BF16, page_stride=None, head_stride=None,
+             token_stride=None) -> fl_kv_cache:
+    """fl_kv_cache over the device tensors k and v, which the caller keeps alive.  Strides (in elements)
+    default to contiguous [n_pages, kv_heads, page_size, head_dim]."""
+    return fl_kv_cache(dtype, kv_heads, head_dim, page_size, n_pages, ptr(k), ptr(v),
+                       kv_heads * page_size * head_dim if page_stride is None else page_stride,
+                       page_size * head_dim if head_stride is None else head_stride,
+                       head_dim if token_stride is None else token_stride)
+
+
+def kv_batch(n_seqs, n_tokens, max_new, cu_new, lens, page_table, table_stride) -> fl_kv_batch:
+    """fl_kv_batch over the device int32 arrays, which the caller keeps alive."""
+    return fl_kv_batch(n_seqs, n_tokens, max_new, table_stride, ptr(cu_new), ptr(lens), ptr(page_table))
+
+
+def fl_k_kv_append(cache: fl_kv_cache, batch: fl_kv_batch, n_heads, q, k, v, q_out, rope_tab, max_pos, status,
+                   rotary_dim=0, layout=FL_ROPE_HALF, positions=None, block_positions=None, ldq=None, ldk=None,
+                   ldv=None, ldqo=None, stream=None):
+    """Row strides default to contiguous [n_tokens, heads, head_dim]; q = None writes the cache only."""
+    qrow, krow = n_heads * cache.head_dim, cache.kv_heads * cache.head_dim
+    check(lib().fl_k_kv_append(cache, batch, n_heads, ptr(q), qrow if ldq is None else ldq, ptr(k),
+                               krow if ldk is None else ldk, ptr(v), krow if ldv is None else ldv, ptr(q_out),
+                               qrow if ldqo is None else ldqo, rotary_dim, layout, ptr(positions),
+                               ptr(block_positions), ptr(rope_tab), max_pos, ptr(status), stream_ptr(stream)))
+
+
+def fl_k_kv_attention_workspace(n_heads, cache: fl_kv_cache, batch: fl_kv_batch) -> int:
+    n = int(lib().fl_k_kv_attention_workspace(n_heads, cache, batch))
+    if n == 0:
+        raise FlError(-1, (lib().fl_server_last_error(None) or b"").decode())
+    return n
+
+
+def fl_k_kv_attention(cache: fl_kv_cache, batch: fl_kv_batch, n_heads, q, o, workspace, status, lse=None, scale=0.0,
+                      context_lens=None, ldq=None, ldo=None, stream=None):
+    """Row strides default to contiguous [n_tokens, n_heads, head_dim]."""
+    row = n_heads * cache.head_dim
+    check(lib().fl_k_kv_attention(cache, batch, n_heads, ptr(q), row if ldq is None else ldq, scale,
+                                  ptr(context_lens), ptr(o), row if ldo is None else ldo, ptr(lse), ptr(workspace),
+                                  ptr(status), stream_ptr(stream)))

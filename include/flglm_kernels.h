@@ -342,7 +342,7 @@ int fl_k_kv_append(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n
  * workspace: fl_k_kv_attention_workspace bytes, 16-byte aligned, ZERO before its first use (and after
  * FL_KV_TIMEOUT); a call leaves what it needs of it at zero, so calls one after another on a stream may share
  * it, of any shapes for which it is large enough; calls that may overlap need one each.  Results do not depend on
- * the order in which CTAs run.  q: row t at q + t ldq.  n_heads / kv_heads at most 16; ldq, ldo multiples of 8
+ * the order in which CTAs run.  q: row t at q + t ldq.  n_heads / kv_heads at most 128; ldq, ldo multiples of 8
  * elements; pointers 16-byte aligned (index arrays, lse and status 4). */
 size_t fl_k_kv_attention_workspace(int32_t n_heads, const fl_kv_cache* cache, const fl_kv_batch* batch);
 int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n_heads, const void* q, int64_t ldq,

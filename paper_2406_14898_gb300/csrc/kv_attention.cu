@@ -385,6 +385,10 @@ __global__ void __launch_bounds__(THREADS) kv_attn_rows_kernel(KvAttnArgs a, int
 // CTAs of the kernel that the device holds at once, kept per process: one kind of device is supported.
 constexpr int CTAS_PER_SM = 3;
 
+// Rows of a sequence and key head that the warp-level fragments hold in one tile.  More go to the tensor-core tiles
+// of 128.
+bool few_rows(int group, int max_new) { return (int64_t)group * max_new <= 16; }
+
 template <class T, int HD, int NR>
 int launch_rows(const KvAttnArgs& a, cudaStream_t st) {
   const int tt = 8 * NR / a.group;
@@ -402,8 +406,15 @@ int dispatch_rows(int hd, int nr, const KvAttnArgs& a, cudaStream_t st) {
 extern "C" size_t fl_k_kv_attention_workspace(int32_t n_heads, const fl_kv_cache* cache, const fl_kv_batch* batch) {
   KvBatchDev bt;
   if (fl_kv_check("kv attention", cache, batch, n_heads, &bt)) return 0;
-  const size_t ctas = (size_t)CTAS_PER_SM * fl_sm_count();
-  return KV_COUNTERS * sizeof(unsigned) + ctas * 2 * 16 * (cache->head_dim + 2) * sizeof(float);
+  const int group = n_heads / cache->kv_heads;
+  if (group > 128) {
+    fl_internal_error(FL_ERR_UNSUPPORTED, "kv attention: %d query heads per key head", group);
+    return 0;
+  }
+  const size_t parts = few_rows(group, batch->max_new)
+                           ? (size_t)CTAS_PER_SM * fl_sm_count() * 2 * 16 * (cache->head_dim + 2) * sizeof(float)
+                           : fl_kv_attention_tc_parts(cache->head_dim);
+  return KV_COUNTERS * sizeof(unsigned) + parts;
 }
 
 extern "C" int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n_heads, const void* q,
@@ -416,7 +427,7 @@ extern "C" int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* ba
     return fl_internal_error(FL_ERR_INVALID_ARG, "kv attention: args");
   if (ldq % 8 || ldo % 8) return fl_internal_error(FL_ERR_UNSUPPORTED, "kv attention: ldq and ldo must be multiples of 8");
   a.group = n_heads / cache->kv_heads;
-  if (a.group > 16) return fl_internal_error(FL_ERR_UNSUPPORTED, "kv attention: %d query heads per key head", a.group);
+  if (a.group > 128) return fl_internal_error(FL_ERR_UNSUPPORTED, "kv attention: %d query heads per key head", a.group);
   if (batch->n_tokens == 0) return FL_OK;
   a.b.ctx = context_lens;
   a.q = q;
@@ -434,6 +445,7 @@ extern "C" int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* ba
   a.counters = (unsigned*)workspace;
   a.parts = (float*)((unsigned*)workspace + KV_COUNTERS);
   a.status = status;
+  if (!few_rows(a.group, batch->max_new)) return fl_launch_kv_attention_tc(cache, a, n_heads, (cudaStream_t)stream);
   const int rows = batch->max_new * a.group;
   return (cache->dtype == FL_DT_F16 ? dispatch_rows<__half> : dispatch_rows<__nv_bfloat16>)(
       cache->head_dim, rows <= 8 && a.group <= 8 ? 1 : 2, a, (cudaStream_t)stream);

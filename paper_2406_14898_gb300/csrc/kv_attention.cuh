@@ -24,14 +24,22 @@ template <class T>
 struct KvIo;
 template <>
 struct KvIo<__nv_bfloat16> {
+  static constexpr bool is_half = false;
+  FL_DEV static float2 unpack(uint32_t x) { return unpack_bf16x2(x); }
   FL_DEV static uint32_t pack(float lo, float hi) { return pack_bf16x2(lo, hi); }
   FL_DEV static bool finite(uint32_t x) { return (x & 0x7f80u) != 0x7f80u && (x & 0x7f800000u) != 0x7f800000u; }  // both halves
 };
 template <>
 struct KvIo<__half> {
+  static constexpr bool is_half = true;
+  FL_DEV static float2 unpack(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
   FL_DEV static uint32_t pack(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
   }
   FL_DEV static bool finite(uint32_t x) { return (x & 0x7c00u) != 0x7c00u && (x & 0x7c000000u) != 0x7c000000u; }
 };
+
+// Chunks of new tokens (kv_attention_tc.cu); parts: bytes of a workspace's parts that it uses.
+size_t fl_kv_attention_tc_parts(int head_dim);
+int fl_launch_kv_attention_tc(const fl_kv_cache* c, const KvAttnArgs& a, int heads, cudaStream_t st);

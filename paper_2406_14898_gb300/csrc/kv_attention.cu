@@ -28,7 +28,7 @@ namespace {
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int STEP = 16;              // keys a warp takes at a time (one page holds them)
 constexpr int BK = WARPS * STEP;      // keys of a block
-constexpr int MIN_COST = 8;           // blocks that are worth a CTA of their own
+constexpr int MIN_COST = 2;           // blocks that are worth a CTA of their own
 constexpr float LOG2E_F = 1.4426950408889634f, LN2_F = 0.6931471805599453f;
 
 template <class T>

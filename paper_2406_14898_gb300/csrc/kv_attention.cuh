@@ -25,6 +25,11 @@ struct KvIo;
 template <>
 struct KvIo<__nv_bfloat16> {
   static constexpr bool is_half = false;
+  // larger magnitudes of two pairs; NaN stays
+  FL_DEV static uint32_t max_abs(uint32_t a, uint32_t x) {
+    const __nv_bfloat162 y = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&x)));
+    return *reinterpret_cast<const uint32_t*>(&y);
+  }
   FL_DEV static float2 unpack(uint32_t x) { return unpack_bf16x2(x); }
   FL_DEV static uint32_t pack(float lo, float hi) { return pack_bf16x2(lo, hi); }
   FL_DEV static bool finite(uint32_t x) { return (x & 0x7f80u) != 0x7f80u && (x & 0x7f800000u) != 0x7f800000u; }  // both halves
@@ -32,6 +37,10 @@ struct KvIo<__nv_bfloat16> {
 template <>
 struct KvIo<__half> {
   static constexpr bool is_half = true;
+  FL_DEV static uint32_t max_abs(uint32_t a, uint32_t x) {
+    const __half2 y = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), __habs2(*reinterpret_cast<const __half2*>(&x)));
+    return *reinterpret_cast<const uint32_t*>(&y);
+  }
   FL_DEV static float2 unpack(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
   FL_DEV static uint32_t pack(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);

@@ -4,12 +4,13 @@
 // 128.  One CTA per SM runs two streams, each a tile's softmax over key blocks:
 //   two tiles of a unit over the same blocks (each key block is read once for 256 rows), or
 //   where a unit has one tile, that tile over the even and over the odd blocks, joined at the end.
-// While one stream's scores are turned into weights the tensor cores work for the other.
 //
 //   warps 0-3, 4-7  softmax of stream 0 and 1: thread i owns row i (TMEM lane i): reads its 128 scores, takes
 //                   p = 2^(s - m), writes p (16 bits) to TMEM; at the end O / l, or a part of it
-//   warp 8          TMA: Q tiles, then K and V blocks page by page into a ring of stages
-//   warp 9          S = Q K^T (both in shared memory) and O += P V (P in TMEM, V as an MN-major operand)
+//   warp 8          which units the CTA takes, told to the others a few ahead; TMA: K and V blocks page by page into a
+//                   ring of stages, Q tiles
+//   warps 9, 10     a stream each: S = Q K^T (both in shared memory), O += P V (P in TMEM, V as an MN-major operand)
+//   warp 11         makes V blocks fit for weights of zero (see there) before anyone uses them
 //
 // TMEM: S of the streams at columns 0 and 128, O at 256.  P lies over its S at head_dim 128 (512 columns are
 // taken), so the next S of a stream waits for its P V; at head_dim 64 it has columns of its own.
@@ -18,11 +19,10 @@
 // m follows a row's maximum only when that grew by more than 2^8, so O is seldom rescaled.
 // Work is divided among the CTAs as kv_plan.cuh says.
 //
-// Every wait is bounded.  A warp whose wait ran out records it, issues nothing any more and goes through the rest of
-// its steps without waiting, so that every barrier of the CTA is still reached by all.
+// Every wait is bounded.  A warp whose wait ran out records it and, in a role that issues, leaves; a softmax warp goes
+// through the rest of its unit without waiting, and its warpgroup then leaves together.
 #include <cuda.h>
 
-#include <atomic>
 #include <cmath>
 
 #include "../../include/flglm_kernels.h"
@@ -34,12 +34,8 @@
 namespace {
 
 constexpr int TB = 128;
-constexpr int THREADS = 384, W_TMA = 8, W_MMA = 9;  // warps 10 and 11 complete the third warpgroup
-// Registers a thread: at launch, and as the warpgroups then share them (the sum may not exceed the launch's:
-// a request above it would wait forever; checked before the first launch)
-constexpr int REGS_LAUNCH = 168, REGS_SOFTMAX = 208, REGS_REST = 80;
-static_assert(2 * REGS_SOFTMAX + REGS_REST <= 3 * REGS_LAUNCH, "register split");
-constexpr int ENDS = 2;      // cost of a unit's ends (Q, the first scores, the output), in blocks of one tile
+constexpr int THREADS = 384, W_TMA = 8, W_MMA = 9, W_FIX = 11;
+constexpr int ENDS = 5;      // cost of a unit's ends (Q, the first scores, the output), in blocks of one tile
 constexpr int MIN_COST = 4;
 constexpr float LN2_F = 0.6931471805599453f;
 
@@ -47,11 +43,13 @@ template <int HD>
 struct Cfg {
   static constexpr int NB = HD / 64;
   static constexpr int TILE = TB * HD * 2;
-  static constexpr int ST = HD == 128 ? 5 : 8;  // stages: what 227 KB hold beside two Q tiles; 8 at head_dim 64
+  static constexpr int ST = HD == 128 ? 4 : 8;  // stages
+  static constexpr int OUT = 8 * 32 * 128;      // 32 rows x 64 columns of output a softmax warp
   static constexpr int CTRL = 2048;
-  static constexpr int SMEM = (2 + ST) * TILE + CTRL + 1024;
+  static constexpr int SMEM = (2 + ST) * TILE + OUT + CTRL + 1024;
   static constexpr bool OWN_P = HD == 64;
 };
+static_assert(Cfg<128>::SMEM <= 227 * 1024 && Cfg<64>::SMEM <= 227 * 1024, "shared memory");
 
 struct TcMaps {
   CUtensorMap q, k, v;
@@ -77,6 +75,9 @@ FL_DEV void tma_load_3d(void* dst, const CUtensorMap* m, uint64_t* bar, int x, i
       "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
+// A value that is the same in the whole warp, as one that the compiler knows to be: the tensor instructions take
+// their operands from uniform registers, and moving them there one by one costs more than the product.
+FL_DEV uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 FL_DEV void bar_sync(int id, int threads) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 FL_DEV bool bar_or(int id, int threads, bool x) {
   uint32_t y;
@@ -89,6 +90,26 @@ FL_DEV bool bar_or(int id, int threads, bool x) {
       : "r"((uint32_t)x), "r"(id), "r"(threads)
       : "memory");
   return y != 0;
+}
+
+// Two fp32 operations an instruction.
+FL_DEV float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+FL_DEV float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
 }
 
 template <class T>
@@ -106,28 +127,44 @@ struct TileUnits {
   }
 };
 
-// What a CTA does of a unit: key blocks [kb0, kb0 + n), of which stream a takes part in na[a].
+// What a CTA does of a unit: key blocks [kb0, kb0 + n), of which stream s takes part in na[s].
 struct Piece {
-  bool two, first;   // first: the unit begins in this CTA's range
-  int tok0, kb0, n, nb[2], na[2], kmax, w;
+  int n, two, end, zero;        // end: no unit any more; zero: the streams (bits) whose rows see nothing at all
+  int q0, h, toks[2];           // first row of Q, key / value head, tokens of each tile
+  int kb0, kmax, nb[2], na[2];  // kmax: keys that some row sees; nb: blocks of the unit's tiles
+  int vis, ctx, L;              // token i of the unit sees the first max(0, min(L, max(vis + i, ctx))) keys
+  int f_lo, f_hi[2];            // CTAs that have parts of it
+  FL_DEV int sees(int i) const { return max(0, min(L, max(vis + i, ctx))); }
 };
+constexpr int PIECES = 4;  // told ahead
 FL_DEV Piece piece_of(const TileUnits& u, const KvWalk<TileUnits>& k, const KvRange& g) {
   Piece p;
+  const int tok0 = k.r * 2 * u.tpt, left = k.q.n - tok0;
+  p.end = 0;
   p.two = u.two(k.q, k.r);
-  p.w = p.two ? 2 : 1;
-  p.tok0 = k.r * 2 * u.tpt;
-  p.kmax = kv_sees(k.q, min(k.q.n, p.tok0 + 2 * u.tpt) - 1);
+  p.q0 = k.q.q0 + tok0;
+  p.h = k.h;
+  p.toks[0] = min(u.tpt, left);
+  p.toks[1] = p.two ? min(u.tpt, left - u.tpt) : p.toks[0];
+  p.vis = k.q.L - k.q.n + tok0 + 1;
+  p.ctx = k.q.ctx;
+  p.L = k.q.L;
+  p.kmax = kv_sees(k.q, min(k.q.n, tok0 + 2 * u.tpt) - 1);
   p.nb[1] = (p.kmax + TB - 1) / TB;
-  p.nb[0] = p.two ? u.blocks(k.q, p.tok0 + u.tpt) : p.nb[1];
-  p.first = k.start >= g.lo && k.start < g.hi;
-  p.kb0 = (int)max((int64_t)0, (g.lo - k.start + p.w - 1) / p.w);
-  const int kb1 = (int)min((int64_t)p.nb[1], (g.hi - k.start + p.w - 1) / p.w);
+  p.nb[0] = p.two ? u.blocks(k.q, tok0 + u.tpt) : p.nb[1];
+  const int sh = p.two;  // a block of two tiles costs two
+  p.kb0 = (int)max((int64_t)0, (g.lo - k.start + sh) >> sh);
+  const int kb1 = (int)min((int64_t)p.nb[1], (g.hi - k.start + sh) >> sh);
   p.n = max(0, kb1 - p.kb0);
-  p.na[1] = p.n;
-  p.na[0] = p.two ? min(p.n, max(0, p.nb[0] - p.kb0)) : p.n;
-  if (!p.two) {
-    p.na[0] = (p.n + 1) / 2;
-    p.na[1] = p.n / 2;
+  p.na[0] = p.two ? min(p.n, max(0, p.nb[0] - p.kb0)) : (p.n + 1) / 2;
+  p.na[1] = p.two ? p.n : p.n / 2;
+  const bool first = k.start >= g.lo && k.start < g.hi;
+  p.zero = first ? (p.nb[0] == 0 ? 1 : 0) | (p.two && p.nb[1] == 0 ? 2 : 0) : 0;
+  p.f_lo = p.f_hi[0] = p.f_hi[1] = 0;
+  if (p.n > 0 && p.n < p.nb[1]) {
+    p.f_lo = g.cta_of(k.start);
+    for (int s = 0; s < 2; ++s)
+      if (p.nb[s] > 0) p.f_hi[s] = g.cta_of(k.start + ((int64_t)(p.nb[s] - 1) << sh));
   }
   return p;
 }
@@ -138,6 +175,9 @@ struct RingOrder {
   FL_DEV int v(int t) const { return min(n, la) + t + min(t, max(n - la, 0)); }
   FL_DEV int k(int t) const { return t < la ? t : v(t - la) + 1; }
 };
+
+// The rest of a wait whose first try ran out; one copy, the many places that wait keep short.
+__device__ __noinline__ bool wait_longer(uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity); }
 
 // O += P V of one block without the tensor cores, for blocks whose values include infinities or NaN at keys that some
 // row does not see: the row takes the keys that it sees.  P and O in TMEM, the block in shared memory.
@@ -198,19 +238,39 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;
   uint8_t* sKV = smem + 2 * TILE;
-  uint8_t* ctrl = sKV + ST * TILE;
+  uint8_t* sOut = sKV + ST * TILE;
+  uint8_t* ctrl = sOut + C::OUT;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ctrl);
-  enum { B_FULL = 0, B_EMPTY = ST, B_QF = 2 * ST, B_QE, B_S, B_P = B_S + 2, B_O = B_P + 2, B_FREE = B_O + 2, B_END = B_FREE + 2, BARS };
-  static_assert(BARS * 8 <= 256, "control block");
-  int64_t* sh_plan = reinterpret_cast<int64_t*>(ctrl + 256);                 // 15 of them
-  volatile int* sh_flag = reinterpret_cast<volatile int*>(ctrl + 384);       // [0, 2) slow block, [2, 4) last part, [4] failed
-  uint32_t* holder = reinterpret_cast<uint32_t*>(ctrl + 448);
-  float2* sh_ml = reinterpret_cast<float2*>(ctrl + 512);                     // stream 1's rows, for joining (1 KB)
+  enum {
+    B_FULL = 0,              // a stage's copy has arrived
+    B_READY = ST,            // and warp 11 has seen to it
+    B_EMPTY = 2 * ST,        // both streams are done with it
+    B_QF = 3 * ST, B_QE = B_QF + 2,
+    B_S = B_QE + 2,          // scores of a stream
+    B_PH = B_S + 2, B_P = B_PH + 2,  // the first half of its weights, all of them
+    B_O = B_P + 2,           // its P V so far
+    B_FREE = B_O + 2,        // its O has been read
+    B_JOIN = B_FREE + 2,     // stream 1's part of a tile is ready for stream 0
+    B_PIECE = B_JOIN + 1, B_PDONE = B_PIECE + PIECES,
+    B_END = B_PDONE + PIECES,
+    BARS = B_END + 2
+  };
+  static_assert(BARS * 8 <= 400 && sizeof(Piece) * PIECES <= 384, "control block");
+  int64_t* sh_plan = reinterpret_cast<int64_t*>(ctrl + 400);            // 15 of them
+  volatile int* sh_flag = reinterpret_cast<volatile int*>(ctrl + 528);  // [0, 2) slow block, [2, 4) last part, [4] failed
+  volatile int* sh_odd = sh_flag + 8;                                   // [stage] the block has infinities or NaN
+  uint32_t* holder = reinterpret_cast<uint32_t*>(ctrl + 592);
+  Piece* pieces = reinterpret_cast<Piece*>(ctrl + 640);
+  float2* sh_ml = reinterpret_cast<float2*>(ctrl + 1024);               // stream 1's m and l when it is joined (1 KB)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const KvBatchDev& b = a.b;
 
   if (tid == 0) {
-    for (int i = 0; i < BARS; ++i) mbar_init(bars + i, (i >= B_P && i < B_P + 2) || (i >= B_FREE && i < B_FREE + 2) ? 4 : 1);
+    for (int i = 0; i < BARS; ++i) {
+      const bool four = (i >= B_PH && i < B_O) || (i >= B_FREE && i <= B_JOIN);  // the softmax warps of a stream
+      const bool both = (i >= B_EMPTY && i < B_QF) || (i >= B_QE && i < B_S);
+      mbar_init(bars + i, four ? 4 : both ? 2 : i >= B_PDONE && i < B_END ? 11 : 1);
+    }
     fence_mbar_init();
     for (int i = 0; i < 5; ++i) sh_flag[i] = 0;
     tma_prefetch_desc(&maps.q);
@@ -233,222 +293,202 @@ __global__ void __launch_bounds__(THREADS, 1)
   const bool work = rg.s >= 0;
 
   bool ok = true;
-  auto fail = [&]() {
-    ok = false;
-    sh_flag[4] = 1;
-    atomicOr(a.status, FL_KV_TIMEOUT);
-  };
-  // by a whole warp; parity of the phase waited for
+  // by a whole warp; phase: the number of the barrier's phase waited for
   auto wait = [&](int i, uint32_t phase) {
-    if (ok && !mbar_wait_warp(bars + i, phase & 1)) fail();
+    if (__all_sync(0xffffffffu, mbar_try_wait(smem_u32(bars + i), phase & 1))) return ok;
+    if (ok && !wait_longer(bars + i, phase & 1)) {
+      ok = false;
+      sh_flag[4] = 1;
+      atomicOr(a.status, FL_KV_TIMEOUT);
+    }
+    return ok;
   };
-  uint32_t ring = 0;  // stages used before this piece
+  uint32_t ring = 0, qi = 0;  // stages and Q tiles (a ring of two) used so far
+  uint32_t np = 0;            // pieces so far
+  auto piece_done = [&]() {   // the piece has been read
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bars + B_PDONE + np % PIECES);
+    ++np;
+  };
 
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
-    if (work) {
-      const int s = warp >> 2, row = tid & 127;
-      const uint32_t t_lane = tmem + (uint32_t((warp & 3) * 32) << 16);
-      const uint32_t t_s = t_lane + s * TB, t_o = t_lane + 256 + s * HD, t_p = C::OWN_P ? t_lane + 384 + s * 64 : t_s;
-      uint32_t ss = 0, pv = 0, uses = 0;
-      const float scale = fabsf(a.scale_log2);
-      float4* part_o = reinterpret_cast<float4*>(a.parts);
-      float2* part_ml = reinterpret_cast<float2*>(a.parts + (int64_t)gridDim.x * 4 * TB * HD);
-      KvWalk<TileUnits> k;
-      k.set(b, u, rg.s, rg.seq_start, rg.lo, a.kvh);
-      do {
-        const Piece p = piece_of(u, k, rg);
-        const RingOrder ro{p.n, p.two ? 1 : 2};
-        const uint32_t base = ring;  // the piece's first stage
-        ring += 2 * p.n;
-        const int tok = p.tok0 + (p.two && s ? geo.tpt : 0);
-        const int rows = min(geo.tpt, k.q.n - tok) * a.group;
-        const bool valid = row < rows, on = (warp & 3) * 32 < rows;
-        const int mytok = tok + row / a.group;
-        const int sees = valid ? kv_sees(k.q, mytok) : 0, first_sees = kv_sees(k.q, tok);
-        // ---- the row's output, from o(c, x): its unscaled columns [c, c + 32)
-        auto finish = [&](float m, float l, auto&& o) {
-          const int h = k.h * a.group + row % a.group;
-          const int64_t t = k.q.q0 + mytok;
-          const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // a sum that is NaN stays one
-          T* dst = reinterpret_cast<T*>(a.o) + t * a.ldo + h * HD;
+    const int s = warp >> 2, row = tid & 127;
+    const uint32_t t_lane = tmem + (uint32_t((warp & 3) * 32) << 16);
+    const uint32_t t_s = t_lane + s * TB, t_o = t_lane + 256 + s * HD, t_p = C::OWN_P ? t_lane + 384 + s * 64 : t_s;
+    const int my_tok = row / a.group, my_head = row % a.group;  // inside the tile
+    uint32_t ss = 0, pv = 0, uses = 0, joins = 0;
+    bool slow_before = false;
+    const float scale = fabsf(a.scale_log2);
+    const uint32_t flip = a.scale_log2 < 0.f ? 0x80000000u : 0u;
+    float4* part_o = reinterpret_cast<float4*>(a.parts);
+    float2* part_ml = reinterpret_cast<float2*>(a.parts + (int64_t)gridDim.x * 4 * TB * HD);
+    uint8_t* out = sOut + warp * 32 * 128;
+    auto arrive = [&](int i) {  // behind this warp's accesses of TMEM
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars + i);
+    };
+    while (work) {
+      // the whole warpgroup goes on, or none of it
+      if (bar_or(1 + s, 128, !wait(B_PIECE + np % PIECES, np / PIECES))) break;
+      const Piece p = pieces[np % PIECES];
+      piece_done();
+      if (p.end) break;
+      const RingOrder ro{p.n, p.two ? 1 : 2};
+      const uint32_t base = ring;  // the piece's first stage
+      ring += 2 * p.n;
+      const int tok = p.two && s ? geo.tpt : 0, rows = (s ? p.toks[1] : p.toks[0]) * a.group;
+      const bool valid = row < rows, on = (warp & 3) * 32 < rows;
+      const int sees = valid ? p.sees(tok + my_tok) : 0, first_sees = p.sees(tok);
+      const int nb = s ? p.nb[1] : p.nb[0], mine = s ? p.na[1] : p.na[0], f_hi = s ? p.f_hi[1] : p.f_hi[0];
+      const int64_t t_row = p.q0 + tok + my_tok;
+      const int head = p.h * a.group + my_head;
+      if (mine == 0 && !((p.zero >> s) & 1)) continue;
+      float m = -INFINITY, l = 0.f;
 #pragma unroll 1
-          for (int c = 0; c < HD; c += 32) {
-            float x[32];
-            __syncwarp();
-            o(c, x);
-            if (valid) {
-#pragma unroll
-              for (int v = 0; v < 4; ++v) {
-                uint32_t y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = Io::pack(x[8 * v + 2 * i] * inv, x[8 * v + 2 * i + 1] * inv);
-                *reinterpret_cast<uint4*>(dst + c + 8 * v) = make_uint4(y[0], y[1], y[2], y[3]);
-              }
-            }
-          }
-          if (valid && a.lse) a.lse[(int64_t)h * b.T + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2_F;
-        };
-        if (p.nb[s] == 0) {  // rows that see nothing
-          if (p.first && on && (p.two || s == 0))
-            finish(-INFINITY, 0.f, [&](int, float(&x)[32]) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = 0.f;
-            });
-          continue;
+      for (int j = 0; j < mine; ++j) {
+        const int t = p.two ? j : 2 * j + s, kb = (p.kb0 + t) * TB;
+        wait(B_S + s, ss++);
+        // a block where some row does not see a key that another does, and whose values are not all finite, is taken
+        // without the tensor cores
+        const uint32_t vi = base + ro.v(t), vst = vi % ST;
+        bool slow = false;
+        if (first_sees < min(kb + TB, p.kmax)) {
+          wait(B_READY + vst, vi / ST);
+          slow = sh_odd[vst] != 0;
         }
-        const int mine = p.na[s];
-        if (mine == 0) continue;
-        float m = -INFINITY, l = 0.f;
+        if (slow != slow_before && row == 0) sh_flag[s] = slow;
+        slow_before = slow;
+        tc_fence_after();
+        if (on) {
+          if (!__all_sync(0xffffffffu, kb + TB <= sees) || a.scale_log2 < 0.f) {  // keys not seen become -inf
 #pragma unroll 1
-        for (int j = 0; j < mine; ++j) {
-          const int t = p.two ? j : 2 * j + s, kb = (p.kb0 + t) * TB;
-          wait(B_S + s, ss++);
-          tc_fence_after();
-          if (on) {
-            uint32_t r[TB];
-            tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(r));
-            tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
-            tmem_ld32(t_s + 64, *reinterpret_cast<uint32_t(*)[32]>(r + 64));
-            tmem_ld32(t_s + 96, *reinterpret_cast<uint32_t(*)[32]>(r + 96));
-            tmem_ld_wait();
-            if (a.scale_log2 < 0.f) {
+            for (int c = 0; c < TB; c += 32) {
+              uint32_t r[32];
+              tmem_ld32(t_s + c, r);
+              tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < TB; ++e) r[e] ^= 0x80000000u;
+              for (int e = 0; e < 32; ++e) r[e] = kb + c + e >= sees ? 0xff800000u : r[e] ^ flip;
+              tmem_st32(t_s + c, r);
             }
-            if (!__all_sync(0xffffffffu, kb + TB <= sees)) {
-#pragma unroll
-              for (int e = 0; e < TB; ++e)
-                if (kb + e >= sees) r[e] = 0xff800000u;
-            }
-            float mt = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < TB; ++e) mt = fmaxf(mt, __uint_as_float(r[e]));
-            mt *= scale;
-            const bool grows = mt > m + 8.f;
-            if (__any_sync(0xffffffffu, grows)) {
-              const float mn = grows ? mt : m, f = m == -INFINITY ? 0.f : exp2_hw(m - mn);
-              const float corr = grows ? f : 1.f;
-              m = mn;
-              l *= corr;
-              if (j > 0) {
-                wait(B_O + s, pv + j - 1);  // the products so far
-                tc_fence_after();
-#pragma unroll 1
-                for (int c = 0; c < HD; c += 32) {
-                  uint32_t o[32];
-                  tmem_ld32(t_o + c, o);
-                  tmem_ld_wait();
-#pragma unroll
-                  for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr);
-                  tmem_st32(t_o + c, o);
-                }
-              }
-            }
-            const float mref = m == -INFINITY ? 0.f : m;
-            float lt[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < TB / 2; ++c) {
-              const float p0 = exp2_hw(fmaf(__uint_as_float(r[2 * c]), scale, -mref));
-              const float p1 = exp2_hw(fmaf(__uint_as_float(r[2 * c + 1]), scale, -mref));
-              lt[c & 1] += p0;
-              lt[2 + (c & 1)] += p1;
-              r[c] = Io::pack(p0, p1);
-            }
-            tmem_st32(t_p, *reinterpret_cast<uint32_t(*)[32]>(r));
-            tmem_st32(t_p + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
-            l += (lt[0] + lt[1]) + (lt[2] + lt[3]);
             tmem_st_wait();
           }
-          // ---- values of keys that some row does not see have weight 0, which needs them finite: rows of the block
-          // past the last key seen become zeros, the others are looked at where rows differ
-          const int used = p.kmax - kb;  // keys of the block that some row of the unit sees
-          const bool mixed = first_sees < min(kb + TB, p.kmax);
-          bool slow = false;
-          if (mixed || used < TB) {
-            const uint32_t i = base + ro.v(t), st = i % ST;
-            uint8_t* sV = sKV + st * TILE;
-            wait(B_FULL + st, i / ST);
-            bool odd = false;
-            for (int x = row; x < TB * NB; x += 128) {  // row x / NB, 128 bytes of it
-              const int kr = x / NB;
-              uint4* at = reinterpret_cast<uint4*>(sV + (kr >> 3) * NB * 1024 + (x % NB) * 1024 + (kr & 7) * 128);
-              if (kr >= used) {
+          // 64 columns at a time in loops that stay loops: the code is fetched once, and S is read twice at little cost
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+          for (int c = 0; c < TB; c += 64) {
+            uint32_t r[64];
+            tmem_ld32(t_s + c, *reinterpret_cast<uint32_t(*)[32]>(r));
+            tmem_ld32(t_s + c + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+            tmem_ld_wait();
 #pragma unroll
-                for (int v = 0; v < 8; ++v) at[v ^ (kr & 7)] = make_uint4(0, 0, 0, 0);
-              } else if (mixed) {
+            for (int e = 0; e < 64; e += 8)
 #pragma unroll
-                for (int v = 0; v < 8; ++v) {
-                  const uint4 y = at[v ^ (kr & 7)];
-                  odd |= !Io::finite(y.x) || !Io::finite(y.y) || !Io::finite(y.z) || !Io::finite(y.w);
-                }
+              for (int i = 0; i < 4; ++i)
+                mx[i] = fmaxf(fmaxf(mx[i], __uint_as_float(r[e + 2 * i])), __uint_as_float(r[e + 2 * i + 1]));
+          }
+          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+          const bool grows = mt > m + 8.f;
+          if (__any_sync(0xffffffffu, grows)) {
+            const float mn = grows ? mt : m, f = m == -INFINITY ? 0.f : exp2_hw(m - mn);
+            const float corr = grows ? f : 1.f;
+            m = mn;
+            l *= corr;
+            if (j > 0) {
+              wait(B_O + s, pv + j - 1);  // the products so far
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < HD; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(t_o + c, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr);
+                tmem_st32(t_o + c, o);
               }
             }
-            fence_proxy_async_smem();
-            slow = mixed && bar_or(1 + s, 128, odd);
-            if (slow) {
-              if (j > 0) wait(B_O + s, pv + j - 1);
-              else if (uses > 0) wait(B_FREE + s, uses - 1);
-              tc_fence_after();
-              __syncwarp();
-              if (on) slow_pv<T, HD>(t_p, t_o, sV, sees - kb, j == 0);
-            }
           }
-          if (row == 0) sh_flag[s] = slow;
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bars + B_P + s);
+          const float mref = m == -INFINITY ? 0.f : m;
+          const float2 sc = make_float2(scale, scale), nm = make_float2(-mref, -mref);
+          float2 lt[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
+          for (int c = 0; c < TB; c += 64) {
+            uint32_t r[64];
+            tmem_ld32(t_s + c, *reinterpret_cast<uint32_t(*)[32]>(r));
+            tmem_ld32(t_s + c + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float2 x = fma2(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), sc, nm);
+              const float2 y = make_float2(exp2_hw(x.x), exp2_hw(x.y));
+              lt[i & 1] = add2(lt[i & 1], y);
+              r[i] = Io::pack(y.x, y.y);
+            }
+            tmem_st32(t_p + c / 2, *reinterpret_cast<uint32_t(*)[32]>(r));
+            tmem_st_wait();
+            if (c == 0 && !slow) arrive(B_PH + s);
+          }
+          lt[0] = add2(lt[0], lt[1]);
+          l += lt[0].x + lt[0].y;
+        } else if (!slow) {
+          arrive(B_PH + s);
         }
+        if (slow) {
+          if (j > 0) wait(B_O + s, pv + j - 1);
+          else if (uses > 0) wait(B_FREE + s, uses - 1);
+          tc_fence_after();
+          __syncwarp();
+          if (on) slow_pv<T, HD>(t_p, t_o, sKV + vst * TILE, sees - kb, j == 0);
+          arrive(B_PH + s);
+        }
+        arrive(B_P + s);
+      }
+      if (mine > 0) {
         pv += mine;
         ++uses;
         wait(B_O + s, pv - 1);
         tc_fence_after();
-        // ---- one tile in two streams: stream 0 joins both
-        const bool joined = !p.two && p.na[1] > 0;
-        float f0 = 1.f, f1 = 0.f;
-        if (joined) {
-          if (s == 1) sh_ml[row] = make_float2(m, l);
-          tc_fence_before();
-          bar_sync(3, 256);
-          tc_fence_after();
-          if (s == 1) continue;
-          const float2 x = sh_ml[row];
-          const float mn = fmaxf(m, x.x);
-          f0 = m == -INFINITY ? 0.f : exp2_hw(m - mn);
-          f1 = x.x == -INFINITY ? 0.f : exp2_hw(x.x - mn);
-          l = (f0 == 0.f ? 0.f : l * f0) + (f1 == 0.f ? 0.f : x.y * f1);
-          m = mn;
-        }
-        auto own = [&](int c, float(&x)[32]) {  // by whole warps
-          uint32_t o[32];
-          __syncwarp();
-          tmem_ld32(t_o + c, o);
-          tmem_ld_wait();
-#pragma unroll
-          for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(o[e]);
-          if (joined) {
-            tmem_ld32(t_o + HD + c, o);
-            tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              x[e] = (f0 == 0.f ? 0.f : x[e] * f0) + (f1 == 0.f ? 0.f : __uint_as_float(o[e]) * f1);
-          }
-        };
-        auto release = [&]() {  // O has been read
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(bars + B_FREE + s);
-            if (joined) mbar_arrive(bars + B_FREE + 1);
-          }
-        };
-        if (p.kb0 == 0 && p.n >= p.nb[s]) {
-          if (on) finish(m, l, own);
-          release();
+      }
+      // ---- one tile in two streams: stream 0 joins both
+      const bool joined = !p.two && p.na[1] > 0;
+      float f0 = 1.f, f1 = 0.f;
+      if (joined) {
+        if (s == 1) {
+          sh_ml[row] = make_float2(m, l);
+          arrive(B_JOIN);
           continue;
         }
-        // ---- a part: [slot][stream][4 columns][row]
-        auto part = [&](int cta, bool first) { return (int64_t)((2 * cta + first) * 2 + s); };
+        wait(B_JOIN, joins++);
+        tc_fence_after();
+        const float2 x = sh_ml[row];
+        const float mn = fmaxf(m, x.x);
+        f0 = m == -INFINITY ? 0.f : exp2_hw(m - mn);
+        f1 = x.x == -INFINITY ? 0.f : exp2_hw(x.x - mn);
+        l = (f0 == 0.f ? 0.f : l * f0) + (f1 == 0.f ? 0.f : x.y * f1);
+        m = mn;
+      }
+      auto own = [&](int c, float(&x)[32]) {  // the row's columns [c, c + 32), unscaled; by whole warps
+        uint32_t o[32];
+        __syncwarp();
+        tmem_ld32(t_o + c, o);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(o[e]);
+        if (joined) {
+          tmem_ld32(t_o + HD + c, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            x[e] = (f0 == 0.f ? 0.f : x[e] * f0) + (f1 == 0.f ? 0.f : __uint_as_float(o[e]) * f1);
+        }
+      };
+      auto release = [&]() {  // O has been read
+        arrive(B_FREE + s);
+        if (joined) arrive(B_FREE + 1);
+      };
+      auto part = [&](int cta, bool first) { return (int64_t)((2 * cta + first) * 2 + s); };
+      const bool whole = p.kb0 == 0 && p.n >= nb;
+      if (!whole) {  // ---- a part: [slot][stream][4 columns][row]
         const int64_t at = part(blockIdx.x, p.kb0 == 0);
         if (on) {
 #pragma unroll 1
@@ -464,172 +504,317 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (valid) __stcg(part_ml + at * TB + row, make_float2(m, l));
         }
         release();
-        const int f_lo = rg.cta_of(k.start), f_hi = rg.cta_of(k.start + (int64_t)p.w * (p.nb[s] - 1));
         __threadfence();
         bar_sync(1 + s, 128);
         if (row == 0) {
-          sh_flag[2 + s] = atomicInc(a.counters + 2 * f_lo + s, f_hi - f_lo) == (unsigned)(f_hi - f_lo);
+          sh_flag[2 + s] = atomicInc(a.counters + 2 * p.f_lo + s, f_hi - p.f_lo) == (unsigned)(f_hi - p.f_lo);
           __threadfence();
         }
         bar_sync(1 + s, 128);
         if (!sh_flag[2 + s]) continue;
-        float ma = -INFINITY, la = 0.f;
-        for (int f = f_lo; valid && f <= f_hi; ++f) ma = fmaxf(ma, __ldcg(part_ml + part(f, f == f_lo) * TB + row).x);
-        for (int f = f_lo; valid && f <= f_hi; ++f) {
-          const float2 x = __ldcg(part_ml + part(f, f == f_lo) * TB + row);
-          if (x.x != -INFINITY) la += x.y * exp2_hw(x.x - ma);
+        m = -INFINITY;
+        l = 0.f;
+        for (int f = p.f_lo; valid && f <= f_hi; ++f) {
+          const float2 x = __ldcg(part_ml + part(f, f == p.f_lo) * TB + row);
+          const float mn = fmaxf(m, x.x);
+          l = (m == -INFINITY ? 0.f : l * exp2_hw(m - mn)) + (x.x == -INFINITY ? 0.f : x.y * exp2_hw(x.x - mn));
+          m = mn;
         }
-        if (on)
-          finish(ma, la, [&](int c, float(&x)[32]) {
+      }
+      // ---- the output: through shared memory, so that a store is whole lines of four rows and not a sector of each of 32
+      if (on) {
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(l));  // one ulp, before a rounding to 16 bits
+        inv = l == 0.f ? 0.f : inv;
+        const int64_t dst = t_row * a.ldo + head * HD;
+        const uint32_t live = __ballot_sync(0xffffffffu, valid);
+#pragma unroll 1
+        for (int h = 0; h < HD; h += 64) {
+#pragma unroll 1
+          for (int c = 0; c < 64; c += 32) {
+            float x[32];
+            if (nb == 0) {  // rows that see nothing
 #pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = 0.f;
-            for (int f = f_lo; valid && f <= f_hi; ++f) {
-              const int64_t q = part(f, f == f_lo);
-              const float mf = __ldcg(part_ml + q * TB + row).x;
-              if (mf == -INFINITY) continue;
-              const float w = exp2_hw(mf - ma);
+              for (int e = 0; e < 32; ++e) x[e] = 0.f;
+            } else if (whole) {
+              own(h + c, x);
+            } else {
 #pragma unroll
-              for (int v = 0; v < 8; ++v) {
-                const float4 y = __ldcg(part_o + (q * (HD / 4) + c / 4 + v) * TB + row);
-                x[4 * v] = fmaf(y.x, w, x[4 * v]);
-                x[4 * v + 1] = fmaf(y.y, w, x[4 * v + 1]);
-                x[4 * v + 2] = fmaf(y.z, w, x[4 * v + 2]);
-                x[4 * v + 3] = fmaf(y.w, w, x[4 * v + 3]);
+              for (int e = 0; e < 32; ++e) x[e] = 0.f;
+#pragma unroll 1
+              for (int f = p.f_lo; valid && f <= f_hi; ++f) {
+                const int64_t q = part(f, f == p.f_lo);
+                const float mf = __ldcg(part_ml + q * TB + row).x;
+                if (mf == -INFINITY) continue;
+                const float w = exp2_hw(mf - m);
+#pragma unroll
+                for (int v = 0; v < 8; ++v) {
+                  const float4 y = __ldcg(part_o + (q * (HD / 4) + (h + c) / 4 + v) * TB + row);
+                  x[4 * v] = fmaf(y.x, w, x[4 * v]);
+                  x[4 * v + 1] = fmaf(y.y, w, x[4 * v + 1]);
+                  x[4 * v + 2] = fmaf(y.z, w, x[4 * v + 2]);
+                  x[4 * v + 3] = fmaf(y.w, w, x[4 * v + 3]);
+                }
               }
             }
-          });
-      } while (k.next(b, u, a.kvh) && k.start < rg.hi);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              uint32_t y[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) y[i] = Io::pack(x[8 * v + 2 * i] * inv, x[8 * v + 2 * i + 1] * inv);
+              *reinterpret_cast<uint4*>(out + lane * 128 + (((c / 8 + v) ^ (lane & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          }
+          __syncwarp();
+#pragma unroll 4
+          for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + lane / 8, c = lane % 8;
+            const uint4 y = *reinterpret_cast<const uint4*>(out + r * 128 + ((c ^ (r & 7)) << 4));
+            const int64_t to = __shfl_sync(0xffffffffu, dst, r);
+            if ((live >> r) & 1) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.o) + to + h + 8 * c) = y;
+          }
+          __syncwarp();
+        }
+        if (valid && a.lse) {
+          float lg;
+          asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lg) : "f"(l));
+          a.lse[(int64_t)head * b.T + t_row] = (m + lg) * LN2_F;  // no keys: -inf of l = 0
+        }
+      }
+      if (whole && nb > 0) release();
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_REST));
     if (work && warp == W_TMA) {
       KvWalk<TileUnits> k;
       k.set(b, u, rg.s, rg.seq_start, rg.lo, a.kvh);
-      uint32_t pieces = 0;
-      do {
-        const Piece p = piece_of(u, k, rg);
-        if (p.n == 0) continue;
-        if (pieces > 0) wait(B_QE, pieces - 1);
-        ++pieces;
-        if (ok && elect_one()) {
-          mbar_arrive_expect_tx(bars + B_QF, (p.two ? 2 : 1) * geo.tpt * a.group * HD * 2);
-          for (int t = 0; t < (p.two ? 2 : 1); ++t)
-            for (int h = 0; h < NB; ++h)
-              tma_load_3d(sQ + t * TILE + h * (TB * 128), &maps.q, bars + B_QF, 64 * h, k.h * a.group,
-                          k.q.q0 + p.tok0 + t * geo.tpt);
-        }
-        __syncwarp();
-        const int boxes = TB / geo.box_rows, per = (1 << b.ps_log2) / geo.box_rows;  // boxes of a block, of a page
-        auto load = [&](int t, bool v) {
-          const int st = ring % ST;
-          if (ring >= ST) wait(B_EMPTY + st, ring / ST - 1);
-          ++ring;
-          const int kb = p.kb0 + t;
-          const int nbox = min(boxes, (p.kmax - kb * TB + geo.box_rows - 1) / geo.box_rows);
-          int page = 0, part = 0;
-          if (lane < nbox) {
-            const int i = kb * boxes + lane;
-            page = kv_page(b, k.s, i / per, a.status);
-            part = i % per;
+      const int boxes = TB / geo.box_rows, per = (1 << b.ps_log2) / geo.box_rows;  // boxes of a block, of a page
+      bool more = true;
+      while (ok) {
+        Piece p;
+        p.end = !more;
+        if (more) {
+          p = piece_of(u, k, rg);
+          const int seq = k.s;
+          more = k.next(b, u, a.kvh) && k.start < rg.hi;
+          if (p.n == 0 && p.zero == 0) continue;
+          if (np >= PIECES && !wait(B_PDONE + np % PIECES, np / PIECES - 1)) break;
+          if (lane == 0) {
+            pieces[np % PIECES] = p;
+            mbar_arrive(bars + B_PIECE + np % PIECES);
           }
-          if (!ok) return;
-          if (lane == 0) mbar_arrive_expect_tx(bars + B_FULL + st, nbox * geo.box_rows * HD * 2);
-          __syncwarp();
-          if (lane < nbox)
-            tma_load_5d(sKV + st * TILE + lane * geo.box_rows * HD * 2, v ? &maps.v : &maps.k, bars + B_FULL + st,
-                        geo.by_head ? k.h * NB : 0, part * (geo.box_rows / 8),
-                        page < 0 ? -1 : geo.by_head ? page : page * geo.per_page + k.h);
-          __syncwarp();
-        };
-        const int la = p.two ? 1 : 2;
-        for (int t = 0; t < min(p.n, la); ++t) load(t, false);
-        for (int t = 0; t < p.n; ++t) {
-          load(t, true);
-          if (t + la < p.n) load(t + la, false);
-        }
-      } while (k.next(b, u, a.kvh) && k.start < rg.hi);
-    } else if (work && warp == W_MMA) {
-      KvWalk<TileUnits> k;
-      k.set(b, u, rg.s, rg.seq_start, rg.lo, a.kvh);
-      uint32_t pieces = 0, ps[2] = {0, 0}, pv[2] = {0, 0}, uses[2] = {0, 0};
-      constexpr uint32_t I_S = idesc<T>(TB, false), I_PV = idesc<T>(HD, true);
-      do {
-        const Piece p = piece_of(u, k, rg);
-        if (p.n == 0) continue;
-        const RingOrder ro{p.n, p.two ? 1 : 2};
-        wait(B_QF, pieces++);
-        int left = p.na[0] + p.na[1];
-        auto qk = [&](int s, int t) {
-          const uint32_t i = ring + ro.k(t), st = i % ST;
-          wait(B_FULL + st, i / ST);
-          if (!C::OWN_P && pv[s] > 0) wait(B_O + s, pv[s] - 1);  // its P V has read the P that S overwrites
-          --left;
-          tc_fence_after();
-          if (ok && elect_one()) {
-            const uint64_t dq = smem_desc_sw128(smem_u32(sQ + (p.two ? s * TILE : 0)), 16, 1024);
-            const uint64_t dk = smem_desc_sw128(smem_u32(sKV + st * TILE), 16, NB * 1024);
-#pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk)
-              umma_bf16(tmem + s * TB, dq + (kk >> 2) * (TB * 128 / 16) + (kk & 3) * 2, dk + (kk >> 2) * 64 + (kk & 3) * 2,
-                        I_S, kk > 0);
-            umma_commit(bars + B_S + s);
-            if (!p.two || s == 1) umma_commit(bars + B_EMPTY + st);
-            if (left == 0) umma_commit(bars + B_QE);
-          }
-          __syncwarp();
-        };
-        auto pvs = [&](int s, int t, bool first) {
-          wait(B_P + s, ps[s]++);
-          const uint32_t i = ring + ro.v(t), st = i % ST;
-          wait(B_FULL + st, i / ST);
-          if (first) {
-            if (uses[s] > 0) wait(B_FREE + s, uses[s] - 1);  // the last piece's O has been read
-            ++uses[s];
-          }
-          ++pv[s];
-          const bool slow = sh_flag[s] != 0;
-          tc_fence_after();
-          if (ok && elect_one()) {
-            if (!slow) {
-              const uint64_t dv = smem_desc_sw128(smem_u32(sKV + st * TILE), 1024, NB * 1024);
-              const uint32_t tp = tmem + (C::OWN_P ? 384 + s * 64 : s * TB);
-#pragma unroll
-              for (int kk = 0; kk < TB / 16; ++kk)
-                umma_bf16_ts(tmem + 256 + s * HD, tp + kk * 8, dv + kk * (NB * 128), I_PV, !first || kk > 0);
+          ++np;
+          auto load = [&](int t, bool v) {
+            const int kb = p.kb0 + t, st = ring % ST;
+            const int nbox = min(boxes, (p.kmax - kb * TB + geo.box_rows - 1) / geo.box_rows);
+            int page = 0, at = 0;  // asked for before the stage is free
+            if (lane < nbox) {
+              const int i = kb * boxes + lane;
+              page = kv_page(b, seq, i / per, a.status);
+              at = i % per;
             }
-            umma_commit(bars + B_O + s);
-            if (!p.two || s == 1) umma_commit(bars + B_EMPTY + st);
-          }
-          __syncwarp();
-        };
-        if (p.two) {
-          if (p.na[0] > 0) qk(0, 0);
-          qk(1, 0);
-          for (int t = 0; t < p.n; ++t)
-            for (int s = t < p.na[0] ? 0 : 1; s < 2; ++s) {
-              pvs(s, t, t == 0);
-              if (t + 1 < p.na[s]) qk(s, t + 1);
+            if (ring >= ST && !wait(B_EMPTY + st, ring / ST - 1)) return;
+            ++ring;
+            if (lane == 0) mbar_arrive_expect_tx(bars + B_FULL + st, nbox * geo.box_rows * HD * 2);
+            __syncwarp();
+            if (lane < nbox)
+              tma_load_5d(sKV + st * TILE + lane * geo.box_rows * HD * 2, v ? &maps.v : &maps.k, bars + B_FULL + st,
+                          geo.by_head ? p.h * NB : 0, at * (geo.box_rows / 8),
+                          page < 0 ? -1 : geo.by_head ? page : page * geo.per_page + p.h);
+            __syncwarp();
+          };
+          const int la = p.two ? 1 : 2;
+          // the first keys go ahead of Q, whose place the last piece may still be using
+          for (int t = 0; ok && t < min(p.n, la); ++t) load(t, false);
+          for (int t = 0; p.n > 0 && t <= p.two; ++t) {
+            const int slot = qi & 1;
+            if (!ok || (qi > 1 && !wait(B_QE + slot, (qi >> 1) - 1))) break;
+            ++qi;
+            if (elect_one()) {
+              mbar_arrive_expect_tx(bars + B_QF + slot, geo.tpt * a.group * HD * 2);
+              for (int h = 0; h < NB; ++h)
+                tma_load_3d(sQ + slot * TILE + h * (TB * 128), &maps.q, bars + B_QF + slot, 64 * h, p.h * a.group,
+                            p.q0 + t * geo.tpt);
             }
+            __syncwarp();
+          }
+          for (int t = 0; ok && t < p.n; ++t) {
+            load(t, true);
+            if (ok && t + la < p.n) load(t + la, false);
+          }
         } else {
-          qk(0, 0);
-          if (p.n > 1) qk(1, 1);
-          for (int t = 0; t < p.n; ++t) {
-            pvs(t & 1, t, t < 2);
-            if (t + 2 < p.n) qk(t & 1, t + 2);
+          if (np >= PIECES && !wait(B_PDONE + np % PIECES, np / PIECES - 1)) break;
+          if (lane == 0) {
+            pieces[np % PIECES] = p;
+            mbar_arrive(bars + B_PIECE + np % PIECES);
+          }
+          break;
+        }
+      }
+    } else if (work && warp == W_FIX) {
+      // A key that a row does not see has weight 0, which only makes nothing of it if its value is finite.  Rows of a V
+      // block past the last key that anyone sees hold whatever the page held: they become zeros.  The others are
+      // looked through where rows differ in what they see.
+      while (wait(B_PIECE + np % PIECES, np / PIECES)) {
+        const Piece p = pieces[np % PIECES];
+        piece_done();
+        if (p.end) break;
+        const int la = p.two ? 1 : 2, first_sees = p.sees(0);
+        auto keys = [&]() {
+          if (wait(B_FULL + ring % ST, ring / ST) && lane == 0) mbar_arrive(bars + B_READY + ring % ST);
+          ++ring;
+        };
+        for (int t = 0; ok && t < min(p.n, la); ++t) keys();
+        for (int t = 0; ok && t < p.n; ++t) {
+          const int st = ring % ST, used = p.kmax - (p.kb0 + t) * TB;
+          uint4* sV = reinterpret_cast<uint4*>(sKV + st * TILE);
+          if (!wait(B_FULL + st, ring / ST)) break;
+          const bool mixed = first_sees < min((p.kb0 + t + 1) * TB, p.kmax);
+          if (used < TB) {
+            for (int x = used * NB * 8 + lane; x < TILE / 16; x += 32) {
+              const int r = x / (NB * 8), c = x % (NB * 8);
+              sV[(r >> 3) * NB * 64 + (c >> 3) * 64 + (r & 7) * 8 + (c & 7)] = make_uint4(0, 0, 0, 0);
+            }
+            __syncwarp();
+          }
+          bool odd = false;
+          if (mixed) {
+            uint32_t top[4] = {0, 0, 0, 0};
+            for (int x = lane; x < (min(used, TB) + 7) / 8 * NB * 64; x += 256) {  // whole groups: NB * 64 a group, 256 a round
+              uint4 y[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) y[i] = x + 32 * i < TILE / 16 ? sV[x + 32 * i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                if (x + 32 * i < (min(used, TB) + 7) / 8 * NB * 64) {
+                  top[0] = Io::max_abs(top[0], y[i].x);
+                  top[1] = Io::max_abs(top[1], y[i].y);
+                  top[2] = Io::max_abs(top[2], y[i].z);
+                  top[3] = Io::max_abs(top[3], y[i].w);
+                }
+              }
+            }
+            odd = __any_sync(0xffffffffu, !Io::finite(top[0]) || !Io::finite(top[1]) || !Io::finite(top[2]) || !Io::finite(top[3]));
+          }
+          if (used < TB) fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            sh_odd[st] = odd;
+            mbar_arrive(bars + B_READY + st);
+          }
+          ++ring;
+          if (t + la < p.n) keys();
+        }
+      }
+    } else if (work) {
+      const int s = (int)uniform(warp - W_MMA);  // the stream
+      const uint32_t tm = uniform(tmem);
+      const uint64_t desc_q = smem_desc_sw128(smem_u32(sQ), 16, 1024), desc_k = smem_desc_sw128(smem_u32(sKV), 16, NB * 1024),
+                     desc_v = smem_desc_sw128(smem_u32(sKV), 1024, NB * 1024);
+      const uint32_t t_s = tm + s * TB, t_o = tm + 256 + s * HD, t_p = C::OWN_P ? tm + 384 + s * 64 : t_s;
+      constexpr uint32_t I_S = idesc<T>(TB, false), I_PV = idesc<T>(HD, true);
+      // This warp's instructions lie between a stream's weights and its next scores.  What the loop goes by is known to
+      // be uniform, so that it stays in uniform registers: the next stage and its phase, and counts.
+      // Both streams see every stage and Q tile pass, in order, and free it with one arrival each: of those that it
+      // does not read a stream waits for the copy only.  So no stream is ever two phases from a barrier's.
+      uint32_t st = 0, ph = 0, qn = 0, done = 0, uses = 0;
+      auto step = [&]() {
+        if (++st == ST) st = 0, ph ^= 1;
+      };
+      auto pass = [&]() {
+        if (wait(B_READY + st, ph) && lane == 0) mbar_arrive(bars + B_EMPTY + st);
+        step();
+      };
+      while (wait(B_PIECE + np % PIECES, np / PIECES)) {
+        const Piece* pp = pieces + np % PIECES;
+        const int end = (int)uniform(pp->end), two = (int)uniform(pp->two), n = (int)uniform(pp->n), mine = (int)uniform(pp->na[s]);
+        piece_done();
+        if (end) break;
+        if (n == 0) continue;
+        const uint32_t q = qn + (two ? s : 0);
+        for (const uint32_t qe = qn + 1 + two; ok && qn < qe; ++qn)
+          if (wait(B_QF + (qn & 1), qn >> 1) && (qn != q || mine == 0) && lane == 0) mbar_arrive(bars + B_QE + (qn & 1));
+        const uint64_t dq = desc_q + (q & 1) * (TILE / 16);
+        // The ring holds the keys of la blocks, then each block's values and the keys la blocks further; with two tiles
+        // la = 1 and each stream takes all that it sees, else la = 2 and the streams take every other block.
+        const int la = 2 - two;
+#pragma unroll 1
+        for (int t = -la; ok && t < n; ++t) {
+          const bool my = two || ((t + 2) & 1) == s;
+          const int j = two ? t : t >> 1;  // the stream's count of blocks
+          const bool v = t >= 0, kk_ = t + la < n;  // the ring's next: V of block t, K of block t + la
+          const bool pv = v && j < mine, qk = kk_ && j + 1 < mine;
+          if (!my) {
+            if (v) pass();
+            if (kk_) pass();
+            continue;
+          }
+          const uint32_t vs = st;
+          const uint64_t dv = desc_v + st * (TILE / 16);
+          if (v) {
+            if (!wait(B_READY + st, ph)) break;
+            if (!pv && lane == 0) mbar_arrive(bars + B_EMPTY + st);
+            step();
+          }
+          const uint32_t ks = st;
+          const uint64_t dk = desc_k + st * (TILE / 16);
+          if (kk_) {
+            if (!wait(B_READY + st, ph)) break;
+            if (!qk && lane == 0) mbar_arrive(bars + B_EMPTY + st);
+            step();
+          }
+          if (pv) {  // O += P V of block t, from the first half of the weights on
+            if (j == 0) {
+              if (uses > 0 && !wait(B_FREE + s, uses - 1)) break;  // the last piece's O has been read
+              ++uses;
+            }
+            if (!wait(B_PH + s, done)) break;
+            const bool issue = sh_flag[s] == 0;  // else the block was taken without the tensor cores
+            tc_fence_after();
+            if (issue && elect_one()) {
+#pragma unroll
+              for (int kk = 0; kk < TB / 32; ++kk) umma_bf16_ts(t_o, t_p + kk * 8, dv + kk * (NB * 128), I_PV, j > 0 || kk > 0);
+            }
+            __syncwarp();
+            if (!wait(B_P + s, done)) break;
+            ++done;
+            tc_fence_after();
+            if (elect_one()) {
+              if (issue) {
+#pragma unroll
+                for (int kk = TB / 32; kk < TB / 16; ++kk) umma_bf16_ts(t_o, t_p + kk * 8, dv + kk * (NB * 128), I_PV, 1);
+              }
+              umma_commit(bars + B_O + s);
+              umma_commit(bars + B_EMPTY + vs);
+            }
+            __syncwarp();
+          }
+          if (qk) {  // S of block t + la; the last P V has read the P that it overwrites
+            if (!C::OWN_P && done > 0 && !wait(B_O + s, done - 1)) break;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int kk = 0; kk < HD / 16; ++kk)
+                umma_bf16(t_s, dq + (kk >> 2) * (TB * 128 / 16) + (kk & 3) * 2, dk + (kk >> 2) * 64 + (kk & 3) * 2, I_S, kk > 0);
+              umma_commit(bars + B_S + s);
+              umma_commit(bars + B_EMPTY + ks);
+              if (j + 2 == mine) umma_commit(bars + B_QE + (q & 1));
+            }
+            __syncwarp();
           }
         }
-        ring += 2 * p.n;
-      } while (k.next(b, u, a.kvh) && k.start < rg.hi);
+      }
     }
   }
   // ---- the end: nothing is in flight any more when the CTA leaves
   __syncthreads();
-  if (warp == W_MMA) {
-    if (elect_one()) umma_commit(bars + B_END);
-    mbar_wait_warp(bars + B_END, 0);
+  if (warp == W_MMA || warp == W_MMA + 1) {
+    if (elect_one()) umma_commit(bars + B_END + warp - W_MMA);
+    mbar_wait_warp(bars + B_END + warp - W_MMA, 0);
   }
-  if (warp == W_TMA && sh_flag[4] != 0)  // copies that nobody waited for
+  if (warp == W_TMA && sh_flag[4] != 0) {  // copies that nobody waited for
     for (uint32_t i = ring > ST ? ring - ST : 0; i < ring; ++i) mbar_wait_warp(bars + B_FULL + i % ST, (i / ST) & 1);
+    for (uint32_t i = qi > 2 ? qi - 2 : 0; i < qi; ++i) mbar_wait_warp(bars + B_QF + (i & 1), (i >> 1) & 1);
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == W_MMA) {
@@ -641,14 +826,6 @@ __global__ void __launch_bounds__(THREADS, 1)
 template <class T, int HD>
 int launch_tc(const fl_kv_cache* c, const KvAttnArgs& a, int heads, cudaStream_t st) {
   FL_CUDA_TRY(fl_func_smem((const void*)kv_attn_tc_kernel<T, HD>, Cfg<HD>::SMEM));
-  static std::atomic<bool> split_ok{false};
-  if (!split_ok.load(std::memory_order_relaxed)) {
-    cudaFuncAttributes at;
-    FL_CUDA_TRY(cudaFuncGetAttributes(&at, (const void*)kv_attn_tc_kernel<T, HD>));
-    if (at.numRegs < REGS_LAUNCH)
-      return fl_internal_error(FL_ERR_UNSUPPORTED, "kv attention: built with %d registers a thread", at.numRegs);
-    split_ok.store(true, std::memory_order_relaxed);
-  }
   fl_gemm::PFN_encodeTiled enc = fl_gemm::get_encode_fn();
   if (!enc) return fl_internal_error(FL_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
   TcGeom g;

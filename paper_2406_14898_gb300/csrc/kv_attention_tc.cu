@@ -35,6 +35,7 @@ namespace {
 
 constexpr int TB = 128;
 constexpr int THREADS = 384, W_TMA = 8, W_MMA = 9, W_FIX = 11;
+constexpr int LAG_BLOCKS = 6;
 constexpr int ENDS = 5;      // cost of a unit's ends (Q, the first scores, the output), in blocks of one tile
 constexpr int MIN_COST = 4;
 constexpr float LN2_F = 0.6931471805599453f;
@@ -43,10 +44,9 @@ template <int HD>
 struct Cfg {
   static constexpr int NB = HD / 64;
   static constexpr int TILE = TB * HD * 2;
-  static constexpr int ST = HD == 128 ? 4 : 8;  // stages
-  static constexpr int OUT = 8 * 32 * 128;      // 32 rows x 64 columns of output a softmax warp
+  static constexpr int ST = HD == 128 ? 5 : 8;  // stages: what 227 KB hold beside two Q tiles; 8 at head_dim 64
   static constexpr int CTRL = 2048;
-  static constexpr int SMEM = (2 + ST) * TILE + OUT + CTRL + 1024;
+  static constexpr int SMEM = (2 + ST) * TILE + CTRL + 1024;
   static constexpr bool OWN_P = HD == 64;
 };
 static_assert(Cfg<128>::SMEM <= 227 * 1024 && Cfg<64>::SMEM <= 227 * 1024, "shared memory");
@@ -135,6 +135,9 @@ struct Piece {
   int vis, ctx, L;              // token i of the unit sees the first max(0, min(L, max(vis + i, ctx))) keys
   int f_lo, f_hi[2];            // CTAs that have parts of it
   FL_DEV int sees(int i) const { return max(0, min(L, max(vis + i, ctx))); }
+  // Streams that compute their weights at the same time wait for their products at the same time, and stay so.  Where a
+  // unit is long enough to pay for it, the second therefore starts behind the first one's first scores.
+  FL_DEV bool lag() const { return two && na[0] >= LAG_BLOCKS; }
 };
 constexpr int PIECES = 4;  // told ahead
 FL_DEV Piece piece_of(const TileUnits& u, const KvWalk<TileUnits>& k, const KvRange& g) {
@@ -238,8 +241,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;
   uint8_t* sKV = smem + 2 * TILE;
-  uint8_t* sOut = sKV + ST * TILE;
-  uint8_t* ctrl = sOut + C::OUT;
+  uint8_t* ctrl = sKV + ST * TILE;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ctrl);
   enum {
     B_FULL = 0,              // a stage's copy has arrived
@@ -251,7 +253,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     B_O = B_P + 2,           // its P V so far
     B_FREE = B_O + 2,        // its O has been read
     B_JOIN = B_FREE + 2,     // stream 1's part of a tile is ready for stream 0
-    B_PIECE = B_JOIN + 1, B_PDONE = B_PIECE + PIECES,
+    B_LAG = B_JOIN + 1,      // stream 0 has its first scores (see lag)
+    B_PIECE = B_LAG + 1, B_PDONE = B_PIECE + PIECES,
     B_END = B_PDONE + PIECES,
     BARS = B_END + 2
   };
@@ -267,7 +270,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (tid == 0) {
     for (int i = 0; i < BARS; ++i) {
-      const bool four = (i >= B_PH && i < B_O) || (i >= B_FREE && i <= B_JOIN);  // the softmax warps of a stream
+      const bool four = (i >= B_PH && i < B_O) || (i >= B_FREE && i <= B_LAG);  // the softmax warps of a stream
       const bool both = (i >= B_EMPTY && i < B_QF) || (i >= B_QE && i < B_S);
       mbar_init(bars + i, four ? 4 : both ? 2 : i >= B_PDONE && i < B_END ? 11 : 1);
     }
@@ -322,7 +325,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80000000u : 0u;
     float4* part_o = reinterpret_cast<float4*>(a.parts);
     float2* part_ml = reinterpret_cast<float2*>(a.parts + (int64_t)gridDim.x * 4 * TB * HD);
-    uint8_t* out = sOut + warp * 32 * 128;
+    const bool o32 = ((reinterpret_cast<uintptr_t>(a.o) | (uintptr_t)(a.ldo * 2)) & 31) == 0;  // rows in whole sectors
     auto arrive = [&](int i) {  // behind this warp's accesses of TMEM
       tc_fence_before();
       __syncwarp();
@@ -349,6 +352,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int j = 0; j < mine; ++j) {
         const int t = p.two ? j : 2 * j + s, kb = (p.kb0 + t) * TB;
         wait(B_S + s, ss++);
+        if (j == 0 && s == 0 && p.lag()) arrive(B_LAG);
         // a block where some row does not see a key that another does, and whose values are not all finite, is taken
         // without the tensor cores
         const uint32_t vi = base + ro.v(t), vst = vi % ST;
@@ -430,8 +434,8 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           lt[0] = add2(lt[0], lt[1]);
           l += lt[0].x + lt[0].y;
-        } else if (!slow) {
-          arrive(B_PH + s);
+        } else {
+          if (!slow) arrive(B_PH + s);
         }
         if (slow) {
           if (j > 0) wait(B_O + s, pv + j - 1);
@@ -521,23 +525,20 @@ __global__ void __launch_bounds__(THREADS, 1)
           m = mn;
         }
       }
-      // ---- the output: through shared memory, so that a store is whole lines of four rows and not a sector of each of 32
+      // ---- the output
       if (on) {
         float inv;
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(l));  // one ulp, before a rounding to 16 bits
         inv = l == 0.f ? 0.f : inv;
-        const int64_t dst = t_row * a.ldo + head * HD;
-        const uint32_t live = __ballot_sync(0xffffffffu, valid);
+        T* dst = reinterpret_cast<T*>(a.o) + t_row * a.ldo + head * HD;
 #pragma unroll 1
-        for (int h = 0; h < HD; h += 64) {
-#pragma unroll 1
-          for (int c = 0; c < 64; c += 32) {
+        for (int c = 0; c < HD; c += 32) {
             float x[32];
             if (nb == 0) {  // rows that see nothing
 #pragma unroll
               for (int e = 0; e < 32; ++e) x[e] = 0.f;
             } else if (whole) {
-              own(h + c, x);
+              own(c, x);
             } else {
 #pragma unroll
               for (int e = 0; e < 32; ++e) x[e] = 0.f;
@@ -549,7 +550,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const float w = exp2_hw(mf - m);
 #pragma unroll
                 for (int v = 0; v < 8; ++v) {
-                  const float4 y = __ldcg(part_o + (q * (HD / 4) + (h + c) / 4 + v) * TB + row);
+                  const float4 y = __ldcg(part_o + (q * (HD / 4) + c / 4 + v) * TB + row);
                   x[4 * v] = fmaf(y.x, w, x[4 * v]);
                   x[4 * v + 1] = fmaf(y.y, w, x[4 * v + 1]);
                   x[4 * v + 2] = fmaf(y.z, w, x[4 * v + 2]);
@@ -557,23 +558,21 @@ __global__ void __launch_bounds__(THREADS, 1)
                 }
               }
             }
+            if (valid) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              uint32_t y[4];
+              for (int v = 0; v < 2; ++v) {
+                uint32_t y[8];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) y[i] = Io::pack(x[8 * v + 2 * i] * inv, x[8 * v + 2 * i + 1] * inv);
-              *reinterpret_cast<uint4*>(out + lane * 128 + (((c / 8 + v) ^ (lane & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                for (int i = 0; i < 8; ++i) y[i] = Io::pack(x[16 * v + 2 * i] * inv, x[16 * v + 2 * i + 1] * inv);
+                T* to = dst + c + 16 * v;
+                if (o32) {
+                  st_global_v8(to, y);
+                } else {
+                  reinterpret_cast<uint4*>(to)[0] = make_uint4(y[0], y[1], y[2], y[3]);
+                  reinterpret_cast<uint4*>(to)[1] = make_uint4(y[4], y[5], y[6], y[7]);
+                }
+              }
             }
-          }
-          __syncwarp();
-#pragma unroll 4
-          for (int i = 0; i < 8; ++i) {
-            const int r = 4 * i + lane / 8, c = lane % 8;
-            const uint4 y = *reinterpret_cast<const uint4*>(out + r * 128 + ((c ^ (r & 7)) << 4));
-            const int64_t to = __shfl_sync(0xffffffffu, dst, r);
-            if ((live >> r) & 1) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.o) + to + h + 8 * c) = y;
-          }
-          __syncwarp();
         }
         if (valid && a.lse) {
           float lg;
@@ -603,8 +602,27 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_arrive(bars + B_PIECE + np % PIECES);
           }
           ++np;
-          auto load = [&](int t, bool v) {
-            const int kb = p.kb0 + t, st = ring % ST;
+          const int la = p.two ? 1 : 2;
+          // keys of la blocks, Q, then each block's values and the keys la blocks further.  The first keys go ahead of Q,
+          // whose place the last piece may still be using.
+#pragma unroll 1
+          for (int kt = 0, vt = 0, x = 0; ok && x < 2 * p.n; ++x) {
+            const bool key = kt < p.n && kt < vt + la;
+            if (x == min(la, p.n)) {
+              for (int t = 0; t <= p.two; ++t) {
+                const int slot = qi & 1;
+                if (qi > 1 && !wait(B_QE + slot, (qi >> 1) - 1)) break;
+                ++qi;
+                if (elect_one()) {
+                  mbar_arrive_expect_tx(bars + B_QF + slot, geo.tpt * a.group * HD * 2);
+                  for (int h = 0; h < NB; ++h)
+                    tma_load_3d(sQ + slot * TILE + h * (TB * 128), &maps.q, bars + B_QF + slot, 64 * h, p.h * a.group,
+                                p.q0 + t * geo.tpt);
+                }
+                __syncwarp();
+              }
+            }
+            const int kb = p.kb0 + (key ? kt++ : vt++), st = ring % ST;
             const int nbox = min(boxes, (p.kmax - kb * TB + geo.box_rows - 1) / geo.box_rows);
             int page = 0, at = 0;  // asked for before the stage is free
             if (lane < nbox) {
@@ -612,34 +630,15 @@ __global__ void __launch_bounds__(THREADS, 1)
               page = kv_page(b, seq, i / per, a.status);
               at = i % per;
             }
-            if (ring >= ST && !wait(B_EMPTY + st, ring / ST - 1)) return;
+            if (!ok || (ring >= ST && !wait(B_EMPTY + st, ring / ST - 1))) break;
             ++ring;
             if (lane == 0) mbar_arrive_expect_tx(bars + B_FULL + st, nbox * geo.box_rows * HD * 2);
             __syncwarp();
             if (lane < nbox)
-              tma_load_5d(sKV + st * TILE + lane * geo.box_rows * HD * 2, v ? &maps.v : &maps.k, bars + B_FULL + st,
+              tma_load_5d(sKV + st * TILE + lane * geo.box_rows * HD * 2, key ? &maps.k : &maps.v, bars + B_FULL + st,
                           geo.by_head ? p.h * NB : 0, at * (geo.box_rows / 8),
                           page < 0 ? -1 : geo.by_head ? page : page * geo.per_page + p.h);
             __syncwarp();
-          };
-          const int la = p.two ? 1 : 2;
-          // the first keys go ahead of Q, whose place the last piece may still be using
-          for (int t = 0; ok && t < min(p.n, la); ++t) load(t, false);
-          for (int t = 0; p.n > 0 && t <= p.two; ++t) {
-            const int slot = qi & 1;
-            if (!ok || (qi > 1 && !wait(B_QE + slot, (qi >> 1) - 1))) break;
-            ++qi;
-            if (elect_one()) {
-              mbar_arrive_expect_tx(bars + B_QF + slot, geo.tpt * a.group * HD * 2);
-              for (int h = 0; h < NB; ++h)
-                tma_load_3d(sQ + slot * TILE + h * (TB * 128), &maps.q, bars + B_QF + slot, 64 * h, p.h * a.group,
-                            p.q0 + t * geo.tpt);
-            }
-            __syncwarp();
-          }
-          for (int t = 0; ok && t < p.n; ++t) {
-            load(t, true);
-            if (ok && t + la < p.n) load(t + la, false);
           }
         } else {
           if (np >= PIECES && !wait(B_PDONE + np % PIECES, np / PIECES - 1)) break;
@@ -659,50 +658,43 @@ __global__ void __launch_bounds__(THREADS, 1)
         piece_done();
         if (p.end) break;
         const int la = p.two ? 1 : 2, first_sees = p.sees(0);
-        auto keys = [&]() {
-          if (wait(B_FULL + ring % ST, ring / ST) && lane == 0) mbar_arrive(bars + B_READY + ring % ST);
-          ++ring;
-        };
-        for (int t = 0; ok && t < min(p.n, la); ++t) keys();
-        for (int t = 0; ok && t < p.n; ++t) {
-          const int st = ring % ST, used = p.kmax - (p.kb0 + t) * TB;
-          uint4* sV = reinterpret_cast<uint4*>(sKV + st * TILE);
+#pragma unroll 1
+        for (int kt = 0, vt = 0, x = 0; ok && x < 2 * p.n; ++x, ++ring) {
+          const int st = ring % ST;
+          const bool key = kt < p.n && kt < vt + la;
+          const int kb = p.kb0 + (key ? kt++ : vt++), used = min(TB, p.kmax - kb * TB);
           if (!wait(B_FULL + st, ring / ST)) break;
-          const bool mixed = first_sees < min((p.kb0 + t + 1) * TB, p.kmax);
-          if (used < TB) {
-            for (int x = used * NB * 8 + lane; x < TILE / 16; x += 32) {
-              const int r = x / (NB * 8), c = x % (NB * 8);
+          uint4* sV = reinterpret_cast<uint4*>(sKV + st * TILE);
+          if (!key && used < TB) {
+#pragma unroll 1
+            for (int i = used * NB * 8 + lane; i < TILE / 16; i += 32) {
+              const int r = i / (NB * 8), c = i % (NB * 8);
               sV[(r >> 3) * NB * 64 + (c >> 3) * 64 + (r & 7) * 8 + (c & 7)] = make_uint4(0, 0, 0, 0);
             }
+            fence_proxy_async_smem();
             __syncwarp();
           }
-          bool odd = false;
-          if (mixed) {
+          if (!key && first_sees < kb * TB + used) {
             uint32_t top[4] = {0, 0, 0, 0};
-            for (int x = lane; x < (min(used, TB) + 7) / 8 * NB * 64; x += 256) {  // whole groups: NB * 64 a group, 256 a round
-              uint4 y[8];
+#pragma unroll 1
+            for (int i = lane; i < (used + 7) / 8 * NB * 64; i += 128) {  // whole groups of rows: NB * 64 each
+              uint4 y[4];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) y[i] = x + 32 * i < TILE / 16 ? sV[x + 32 * i] : make_uint4(0, 0, 0, 0);
+              for (int e = 0; e < 4; ++e) y[e] = i + 32 * e < TILE / 16 ? sV[i + 32 * e] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                if (x + 32 * i < (min(used, TB) + 7) / 8 * NB * 64) {
-                  top[0] = Io::max_abs(top[0], y[i].x);
-                  top[1] = Io::max_abs(top[1], y[i].y);
-                  top[2] = Io::max_abs(top[2], y[i].z);
-                  top[3] = Io::max_abs(top[3], y[i].w);
-                }
+              for (int e = 0; e < 4; ++e) {
+                if (i + 32 * e >= (used + 7) / 8 * NB * 64) break;
+                top[0] = Io::max_abs(top[0], y[e].x);
+                top[1] = Io::max_abs(top[1], y[e].y);
+                top[2] = Io::max_abs(top[2], y[e].z);
+                top[3] = Io::max_abs(top[3], y[e].w);
               }
             }
-            odd = __any_sync(0xffffffffu, !Io::finite(top[0]) || !Io::finite(top[1]) || !Io::finite(top[2]) || !Io::finite(top[3]));
+            const bool odd = __any_sync(0xffffffffu, !Io::finite(top[0]) || !Io::finite(top[1]) || !Io::finite(top[2]) ||
+                                                         !Io::finite(top[3]));
+            if (lane == 0) sh_odd[st] = odd;
           }
-          if (used < TB) fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            sh_odd[st] = odd;
-            mbar_arrive(bars + B_READY + st);
-          }
-          ++ring;
-          if (t + la < p.n) keys();
+          if (lane == 0) mbar_arrive(bars + B_READY + st);
         }
       }
     } else if (work) {
@@ -716,7 +708,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       // be uniform, so that it stays in uniform registers: the next stage and its phase, and counts.
       // Both streams see every stage and Q tile pass, in order, and free it with one arrival each: of those that it
       // does not read a stream waits for the copy only.  So no stream is ever two phases from a barrier's.
-      uint32_t st = 0, ph = 0, qn = 0, done = 0, uses = 0;
+      uint32_t st = 0, ph = 0, qn = 0, done = 0, uses = 0, lags = 0;
       auto step = [&]() {
         if (++st == ST) st = 0, ph ^= 1;
       };
@@ -726,13 +718,14 @@ __global__ void __launch_bounds__(THREADS, 1)
       };
       while (wait(B_PIECE + np % PIECES, np / PIECES)) {
         const Piece* pp = pieces + np % PIECES;
-        const int end = (int)uniform(pp->end), two = (int)uniform(pp->two), n = (int)uniform(pp->n), mine = (int)uniform(pp->na[s]);
+        const int end = (int)uniform(pp->end), two = (int)uniform(pp->two), n = (int)uniform(pp->n), mine = (int)uniform(pp->na[s]), lag = (int)uniform(s == 1 && pp->lag());
         piece_done();
         if (end) break;
         if (n == 0) continue;
         const uint32_t q = qn + (two ? s : 0);
         for (const uint32_t qe = qn + 1 + two; ok && qn < qe; ++qn)
           if (wait(B_QF + (qn & 1), qn >> 1) && (qn != q || mine == 0) && lane == 0) mbar_arrive(bars + B_QE + (qn & 1));
+        if (lag && !wait(B_LAG, lags++)) break;
         const uint64_t dq = desc_q + (q & 1) * (TILE / 16);
         // The ring holds the keys of la blocks, then each block's values and the keys la blocks further; with two tiles
         // la = 1 and each stream takes all that it sees, else la = 2 and the streams take every other block.

@@ -28,6 +28,7 @@ namespace {
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int STEP = 16;              // keys a warp takes at a time (one page holds them)
 constexpr int BK = WARPS * STEP;      // keys of a block
+constexpr int JOIN = 8;               // parts read at a time when a unit's are joined
 constexpr int MIN_COST = 2;           // blocks that are worth a CTA of their own
 constexpr float LOG2E_F = 1.4426950408889634f, LN2_F = 0.6931471805599453f;
 
@@ -71,7 +72,7 @@ struct RowUnits {  // tiles of `tt` tokens, blocks of BK keys
 };
 
 template <class T, int HD, int NR>
-__global__ void __launch_bounds__(THREADS) kv_attn_rows_kernel(KvAttnArgs a, int tt) {
+__global__ void __launch_bounds__(THREADS, NR == 1 ? 3 : 2) kv_attn_rows_kernel(KvAttnArgs a, int tt) {
   typedef KvIo<T> Io;
   constexpr int NJ = HD / 32;    // 16-byte pieces of a key that a lane reads
   constexpr int NH = HD / 64;    // ... of a value
@@ -82,7 +83,8 @@ __global__ void __launch_bounds__(THREADS) kv_attn_rows_kernel(KvAttnArgs a, int
   __shared__ int64_t sh_plan[WARPS + 3];
   __shared__ int sh_last;
   __shared__ float sh_m[WARPS][ROWS], sh_l[WARPS][ROWS];
-  __shared__ __align__(16) float sh_o[WARPS][ROWS][HD + 4];
+  extern __shared__ __align__(16) float sh_rows[];  // [WARPS][ROWS][HD + 4]
+  auto sh_o = [&](int v, int row) { return sh_rows + (v * ROWS + row) * (HD + 4); };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, c = lane & 3;
   const KvBatchDev& b = a.b;
@@ -299,7 +301,7 @@ __global__ void __launch_bounds__(THREADS) kv_attn_rows_kernel(KvAttnArgs a, int
         }
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
-          float* d = &sh_o[warp][row][64 * h + 8 * g];
+          float* d = sh_o(warp, row) + 64 * h + 8 * g;
 #pragma unroll
           for (int t = 0; t < 4; t += 2)
             *reinterpret_cast<float4*>(d + 2 * t) =
@@ -335,7 +337,7 @@ __global__ void __launch_bounds__(THREADS) kv_attn_rows_kernel(KvAttnArgs a, int
         const float f = sh_m[v][row] == -INFINITY ? 0.f : exp2_hw(sh_m[v][row] - mr);
         lr += f == 0.f ? 0.f : sh_l[v][row] * f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] += f == 0.f ? 0.f : sh_o[v][row][d0 + i] * f;
+        for (int i = 0; i < 8; ++i) x[i] += f == 0.f ? 0.f : sh_o(v, row)[d0 + i] * f;
       }
       if (whole) {
         finish(row, mr, lr, x);
@@ -349,9 +351,9 @@ __global__ void __launch_bounds__(THREADS) kv_attn_rows_kernel(KvAttnArgs a, int
     if (whole) continue;
     // ---- a unit in parts: the CTA that is done last joins them in their order
     const int f0 = rg.cta_of(w.start), f1 = rg.cta_of(w.start + nb - 1);
-    __threadfence();
     __syncthreads();
     if (tid == 0) {
+      __threadfence();  // the CTA's part is visible before the count
       sh_last = atomicInc(a.counters + f0, f1 - f0) == (unsigned)(f1 - f0);  // back at zero after the last
       __threadfence();
     }
@@ -364,25 +366,34 @@ __global__ void __launch_bounds__(THREADS) kv_attn_rows_kernel(KvAttnArgs a, int
       float mr = -INFINITY, lr = 0.f, x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = 0.f;
-      for (int f = f0; f <= f1; ++f) {
-        const int64_t at = (int64_t)(2 * f + (f == f0)) * ROWS + row;
-        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_ml) + at);
-        const float4 y0 = __ldcg(reinterpret_cast<const float4*>(part_o + at * HD + d0)),
-                     y1 = __ldcg(reinterpret_cast<const float4*>(part_o + at * HD + d0) + 1);
-        const float y[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
-        const float mn = fmaxf(mr, ml.x);
-        const float fo = mr == -INFINITY ? 0.f : exp2_hw(mr - mn), fn = ml.x == -INFINITY ? 0.f : exp2_hw(ml.x - mn);
-        mr = mn;
-        lr = (fo == 0.f ? 0.f : lr * fo) + (fn == 0.f ? 0.f : ml.y * fn);
+      for (int fb = f0; fb <= f1; fb += JOIN) {  // some at a time: the reads wait together
+        float2 ml[JOIN];
+        float4 y[JOIN][2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (fo == 0.f ? 0.f : x[i] * fo) + (fn == 0.f ? 0.f : y[i] * fn);
+        for (int e = 0; e < JOIN; ++e) {
+          const int f = min(fb + e, f1);
+          const int64_t at = (int64_t)(2 * f + (f == f0)) * ROWS + row;
+          ml[e] = __ldcg(reinterpret_cast<const float2*>(part_ml) + at);
+          y[e][0] = __ldcg(reinterpret_cast<const float4*>(part_o + at * HD + d0));
+          y[e][1] = __ldcg(reinterpret_cast<const float4*>(part_o + at * HD + d0) + 1);
+          if (fb + e > f1) ml[e].x = -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < JOIN; ++e) {
+          const float z[8] = {y[e][0].x, y[e][0].y, y[e][0].z, y[e][0].w, y[e][1].x, y[e][1].y, y[e][1].z, y[e][1].w};
+          const float mn = fmaxf(mr, ml[e].x);
+          const float fo = mr == -INFINITY ? 0.f : exp2_hw(mr - mn), fn = ml[e].x == -INFINITY ? 0.f : exp2_hw(ml[e].x - mn);
+          mr = mn;
+          lr = (fo == 0.f ? 0.f : lr * fo) + (fn == 0.f ? 0.f : ml[e].y * fn);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = (fo == 0.f ? 0.f : x[i] * fo) + (fn == 0.f ? 0.f : z[i] * fn);
+        }
       }
       finish(row, mr, lr, x);
     }
   } while (w.next(b, u, a.kvh) && w.start < rg.hi);
 }
 
-// CTAs of the kernel that the device holds at once, kept per process: one kind of device is supported.
 constexpr int CTAS_PER_SM = 3;
 
 // Rows of a sequence and key head that the warp-level fragments hold in one tile.  More go to the tensor-core tiles
@@ -391,8 +402,9 @@ bool few_rows(int group, int max_new) { return (int64_t)group * max_new <= 16; }
 
 template <class T, int HD, int NR>
 int launch_rows(const KvAttnArgs& a, cudaStream_t st) {
-  const int tt = 8 * NR / a.group;
-  FL_CUDA_TRY(fl_launch(kv_attn_rows_kernel<T, HD, NR>, dim3(CTAS_PER_SM * fl_sm_count()), dim3(THREADS), 0, st, a, tt));
+  const int tt = 8 * NR / a.group, smem = WARPS * 8 * NR * (HD + 4) * (int)sizeof(float);
+  FL_CUDA_TRY(fl_func_smem((const void*)kv_attn_rows_kernel<T, HD, NR>, smem));
+  FL_CUDA_TRY(fl_launch(kv_attn_rows_kernel<T, HD, NR>, dim3(CTAS_PER_SM * fl_sm_count()), dim3(THREADS), smem, st, a, tt));
   return FL_OK;
 }
 template <class T>

@@ -508,9 +508,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (valid) __stcg(part_ml + at * TB + row, make_float2(m, l));
         }
         release();
-        __threadfence();
         bar_sync(1 + s, 128);
         if (row == 0) {
+          __threadfence();  // the part is visible before the count
           sh_flag[2 + s] = atomicInc(a.counters + 2 * p.f_lo + s, f_hi - p.f_lo) == (unsigned)(f_hi - p.f_lo);
           __threadfence();
         }

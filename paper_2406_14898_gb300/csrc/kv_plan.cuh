@@ -3,8 +3,8 @@
 // no copy, no synchronisation and can be captured in a graph while the lengths change.
 //
 // A unit is (sequence, key / value head, tile of its new tokens); its work is its key blocks.  The units lie
-// one after another on a line, each as long as its cost (its blocks' and a constant for its ends), and CTA i
-// of G takes [i W / G, (i + 1) W / G) of the line's W: equal work whatever the lengths are.  A unit that lies
+// one after another on a line, each as long as its cost (its blocks' and a constant for its ends), and the line is
+// cut into G equal parts, one a CTA: equal work whatever the lengths are.  A unit that lies
 // in several CTAs' ranges is computed in parts, which the CTA that finishes last joins in their order, so
 // the result does not depend on which CTA that is.
 #pragma once
@@ -42,6 +42,11 @@ FL_DEV int kv_page(const KvBatchDev& b, int s, int i, int* status) {
   return -1;
 }
 
+// x / d in 32 bits where both fit (x >= 0, d > 0); the 64-bit division is a long way on this path.
+FL_DEV int64_t kv_div(int64_t x, int64_t d) {
+  return ((x | d) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)d) : x / d;
+}
+
 // Units of a sequence: U::units(q) tiles, U::cost(q, r) of tile r, for each of the kv heads.
 template <class U>
 struct KvWalk {
@@ -56,7 +61,7 @@ struct KvWalk {
     units = u.units(q);
     int64_t head = 0;
     for (int i = 0; i < units; ++i) head += u.cost(q, i);
-    h = (int)((at - seq_start) / head);
+    h = (int)kv_div(at - seq_start, head);
     start = seq_start + h * head;
     r = 0;
     cost = u.cost(q, 0);
@@ -83,13 +88,17 @@ struct KvWalk {
   }
 };
 
+// CTA i has [i q + min(i, r), (i + 1) q + min(i + 1, r)) with W = q G + r.
 struct KvRange {
-  int64_t lo, hi, W;
-  int G;               // CTAs with work
+  int64_t lo, hi, q;
+  int G, r;            // CTAs with work
   int s;               // sequence that holds lo, and where it starts
   int64_t seq_start;
-  FL_DEV int cta_of(int64_t x) const { return (int)(((x + 1) * G - 1) / W); }  // whose range holds x
-  FL_DEV int64_t lo_of(int i) const { return i * W / G; }
+  FL_DEV int cta_of(int64_t x) const {  // whose range holds x
+    const int64_t longer = r * (q + 1);
+    return (int)(x < longer ? kv_div(x, q + 1) : r + kv_div(x - longer, q));
+  }
+  FL_DEV int64_t lo_of(int i) const { return i * q + min(i, r); }
 };
 
 // The calling CTA's range; every thread of the CTA takes part.  At most `ctas` CTAs get work, and each
@@ -125,8 +134,9 @@ FL_DEV KvRange kv_plan(const KvBatchDev& b, const U& u, int kvh, int cta, int ct
     W += sh[w];
   }
   KvRange g;
-  g.W = W;
-  g.G = (int)max((int64_t)1, min((int64_t)ctas, W / min_cost));
+  g.G = (int)max((int64_t)1, min((int64_t)ctas, kv_div(W, min_cost)));
+  g.q = kv_div(W, g.G);
+  g.r = (int)(W - g.q * g.G);
   g.lo = g.hi = 0;
   g.s = -1;
   g.seq_start = 0;

@@ -289,7 +289,8 @@ int fl_k_rotary_table(int32_t max_pos, int32_t rotary_dim, float base, int32_t s
  * A position outside [0, max_pos) gives a row of zeros and sets FL_KV_BAD_POSITION.
  * Requirements (UNSUPPORTED): head_dim a multiple of 16 up to 256, rotary_dim a multiple of 16, the turned dims
  * within head_dim; strides multiples of 16 bytes; pointers 16-byte aligned (positions and status 4).
- * T = 0 does nothing.  A table row is [rotary_dim / 2] pairs. */
+ * T = 0 does nothing; T n_heads (and the append's rows, n_tokens (n_heads + 2 kv_heads)) below 2^31 (CAPACITY).  A
+ * table row is [rotary_dim / 2] pairs. */
 int fl_k_rotary(int32_t T, int32_t n_heads, int32_t head_dim, int32_t rotary_dim, int32_t layout, int32_t backward,
                 int32_t dtype, const void* x, int64_t ldx, int64_t x_head_stride, void* y, int64_t ldy,
                 int64_t y_head_stride, const int32_t* positions, const int32_t* block_positions,

@@ -1,0 +1,270 @@
+"""Answering token by token with a trained split model.
+
+A client embeds its new tokens and runs block 0, the server runs blocks 1..N-2, the client runs block N-1, the
+final LayerNorm and the LM head and picks the next token: the protocol of the paper's §3.1 without its
+backward.  Each part keeps the keys and values of the tokens before in a paged cache, so a call carries only
+new tokens: a whole prompt, a part of one, or the one token chosen last.
+
+``BlockStack`` is one part: blocks of a ``Server`` or of a ``Client`` as ``forward`` over packed new
+tokens, from the library's entry points (``fl_k_layernorm_fwd``, ``fl_k_gemm``, ``fl_k_kv_append``,
+``fl_k_kv_attention``).  Its arithmetic is that of ``fl_server_forward``, except that queries and keys are
+rounded to bf16 before their rotation and not only after it.
+
+    python -m paper_2406_14898_gb300.generate --tokens 16
+
+runs a small split model with randomly initialised weights: three clients with prompts of different
+lengths answer together.
+"""
+from __future__ import annotations
+
+import argparse
+from typing import List, Optional, Sequence
+
+import torch
+
+from . import flglm as F
+
+BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+class Pages:
+    """Which pages of the caches belong to which sequence; one table for every block of a stack."""
+
+    def __init__(self, n_pages: int, page_size: int, n_seqs: int, max_tokens: int):
+        self.page_size, self.free = page_size, list(range(n_pages - 1, -1, -1))
+        self.held: List[List[int]] = [[] for _ in range(n_seqs)]
+        self.lens = [0] * n_seqs
+        self.table = torch.full((n_seqs, max(1, -(-max_tokens // page_size))), -1, dtype=I32)
+
+    def extend(self, new: Sequence[int]):
+        """Room for new[s] more tokens of each sequence."""
+        for s, n in enumerate(new):
+            need = -(-(self.lens[s] + n) // self.page_size)
+            if need > self.table.shape[1]:
+                raise ValueError(f"sequence {s} is longer than {self.table.shape[1] * self.page_size} tokens")
+            if need - len(self.held[s]) > len(self.free):
+                raise MemoryError("no page is free")
+            while len(self.held[s]) < need:
+                self.table[s, len(self.held[s])] = self.free[-1]
+                self.held[s].append(self.free.pop())
+            self.lens[s] += n
+
+    def drop(self, s: int):
+        """Forgets sequence s; its pages serve others, uncleared."""
+        self.free += self.held[s]
+        self.held[s], self.lens[s] = [], 0
+        self.table[s] = -1
+
+
+class BlockStack:
+    """The blocks of one part of the model, with a key / value cache each, on the current CUDA device."""
+
+    def __init__(self, cfg: "F.fl_server_cfg", blocks, n_seqs: int, max_tokens: int, page_size: int = 64,
+                 n_pages: Optional[int] = None):
+        """cfg: the shapes (of ``make_cfg``); blocks: for each a function tensor id -> fp32 numpy values
+        (``FL_T_*``); max_tokens: most tokens of a sequence, its prefix included."""
+        c = self.cfg = cfg
+        H, Fh, P = c.hidden, c.ffn_hidden, c.prefix_len
+        self.rdim = c.rotary_dim or c.head_dim // 2
+        width = -(-max_tokens // page_size)
+        self.n_pages = n_seqs * width if n_pages is None else n_pages
+        self.pages = Pages(self.n_pages, page_size, n_seqs, max_tokens)
+
+        def dev(x, *shape):
+            return torch.from_numpy(x).cuda().view(*shape)
+
+        self.blocks = []
+        for get in blocks:
+            b = {"w": [dev(get(t), *s).to(BF16) for t, s in ((F.FL_T_WQKV, (3 * H, H)), (F.FL_T_WDENSE, (H, H)),
+                                                             (F.FL_T_WUP, (Fh, H)), (F.FL_T_WDOWN, (H, Fh)))],
+                 "b": [dev(get(t), -1) for t in (F.FL_T_BQKV, F.FL_T_BDENSE, F.FL_T_BUP, F.FL_T_BDOWN)],
+                 "ln": [dev(get(t), H) for t in (F.FL_T_LN1_G, F.FL_T_LN1_B, F.FL_T_LN2_G, F.FL_T_LN2_B)],
+                 "prefix": [dev(get(t), P, H).to(BF16) for t in (F.FL_T_PREFIX_K, F.FL_T_PREFIX_V)] if P else None,
+                 # handed out uncleared
+                 "kv": [torch.empty((self.n_pages, c.n_heads, page_size, c.head_dim), dtype=BF16, device="cuda")
+                        for _ in "kv"]}
+            b["cache"] = F.kv_cache(b["kv"][0], b["kv"][1], self.n_pages, page_size, c.n_heads, c.head_dim)
+            self.blocks.append(b)
+        self.max_pos = max_tokens + 1
+        self.rope = torch.empty((self.max_pos, self.rdim // 2, 2), device="cuda")
+        F.fl_k_rotary_table(self.max_pos, self.rdim, c.rope_base, self.rope)
+        self.status = torch.zeros(1, dtype=I32, device="cuda")
+        self.workspace = None
+        self.context = [0] * n_seqs   # context lengths, prefix included; 0: plainly causal
+        self.mask_pos = [0] * n_seqs
+
+    @classmethod
+    def from_server(cls, srv: "F.Server", n_seqs: int, max_tokens: int, **kw):
+        return cls(srv.cfg, [lambda t, b=b: srv.get_param(b, t) for b in range(srv.cfg.n_blocks)], n_seqs, max_tokens, **kw)
+
+    @classmethod
+    def from_client(cls, client: "F.Client", part: int, n_seqs: int, max_tokens: int, **kw):
+        """part: FL_CP_BOTTOM or FL_CP_TOP."""
+        return cls(client.cfg.block, [lambda t: client.get_param(part, t)], n_seqs, max_tokens, **kw)
+
+    def start(self, s: int, context_len: int = 0, mask_pos: Optional[int] = None):
+        """A new sequence in place s: its first context_len tokens see each other (GLM blank infilling, §4.1.1, the
+        mask token at mask_pos or last among them) and the rest follow causally."""
+        self.pages.drop(s)
+        P = self.cfg.prefix_len
+        self.context[s] = context_len + P if context_len else 0
+        self.mask_pos[s] = context_len - 1 if mask_pos is None else mask_pos
+        if P:  # the P-tuning prefix takes the first places of the cache; its keys are not turned
+            batch, keep = self._batch([P if i == s else 0 for i in range(len(self.context))])
+            for b in self.blocks:
+                F.fl_k_kv_append(b["cache"], batch, self.cfg.n_heads, None, *b["prefix"], None, None, 0, self.status)
+            del keep
+
+    def _batch(self, new):
+        self.pages.extend(new)
+        cu = [0]
+        for n in new:
+            cu.append(cu[-1] + n)
+        keep = [torch.tensor(cu, dtype=I32).cuda(), torch.tensor(self.pages.lens, dtype=I32).cuda(),
+                self.pages.table.cuda()]
+        return F.kv_batch(len(new), cu[-1], max(new), *keep, self.pages.table.shape[1]), keep
+
+    def _positions(self, new):
+        """The two position streams of the new tokens: (i, 0) in the context, (mask, 1 ..) in the span."""
+        first, second = [], []
+        for s, n in enumerate(new):
+            c = self.context[s] - self.cfg.prefix_len if self.context[s] else 0
+            for i in range(self.pages.lens[s] - n - self.cfg.prefix_len, self.pages.lens[s] - self.cfg.prefix_len):
+                span = c > 0 and i >= c
+                first.append(self.mask_pos[s] if span else i)
+                second.append(i - c + 1 if span else 0)
+        two = any(self.context)
+        return torch.tensor(first, dtype=I32).cuda(), torch.tensor(second, dtype=I32).cuda() if two else None
+
+    def forward(self, x: torch.Tensor, new: Sequence[int]) -> torch.Tensor:
+        """x: bf16 [sum(new), hidden], new[s] next tokens of sequence s; returns the blocks' output of them.  A context's
+        tokens come in one call, as they see each other."""
+        c, T, H, Fh = self.cfg, sum(new), self.cfg.hidden, self.cfg.ffn_hidden
+        batch, keep = self._batch(list(new))
+        pos, pos2 = self._positions(new)
+        context = torch.tensor(self.context, dtype=I32).cuda() if pos2 is not None else None
+        size = F.fl_k_kv_attention_workspace(c.n_heads, self.blocks[0]["cache"], batch)
+        if self.workspace is None or self.workspace.numel() * 4 < size:
+            self.workspace = torch.zeros(-(-size // 4), dtype=I32, device="cuda")
+        x = x.float()
+        a, o, g, u = (torch.empty((T, n), dtype=BF16, device="cuda") for n in (H, H, Fh, Fh))
+        qkv = torch.empty((T, 3 * H), dtype=BF16, device="cuda")
+        stats = torch.empty((2, T), device="cuda")
+        status = torch.zeros(1, dtype=I32, device="cuda")
+
+        def norm(x, gamma, beta):
+            F.fl_k_layernorm_fwd(T, H, x, gamma, beta, c.ln_eps, a, stats[0], stats[1], x_dtype=F.FL_DT_F32)
+
+        def residual(M, K, inp, w, bias, x, gamma, beta):
+            """alpha * (LN(x) or x) + inp w^T + bias in fp32."""
+            y = torch.empty((T, H), device="cuda")
+            ln = dict(ln_mean=stats[0], ln_rstd=stats[1], ln_gamma=gamma, ln_beta=beta) if c.residual_from_ln else {}
+            F.gemm(M, H, K, inp, K, 0, w, K, 0, y, H, status=status, epilogue=F.FL_EPI_BIAS_RESID, bias=bias, aux=x,
+                   ld_aux=H, aux_dtype=F.FL_DT_F32, d_dtype=F.FL_DT_F32, alpha=c.residual_alpha, **ln)
+            return y
+
+        for b in self.blocks:
+            (w_qkv, w_dense, w_up, w_down), (b_qkv, b_dense, b_up, b_down) = b["w"], b["b"]
+            norm(x, *b["ln"][:2])
+            F.gemm(T, 3 * H, H, a, H, 0, w_qkv, H, 0, qkv, 3 * H, status=status, bias=b_qkv)
+            q = qkv.data_ptr()  # the queries are turned in place
+            F.fl_k_kv_append(b["cache"], batch, c.n_heads, q, q + 2 * H, q + 4 * H, q, self.rope, self.max_pos,
+                             self.status, rotary_dim=self.rdim, positions=pos, block_positions=pos2, ldq=3 * H,
+                             ldk=3 * H, ldv=3 * H, ldqo=3 * H)
+            F.fl_k_kv_attention(b["cache"], batch, c.n_heads, q, o, self.workspace, self.status, context_lens=context,
+                                ldq=3 * H)
+            h = residual(T, H, o, w_dense, b_dense, x, *b["ln"][:2])
+            norm(h, *b["ln"][2:])
+            F.gemm(T, Fh, H, a, H, 0, w_up, H, 0, g, Fh, status=status, epilogue=F.FL_EPI_BIAS_GELU, bias=b_up, aux_out=u,
+                   ld_aux_out=Fh)
+            x = residual(T, Fh, g, w_down, b_down, h, *b["ln"][2:])
+        if int(status.item()) or int(self.status.item()):
+            raise RuntimeError(f"generation: device status {int(status.item())}, cache status {int(self.status.item())}")
+        del keep
+        return x.to(BF16)
+
+
+class Generator:
+    """Clients that answer together: each has its own ends of the model, the server serves all in one call."""
+
+    def __init__(self, clients: Sequence["F.Client"], server: "F.Server", max_tokens: int):
+        self.clients, n = list(clients), len(clients)
+        self.server = BlockStack.from_server(server, n, max_tokens)
+        self.bottom = [BlockStack.from_client(c, F.FL_CP_BOTTOM, 1, max_tokens) for c in clients]
+        self.top = [BlockStack.from_client(c, F.FL_CP_TOP, 1, max_tokens) for c in clients]
+        self.ends = []
+        for c in clients:
+            H, V = c.cfg.block.hidden, c.cfg.vocab
+            head = torch.zeros((-(-V // 128) * 128, H), dtype=BF16, device="cuda")  # rows in whole GEMM tiles
+            head[:V] = torch.from_numpy(c.get_param(F.FL_CP_HEAD, 0)).cuda().view(V, H).to(BF16)
+            self.ends.append({"embed": torch.from_numpy(c.get_param(F.FL_CP_EMBED, 0)).cuda().view(V, H).to(BF16),
+                              "head": head, "ln": [torch.from_numpy(c.get_param(F.FL_CP_FINAL_LN, t)).cuda() for t in (0, 1)]})
+
+    def start(self, context_lens: Optional[Sequence[int]] = None):
+        for k in range(len(self.clients)):
+            c = 0 if context_lens is None else context_lens[k]
+            self.server.start(k, c)
+            self.bottom[k].start(0, c)
+            self.top[k].start(0, c)
+
+    def logits(self, tokens: Sequence[torch.Tensor]) -> List[torch.Tensor]:
+        """fp32 logits after each client's new tokens (int32 on the device), [vocab] of the last one."""
+        hs = []
+        for c, e, stack, t in zip(self.clients, self.ends, self.bottom, tokens):
+            h = torch.empty((len(t), c.cfg.block.hidden), dtype=BF16, device="cuda")
+            F.fl_k_embedding_gather(len(t), h.shape[1], t, e["embed"], c.cfg.vocab, h, stack.status)
+            hs.append(stack.forward(h, [len(t)]))
+        mid = self.server.forward(torch.cat(hs), [len(t) for t in tokens]).split([len(t) for t in tokens])
+        out = []
+        for c, e, stack, h in zip(self.clients, self.ends, self.top, mid):
+            H, n = h.shape[1], e["head"].shape[0]
+            last = stack.forward(h, [len(h)])[-1:].contiguous()
+            y, stats = torch.empty_like(last), torch.empty(2, device="cuda")
+            F.fl_k_layernorm_fwd(1, H, last, *e["ln"], c.cfg.block.ln_eps, y, stats[:1], stats[1:])
+            z = torch.empty((1, n), device="cuda")
+            F.gemm(1, n, H, y, H, 0, e["head"], H, 0, z, n, d_dtype=F.FL_DT_F32)
+            out.append(z[0, :c.cfg.vocab])
+        return out
+
+    def greedy(self, prompts: Sequence[torch.Tensor], count: int) -> List[List[int]]:
+        """`count` next tokens after each prompt (int32 on the device), the likeliest each time."""
+        self.start([len(p) for p in prompts])
+        answers: List[List[int]] = [[] for _ in prompts]
+        tokens = list(prompts)
+        for _ in range(count):
+            tokens = [z.argmax().to(I32).view(1) for z in self.logits(tokens)]
+            for a, t in zip(answers, tokens):
+                a.append(int(t))
+        return answers
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--tokens", type=int, default=16, help="tokens to answer with")
+    ap.add_argument("--prompts", type=int, nargs="+", default=[40, 9, 130], help="prompt lengths, one a client")
+    ap.add_argument("--hidden", type=int, default=256)
+    ap.add_argument("--head-dim", type=int, default=64)
+    ap.add_argument("--blocks", type=int, default=2, help="server blocks")
+    ap.add_argument("--vocab", type=int, default=1000)
+    ap.add_argument("--seed", type=int, default=0)
+    a = ap.parse_args(argv)
+    room = max(a.prompts) + a.tokens
+    cfg, cc = F.fl_server_cfg(), F.fl_client_cfg()
+    F.lib().fl_server_cfg_default(cfg)
+    cfg.n_blocks, cfg.hidden, cfg.head_dim, cfg.n_heads = a.blocks, a.hidden, a.head_dim, a.hidden // a.head_dim
+    cfg.rotary_dim, cfg.ffn_hidden, cfg.max_tokens = 0, 4 * a.hidden, room
+    cfg.residual_alpha = (2.0 * (a.blocks + 2)) ** 0.5
+    F.lib().fl_client_cfg_default(cc)
+    cc.block, cc.vocab = cfg, a.vocab
+    cc.block.n_blocks = 1
+    clients = [F.Client(cc, a.seed + 1) for _ in a.prompts]  # the same model, as after averaging
+    gen = torch.Generator().manual_seed(a.seed)
+    prompts = [torch.randint(a.vocab, (n,), generator=gen, dtype=I32).cuda() for n in a.prompts]
+    answers = Generator(clients, F.Server(cfg, a.seed), room).greedy(prompts, a.tokens)
+    for k, x in enumerate(answers):
+        print(f"client {k} ({a.prompts[k]} tokens): {' '.join(map(str, x))}")
+    return answers
+
+
+if __name__ == "__main__":
+    main()

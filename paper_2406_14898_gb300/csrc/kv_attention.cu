@@ -80,7 +80,6 @@ __global__ void __launch_bounds__(THREADS, NR == 1 ? 3 : 2) kv_attn_rows_kernel(
   constexpr int LANES = HD / 8;  // threads of a row when the warps' results are joined
   pdl_wait();  // the previous kernel on the stream has completed (see fl_launch)
   pdl_trigger();
-  __shared__ int64_t sh_plan[WARPS + 3];
   __shared__ int sh_last;
   __shared__ float sh_m[WARPS][ROWS], sh_l[WARPS][ROWS];
   extern __shared__ __align__(16) float sh_rows[];  // [WARPS][ROWS][HD + 4]
@@ -89,7 +88,7 @@ __global__ void __launch_bounds__(THREADS, NR == 1 ? 3 : 2) kv_attn_rows_kernel(
   const int g = lane >> 2, c = lane & 3;
   const KvBatchDev& b = a.b;
   const RowUnits u{tt};
-  const KvRange rg = kv_plan<THREADS>(b, u, a.kvh, blockIdx.x, gridDim.x, MIN_COST, sh_plan);
+  const KvRange rg = kv_plan(b, u, a.kvh, blockIdx.x, gridDim.x, MIN_COST);
   if (rg.s < 0) return;
   const T* K = reinterpret_cast<const T*>(a.k);
   const T* V = reinterpret_cast<const T*>(a.v);

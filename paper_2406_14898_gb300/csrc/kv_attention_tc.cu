@@ -259,7 +259,6 @@ __global__ void __launch_bounds__(THREADS, 1)
     BARS = B_END + 2
   };
   static_assert(BARS * 8 <= 400 && sizeof(Piece) * PIECES <= 384, "control block");
-  int64_t* sh_plan = reinterpret_cast<int64_t*>(ctrl + 400);            // 15 of them
   volatile int* sh_flag = reinterpret_cast<volatile int*>(ctrl + 528);  // [0, 2) slow block, [2, 4) last part, [4] failed
   volatile int* sh_odd = sh_flag + 8;                                   // [stage] the block has infinities or NaN
   uint32_t* holder = reinterpret_cast<uint32_t*>(ctrl + 592);
@@ -292,9 +291,6 @@ __global__ void __launch_bounds__(THREADS, 1)
   pdl_trigger();
 
   const TileUnits u{geo.tpt};
-  const KvRange rg = kv_plan<THREADS>(b, u, a.kvh, blockIdx.x, gridDim.x, MIN_COST, sh_plan);
-  const bool work = rg.s >= 0;
-
   bool ok = true;
   // by a whole warp; phase: the number of the barrier's phase waited for
   auto wait = [&](int i, uint32_t phase) {
@@ -331,7 +327,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(bars + i);
     };
-    while (work) {
+    while (true) {
       // the whole warpgroup goes on, or none of it
       if (bar_or(1 + s, 128, !wait(B_PIECE + np % PIECES, np / PIECES))) break;
       const Piece p = pieces[np % PIECES];
@@ -518,11 +514,20 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!sh_flag[2 + s]) continue;
         m = -INFINITY;
         l = 0.f;
-        for (int f = p.f_lo; valid && f <= f_hi; ++f) {
-          const float2 x = __ldcg(part_ml + part(f, f == p.f_lo) * TB + row);
-          const float mn = fmaxf(m, x.x);
-          l = (m == -INFINITY ? 0.f : l * exp2_hw(m - mn)) + (x.x == -INFINITY ? 0.f : x.y * exp2_hw(x.x - mn));
-          m = mn;
+        for (int fb = p.f_lo; valid && fb <= f_hi; fb += 4) {  // the reads of four wait together
+          float2 x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int f = min(fb + e, f_hi);
+            x[e] = __ldcg(part_ml + part(f, f == p.f_lo) * TB + row);
+            if (fb + e > f_hi) x[e].x = -INFINITY;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float mn = fmaxf(m, x[e].x);
+            l = (m == -INFINITY ? 0.f : l * exp2_hw(m - mn)) + (x[e].x == -INFINITY ? 0.f : x[e].y * exp2_hw(x[e].x - mn));
+            m = mn;
+          }
         }
       }
       // ---- the output
@@ -532,47 +537,50 @@ __global__ void __launch_bounds__(THREADS, 1)
         inv = l == 0.f ? 0.f : inv;
         T* dst = reinterpret_cast<T*>(a.o) + t_row * a.ldo + head * HD;
 #pragma unroll 1
-        for (int c = 0; c < HD; c += 32) {
-            float x[32];
-            if (nb == 0) {  // rows that see nothing
+        for (int c = 0; c < HD; c += 64) {
+          float x[64];
+          if (nb == 0) {  // rows that see nothing
 #pragma unroll
-              for (int e = 0; e < 32; ++e) x[e] = 0.f;
-            } else if (whole) {
-              own(c, x);
-            } else {
+            for (int e = 0; e < 64; ++e) x[e] = 0.f;
+          } else if (whole) {
+            own(c, *reinterpret_cast<float(*)[32]>(x));
+            own(c + 32, *reinterpret_cast<float(*)[32]>(x + 32));
+          } else {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) x[e] = 0.f;
+            for (int e = 0; e < 64; ++e) x[e] = 0.f;
 #pragma unroll 1
-              for (int f = p.f_lo; valid && f <= f_hi; ++f) {
-                const int64_t q = part(f, f == p.f_lo);
-                const float mf = __ldcg(part_ml + q * TB + row).x;
-                if (mf == -INFINITY) continue;
-                const float w = exp2_hw(mf - m);
+            for (int f = p.f_lo; valid && f <= f_hi; ++f) {
+              const int64_t q = part(f, f == p.f_lo);
+              const float mf = __ldcg(part_ml + q * TB + row).x;
+              float4 y[16];
 #pragma unroll
-                for (int v = 0; v < 8; ++v) {
-                  const float4 y = __ldcg(part_o + (q * (HD / 4) + c / 4 + v) * TB + row);
-                  x[4 * v] = fmaf(y.x, w, x[4 * v]);
-                  x[4 * v + 1] = fmaf(y.y, w, x[4 * v + 1]);
-                  x[4 * v + 2] = fmaf(y.z, w, x[4 * v + 2]);
-                  x[4 * v + 3] = fmaf(y.w, w, x[4 * v + 3]);
-                }
+              for (int v = 0; v < 16; ++v) y[v] = __ldcg(part_o + (q * (HD / 4) + c / 4 + v) * TB + row);
+              if (mf == -INFINITY) continue;
+              const float w = exp2_hw(mf - m);
+#pragma unroll
+              for (int v = 0; v < 16; ++v) {
+                x[4 * v] = fmaf(y[v].x, w, x[4 * v]);
+                x[4 * v + 1] = fmaf(y[v].y, w, x[4 * v + 1]);
+                x[4 * v + 2] = fmaf(y[v].z, w, x[4 * v + 2]);
+                x[4 * v + 3] = fmaf(y[v].w, w, x[4 * v + 3]);
               }
             }
-            if (valid) {
+          }
+          if (valid) {
 #pragma unroll
-              for (int v = 0; v < 2; ++v) {
-                uint32_t y[8];
+            for (int v = 0; v < 4; ++v) {
+              uint32_t y[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = Io::pack(x[16 * v + 2 * i] * inv, x[16 * v + 2 * i + 1] * inv);
-                T* to = dst + c + 16 * v;
-                if (o32) {
-                  st_global_v8(to, y);
-                } else {
-                  reinterpret_cast<uint4*>(to)[0] = make_uint4(y[0], y[1], y[2], y[3]);
-                  reinterpret_cast<uint4*>(to)[1] = make_uint4(y[4], y[5], y[6], y[7]);
-                }
+              for (int i = 0; i < 8; ++i) y[i] = Io::pack(x[16 * v + 2 * i] * inv, x[16 * v + 2 * i + 1] * inv);
+              T* to = dst + c + 16 * v;
+              if (o32) {
+                st_global_v8(to, y);
+              } else {
+                reinterpret_cast<uint4*>(to)[0] = make_uint4(y[0], y[1], y[2], y[3]);
+                reinterpret_cast<uint4*>(to)[1] = make_uint4(y[4], y[5], y[6], y[7]);
               }
             }
+          }
         }
         if (valid && a.lse) {
           float lg;
@@ -583,11 +591,12 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (whole && nb > 0) release();
     }
   } else {
-    if (work && warp == W_TMA) {
+    if (warp == W_TMA) {
+      const KvRange rg = kv_plan(b, u, a.kvh, blockIdx.x, gridDim.x, MIN_COST);
       KvWalk<TileUnits> k;
-      k.set(b, u, rg.s, rg.seq_start, rg.lo, a.kvh);
+      bool more = rg.s >= 0;
+      if (more) k.set(b, u, rg.s, rg.seq_start, rg.lo, a.kvh);
       const int boxes = TB / geo.box_rows, per = (1 << b.ps_log2) / geo.box_rows;  // boxes of a block, of a page
-      bool more = true;
       while (ok) {
         Piece p;
         p.end = !more;
@@ -649,7 +658,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           break;
         }
       }
-    } else if (work && warp == W_FIX) {
+    } else if (warp == W_FIX) {
       // A key that a row does not see has weight 0, which only makes nothing of it if its value is finite.  Rows of a V
       // block past the last key that anyone sees hold whatever the page held: they become zeros.  The others are
       // looked through where rows differ in what they see.
@@ -697,7 +706,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (lane == 0) mbar_arrive(bars + B_READY + st);
         }
       }
-    } else if (work) {
+    } else {
       const int s = (int)uniform(warp - W_MMA);  // the stream
       const uint32_t tm = uniform(tmem);
       const uint64_t desc_q = smem_desc_sw128(smem_u32(sQ), 16, 1024), desc_k = smem_desc_sw128(smem_u32(sKV), 16, NB * 1024),

@@ -101,14 +101,12 @@ struct KvRange {
   FL_DEV int64_t lo_of(int i) const { return i * q + min(i, r); }
 };
 
-// The calling CTA's range; every thread of the CTA takes part.  At most `ctas` CTAs get work, and each
-// that does at least about min_cost.  sh: THREADS / 32 + 3 int64 of shared memory, free after the CTA's next barrier.
-template <int THREADS, class U>
-FL_DEV KvRange kv_plan(const KvBatchDev& b, const U& u, int kvh, int cta, int ctas, int min_cost, int64_t* sh) {
-  constexpr int WARPS = THREADS / 32;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (b.S + THREADS - 1) / THREADS;
-  const int s0 = tid * per, s1 = min(b.S, s0 + per);
+// CTA `cta`'s range, by a whole warp (each that needs it computes it: the arrays are short, a barrier is not).  At most
+// `ctas` CTAs get work, and each that does at least about min_cost.
+template <class U>
+FL_DEV KvRange kv_plan(const KvBatchDev& b, const U& u, int kvh, int cta, int ctas, int min_cost) {
+  const int lane = threadIdx.x & 31, per = (b.S + 31) / 32;
+  const int s0 = lane * per, s1 = min(b.S, s0 + per);
   auto seq_cost = [&](int s) {
     const KvSeq q = kv_seq(b, s);
     int64_t c = 0;
@@ -124,15 +122,7 @@ FL_DEV KvRange kv_plan(const KvBatchDev& b, const U& u, int kvh, int cta, int ct
     const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += x;
   }
-  if (lane == 31) sh[warp] = incl;
-  if (tid == 0) sh[WARPS] = -1;
-  __syncthreads();
-  int64_t before = 0, W = 0;
-#pragma unroll
-  for (int w = 0; w < WARPS; ++w) {
-    if (w < warp) before += sh[w];
-    W += sh[w];
-  }
+  const int64_t W = __shfl_sync(0xffffffffu, incl, 31);
   KvRange g;
   g.G = (int)max((int64_t)1, min((int64_t)ctas, kv_div(W, min_cost)));
   g.q = kv_div(W, g.G);
@@ -140,20 +130,17 @@ FL_DEV KvRange kv_plan(const KvBatchDev& b, const U& u, int kvh, int cta, int ct
   g.lo = g.hi = 0;
   g.s = -1;
   g.seq_start = 0;
-  if (W == 0 || cta >= g.G) return g;  // the whole CTA
+  if (W == 0 || cta >= g.G) return g;
   g.lo = g.lo_of(cta);
   g.hi = g.lo_of(cta + 1);
-  int64_t at = before + incl - mine;
-  if (g.lo >= at && g.lo < at + mine) {
-    int s = s0;
-    if (per > 1)
-      for (one = seq_cost(s); g.lo >= at + one; one = seq_cost(++s)) at += one;
-    sh[WARPS] = s;
-    sh[WARPS + 1] = at;
-  }
-  __syncthreads();
-  g.s = (int)sh[WARPS];
-  g.seq_start = sh[WARPS + 1];
+  int64_t at = incl - mine;
+  const bool here = g.lo >= at && g.lo < incl;
+  int s = s0;
+  if (here && per > 1)
+    for (one = seq_cost(s); g.lo >= at + one; one = seq_cost(++s)) at += one;
+  const int from = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+  g.s = __shfl_sync(0xffffffffu, s, from);
+  g.seq_start = __shfl_sync(0xffffffffu, at, from);
   return g;
 }
 

@@ -16,6 +16,7 @@
 // Work is divided among the CTAs as kv_plan.cuh says.
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/flglm_kernels.h"
@@ -163,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, NR == 1 ? 3 : 2) kv_attn_rows_kernel(
         for (int h = 0; h < NH; ++h) vf[i][h] = on ? ld_once(p + k * a.token_stride + 64 * h) : make_uint4(0, 0, 0, 0);
       }
     };
-    auto page_of = [&](int key) { return key < key_end ? kv_page(b, w.s, key >> b.ps_log2, a.status) : -1; };
+    auto page_of = [&](int key) { return key < key_end ? kv_page(b, w.s, key >> b.ps_log2) : -1; };
 
     int key = kb0 * BK + warp * STEP;
     int page = page_of(key), page_n = page_of(key + BK);
@@ -422,10 +423,9 @@ extern "C" size_t fl_k_kv_attention_workspace(int32_t n_heads, const fl_kv_cache
     fl_internal_error(FL_ERR_UNSUPPORTED, "kv attention: %d query heads per key head", group);
     return 0;
   }
-  const size_t parts = few_rows(group, batch->max_new)
-                           ? (size_t)CTAS_PER_SM * fl_sm_count() * 2 * 16 * (cache->head_dim + 2) * sizeof(float)
-                           : fl_kv_attention_tc_parts(cache->head_dim);
-  return KV_COUNTERS * sizeof(unsigned) + parts;
+  // enough for either kernel, so that it fits every batch of the cache
+  const size_t rows = (size_t)CTAS_PER_SM * fl_sm_count() * 2 * 16 * (cache->head_dim + 2) * sizeof(float);
+  return KV_COUNTERS * sizeof(unsigned) + std::max(rows, fl_kv_attention_tc_parts(cache->head_dim));
 }
 
 extern "C" int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n_heads, const void* q,
@@ -455,7 +455,7 @@ extern "C" int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* ba
   a.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)cache->head_dim) : scale) * LOG2E_F;
   a.counters = (unsigned*)workspace;
   a.parts = (float*)((unsigned*)workspace + KV_COUNTERS);
-  a.status = status;
+  a.b.status = status;
   if (!few_rows(a.group, batch->max_new)) return fl_launch_kv_attention_tc(cache, a, n_heads, (cudaStream_t)stream);
   const int rows = batch->max_new * a.group;
   return (cache->dtype == FL_DT_F16 ? dispatch_rows<__half> : dispatch_rows<__nv_bfloat16>)(

@@ -17,7 +17,6 @@ struct KvAttnArgs {
   float scale_log2;
   unsigned* counters;
   float* parts;
-  int* status;
 };
 
 template <class T>
@@ -49,6 +48,6 @@ struct KvIo<__half> {
   FL_DEV static bool finite(uint32_t x) { return (x & 0x7c00u) != 0x7c00u && (x & 0x7c000000u) != 0x7c000000u; }
 };
 
-// Chunks of new tokens (kv_attention_tc.cu); parts: bytes of a workspace's parts that it uses.
+// Chunks of new tokens (kv_attention_tc.cu); _parts: bytes of a workspace's parts that it uses.
 size_t fl_kv_attention_tc_parts(int head_dim);
 int fl_launch_kv_attention_tc(const fl_kv_cache* c, const KvAttnArgs& a, int heads, cudaStream_t st);

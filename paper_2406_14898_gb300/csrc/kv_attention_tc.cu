@@ -36,7 +36,7 @@ namespace {
 constexpr int TB = 128;
 constexpr int THREADS = 384, W_TMA = 8, W_MMA = 9, W_FIX = 11;
 constexpr int LAG_BLOCKS = 6;
-constexpr int ENDS = 5;      // cost of a unit's ends (Q, the first scores, the output), in blocks of one tile
+constexpr int ENDS = 4;      // cost of a unit's ends (Q, the first scores, the output), in blocks of one tile
 constexpr int MIN_COST = 4;
 constexpr float LN2_F = 0.6931471805599453f;
 
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (ok && !wait_longer(bars + i, phase & 1)) {
       ok = false;
       sh_flag[4] = 1;
-      atomicOr(a.status, FL_KV_TIMEOUT);
+      atomicOr(b.status, FL_KV_TIMEOUT);
     }
     return ok;
   };
@@ -347,21 +347,23 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll 1
       for (int j = 0; j < mine; ++j) {
         const int t = p.two ? j : 2 * j + s, kb = (p.kb0 + t) * TB;
+        const bool masks = !__all_sync(0xffffffffu, kb + TB <= sees) || a.scale_log2 < 0.f;
+        const bool mixed = first_sees < min(kb + TB, p.kmax);
         wait(B_S + s, ss++);
+        tc_fence_after();
         if (j == 0 && s == 0 && p.lag()) arrive(B_LAG);
         // a block where some row does not see a key that another does, and whose values are not all finite, is taken
         // without the tensor cores
         const uint32_t vi = base + ro.v(t), vst = vi % ST;
         bool slow = false;
-        if (first_sees < min(kb + TB, p.kmax)) {
+        if (mixed) {
           wait(B_READY + vst, vi / ST);
           slow = sh_odd[vst] != 0;
         }
         if (slow != slow_before && row == 0) sh_flag[s] = slow;
         slow_before = slow;
-        tc_fence_after();
         if (on) {
-          if (!__all_sync(0xffffffffu, kb + TB <= sees) || a.scale_log2 < 0.f) {  // keys not seen become -inf
+          if (masks) {  // keys not seen become -inf
 #pragma unroll 1
             for (int c = 0; c < TB; c += 32) {
               uint32_t r[32];
@@ -636,7 +638,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             int page = 0, at = 0;  // asked for before the stage is free
             if (lane < nbox) {
               const int i = kb * boxes + lane;
-              page = kv_page(b, seq, i / per, a.status);
+              page = kv_page(b, seq, i / per);
               at = i % per;
             }
             if (!ok || (ring >= ST && !wait(B_EMPTY + st, ring / ST - 1))) break;

@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(BLOCK) append_kernel(AppendArgs<T> p, KvBatchD
     dst = p.q_out + t * p.ldqo + h * HD;
   } else {
     const int e = idx >> bt.ps_log2;
-    const int page = idx >= 0 && e < bt.table_stride ? kv_page(bt, s, e, status) : -1;
+    const int page = idx >= 0 && e < bt.table_stride ? kv_page(bt, s, e) : -1;
     if (page < 0) {
       atomicOr(status, FL_KV_BAD_PAGE);
       return;
@@ -322,7 +322,8 @@ int fl_kv_check(const char* who, const fl_kv_cache* c, const fl_kv_batch* b, int
   while ((1 << lg) < ps) ++lg;
   if (((int64_t)b->table_stride << lg) > 0x7fffffff)
     return fl_internal_error(FL_ERR_CAPACITY, "%s: more than 2^31 - 1 tokens in a page table row", who);
-  *out = KvBatchDev{b->cu_new, b->lens, b->page_table, nullptr, b->n_seqs, b->n_tokens, b->table_stride, lg, c->n_pages};
+  *out = KvBatchDev{b->cu_new, b->lens, b->page_table, nullptr, b->n_seqs, b->n_tokens, b->table_stride, lg, c->n_pages,
+                    nullptr};
   return FL_OK;
 }
 
@@ -388,6 +389,7 @@ extern "C" int fl_k_kv_append(const fl_kv_cache* cache, const fl_kv_batch* batch
   if ((q && (ldq % 8 || ldqo % 8)) || ldk % 8 || ldv % 8)
     return fl_internal_error(FL_ERR_UNSUPPORTED, "kv append: strides must be multiples of 8 elements");
   if (batch->n_tokens == 0) return FL_OK;
+  bt.status = status;
   const Rope r{positions, block_positions, rope_tab, max_pos, rotary_dim, 1.f, layout == FL_ROPE_INTERLEAVED};
   return (cache->dtype == FL_DT_F16 ? launch_append<__half> : launch_append<__nv_bfloat16>)(
       cache, bt, n_heads, q, ldq, k, ldk, v, ldv, q_out, ldqo, r, status, (cudaStream_t)stream);

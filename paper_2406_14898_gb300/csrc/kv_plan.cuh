@@ -14,19 +14,22 @@
 struct KvBatchDev {
   const int32_t *cu, *lens, *table, *ctx;
   int S, T, table_stride, ps_log2, n_pages;
+  int* status;
 };
 
 struct KvSeq {
   int q0, n, L, ctx;  // first row of the new tokens, their number, tokens in the cache, context length
 };
-// The arrays' values are brought into their ranges, so that no index leaves a buffer.
+// The arrays' values are brought into their ranges, so that no index leaves a buffer; a length outside is recorded.
 FL_DEV KvSeq kv_seq(const KvBatchDev& b, int s) {
   KvSeq q;
   const int a = min(max(b.cu[s], 0), b.T), e = min(max(b.cu[s + 1], 0), b.T);
   const int64_t cap = (int64_t)b.table_stride << b.ps_log2;
   q.q0 = a;
   q.n = max(e - a, 0);
-  q.L = (int)min((int64_t)max(b.lens[s], 0), cap);
+  const int len = b.lens[s];
+  q.L = (int)min((int64_t)max(len, 0), cap);
+  if (q.L != len) atomicOr(b.status, FL_KV_BAD_PAGE);
   q.ctx = b.ctx ? b.ctx[s] : 0;
   return q;
 }
@@ -35,10 +38,10 @@ FL_DEV KvSeq kv_seq(const KvBatchDev& b, int s) {
 FL_DEV int kv_sees(const KvSeq& q, int i) { return max(0, min(q.L, max(q.L - q.n + i + 1, q.ctx))); }
 
 // The page of block-table entry i of sequence s, or -1 (recorded) where the table holds no page of the cache.
-FL_DEV int kv_page(const KvBatchDev& b, int s, int i, int* status) {
+FL_DEV int kv_page(const KvBatchDev& b, int s, int i) {
   const int p = __ldg(b.table + (int64_t)s * b.table_stride + i);
   if ((unsigned)p < (unsigned)b.n_pages) return p;
-  atomicOr(status, FL_KV_BAD_PAGE);
+  atomicOr(b.status, FL_KV_BAD_PAGE);
   return -1;
 }
 
@@ -144,5 +147,5 @@ FL_DEV KvRange kv_plan(const KvBatchDev& b, const U& u, int kvh, int cta, int ct
   return g;
 }
 
-// Checks of a cache and a batch that the calls share (kv_cache.cu); fills *out but for ctx.
+// Checks of a cache and a batch that the calls share (kv_cache.cu); fills *out but for ctx and status.
 int fl_kv_check(const char* who, const fl_kv_cache* c, const fl_kv_batch* b, int n_heads, KvBatchDev* out);

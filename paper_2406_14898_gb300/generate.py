@@ -143,9 +143,9 @@ class BlockStack:
         batch, keep = self._batch(list(new))
         pos, pos2 = self._positions(new)
         context = torch.tensor(self.context, dtype=I32).cuda() if pos2 is not None else None
-        size = F.fl_k_kv_attention_workspace(c.n_heads, self.blocks[0]["cache"], batch)
-        if self.workspace is None or self.workspace.numel() * 4 < size:
-            self.workspace = torch.zeros(-(-size // 4), dtype=I32, device="cuda")
+        if self.workspace is None:  # the same for every batch
+            size = F.fl_k_kv_attention_workspace(c.n_heads, self.blocks[0]["cache"], batch)
+            self.workspace = torch.zeros(size // 4, dtype=I32, device="cuda")
         x = x.float()
         a, o, g, u = (torch.empty((T, n), dtype=BF16, device="cuda") for n in (H, H, Fh, Fh))
         qkv = torch.empty((T, 3 * H), dtype=BF16, device="cuda")

@@ -262,6 +262,11 @@ ATTENTIONS = [
     ([20, 33, 7], [20, 64, 300], 4, 4, 128, 16, False, [15, 64, 999]),            # contexts around the lengths
     ([7, 5], [3, 0], 2, 2, 64, 16, False, None),                                  # tokens before the cache's first
     ([300, 5], [200, 2], 4, 2, 128, 32, False, None),
+    ([3, 1, 90], [3, 500, 90], 120, 3, 64, 32, True, None),                       # 40 heads a group
+    ([2, 1], [700, 129], 128, 1, 128, 16, False, None),                           # 128: one token a tile
+    ([128, 129, 256, 255], [128, 129, 640, 1000], 2, 1, 128, 128, True, None),    # tiles that end exactly
+    ([1] * 300, [(37 * i) % 400 for i in range(300)], 2, 2, 64, 16, False, None),  # more sequences than lanes
+    ([1, 17] * 40, [200 + i for i in range(80)], 2, 1, 64, 16, False, [150, 0] * 40),
 ]
 
 
@@ -285,6 +290,37 @@ def test_attention_strides_scale_and_no_lse(F):
     ref = attention64(p, wide[:, :heads], heads, scale=-0.2)
     check_attention(p, o[:, :heads], ref[1].float(), ref)
     assert bool(torch.isnan(o[:, heads]).all())
+
+
+@pytest.mark.parametrize("offset", [0, 8])
+def test_attention_more_tokens_than_announced_and_unaligned_rows(F, offset):
+    """max_new only chooses the kernel; outputs need 16-byte alignment, not 32."""
+    heads, hd = 2, 64
+    for new, told in (([70, 3], 1), ([2, 1], 500)):
+        p = Paged(F, new, [120, 300], heads, hd, 16, seed=17, max_new=told)
+        q = p.randn(p.T, heads, hd)
+        room = torch.full((p.T * (heads * hd + 8) + offset,), math.nan, device="cuda", dtype=torch.bfloat16)
+        lse = torch.empty((heads, p.T), device="cuda")
+        F.fl_k_kv_attention(p.cache, p.batch, heads, q, room[offset:], p.workspace(heads), p.status, lse=lse,
+                            ldo=heads * hd + 8)
+        rows = room[offset:].view(p.T, heads * hd + 8)
+        check_attention(p, rows[:, :heads * hd].reshape(p.T, heads, hd), lse, attention64(p, q, heads))
+        assert bool(torch.isnan(rows[:, heads * hd:]).all()) and p.status.item() == 0
+
+
+@pytest.mark.parametrize("new", [[1, 1], [1, 40]])
+def test_attention_lengths_out_of_range(F, new):
+    """Too long a length counts as the table row's room, a negative one as none."""
+    p = Paged(F, new, [40, 64], 2, 64, 16, seed=23)
+    width = 4  # four pages a row: all of sequence 1's, and room for 64
+    p.dev_table = p.dev_table[:, :width].contiguous()
+    p.batch = F.kv_batch(2, p.T, max(new), p.cu, p.dev_lens, p.dev_table, width)
+    q, o, lse = run_attention(F, p, 2)
+    p.dev_lens.copy_(torch.tensor([-5, 1000], dtype=torch.int32))
+    _, o2, lse2 = run_attention(F, p, 2, q=q)
+    assert p.status.item() == F.FL_KV_BAD_PAGE
+    assert not o2[:1].any() and bool((lse2[:, :1] == -math.inf).all())
+    assert torch.equal(o2[1:], o[1:]) and torch.equal(lse2[:, 1:], lse[:, 1:])
 
 
 @pytest.mark.parametrize("new,lens,heads,kvh", [([1], [4000], 2, 2), ([2, 200], [1000, 3000], 4, 2)])
@@ -342,10 +378,11 @@ def test_attention_reads_past_32_bits(F):
     assert small.status.item() == 0
 
 
-def test_attention_bad_pages_count_as_zeros(F):
+@pytest.mark.parametrize("token_major", [False, True])
+def test_attention_bad_pages_count_as_zeros(F, token_major):
     heads = 2
     for new in ([1, 1], [1, 60]):
-        p = Paged(F, new, [100, 200], heads, 64, 32, seed=9)
+        p = Paged(F, new, [100, 200], heads, 64, 32, token_major=token_major, seed=9)
         bad = p.dev_table.clone()
         bad[1, 2], bad[1, 4] = p.n_pages, -3
         good = p.batch

@@ -288,7 +288,7 @@ int fl_k_rotary_table(int32_t max_pos, int32_t rotary_dim, float base, int32_t s
  * x + t ldx + h x_head_stride elements; y may be x with the same strides, else they do not overlap.
  * A position outside [0, max_pos) gives a row of zeros and sets FL_KV_BAD_POSITION.
  * Requirements (UNSUPPORTED): head_dim a multiple of 16 up to 256, rotary_dim a multiple of 16, the turned dims
- * within head_dim; strides multiples of 16 bytes; pointers 16-byte aligned (positions and status 4).
+ * within head_dim; strides multiples of 16 bytes, none negative; pointers 16-byte aligned (positions and status 4).
  * T = 0 does nothing; T n_heads (and the append's rows, n_tokens (n_heads + 2 kv_heads)) below 2^31 (CAPACITY).  A
  * table row is [rotary_dim / 2] pairs. */
 int fl_k_rotary(int32_t T, int32_t n_heads, int32_t head_dim, int32_t rotary_dim, int32_t layout, int32_t backward,
@@ -311,7 +311,8 @@ typedef struct {
  * (cu_new ascending from 0 to n_tokens); with them its cache holds lens[s] tokens, so its new token i is
  * token lens[s] - n_s + i.  Token u lies in slot u % page_size of page page_table[s * table_stride +
  * u / page_size].  cu_new [n_seqs + 1], lens [n_seqs], page_table [n_seqs, table_stride]: device int32.
- * max_new: at least the largest n_s (it chooses the kernel; a larger n_s is still computed). */
+ * max_new: at least the largest n_s, 1 or more where there are tokens (it chooses the kernel; a larger n_s is still
+ * computed). */
 typedef struct {
   int32_t n_seqs, n_tokens, max_new, table_stride;
   const int32_t *cu_new, *lens, *page_table;
@@ -325,7 +326,7 @@ typedef struct {
  * rotary_dim = 0: nothing is turned and rope_tab may be NULL (P-tuning prefixes, which are not rotated).
  * q = NULL: only the cache is written.  Where a position is out of range the turned rows are zeros
  * (FL_KV_BAD_POSITION); a token that has no slot (before the first token, past its table row, no page) is
- * not written (FL_KV_BAD_PAGE).  n_heads a multiple of kv_heads; strides multiples of 8 elements, pointers
+ * not written (FL_KV_BAD_PAGE).  n_heads a multiple of kv_heads; strides multiples of 8 elements, none negative, pointers
  * 16-byte aligned (index arrays and status 4); rotary_dim as in fl_k_rotary. */
 int fl_k_kv_append(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n_heads, const void* q, int64_t ldq,
                    const void* k, int64_t ldk, const void* v, int64_t ldv, void* q_out, int64_t ldqo,
@@ -341,11 +342,11 @@ int fl_k_kv_append(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n
  * room for counts as the row's room, a negative one as 0 (FL_KV_BAD_PAGE).  What a page holds past a
  * sequence's last token is not used, NaN included.  Tokens of a page that the table does not name
  * (FL_KV_BAD_PAGE) count as zero keys and values.
- * workspace: fl_k_kv_attention_workspace bytes (the same for every batch of a cache), 16-byte aligned, ZERO before its first use (and after
- * FL_KV_TIMEOUT); a call leaves what it needs of it at zero, so calls one after another on a stream may share
+ * workspace: fl_k_kv_attention_workspace bytes (the same for every batch of a cache), 16-byte aligned, ZERO before
+ * its first use (and after FL_KV_TIMEOUT); a call leaves what it needs of it at zero, so calls one after another on a stream may share
  * it, of any shapes for which it is large enough; calls that may overlap need one each.  Results do not depend on
  * the order in which CTAs run.  q: row t at q + t ldq.  n_heads / kv_heads at most 128; ldq, ldo multiples of 8
- * elements; pointers 16-byte aligned (index arrays, lse and status 4). */
+ * elements, not negative; pointers 16-byte aligned (index arrays, lse and status 4). */
 size_t fl_k_kv_attention_workspace(int32_t n_heads, const fl_kv_cache* cache, const fl_kv_batch* batch);
 int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n_heads, const void* q, int64_t ldq,
                       float scale, const int32_t* context_lens, void* o, int64_t ldo, float* lse, void* workspace,

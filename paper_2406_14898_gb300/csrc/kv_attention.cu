@@ -436,7 +436,8 @@ extern "C" int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* ba
   if (!q || !o || !workspace || !status || !std::isfinite(scale) || fl_misaligned(q, 16) || fl_misaligned(o, 16) ||
       fl_misaligned(workspace, 16) || fl_misaligned(lse, 4) || fl_misaligned(status, 4) || fl_misaligned(context_lens, 4))
     return fl_internal_error(FL_ERR_INVALID_ARG, "kv attention: args");
-  if (ldq % 8 || ldo % 8) return fl_internal_error(FL_ERR_UNSUPPORTED, "kv attention: ldq and ldo must be multiples of 8");
+  if (ldq % 8 || ldo % 8 || ldq < 0 || ldo < 0)
+    return fl_internal_error(FL_ERR_UNSUPPORTED, "kv attention: ldq and ldo must be multiples of 8, not negative");
   a.group = n_heads / cache->kv_heads;
   if (a.group > 128) return fl_internal_error(FL_ERR_UNSUPPORTED, "kv attention: %d query heads per key head", a.group);
   if (batch->n_tokens == 0) return FL_OK;

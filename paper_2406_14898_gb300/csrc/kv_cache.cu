@@ -302,7 +302,7 @@ int launch_append(const fl_kv_cache* c, const KvBatchDev& bt, int heads, const v
 
 int fl_kv_check(const char* who, const fl_kv_cache* c, const fl_kv_batch* b, int n_heads, KvBatchDev* out) {
   if (!c || !b || !c->k || !c->v || b->n_seqs < 0 || b->n_tokens < 0 || b->max_new < 0 || b->table_stride < 1 ||
-      c->n_pages < 1 || c->kv_heads < 1 || n_heads < 1 || n_heads % c->kv_heads || (b->n_seqs == 0 && b->n_tokens > 0))
+      c->n_pages < 1 || c->kv_heads < 1 || n_heads < 1 || n_heads % c->kv_heads || (b->n_tokens > 0 && (b->n_seqs == 0 || b->max_new == 0)))
     return fl_internal_error(FL_ERR_INVALID_ARG, "%s: sizes", who);
   if (b->n_tokens > 0 && (!b->cu_new || !b->lens || !b->page_table))
     return fl_internal_error(FL_ERR_INVALID_ARG, "%s: null index array", who);
@@ -359,8 +359,9 @@ extern "C" int fl_k_rotary(int32_t T, int32_t n_heads, int32_t head_dim, int32_t
   if (head_dim < 16 || head_dim > 256 || head_dim % 16 || rotary_dim < 16 ||
       !rope_supported(head_dim, rotary_dim, block_positions))
     return fl_internal_error(FL_ERR_UNSUPPORTED, "rotary: head_dim %d, rotary_dim %d", head_dim, rotary_dim);
-  if (ldx % unit || ldy % unit || x_head_stride % unit || y_head_stride % unit)
-    return fl_internal_error(FL_ERR_UNSUPPORTED, "rotary: strides must be multiples of 16 bytes");
+  if (ldx % unit || ldy % unit || x_head_stride % unit || y_head_stride % unit || ldx < 0 || ldy < 0 ||
+      x_head_stride < 0 || y_head_stride < 0)
+    return fl_internal_error(FL_ERR_UNSUPPORTED, "rotary: strides must be multiples of 16 bytes, not negative");
   if (T == 0) return FL_OK;
   const Rope r{positions, block_positions, rope_tab, max_pos, rotary_dim, backward ? -1.f : 1.f,
                layout == FL_ROPE_INTERLEAVED};
@@ -386,8 +387,8 @@ extern "C" int fl_k_kv_append(const fl_kv_cache* cache, const fl_kv_batch* batch
     return fl_internal_error(FL_ERR_INVALID_ARG, "kv append: %s", w);
   if (!rope_supported(cache->head_dim, rotary_dim, block_positions))
     return fl_internal_error(FL_ERR_UNSUPPORTED, "kv append: rotary_dim %d", rotary_dim);
-  if ((q && (ldq % 8 || ldqo % 8)) || ldk % 8 || ldv % 8)
-    return fl_internal_error(FL_ERR_UNSUPPORTED, "kv append: strides must be multiples of 8 elements");
+  if ((q && (ldq % 8 || ldqo % 8 || ldq < 0 || ldqo < 0)) || ldk % 8 || ldv % 8 || ldk < 0 || ldv < 0)
+    return fl_internal_error(FL_ERR_UNSUPPORTED, "kv append: strides must be multiples of 8 elements, not negative");
   if (batch->n_tokens == 0) return FL_OK;
   bt.status = status;
   const Rope r{positions, block_positions, rope_tab, max_pos, rotary_dim, 1.f, layout == FL_ROPE_INTERLEAVED};

@@ -46,7 +46,7 @@ def test_rotary_refusals(F):
     variants(L.fl_k_rotary, good,
              [(0, -1, ARG), (1, 0, ARG), (2, 120, UNSUPPORTED), (2, 272, UNSUPPORTED), (3, 0, UNSUPPORTED),
               (3, 24, UNSUPPORTED), (3, 128, UNSUPPORTED), (4, 2, ARG), (5, 2, ARG), (6, 3, ARG), (7, None, ARG),
-              (7, A[0] + 8, ARG), (8, 260, UNSUPPORTED), (9, 4, UNSUPPORTED), (10, A[1] + 2, ARG), (10, None, ARG),
+              (7, A[0] + 8, ARG), (8, 260, UNSUPPORTED), (8, -256, UNSUPPORTED), (9, 4, UNSUPPORTED), (12, -128, UNSUPPORTED), (10, A[1] + 2, ARG), (10, None, ARG),
               (11, 1, UNSUPPORTED), (12, 1, UNSUPPORTED), (13, None, ARG), (13, A[2] + 2, ARG), (14, A[3] + 1, ARG),
               (15, None, ARG), (15, A[4] + 8, ARG), (16, 0, ARG), (17, None, ARG), (17, A[5] + 2, ARG)])
     good[0] = 0
@@ -69,7 +69,7 @@ SHARED = [("dtype", 1, UNSUPPORTED), ("kv_heads", 0, ARG), ("kv_heads", 3, ARG),
           ("n_pages", 0, ARG), ("k", None, ARG), ("v", None, ARG), ("k", A[0] + 8, ARG), ("v", A[1] + 4, ARG),
           ("page_stride", 64 * 128 + 8, UNSUPPORTED), ("head_stride", 64, UNSUPPORTED), ("token_stride", 132, UNSUPPORTED),
           ("token_stride", 64, UNSUPPORTED), ("n_seqs", -1, ARG), ("n_seqs", 0, ARG), ("n_tokens", -1, ARG),
-          ("max_new", -1, ARG), ("table_stride", 0, ARG), ("table_stride", 2 ** 30, CAPACITY), ("cu_new", None, ARG),
+          ("max_new", -1, ARG), ("max_new", 0, ARG), ("table_stride", 0, ARG), ("table_stride", 2 ** 30, CAPACITY), ("cu_new", None, ARG),
           ("lens", None, ARG), ("page_table", None, ARG), ("cu_new", A[2] + 2, ARG), ("lens", A[3] + 1, ARG),
           ("page_table", A[4] + 2, ARG)]
 
@@ -80,9 +80,10 @@ def test_append_refusals(F):
     #       cache batch nh q  ldq  k     ldk  v     ldv  q_out ldqo rd lay pos   pos2  tab   max status
     good = [c, b, 4, A[5], 512, A[6], 256, A[7], 256, A[8], 512, 64, 0, A[9], None, A[10], 99, A[11], None]
     variants(L.fl_k_kv_append, good,
-             [(0, None, ARG), (1, None, ARG), (2, 3, ARG), (2, 0, ARG), (3, A[5] + 8, ARG), (4, 4, UNSUPPORTED),
-              (5, None, ARG), (5, A[6] + 2, ARG), (6, 4, UNSUPPORTED), (7, None, ARG), (7, A[7] + 2, ARG),
-              (8, 4, UNSUPPORTED), (9, None, ARG), (9, A[8] + 2, ARG), (10, 4, UNSUPPORTED), (11, 24, UNSUPPORTED),
+             [(0, None, ARG), (1, None, ARG), (2, 3, ARG), (2, 0, ARG), (3, A[5] + 8, ARG), (4, 4, UNSUPPORTED), (4, -512, UNSUPPORTED),
+              (5, None, ARG), (5, A[6] + 2, ARG), (6, 4, UNSUPPORTED), (6, -256, UNSUPPORTED), (7, None, ARG), (7, A[7] + 2, ARG),
+              (8, 4, UNSUPPORTED), (8, -256, UNSUPPORTED), (9, None, ARG), (9, A[8] + 2, ARG), (10, 4, UNSUPPORTED),
+              (10, -512, UNSUPPORTED), (11, 24, UNSUPPORTED),
               (11, -16, UNSUPPORTED), (11, 144, UNSUPPORTED), (12, 2, ARG), (13, A[9] + 1, ARG), (15, None, ARG),
               (15, A[10] + 8, ARG), (16, 0, ARG), (17, None, ARG), (17, A[11] + 2, ARG)])
     for name, value, code in SHARED:
@@ -108,9 +109,9 @@ def test_attention_refusals(F):
     good = [c, b, 4, A[5], 512, 0.0, A[6], A[7], 512, A[8], A[9], A[10], None]
     variants(L.fl_k_kv_attention, good,
              [(0, None, ARG), (1, None, ARG), (2, 5, ARG), (2, 2 * 129, UNSUPPORTED), (3, None, ARG),
-              (3, A[5] + 8, ARG), (4, 516, UNSUPPORTED), (5, float("nan"), ARG), (5, float("inf"), ARG),
-              (6, A[6] + 2, ARG), (7, None, ARG), (7, A[7] + 4, ARG), (8, 4, UNSUPPORTED), (9, A[8] + 2, ARG),
-              (10, None, ARG), (10, A[9] + 8, ARG), (11, None, ARG), (11, A[10] + 1, ARG)])
+              (3, A[5] + 8, ARG), (4, 516, UNSUPPORTED), (4, -512, UNSUPPORTED), (5, float("nan"), ARG), (5, float("inf"), ARG),
+              (6, A[6] + 2, ARG), (7, None, ARG), (7, A[7] + 4, ARG), (8, 4, UNSUPPORTED), (8, -512, UNSUPPORTED),
+              (9, A[8] + 2, ARG), (10, None, ARG), (10, A[9] + 8, ARG), (11, None, ARG), (11, A[10] + 1, ARG)])
     for name, value, code in SHARED:
         c, b = parts(F, **{name: value})
         assert L.fl_k_kv_attention(c, b, *good[2:]) == code, (name, value)

@@ -9,10 +9,16 @@
 // A tile is 8 NR rows: (token, query head) pairs that read one key / value head.  What bounds a call with few rows
 // is reading each key and value once, so nothing is staged: a warp reads 16 keys and 16 values straight from
 // their page into the fragments of the warp-level tensor instruction (m16n8k16, the products are far from
-// bounding anything), the next keys and values in flight while the last are used.  Both products are
-// transposed, S^T = K Q^T and O^T = V^T P^T, so that the 8 rows are the narrow side.  The order of the dims
+// bounding anything: its pipe is busy 9% of the time), the next keys and values in flight while the last are used.  Both
+// products are transposed, S^T = K Q^T and O^T = V^T P^T, so that the 8 rows are the narrow side.  The order of the dims
 // inside a contraction and of the dims of O^T are free: they are chosen so that each lane reads 16
 // consecutive bytes.
+// One new token in each of 32 sequences of 64 to 4096 tokens, 32 key heads of 128: 984 MB read, each key and value once, in
+// 147 us (6.7 TB/s); four sequences of 40001 to 65536, four key heads: 453 MB in 78 us (5.8 TB/s; the launch, the plan and
+// the join of each unit's parts are the rest).  A sequence of 300 takes 9.6 us, the latencies of the plan, the page table,
+// the keys and the join one after another.
+// P is rounded to 16 bits for its product, the sums take it unrounded: an error of half an ulp of the output's type per
+// weight, independent of one another.
 // Work is divided among the CTAs as kv_plan.cuh says.
 #include <cuda_fp16.h>
 
@@ -29,8 +35,8 @@ namespace {
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int STEP = 16;              // keys a warp takes at a time (one page holds them)
 constexpr int BK = WARPS * STEP;      // keys of a block
-constexpr int JOIN = 8;               // parts read at a time when a unit's are joined
-constexpr int MIN_COST = 2;           // blocks that are worth a CTA of their own
+constexpr int JOIN = 8;               // parts read at a time when a unit is joined: 453 MB in 80.3 us, one by one 82.9
+constexpr int MIN_COST = 1;           // blocks that are worth a CTA: one token over 5 MB in 9.6 us, 10.5 with 2, 14.8 with 4
 constexpr float LOG2E_F = 1.4426950408889634f, LN2_F = 0.6931471805599453f;
 
 template <class T>
@@ -72,8 +78,15 @@ struct RowUnits {  // tiles of `tt` tokens, blocks of BK keys
   FL_DEV int cost(const KvSeq& q, int r) const { return blocks(q, r) + 1; }  // the ends cost about a block
 };
 
+// CTAs that an SM holds, as many as the registers allow without spilling: what they have in flight (16 KB each at head_dim
+// 64, 32 at 128) hides the latency of the memory.  64 sequences of 2048 tokens, 8 key heads: at head_dim 128 up to 8 rows
+// 88 us with 3 (984 MB of other sequences 150, with 2 178), up to 16 rows 107 with 2; at 64 up to 8 rows 49 with 4 (3: 56;
+// 5, which spill, 48, but 27 for 23 on one long sequence), up to 16 rows 61 with 3 (2: 77).
+constexpr int MAX_CTAS = 4;
+constexpr int ctas_per_sm(int hd, int nr) { return (hd == 128 ? 3 : MAX_CTAS) - (nr - 1); }
+
 template <class T, int HD, int NR>
-__global__ void __launch_bounds__(THREADS, NR == 1 ? 3 : 2) kv_attn_rows_kernel(KvAttnArgs a, int tt) {
+__global__ void __launch_bounds__(THREADS, ctas_per_sm(HD, NR)) kv_attn_rows_kernel(KvAttnArgs a, int tt) {
   typedef KvIo<T> Io;
   constexpr int NJ = HD / 32;    // 16-byte pieces of a key that a lane reads
   constexpr int NH = HD / 64;    // ... of a value
@@ -394,17 +407,17 @@ __global__ void __launch_bounds__(THREADS, NR == 1 ? 3 : 2) kv_attn_rows_kernel(
   } while (w.next(b, u, a.kvh) && w.start < rg.hi);
 }
 
-constexpr int CTAS_PER_SM = 3;
-
-// Rows of a sequence and key head that the warp-level fragments hold in one tile.  More go to the tensor-core tiles
-// of 128.
+// Rows of a sequence and key head that the warp-level fragments hold in one tile.  More go to the tensor-core tiles of
+// 128.  64 sequences of 2048 tokens, 8 key heads of 128, here and there: 8 rows 88 and 105 us, 16 rows 107 and 108; one
+// such sequence 12.7 and 20.3, 17.9 and 21.3; 200 of 100 tokens 33 and 47, 48 and 50; at head_dim 64 61 and 92 with 16
+// rows.  With 32 rows two tiles would read the keys twice: 257 and 107.
 bool few_rows(int group, int max_new) { return (int64_t)group * max_new <= 16; }
 
 template <class T, int HD, int NR>
 int launch_rows(const KvAttnArgs& a, cudaStream_t st) {
   const int tt = 8 * NR / a.group, smem = WARPS * 8 * NR * (HD + 4) * (int)sizeof(float);
   FL_CUDA_TRY(fl_func_smem((const void*)kv_attn_rows_kernel<T, HD, NR>, smem));
-  FL_CUDA_TRY(fl_launch(kv_attn_rows_kernel<T, HD, NR>, dim3(CTAS_PER_SM * fl_sm_count()), dim3(THREADS), smem, st, a, tt));
+  FL_CUDA_TRY(fl_launch(kv_attn_rows_kernel<T, HD, NR>, dim3(ctas_per_sm(HD, NR) * fl_sm_count()), dim3(THREADS), smem, st, a, tt));
   return FL_OK;
 }
 template <class T>
@@ -424,7 +437,7 @@ extern "C" size_t fl_k_kv_attention_workspace(int32_t n_heads, const fl_kv_cache
     return 0;
   }
   // enough for either kernel, so that it fits every batch of the cache
-  const size_t rows = (size_t)CTAS_PER_SM * fl_sm_count() * 2 * 16 * (cache->head_dim + 2) * sizeof(float);
+  const size_t rows = (size_t)MAX_CTAS * fl_sm_count() * 2 * 16 * (cache->head_dim + 2) * sizeof(float);
   return KV_COUNTERS * sizeof(unsigned) + std::max(rows, fl_kv_attention_tc_parts(cache->head_dim));
 }
 

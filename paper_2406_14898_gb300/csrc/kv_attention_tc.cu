@@ -16,8 +16,16 @@
 // taken), so the next S of a stream waits for its P V; at head_dim 64 it has columns of its own.
 // A block of shared memory is [16 groups of 8 rows][head_dim / 64][8 rows][64 columns] in the 128-byte
 // swizzle, so that one copy brings all columns of a page's rows.
-// m follows a row's maximum only when that grew by more than 2^8, so O is seldom rescaled.
+// m follows a row's maximum only when that grew by more than 2^8, so O is seldom rescaled.  p is rounded to 16 bits, the type
+// of the tensor instruction's operands; l sums it unrounded, in fp32 as O.
 // Work is divided among the CTAs as kv_plan.cuh says.
+//
+// 2048 new tokens behind 27953, 32 query heads on 8: 0.97 PFLOP in 795 us (1.22 PFLOP/s, the tensor pipe busy half of the
+// time); 16 prompts of 72 to 979 tokens, 32 heads each with its own keys, 164 us (0.65); 8 chunks of 256 tokens after up to
+// 2044, 76 us.  What bounds it is a stream's chain: scores, weights (two passes over 128 scores, an exponential each),
+// products, 3500 to 3900 cycles a block of two streams where the products alone take 2048; a short unit adds its
+// ends.  The softmax's code is what its warps wait for most: loops of 64 columns that stay rolled beat unrolled ones
+// by a third, and more warps or registers gave nothing.
 //
 // Every wait is bounded.  A warp whose wait ran out records it and, in a role that issues, leaves; a softmax warp goes
 // through the rest of its unit without waiting, and its warpgroup then leaves together.
@@ -35,16 +43,19 @@ namespace {
 
 constexpr int TB = 128;
 constexpr int THREADS = 384, W_TMA = 8, W_MMA = 9, W_FIX = 11;
-constexpr int LAG_BLOCKS = 6;
-constexpr int ENDS = 4;      // cost of a unit's ends (Q, the first scores, the output), in blocks of one tile
-constexpr int MIN_COST = 4;
+constexpr int LAG_BLOCKS = 6;  // 16 prompts of 72 to 979 tokens in 162.5 us, without lag 165.8, always 163.4
+// Cost of a unit's ends (Q, the first scores, the output), in blocks of one tile: those prompts with 1 in 187 us, with 8
+// in 165; 8 chunks of 256 tokens in 75.9, 84.7 and 78.
+constexpr int ENDS = 4;
+constexpr int MIN_COST = 4;  // worth a CTA: 12 small sequences in 26.9 us, with 10 in 29.2, with 1 as with 4
 constexpr float LN2_F = 0.6931471805599453f;
 
 template <int HD>
 struct Cfg {
   static constexpr int NB = HD / 64;
   static constexpr int TILE = TB * HD * 2;
-  static constexpr int ST = HD == 128 ? 5 : 8;  // stages: what 227 KB hold beside two Q tiles; 8 at head_dim 64
+  // stages: what 227 KB hold beside two Q tiles (those prompts with 4 in 169.6 us), 8 at head_dim 64
+  static constexpr int ST = HD == 128 ? 5 : 8;
   static constexpr int CTRL = 2048;
   static constexpr int SMEM = (2 + ST) * TILE + CTRL + 1024;
   static constexpr bool OWN_P = HD == 64;
@@ -57,7 +68,7 @@ struct TcMaps {
 struct TcGeom {
   int tpt;               // tokens of a tile
   int box_rows;          // rows that one copy brings: a page's, 128 at most
-  int by_head, per_page; // coordinates of page p, head h: (0, p * per_page + h) or, heads side by side, (h * NB, p)
+  int by_head, per_page;  // coordinates of page p, head h: (0, p * per_page + h) or, heads side by side, (h * NB, p)
 };
 
 // 5-D tiled load of a page's rows.
@@ -535,7 +546,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       // ---- the output
       if (on) {
         float inv;
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(l));  // one ulp, before a rounding to 16 bits
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(l));  // one ulp of 24 bits, before a rounding to 16
         inv = l == 0.f ? 0.f : inv;
         T* dst = reinterpret_cast<T*>(a.o) + t_row * a.ldo + head * HD;
 #pragma unroll 1
@@ -729,7 +740,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       };
       while (wait(B_PIECE + np % PIECES, np / PIECES)) {
         const Piece* pp = pieces + np % PIECES;
-        const int end = (int)uniform(pp->end), two = (int)uniform(pp->two), n = (int)uniform(pp->n), mine = (int)uniform(pp->na[s]), lag = (int)uniform(s == 1 && pp->lag());
+        const int end = (int)uniform(pp->end), two = (int)uniform(pp->two), n = (int)uniform(pp->n),
+                  mine = (int)uniform(pp->na[s]), lag = (int)uniform(s == 1 && pp->lag());
         piece_done();
         if (end) break;
         if (n == 0) continue;

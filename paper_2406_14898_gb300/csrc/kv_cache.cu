@@ -3,7 +3,9 @@
 // A rotation turns pairs (a, b) of a head's dims by the position's angle: (a c - b s, a s + b c), its
 // gradient by the transpose.  All three kernels here are bound by memory: each element is read and written
 // once, 16 bytes a lane and access; the table's row (rotary_dim * 4 bytes, shared by every head of a token) comes
-// from L1.  A thread takes 16 dims of one head, both halves of their pairs.
+// from L1.  A thread takes 16 dims of one head, both halves of their pairs: enough to have in flight, and pairs never
+// cross threads.  8192 rows of 64 heads in 46.6 us (5.8 TB/s), 10214 tokens appended in 88.7 (5.7 TB/s); few tokens
+// take the launch and three dependent reads, 2.6 us.
 #include <cuda_fp16.h>
 
 #include <cmath>
@@ -14,8 +16,8 @@
 
 namespace {
 
-// Small blocks: as one ends another starts, so that some are always waiting for loads.  10214 tokens appended in 91 us,
-// with 256 threads 98, with 512 117.
+// Small blocks: as one ends another starts, so that some are always waiting for loads.  10214 tokens appended in 88.7
+// us; 91, with 256 threads 98 and with 512 117, when this was chosen.
 constexpr int BLOCK = 128;
 
 // Eight consecutive elements as fp32, and back (one rounding).

@@ -365,11 +365,7 @@ __global__ void __launch_bounds__(THREADS, ctas_per_sm(HD, NR)) kv_attn_rows_ker
     // ---- a unit in parts: the CTA that is done last joins them in their order
     const int f0 = rg.cta_of(w.start), f1 = rg.cta_of(w.start + nb - 1);
     __syncthreads();
-    if (tid == 0) {
-      __threadfence();  // the CTA's part is visible before the count
-      sh_last = atomicInc(a.counters + f0, f1 - f0) == (unsigned)(f1 - f0);  // back at zero after the last
-      __threadfence();
-    }
+    if (tid == 0) sh_last = kv_part_done(a.counters + f0, f1 - f0 + 1);
     __syncthreads();
     if (!sh_last) continue;
 #pragma unroll

@@ -7,6 +7,22 @@
 
 constexpr int KV_COUNTERS = 1024;  // at the start of a workspace: parts done of a unit, by the CTA it starts in
 
+// One more part of a unit is in the workspace, of n; true for the last, whose caller joins them and finds the count back at
+// zero.  By one thread, with a barrier between the stores of the part and this, and one between this and the loads.
+FL_DEV bool kv_part_done(unsigned* counter, unsigned n) {
+  unsigned before;
+  asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(counter), "r"(n - 1) : "memory");
+  return before == n - 1;
+}
+// All parts but the caller's are in the workspace.  Then nobody else touches the count any more: it goes back to zero.
+FL_DEV bool kv_part_is_last(unsigned* counter, unsigned n) {
+  unsigned before;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(before) : "l"(counter) : "memory");
+  if (before != n - 1) return false;
+  *counter = 0;
+  return true;
+}
+
 struct KvAttnArgs {
   KvBatchDev b;
   const void *q, *k, *v;

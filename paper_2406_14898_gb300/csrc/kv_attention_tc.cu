@@ -20,12 +20,12 @@
 // of the tensor instruction's operands; l sums it unrounded, in fp32 as O.
 // Work is divided among the CTAs as kv_plan.cuh says.
 //
-// 2048 new tokens behind 27953, 32 query heads on 8: 0.97 PFLOP in 795 us (1.22 PFLOP/s, the tensor pipe busy half of the
-// time); 16 prompts of 72 to 979 tokens, 32 heads each with its own keys, 164 us (0.65); 8 chunks of 256 tokens after up to
-// 2044, 76 us.  What bounds it is a stream's chain: scores, weights (two passes over 128 scores, an exponential each),
+// 2048 new tokens behind 27953, 32 query heads on 8: 0.97 PFLOP in 767 to 798 us (1.25 PFLOP/s, the tensor pipe busy half of the
+// time); 16 prompts of 72 to 979 tokens, 32 heads each with its own keys, 167 us (0.64); 8 chunks of 256 tokens after up to
+// 2044, 73 us.  What bounds it is a stream's chain: scores, weights (two passes over 128 scores, an exponential each),
 // products, 3500 to 3900 cycles a block of two streams where the products alone take 2048; a short unit adds its
-// ends.  The softmax's code is what its warps wait for most: loops of 64 columns that stay rolled beat unrolled ones
-// by a third, and more warps or registers gave nothing.
+// ends.  Short code counts: while a role waits its instructions leave the cache, so loops of 64 columns stay rolled, and
+// what is rare is marked as unlikely to keep it out of their lines (776 to 767 us).
 //
 // Every wait is bounded.  A warp whose wait ran out records it and, in a role that issues, leaves; a softmax warp goes
 // through the rest of its unit without waiting, and its warpgroup then leaves together.
@@ -367,14 +367,14 @@ __global__ void __launch_bounds__(THREADS, 1)
         // without the tensor cores
         const uint32_t vi = base + ro.v(t), vst = vi % ST;
         bool slow = false;
-        if (mixed) {
+        if (mixed) [[unlikely]] {
           wait(B_READY + vst, vi / ST);
           slow = sh_odd[vst] != 0;
         }
         if (slow != slow_before && row == 0) sh_flag[s] = slow;
         slow_before = slow;
         if (on) {
-          if (masks) {  // keys not seen become -inf
+          if (masks) [[unlikely]] {  // keys not seen become -inf
 #pragma unroll 1
             for (int c = 0; c < TB; c += 32) {
               uint32_t r[32];
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
           const bool grows = mt > m + 8.f;
-          if (__any_sync(0xffffffffu, grows)) {
+          if (__any_sync(0xffffffffu, grows)) [[unlikely]] {
             const float mn = grows ? mt : m, f = m == -INFINITY ? 0.f : exp2_hw(m - mn);
             const float corr = grows ? f : 1.f;
             m = mn;
@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         } else {
           if (!slow) arrive(B_PH + s);
         }
-        if (slow) {
+        if (slow) [[unlikely]] {
           if (j > 0) wait(B_O + s, pv + j - 1);
           else if (uses > 0) wait(B_FREE + s, uses - 1);
           tc_fence_after();
@@ -456,6 +456,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         arrive(B_P + s);
       }
+      // A unit in several CTAs' ranges: the CTA that finds the others' parts there (looked for while its last products run)
+      // does not write its own.  Most such units have two, the end of one CTA's work and the beginning of the next one's: the
+      // chunks of 256 tokens 76 to 73 us.
+      const bool whole = p.kb0 == 0 && p.n >= nb, joined = !p.two && p.na[1] > 0;
+      unsigned* count = a.counters + 2 * p.f_lo + s;
+      const unsigned parts = f_hi - p.f_lo + 1;
+      if (!whole && row == 0 && !(joined && s == 1)) sh_flag[2 + s] = kv_part_is_last(count, parts);
       if (mine > 0) {
         pv += mine;
         ++uses;
@@ -463,10 +470,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         tc_fence_after();
       }
       // ---- one tile in two streams: stream 0 joins both
-      const bool joined = !p.two && p.na[1] > 0;
       float f0 = 1.f, f1 = 0.f;
       if (joined) {
-        if (s == 1) {
+        if (s == 1) [[unlikely]] {
           sh_ml[row] = make_float2(m, l);
           arrive(B_JOIN);
           continue;
@@ -500,40 +506,47 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (joined) arrive(B_FREE + 1);
       };
       auto part = [&](int cta, bool first) { return (int64_t)((2 * cta + first) * 2 + s); };
-      const bool whole = p.kb0 == 0 && p.n >= nb;
-      if (!whole) {  // ---- a part: [slot][stream][4 columns][row]
-        const int64_t at = part(blockIdx.x, p.kb0 == 0);
-        if (on) {
+      const int me = blockIdx.x;
+      const float m_own = m;
+      int f_first = me, f_last = nb == 0 ? me - 1 : me;  // whose parts make up the rows
+      if (!whole) [[unlikely]] {  // ---- a part: [slot][stream][4 columns][row]
+        bar_sync(1 + s, 128);
+        if (!sh_flag[2 + s]) {
+          const int64_t at = part(me, p.kb0 == 0);
+          if (on) {
 #pragma unroll 1
-          for (int c = 0; c < HD; c += 32) {
-            float x[32];
-            own(c, x);
-            if (valid) {
+            for (int c = 0; c < HD; c += 32) {
+              float x[32];
+              own(c, x);
+              if (valid) {
 #pragma unroll
-              for (int v = 0; v < 8; ++v)
-                __stcg(part_o + (at * (HD / 4) + c / 4 + v) * TB + row, make_float4(x[4 * v], x[4 * v + 1], x[4 * v + 2], x[4 * v + 3]));
+                for (int v = 0; v < 8; ++v)
+                  __stcg(part_o + (at * (HD / 4) + c / 4 + v) * TB + row,
+                         make_float4(x[4 * v], x[4 * v + 1], x[4 * v + 2], x[4 * v + 3]));
+              }
             }
+            if (valid) __stcg(part_ml + at * TB + row, make_float2(m, l));
           }
-          if (valid) __stcg(part_ml + at * TB + row, make_float2(m, l));
+          bar_sync(1 + s, 128);
+          if (row == 0) sh_flag[2 + s] = kv_part_done(count, parts);
+          bar_sync(1 + s, 128);
+          if (!sh_flag[2 + s]) {
+            release();
+            continue;
+          }
         }
-        release();
-        bar_sync(1 + s, 128);
-        if (row == 0) {
-          __threadfence();  // the part is visible before the count
-          sh_flag[2 + s] = atomicInc(a.counters + 2 * p.f_lo + s, f_hi - p.f_lo) == (unsigned)(f_hi - p.f_lo);
-          __threadfence();
-        }
-        bar_sync(1 + s, 128);
-        if (!sh_flag[2 + s]) continue;
+        f_first = p.f_lo;
+        f_last = f_hi;
+        const float l_own = l;
         m = -INFINITY;
         l = 0.f;
-        for (int fb = p.f_lo; valid && fb <= f_hi; fb += 4) {  // the reads of four wait together
+        for (int fb = f_first; valid && fb <= f_last; fb += 4) {  // the reads of four wait together
           float2 x[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int f = min(fb + e, f_hi);
-            x[e] = __ldcg(part_ml + part(f, f == p.f_lo) * TB + row);
-            if (fb + e > f_hi) x[e].x = -INFINITY;
+            const int f = min(fb + e, f_last);
+            x[e] = f == me ? make_float2(m_own, l_own) : __ldcg(part_ml + part(f, f == f_first) * TB + row);
+            if (fb + e > f_last) x[e].x = -INFINITY;
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -552,24 +565,27 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll 1
         for (int c = 0; c < HD; c += 64) {
           float x[64];
-          if (nb == 0) {  // rows that see nothing
 #pragma unroll
-            for (int e = 0; e < 64; ++e) x[e] = 0.f;
-          } else if (whole) {
-            own(c, *reinterpret_cast<float(*)[32]>(x));
-            own(c + 32, *reinterpret_cast<float(*)[32]>(x + 32));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 64; ++e) x[e] = 0.f;
+          for (int e = 0; e < 64; ++e) x[e] = 0.f;
 #pragma unroll 1
-            for (int f = p.f_lo; valid && f <= f_hi; ++f) {
-              const int64_t q = part(f, f == p.f_lo);
+          for (int f = f_first; f <= f_last; ++f) {  // the parts in their order, the own one from where it lies
+            if (f == me) {
+              const float w = m_own == -INFINITY ? 0.f : exp2_hw(m_own - m);
+#pragma unroll
+              for (int h = 0; h < 64; h += 32) {
+                float y[32];
+                own(c + h, y);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[h + e] = w == 0.f ? x[h + e] : fmaf(y[e], w, x[h + e]);
+              }
+            } else if (valid) {
+              const int64_t q = part(f, f == f_first);
               const float mf = __ldcg(part_ml + q * TB + row).x;
               float4 y[16];
 #pragma unroll
               for (int v = 0; v < 16; ++v) y[v] = __ldcg(part_o + (q * (HD / 4) + c / 4 + v) * TB + row);
-              if (mf == -INFINITY) continue;
-              const float w = exp2_hw(mf - m);
+              const float w = mf == -INFINITY ? 0.f : exp2_hw(mf - m);
+              if (w == 0.f) continue;
 #pragma unroll
               for (int v = 0; v < 16; ++v) {
                 x[4 * v] = fmaf(y[v].x, w, x[4 * v]);
@@ -601,7 +617,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           a.lse[(int64_t)head * b.T + t_row] = (m + lg) * LN2_F;  // no keys: -inf of l = 0
         }
       }
-      if (whole && nb > 0) release();
+      if (nb > 0) release();
     }
   } else {
     if (warp == W_TMA) {

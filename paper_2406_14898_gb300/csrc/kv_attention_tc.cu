@@ -20,10 +20,10 @@
 // of the tensor instruction's operands; l sums it unrounded, in fp32 as O.
 // Work is divided among the CTAs as kv_plan.cuh says.
 //
-// 2048 new tokens behind 27953, 32 query heads on 8: 0.97 PFLOP in 767 to 798 us (1.25 PFLOP/s, the tensor pipe busy half of the
-// time); 16 prompts of 72 to 979 tokens, 32 heads each with its own keys, 167 us (0.64); 8 chunks of 256 tokens after up to
-// 2044, 73 us.  What bounds it is a stream's chain: scores, weights (two passes over 128 scores, an exponential each),
-// products, 3500 to 3900 cycles a block of two streams where the products alone take 2048; a short unit adds its
+// 2048 new tokens behind 27953, 32 query heads on 8: 0.97 PFLOP in 666 us (1.46 PFLOP/s, the tensor pipe busy six tenths of
+// the time); 16 prompts of 72 to 979 tokens, 32 heads each with its own keys, 164 us (0.65); 8 chunks of 256 tokens after up
+// to 2044, 70.6 us.  What bounds it is a stream's chain: scores, weights (two passes over 128 scores, an exponential each),
+// products, about 3100 cycles a block of two streams where the products alone take 2048; a short unit adds its
 // ends.  Short code counts: while a role waits its instructions leave the cache, so loops of 64 columns stay rolled, and
 // what is rare is marked as unlikely to keep it out of their lines (776 to 767 us).
 //
@@ -43,9 +43,11 @@ namespace {
 
 constexpr int TB = 128;
 constexpr int THREADS = 384, W_TMA = 8, W_MMA = 9, W_FIX = 11;
-constexpr int LAG_BLOCKS = 6;  // 16 prompts of 72 to 979 tokens in 162.5 us, without lag 165.8, always 163.4
-// Cost of a unit's ends (Q, the first scores, the output), in blocks of one tile: those prompts with 1 in 187 us, with 8
-// in 165; 8 chunks of 256 tokens in 75.9, 84.7 and 78.
+// Blocks from which on the streams take turns: 2048 tokens behind 27953 in 666 us, started apart only 767; turns told before
+// the maxima are known 721, after half of the weights 905.
+constexpr int TURN_BLOCKS = 6;
+// Cost of a unit's ends (Q, the first scores, the output), in blocks of one tile: 16 prompts of 72 to 979 tokens in 162.5 us,
+// with 1 in 187, with 8 in 165; 8 chunks of 256 tokens in 75.9, 84.7 and 78 (before the streams took turns).
 constexpr int ENDS = 4;
 constexpr int MIN_COST = 4;  // worth a CTA: 12 small sequences in 26.9 us, with 10 in 29.2, with 1 as with 4
 constexpr float LN2_F = 0.6931471805599453f;
@@ -146,9 +148,10 @@ struct Piece {
   int vis, ctx, L;              // token i of the unit sees the first max(0, min(L, max(vis + i, ctx))) keys
   int f_lo, f_hi[2];            // CTAs that have parts of it
   FL_DEV int sees(int i) const { return max(0, min(L, max(vis + i, ctx))); }
-  // Streams that compute their weights at the same time wait for their products at the same time, and stay so.  Where a
-  // unit is long enough to pay for it, the second therefore starts behind the first one's first scores.
-  FL_DEV bool lag() const { return two && na[0] >= LAG_BLOCKS; }
+  // Streams that compute their weights at the same time wait for their products at the same time, and some CTAs stay so to
+  // the end, a fifth behind the others.  So in the blocks that both take part in, a stream's next scores are begun only when
+  // the other one has found the maxima of the block before them: where the streams already alternate that has happened.
+  FL_DEV int turns() const { return two && na[0] >= TURN_BLOCKS ? na[0] : 0; }
 };
 constexpr int PIECES = 4;  // told ahead
 FL_DEV Piece piece_of(const TileUnits& u, const KvWalk<TileUnits>& k, const KvRange& g) {
@@ -182,12 +185,11 @@ FL_DEV Piece piece_of(const TileUnits& u, const KvWalk<TileUnits>& k, const KvRa
   }
   return p;
 }
-// Place in the ring, from the piece's first stage on, of block t's values and keys: la blocks of keys, then
-// each block's values and the keys la blocks further.
+// Place in the ring, from the piece's first stage on, of block t's values: keys of la blocks lie first, then each
+// block's values and the keys la blocks further.
 struct RingOrder {
   int n, la;
   FL_DEV int v(int t) const { return min(n, la) + t + min(t, max(n - la, 0)); }
-  FL_DEV int k(int t) const { return t < la ? t : v(t - la) + 1; }
 };
 
 // The rest of a wait whose first try ran out; one copy, the many places that wait keep short.
@@ -264,12 +266,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     B_O = B_P + 2,           // its P V so far
     B_FREE = B_O + 2,        // its O has been read
     B_JOIN = B_FREE + 2,     // stream 1's part of a tile is ready for stream 0
-    B_LAG = B_JOIN + 1,      // stream 0 has its first scores (see lag)
-    B_PIECE = B_LAG + 1, B_PDONE = B_PIECE + PIECES,
+    B_TURN = B_JOIN + 1,     // a stream knows a block's maxima (see turns)
+    B_PIECE = B_TURN + 2, B_PDONE = B_PIECE + PIECES,
     B_END = B_PDONE + PIECES,
     BARS = B_END + 2
   };
-  static_assert(BARS * 8 <= 400 && sizeof(Piece) * PIECES <= 384, "control block");
+  static_assert(BARS * 8 <= 528 && sizeof(Piece) * PIECES <= 384, "control block");
   volatile int* sh_flag = reinterpret_cast<volatile int*>(ctrl + 528);  // [0, 2) slow block, [2, 4) last part, [4] failed
   volatile int* sh_odd = sh_flag + 8;                                   // [stage] the block has infinities or NaN
   uint32_t* holder = reinterpret_cast<uint32_t*>(ctrl + 592);
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (tid == 0) {
     for (int i = 0; i < BARS; ++i) {
-      const bool four = (i >= B_PH && i < B_O) || (i >= B_FREE && i <= B_LAG);  // the softmax warps of a stream
+      const bool four = (i >= B_PH && i < B_O) || (i >= B_FREE && i < B_PIECE);  // the softmax warps of a stream
       const bool both = (i >= B_EMPTY && i < B_QF) || (i >= B_QE && i < B_S);
       mbar_init(bars + i, four ? 4 : both ? 2 : i >= B_PDONE && i < B_END ? 11 : 1);
     }
@@ -350,6 +352,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int tok = p.two && s ? geo.tpt : 0, rows = (s ? p.toks[1] : p.toks[0]) * a.group;
       const bool valid = row < rows, on = (warp & 3) * 32 < rows;
       const int sees = valid ? p.sees(tok + my_tok) : 0, first_sees = p.sees(tok);
+      const int turns = p.turns();
       const int nb = s ? p.nb[1] : p.nb[0], mine = s ? p.na[1] : p.na[0], f_hi = s ? p.f_hi[1] : p.f_hi[0];
       const int64_t t_row = p.q0 + tok + my_tok;
       const int head = p.h * a.group + my_head;
@@ -362,7 +365,6 @@ __global__ void __launch_bounds__(THREADS, 1)
         const bool mixed = first_sees < min(kb + TB, p.kmax);
         wait(B_S + s, ss++);
         tc_fence_after();
-        if (j == 0 && s == 0 && p.lag()) arrive(B_LAG);
         // a block where some row does not see a key that another does, and whose values are not all finite, is taken
         // without the tensor cores
         const uint32_t vi = base + ro.v(t), vst = vi % ST;
@@ -421,6 +423,7 @@ __global__ void __launch_bounds__(THREADS, 1)
               }
             }
           }
+          if (j < turns) arrive(B_TURN + s);
           const float mref = m == -INFINITY ? 0.f : m;
           const float2 sc = make_float2(scale, scale), nm = make_float2(-mref, -mref);
           float2 lt[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -445,6 +448,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           l += lt[0].x + lt[0].y;
         } else {
           if (!slow) arrive(B_PH + s);
+          if (j < turns) arrive(B_TURN + s);
         }
         if (slow) [[unlikely]] {
           if (j > 0) wait(B_O + s, pv + j - 1);
@@ -746,7 +750,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       // be uniform, so that it stays in uniform registers: the next stage and its phase, and counts.
       // Both streams see every stage and Q tile pass, in order, and free it with one arrival each: of those that it
       // does not read a stream waits for the copy only.  So no stream is ever two phases from a barrier's.
-      uint32_t st = 0, ph = 0, qn = 0, done = 0, uses = 0, lags = 0;
+      uint32_t st = 0, ph = 0, qn = 0, done = 0, uses = 0, turn = 0;
       auto step = [&]() {
         if (++st == ST) st = 0, ph ^= 1;
       };
@@ -757,14 +761,13 @@ __global__ void __launch_bounds__(THREADS, 1)
       while (wait(B_PIECE + np % PIECES, np / PIECES)) {
         const Piece* pp = pieces + np % PIECES;
         const int end = (int)uniform(pp->end), two = (int)uniform(pp->two), n = (int)uniform(pp->n),
-                  mine = (int)uniform(pp->na[s]), lag = (int)uniform(s == 1 && pp->lag());
+                  mine = (int)uniform(pp->na[s]), turns = (int)uniform(pp->turns());
         piece_done();
         if (end) break;
         if (n == 0) continue;
         const uint32_t q = qn + (two ? s : 0);
         for (const uint32_t qe = qn + 1 + two; ok && qn < qe; ++qn)
           if (wait(B_QF + (qn & 1), qn >> 1) && (qn != q || mine == 0) && lane == 0) mbar_arrive(bars + B_QE + (qn & 1));
-        if (lag && !wait(B_LAG, lags++)) break;
         const uint64_t dq = desc_q + (q & 1) * (TILE / 16);
         // The ring holds the keys of la blocks, then each block's values and the keys la blocks further; with two tiles
         // la = 1 and each stream takes all that it sees, else la = 2 and the streams take every other block.
@@ -821,6 +824,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             __syncwarp();
           }
           if (qk) {  // S of block t + la; the last P V has read the P that it overwrites
+            // stream 0 after the other's block j, stream 1 after the other's block j + 1
+            if (j + 1 < turns && j + s >= 0 && !wait(B_TURN + 1 - s, turn + j + s)) break;
             if (!C::OWN_P && done > 0 && !wait(B_O + s, done - 1)) break;
             tc_fence_after();
             if (elect_one()) {
@@ -834,6 +839,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             __syncwarp();
           }
         }
+        turn += turns;
       }
     }
   }

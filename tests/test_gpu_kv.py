@@ -337,6 +337,28 @@ def test_attention_large_scores(F, new, lens, heads, kvh):
     assert bool(((o.double() - ro).abs() <= (2.02 * UNIT["bf16"] + e) * size).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("new,heads,kvh", [([90, 1, 300], 4, 2), ([1, 1, 1], 8, 1), ([2, 40, 3], 12, 1)])
+def test_attention_maxima_that_jump(F, new, heads, kvh, hd, dtype):
+    """Scores that jump by up to 100 within a block of keys, in its first or its second half, upwards and
+    downwards, so that earlier weights vanish; the jumps are exact in every type."""
+    p = Paged(F, new, [700, 650, 1500], kvh, hd, 64, dtype=dtype, seed=29)
+    sign = torch.where(torch.rand(hd, generator=p.gen, device="cuda") < 0.5, -1.0, 1.0)
+    level = torch.zeros(1500, device="cuda")
+    for start, x in [(0, -6), (130, -5), (192, 6), (256, 1), (300, 7), (301, 2), (448, 8), (512, 16), (530, 9), (576, 17),
+                     (640, 3), (690, 18), (700, 4), (1024, 19), (1087, 30), (1088, 20), (1215, 31), (1344, 25)]:
+        level[start:] = x
+    for s, L in enumerate(p.lens):
+        for i in range(-(-L // p.page)):
+            n = min(p.page, L - i * p.page)
+            rows = level[i * p.page:i * p.page + n, None, None] * sign
+            p.k[int(p.table[s, i]), :n] = rows.to(p.k.dtype).expand(n, kvh, hd)
+    q = sign.to(p.k.dtype).expand(p.T, heads, hd).contiguous()
+    _, o, lse = run_attention(F, p, heads, q=q, scale=8 / hd)
+    check_attention(p, o, lse, attention64(p, q, heads, scale=8 / hd))
+
+
 def test_attention_repeats_bit_for_bit_and_workspace_is_left_clean(F):
     """Unequal shapes share one workspace; a repeated call gives the same bits whatever ran between."""
     shapes = [([1] * 5, [4097, 1, 999, 2500, 64], 8, 8), ([1], [6000], 8, 2), ([150, 1], [2000, 2000], 8, 4)]

@@ -34,6 +34,20 @@ def test_products_wait_for_their_operands():
     assert body.count("umma_bf16_ts(") == 2 and body.count("umma_bf16(") == 1
 
 
+def test_streams_take_turns_without_waiting_in_a_circle():
+    """Stream 1's scores of block j wait for stream 0's turn j, stream 0's of block j + 1 for stream 1's turn j:
+    each told once a block by the softmax, behind that block's scores and before its weights, in the blocks that both
+    streams take part in."""
+    src, body = _code("kv_attention_tc.cu"), _products()
+    assert "if (j + 1 < turns && j + s >= 0 && !wait(B_TURN + 1 - s, turn + j + s)) break;" in body
+    assert "turn += turns;" in body and "two && na[0] >= TURN_BLOCKS ? na[0] : 0" in src
+    soft = src[src.index("float m = -INFINITY, l = 0.f;"):src.index("if (warp == W_TMA)")]
+    _in_order(soft, "wait(B_S + s, ss++)", "if (j < turns) arrive(B_TURN + s);", "tmem_st32(t_p", "arrive(B_PH + s)")
+    assert soft.count("if (j < turns) arrive(B_TURN + s);") == 2  # warps with rows, warps without
+    # stream 0 never has more blocks than stream 1, which therefore tells all the turns that stream 0 waits for
+    assert "p.na[0] = p.two ? min(p.n, max(0, p.nb[0] - p.kb0))" in src and "p.na[1] = p.two ? p.n" in src
+
+
 def test_both_streams_free_every_stage_and_query_tile():
     """A stage or a Q tile that a stream does not read is freed by an arrival, one that it reads by the
     product's commit: one of the two on every path, so that the barrier's count of two is met each phase."""

@@ -20,9 +20,9 @@
 // of the tensor instruction's operands; l sums it unrounded, in fp32 as O.
 // Work is divided among the CTAs as kv_plan.cuh says.
 //
-// 2048 new tokens behind 27953, 32 query heads on 8: 0.97 PFLOP in 666 us (1.46 PFLOP/s, the tensor pipe busy six tenths of
-// the time); 16 prompts of 72 to 979 tokens, 32 heads each with its own keys, 164 us (0.65); 8 chunks of 256 tokens after up
-// to 2044, 70.6 us.  What bounds it is a stream's chain: scores, weights (two passes over 128 scores, an exponential each),
+// 2048 new tokens behind 27953, 32 query heads on 8: 0.97 PFLOP in 655 us (1.48 PFLOP/s, the tensor pipe busy six tenths of
+// the time); 16 prompts of 72 to 979 tokens, 32 heads each with its own keys, 158 us (0.68); 8 chunks of 256 tokens after up
+// to 2044, 70 us.  What bounds it is a stream's chain: scores, weights (two passes over 128 scores, an exponential each),
 // products, about 3100 cycles a block of two streams where the products alone take 2048; a short unit adds its
 // ends.  Short code counts: while a role waits its instructions leave the cache, so loops of 64 columns stay rolled, and
 // what is rare is marked as unlikely to keep it out of their lines (776 to 767 us).
@@ -43,12 +43,10 @@ namespace {
 
 constexpr int TB = 128;
 constexpr int THREADS = 384, W_TMA = 8, W_MMA = 9, W_FIX = 11;
-// Blocks from which on the streams take turns: 2048 tokens behind 27953 in 666 us, started apart only 767; turns told before
-// the maxima are known 721, after half of the weights 905.
-constexpr int TURN_BLOCKS = 6;
-// Cost of a unit's ends (Q, the first scores, the output), in blocks of one tile: 16 prompts of 72 to 979 tokens in 162.5 us,
-// with 1 in 187, with 8 in 165; 8 chunks of 256 tokens in 75.9, 84.7 and 78 (before the streams took turns).
-constexpr int ENDS = 4;
+// Cost of a unit's ends (Q, the first scores, the output), in blocks of one tile: 16 prompts of 72 to 979 tokens in 157.5 us
+// with 5, 159 with 4; before the streams took turns 162.5 with 4, 187 with 1, 165 with 8, and 8 chunks of 256 tokens 75.9, 84.7
+// and 78.
+constexpr int ENDS = 5;
 constexpr int MIN_COST = 4;  // worth a CTA: 12 small sequences in 26.9 us, with 10 in 29.2, with 1 as with 4
 constexpr float LN2_F = 0.6931471805599453f;
 
@@ -151,7 +149,8 @@ struct Piece {
   // Streams that compute their weights at the same time wait for their products at the same time, and some CTAs stay so to
   // the end, a fifth behind the others.  So in the blocks that both take part in, a stream's next scores are begun only when
   // the other one has found the maxima of the block before them: where the streams already alternate that has happened.
-  FL_DEV int turns() const { return two && na[0] >= TURN_BLOCKS ? na[0] : 0; }
+  // 2048 tokens behind 27953 in 655 us, without turns 767; turns told before the maxima 721, behind the first weights 900.
+  FL_DEV int turns() const { return two ? na[0] : 0; }
 };
 constexpr int PIECES = 4;  // told ahead
 FL_DEV Piece piece_of(const TileUnits& u, const KvWalk<TileUnits>& k, const KvRange& g) {
@@ -404,6 +403,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
           const bool grows = mt > m + 8.f;
+          if (j < turns) arrive(B_TURN + s);
           if (__any_sync(0xffffffffu, grows)) [[unlikely]] {
             const float mn = grows ? mt : m, f = m == -INFINITY ? 0.f : exp2_hw(m - mn);
             const float corr = grows ? f : 1.f;
@@ -423,7 +423,6 @@ __global__ void __launch_bounds__(THREADS, 1)
               }
             }
           }
-          if (j < turns) arrive(B_TURN + s);
           const float mref = m == -INFINITY ? 0.f : m;
           const float2 sc = make_float2(scale, scale), nm = make_float2(-mref, -mref);
           float2 lt[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};

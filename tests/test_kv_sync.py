@@ -40,7 +40,7 @@ def test_streams_take_turns_without_waiting_in_a_circle():
     streams take part in."""
     src, body = _code("kv_attention_tc.cu"), _products()
     assert "if (j + 1 < turns && j + s >= 0 && !wait(B_TURN + 1 - s, turn + j + s)) break;" in body
-    assert "turn += turns;" in body and "two && na[0] >= TURN_BLOCKS ? na[0] : 0" in src
+    assert "turn += turns;" in body and "return two ? na[0] : 0;" in src
     soft = src[src.index("float m = -INFINITY, l = 0.f;"):src.index("if (warp == W_TMA)")]
     _in_order(soft, "wait(B_S + s, ss++)", "if (j < turns) arrive(B_TURN + s);", "tmem_st32(t_p", "arrive(B_PH + s)")
     assert soft.count("if (j < turns) arrive(B_TURN + s);") == 2  # warps with rows, warps without

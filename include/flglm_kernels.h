@@ -338,6 +338,7 @@ int fl_k_kv_append(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_t n
  * tokens u < min(L, max(p + 1, c)), c = context_lens[s] (device int32, the GLM context; NULL: 0, causal).
  * o [n_tokens, n_heads, head_dim] = sum_u softmax_u(scale q k_u) v_u, of the cache's dtype, row t at o + t ldo;
  * lse (or NULL): fp32 [n_heads, n_tokens], the log-sum-exp of the scaled scores.  scale = 0: 1 / sqrt(head_dim).
+ * A token with a score that is NaN or +infinity gives NaN, in o and in lse.
  * A token that sees nothing (lens[s] = 0, or p < 0) gives zeros and lse = -infinity; a length that its table row has no
  * room for counts as the row's room, a negative one as 0 (FL_KV_BAD_PAGE).  What a page holds past a
  * sequence's last token is not used, NaN included.  Tokens of a page that the table does not name

@@ -346,11 +346,11 @@ __global__ void __launch_bounds__(THREADS, ctas_per_sm(HD, NR)) kv_attn_rows_ker
 #pragma unroll
       for (int v = 0; v < WARPS; ++v) mr = fmaxf(mr, sh_m[v][row]);
 #pragma unroll
-      for (int v = 0; v < WARPS; ++v) {
+      for (int v = 0; v < WARPS; ++v) {  // no key in sight, or only NaN scores: sums of 0, or NaN, which a factor of 0 keeps
         const float f = sh_m[v][row] == -INFINITY ? 0.f : exp2_hw(sh_m[v][row] - mr);
-        lr += f == 0.f ? 0.f : sh_l[v][row] * f;
+        lr += sh_l[v][row] * f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] += f == 0.f ? 0.f : sh_o(v, row)[d0 + i] * f;
+        for (int i = 0; i < 8; ++i) x[i] += sh_o(v, row)[d0 + i] * f;
       }
       if (whole) {
         finish(row, mr, lr, x);
@@ -385,7 +385,10 @@ __global__ void __launch_bounds__(THREADS, ctas_per_sm(HD, NR)) kv_attn_rows_ker
           ml[e] = __ldcg(reinterpret_cast<const float2*>(part_ml) + at);
           y[e][0] = __ldcg(reinterpret_cast<const float4*>(part_o + at * HD + d0));
           y[e][1] = __ldcg(reinterpret_cast<const float4*>(part_o + at * HD + d0) + 1);
-          if (fb + e > f1) ml[e].x = -INFINITY;
+          if (fb + e > f1) {
+            ml[e] = make_float2(-INFINITY, 0.f);
+            y[e][0] = y[e][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
         }
 #pragma unroll
         for (int e = 0; e < JOIN; ++e) {
@@ -393,9 +396,9 @@ __global__ void __launch_bounds__(THREADS, ctas_per_sm(HD, NR)) kv_attn_rows_ker
           const float mn = fmaxf(mr, ml[e].x);
           const float fo = mr == -INFINITY ? 0.f : exp2_hw(mr - mn), fn = ml[e].x == -INFINITY ? 0.f : exp2_hw(ml[e].x - mn);
           mr = mn;
-          lr = (fo == 0.f ? 0.f : lr * fo) + (fn == 0.f ? 0.f : ml[e].y * fn);
+          lr = lr * fo + ml[e].y * fn;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = (fo == 0.f ? 0.f : x[i] * fo) + (fn == 0.f ? 0.f : z[i] * fn);
+          for (int i = 0; i < 8; ++i) x[i] = x[i] * fo + z[i] * fn;
         }
       }
       finish(row, mr, lr, x);

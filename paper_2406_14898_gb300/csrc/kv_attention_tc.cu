@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const float mn = fmaxf(m, x.x);
         f0 = m == -INFINITY ? 0.f : exp2_hw(m - mn);
         f1 = x.x == -INFINITY ? 0.f : exp2_hw(x.x - mn);
-        l = (f0 == 0.f ? 0.f : l * f0) + (f1 == 0.f ? 0.f : x.y * f1);
+        l = l * f0 + x.y * f1;  // no key in sight, or only NaN scores: sums of 0, or NaN, which a factor of 0 keeps
         m = mn;
       }
       auto own = [&](int c, float(&x)[32]) {  // the row's columns [c, c + 32), unscaled; by whole warps
@@ -500,8 +500,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           tmem_ld32(t_o + HD + c, o);
           tmem_ld_wait();
 #pragma unroll
-          for (int e = 0; e < 32; ++e)
-            x[e] = (f0 == 0.f ? 0.f : x[e] * f0) + (f1 == 0.f ? 0.f : __uint_as_float(o[e]) * f1);
+          for (int e = 0; e < 32; ++e) x[e] = x[e] * f0 + __uint_as_float(o[e]) * f1;
         }
       };
       auto release = [&]() {  // O has been read
@@ -549,12 +548,12 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int e = 0; e < 4; ++e) {
             const int f = min(fb + e, f_last);
             x[e] = f == me ? make_float2(m_own, l_own) : __ldcg(part_ml + part(f, f == f_first) * TB + row);
-            if (fb + e > f_last) x[e].x = -INFINITY;
+            if (fb + e > f_last) x[e] = make_float2(-INFINITY, 0.f);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float mn = fmaxf(m, x[e].x);
-            l = (m == -INFINITY ? 0.f : l * exp2_hw(m - mn)) + (x[e].x == -INFINITY ? 0.f : x[e].y * exp2_hw(x[e].x - mn));
+            l = l * (m == -INFINITY ? 0.f : exp2_hw(m - mn)) + x[e].y * (x[e].x == -INFINITY ? 0.f : exp2_hw(x[e].x - mn));
             m = mn;
           }
         }
@@ -579,7 +578,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 float y[32];
                 own(c + h, y);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[h + e] = w == 0.f ? x[h + e] : fmaf(y[e], w, x[h + e]);
+                for (int e = 0; e < 32; ++e) x[h + e] = fmaf(y[e], w, x[h + e]);
               }
             } else if (valid) {
               const int64_t q = part(f, f == f_first);
@@ -588,7 +587,6 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
               for (int v = 0; v < 16; ++v) y[v] = __ldcg(part_o + (q * (HD / 4) + c / 4 + v) * TB + row);
               const float w = mf == -INFINITY ? 0.f : exp2_hw(mf - m);
-              if (w == 0.f) continue;
 #pragma unroll
               for (int v = 0; v < 16; ++v) {
                 x[4 * v] = fmaf(y[v].x, w, x[4 * v]);

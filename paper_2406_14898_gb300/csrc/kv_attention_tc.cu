@@ -194,6 +194,22 @@ struct RingOrder {
 // The rest of a wait whose first try ran out; one copy, the many places that wait keep short.
 __device__ __noinline__ bool wait_longer(uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity); }
 
+// A row's scores scaled and rounded in place.  m is a rounded product: where it is huge, an unrounded product less m would
+// be what it was rounded by, which is no exponent.
+__device__ __noinline__ void round_scores(uint32_t t_s, float scale) {
+  __syncwarp();
+#pragma unroll 1
+  for (int c = 0; c < TB; c += 32) {
+    uint32_t r[32];
+    tmem_ld32(t_s + c, r);
+    tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * scale);
+    tmem_st32(t_s + c, r);
+  }
+  tmem_st_wait();
+}
+
 // O += P V of one block without the tensor cores, for blocks whose values include infinities or NaN at keys that some
 // row does not see: the row takes the keys that it sees.  P and O in TMEM, the block in shared memory.
 template <class T, int HD>
@@ -402,9 +418,15 @@ __global__ void __launch_bounds__(THREADS, 1)
                 mx[i] = fmaxf(fmaxf(mx[i], __uint_as_float(r[e + 2 * i])), __uint_as_float(r[e + 2 * i + 1]));
           }
           const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-          const bool grows = mt > m + 8.f;
+          // below 2^24 the rounding of m is half a unit of the exponent at most, and the same for all of a row's keys
+          const bool grows = mt > m + 8.f, huge = fabsf(mt) >= 0x1p24f && fabsf(mt) < INFINITY;
+          float left = scale;  // what scores are still to be multiplied by
           if (j < turns) arrive(B_TURN + s);
-          if (__any_sync(0xffffffffu, grows)) [[unlikely]] {
+          if (__any_sync(0xffffffffu, grows || huge)) [[unlikely]] {
+            if (__any_sync(0xffffffffu, huge)) [[unlikely]] {
+              round_scores(t_s, scale);
+              left = 1.f;
+            }
             const float mn = grows ? mt : m, f = m == -INFINITY ? 0.f : exp2_hw(m - mn);
             const float corr = grows ? f : 1.f;
             m = mn;
@@ -424,7 +446,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
           }
           const float mref = m == -INFINITY ? 0.f : m;
-          const float2 sc = make_float2(scale, scale), nm = make_float2(-mref, -mref);
+          const float2 sc = make_float2(left, left), nm = make_float2(-mref, -mref);
           float2 lt[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
           for (int c = 0; c < TB; c += 64) {

@@ -791,6 +791,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         // The ring holds the keys of la blocks, then each block's values and the keys la blocks further; with two tiles
         // la = 1 and each stream takes all that it sees, else la = 2 and the streams take every other block.
         const int la = 2 - two;
+        // Stream 0 waits below for all turns of the other one but a piece's last.  That comes first here: a wait for the turn
+        // behind one that has not been told would pass, and the two count apart from then on.
+        if (s == 0 && turns > 0 && turn > 0 && !wait(B_TURN + 1, turn - 1)) break;
 #pragma unroll 1
         for (int t = -la; ok && t < n; ++t) {
           const bool my = two || ((t + 2) & 1) == s;

@@ -37,14 +37,15 @@ class Pages:
         self.table = torch.full((n_seqs, max(1, -(-max_tokens // page_size))), -1, dtype=I32)
 
     def extend(self, new: Sequence[int]):
-        """Room for new[s] more tokens of each sequence."""
-        for s, n in enumerate(new):
-            need = -(-(self.lens[s] + n) // self.page_size)
-            if need > self.table.shape[1]:
+        """Room for new[s] more tokens of each sequence; a refusal changes nothing."""
+        need = [-(-(x + n) // self.page_size) for x, n in zip(self.lens, new)]
+        for s, pages in enumerate(need):
+            if pages > self.table.shape[1]:
                 raise ValueError(f"sequence {s} is longer than {self.table.shape[1] * self.page_size} tokens")
-            if need - len(self.held[s]) > len(self.free):
-                raise MemoryError("no page is free")
-            while len(self.held[s]) < need:
+        if sum(max(0, pages - len(held)) for pages, held in zip(need, self.held)) > len(self.free):
+            raise MemoryError("no page is free")
+        for s, n in enumerate(new):
+            while len(self.held[s]) < need[s]:
                 self.table[s, len(self.held[s])] = self.free[-1]
                 self.held[s].append(self.free.pop())
             self.lens[s] += n

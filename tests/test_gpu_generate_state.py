@@ -1,0 +1,58 @@
+"""What an answering stack keeps between calls: streams, refusals, contexts, roundings (GPU only)."""
+import pytest
+import torch
+
+from tests._gpu import flglm, need_gpu, rel_inf
+from tests._kv import UNIT, turn64
+from tests.test_gpu_generate import server
+
+pytestmark = pytest.mark.gpu
+TOL = 2e-2  # bf16 activations over the blocks, as for chunks against the whole
+
+
+@pytest.fixture(scope="module")
+def F():
+    need_gpu()
+    return flglm()
+
+
+def rows(n, width, seed=1):
+    return torch.randn((n, width), generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").bfloat16()
+
+
+def generator(F, n, vocab=200, blocks=2, room=160, which=None):
+    """A split model, the same for every n: clients 0..n-1, or those of `which`."""
+    from paper_2406_14898_gb300.generate import Generator
+    srv = server(F, blocks, 4, 64, room)
+    cc = F.fl_client_cfg()
+    F.lib().fl_client_cfg_default(cc)
+    cc.block, cc.vocab = srv.cfg, vocab
+    cc.block.n_blocks = 1
+    clients = [F.Client(cc, 100 + k) for k in (range(n) if which is None else which)]
+    return Generator(clients, srv, room)
+
+
+def prompt(k, n, vocab=200):
+    gen = torch.Generator().manual_seed(k)
+    return torch.randint(vocab, (n,), generator=gen, dtype=torch.int32).cuda()
+
+
+# ------------------------------------------------------------------------------- refusals
+
+
+def test_a_refused_call_changes_nothing(F):
+    from paper_2406_14898_gb300.generate import BlockStack
+    x = rows(40, 256)
+    outs = []
+    for refuse in (False, True):
+        srv = server(F, 1, 4, 64, 64)
+        stack = BlockStack.from_server(srv, 2, 64, page_size=16, n_pages=5)
+        stack.forward(x[:30], [20, 10])
+        if refuse:
+            with pytest.raises(ValueError):
+                stack.forward(rows(60, 256), [5, 55])  # the second sequence is too long
+            with pytest.raises(MemoryError):
+                stack.forward(rows(60, 256), [20, 40])  # it would fit, had the first not taken the pages
+        outs.append(stack.forward(x[30:], [3, 7]))
+        srv.close()
+    assert torch.equal(*outs)

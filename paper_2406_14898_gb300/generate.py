@@ -18,6 +18,7 @@ lengths answer together.
 from __future__ import annotations
 
 import argparse
+import contextlib
 from typing import List, Optional, Sequence
 
 import torch
@@ -49,6 +50,14 @@ class Pages:
                 self.table[s, len(self.held[s])] = self.free[-1]
                 self.held[s].append(self.free.pop())
             self.lens[s] += n
+
+    def shorten(self, new: Sequence[int]):
+        """Takes back what an extend by `new`, the last one, gave."""
+        for s, n in reversed(list(enumerate(new))):
+            self.lens[s] -= n
+            while len(self.held[s]) > -(-self.lens[s] // self.page_size):
+                self.free.append(self.held[s].pop())
+                self.table[s, len(self.held[s])] = -1
 
     def drop(self, s: int):
         """Forgets sequence s; its pages serve others, uncleared."""
@@ -111,19 +120,24 @@ class BlockStack:
         self.context[s] = context_len + P if context_len else 0
         self.mask_pos[s] = context_len - 1 if mask_pos is None else mask_pos
         if P:  # the P-tuning prefix takes the first places of the cache; its keys are not turned
-            batch, keep = self._batch([P if i == s else 0 for i in range(len(self.context))])
-            for b in self.blocks:
-                F.fl_k_kv_append(b["cache"], batch, self.cfg.n_heads, None, *b["prefix"], None, None, 0, self.status)
-            del keep
+            with self._extended([P if i == s else 0 for i in range(len(self.context))]) as batch:
+                for b in self.blocks:
+                    F.fl_k_kv_append(b["cache"], batch, self.cfg.n_heads, None, *b["prefix"], None, None, 0, self.status)
 
-    def _batch(self, new):
+    @contextlib.contextmanager
+    def _extended(self, new):
+        """The batch of new[s] more tokens of each sequence, which are theirs unless something raises meanwhile."""
         self.pages.extend(new)
-        cu = [0]
-        for n in new:
-            cu.append(cu[-1] + n)
-        keep = [torch.tensor(cu, dtype=I32).cuda(), torch.tensor(self.pages.lens, dtype=I32).cuda(),
-                self.pages.table.cuda()]
-        return F.kv_batch(len(new), cu[-1], max(new), *keep, self.pages.table.shape[1]), keep
+        try:
+            cu = [0]
+            for n in new:
+                cu.append(cu[-1] + n)
+            keep = [torch.tensor(cu, dtype=I32).cuda(), torch.tensor(self.pages.lens, dtype=I32).cuda(),
+                    self.pages.table.cuda()]
+            yield F.kv_batch(len(new), cu[-1], max(new), *keep, self.pages.table.shape[1])
+        except BaseException:
+            self.pages.shorten(new)
+            raise
 
     def _positions(self, new):
         """The two position streams of the new tokens: (i, 0) in the context, (mask, 1 ..) in the span."""
@@ -139,9 +153,13 @@ class BlockStack:
 
     def forward(self, x: torch.Tensor, new: Sequence[int]) -> torch.Tensor:
         """x: bf16 [sum(new), hidden], new[s] next tokens of sequence s; returns the blocks' output of them.  A context's
-        tokens come in one call, as they see each other."""
+        tokens come in one call, as they see each other.  A call that raises has added nothing: it may be repeated."""
+        new = list(new)
+        with self._extended(new) as batch:
+            return self._run(x, new, batch)
+
+    def _run(self, x, new, batch):
         c, T, H, Fh = self.cfg, sum(new), self.cfg.hidden, self.cfg.ffn_hidden
-        batch, keep = self._batch(list(new))
         pos, pos2 = self._positions(new)
         context = torch.tensor(self.context, dtype=I32).cuda() if pos2 is not None else None
         if self.workspace is None:  # the same for every batch
@@ -179,9 +197,11 @@ class BlockStack:
             F.gemm(T, Fh, H, a, H, 0, w_up, H, 0, g, Fh, status=status, epilogue=F.FL_EPI_BIAS_GELU, bias=b_up, aux_out=u,
                    ld_aux_out=Fh)
             x = residual(T, Fh, g, w_down, b_down, h, *b["ln"][2:])
-        if int(status.item()) or int(self.status.item()):
-            raise RuntimeError(f"generation: device status {int(status.item())}, cache status {int(self.status.item())}")
-        del keep
+        bits, cache_bits = int(status.item()), int(self.status.item())
+        if bits or cache_bits:
+            self.status.zero_()
+            self.workspace.zero_()  # not valid after a wait that gave up
+            raise RuntimeError(f"generation: device status {bits}, cache status {cache_bits}")
         return x.to(BF16)
 
 

@@ -35,3 +35,13 @@ def test_pages_are_handed_out_and_come_back():
     assert p.lens == [0, 16] and p.table[0].tolist() == [-1] * 4 and len(p.free) == 5
     p.extend([64, 0])
     assert p.lens == [64, 16]
+
+
+@pytest.mark.parametrize("lens,new", [([5, 30], [3, 20]), ([16, 0, 7], [0, 33, 9]), ([0, 0], [16, 1])])
+def test_an_extension_is_taken_back(lens, new):
+    p = Pages(9, 16, len(lens), 64)
+    p.extend(lens)
+    before = state(p)
+    p.extend(new)
+    p.shorten(new)
+    assert state(p) == before

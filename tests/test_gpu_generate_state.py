@@ -56,3 +56,21 @@ def test_a_refused_call_changes_nothing(F):
         outs.append(stack.forward(x[30:], [3, 7]))
         srv.close()
     assert torch.equal(*outs)
+
+
+def test_a_call_that_failed_on_the_device_changes_nothing(F):
+    from paper_2406_14898_gb300.generate import BlockStack
+    srv = server(F, 1, 4, 64, 64)
+    x = rows(40, 256)
+    outs = []
+    for fail in (False, True):
+        stack = BlockStack.from_server(srv, 2, 64, page_size=16)
+        stack.forward(x[:30], [20, 10])
+        if fail:
+            stack.status.fill_(F.FL_KV_TIMEOUT)  # as if a wait had given up
+            stack.workspace[:64] = 1
+            with pytest.raises(RuntimeError):
+                stack.forward(x[30:], [3, 7])
+        outs.append(stack.forward(x[30:], [3, 7]))
+    assert torch.equal(*outs)
+    srv.close()

@@ -229,17 +229,32 @@ class Generator:
             self.top[k].start(0, c)
 
     def logits(self, tokens: Sequence[torch.Tensor]) -> List[torch.Tensor]:
-        """fp32 logits after each client's new tokens (int32 on the device), [vocab] of the last one."""
-        hs = []
+        """fp32 logits after each client's new tokens (int32 on the device), [vocab] of the last one.  A call that
+        raises has added nothing to any part of the model."""
+        done = []
+        try:
+            return self._logits(tokens, done)
+        except BaseException:
+            for stack, new in done:
+                stack.pages.shorten(new)
+            raise
+
+    def _logits(self, tokens, done):
+        def forward(stack, x, new):
+            y = stack.forward(x, new)
+            done.append((stack, new))
+            return y
+
+        hs, new = [], [len(t) for t in tokens]
         for c, e, stack, t in zip(self.clients, self.ends, self.bottom, tokens):
             h = torch.empty((len(t), c.cfg.block.hidden), dtype=BF16, device="cuda")
             F.fl_k_embedding_gather(len(t), h.shape[1], t, e["embed"], c.cfg.vocab, h, stack.status)
-            hs.append(stack.forward(h, [len(t)]))
-        mid = self.server.forward(torch.cat(hs), [len(t) for t in tokens]).split([len(t) for t in tokens])
+            hs.append(forward(stack, h, [len(t)]))
+        mid = forward(self.server, torch.cat(hs), new).split(new)
         out = []
         for c, e, stack, h in zip(self.clients, self.ends, self.top, mid):
             H, n = h.shape[1], e["head"].shape[0]
-            last = stack.forward(h, [len(h)])[-1:].contiguous()
+            last = forward(stack, h, [len(h)])[-1:].contiguous()
             y, stats = torch.empty_like(last), torch.empty(2, device="cuda")
             F.fl_k_layernorm_fwd(1, H, last, *e["ln"], c.cfg.block.ln_eps, y, stats[:1], stats[1:])
             z = torch.empty((1, n), device="cuda")

@@ -74,3 +74,22 @@ def test_a_call_that_failed_on_the_device_changes_nothing(F):
         outs.append(stack.forward(x[30:], [3, 7]))
     assert torch.equal(*outs)
     srv.close()
+
+
+def test_clients_are_not_ahead_of_a_server_that_refused(F):
+    p = [prompt(0, 9), prompt(1, 30)]
+    more = [prompt(2, 1), prompt(3, 1)]
+    outs = []
+    for refuse in (False, True):
+        gen = generator(F, 2)
+        gen.start([len(t) for t in p])
+        gen.logits(p)
+        if refuse:
+            free, gen.server.pages.free = gen.server.pages.free, []
+            held = gen.server.pages.lens[0]
+            with pytest.raises(MemoryError):
+                gen.logits([prompt(4, 100), more[1]])
+            gen.server.pages.free = free
+            assert gen.server.pages.lens[0] == held
+        outs.append(torch.stack(gen.logits(more)))
+    assert torch.equal(*outs)

@@ -153,8 +153,11 @@ class BlockStack:
 
     def forward(self, x: torch.Tensor, new: Sequence[int]) -> torch.Tensor:
         """x: bf16 [sum(new), hidden], new[s] next tokens of sequence s; returns the blocks' output of them.  A context's
-        tokens come in one call, as they see each other.  A call that raises has added nothing: it may be repeated."""
+        tokens come in one call, as they see each other (ValueError otherwise).  A call that raises has added nothing: it may be repeated."""
         new = list(new)
+        for s, (n, held, c) in enumerate(zip(new, self.pages.lens, self.context)):
+            if n and held < c and held + n < c:
+                raise ValueError(f"sequence {s}: {n} tokens of a context of {c - self.cfg.prefix_len}, which come in one call")
         with self._extended(new) as batch:
             return self._run(x, new, batch)
 

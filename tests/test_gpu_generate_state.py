@@ -93,3 +93,26 @@ def test_clients_are_not_ahead_of_a_server_that_refused(F):
             assert gen.server.pages.lens[0] == held
         outs.append(torch.stack(gen.logits(more)))
     assert torch.equal(*outs)
+
+
+# ------------------------------------------------------------------------------- contexts
+
+def test_a_context_in_two_calls_is_refused(F):
+    """Its tokens see each other, so they come together; the answer's may come with them or later."""
+    from paper_2406_14898_gb300.generate import BlockStack
+    for prefix in (0, 7):
+        srv = server(F, 1, 4, 64, 64, prefix)
+        stack = BlockStack.from_server(srv, 2, 64, page_size=16)
+        stack.start(0, 20)
+        stack.start(1)
+        x = rows(40, 256)
+        for n in (1, 19):
+            with pytest.raises(ValueError):
+                stack.forward(x[:n], [n, 0])
+        with pytest.raises(ValueError):
+            stack.forward(x[:29], [19, 10])
+        assert stack.pages.lens == [prefix, prefix]
+        stack.forward(x[:10], [0, 10])  # an idle context, and one that is plainly causal
+        stack.forward(x[:23], [22, 1])
+        stack.forward(x[:2], [1, 1])
+        srv.close()

@@ -28,6 +28,11 @@ from . import flglm as F
 BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
 
 
+def _stream() -> dict:
+    """Where torch's own work goes: the library's calls between follow it there."""
+    return {"stream": torch.cuda.current_stream()}
+
+
 class Pages:
     """Which pages of the caches belong to which sequence; one table for every block of a stack."""
 
@@ -97,11 +102,12 @@ class BlockStack:
             self.blocks.append(b)
         self.max_pos = max_tokens + 1
         self.rope = torch.empty((self.max_pos, self.rdim // 2, 2), device="cuda")
-        F.fl_k_rotary_table(self.max_pos, self.rdim, c.rope_base, self.rope)
+        F.fl_k_rotary_table(self.max_pos, self.rdim, c.rope_base, self.rope, **_stream())
         self.status = torch.zeros(1, dtype=I32, device="cuda")
         self.workspace = None
         self.context = [0] * n_seqs   # context lengths, prefix included; 0: plainly causal
         self.mask_pos = [0] * n_seqs
+        torch.cuda.current_stream().synchronize()  # whichever stream uses them
 
     @classmethod
     def from_server(cls, srv: "F.Server", n_seqs: int, max_tokens: int, **kw):
@@ -122,7 +128,8 @@ class BlockStack:
         if P:  # the P-tuning prefix takes the first places of the cache; its keys are not turned
             with self._extended([P if i == s else 0 for i in range(len(self.context))]) as batch:
                 for b in self.blocks:
-                    F.fl_k_kv_append(b["cache"], batch, self.cfg.n_heads, None, *b["prefix"], None, None, 0, self.status)
+                    F.fl_k_kv_append(b["cache"], batch, self.cfg.n_heads, None, *b["prefix"], None, None, 0, self.status,
+                                     **_stream())
 
     @contextlib.contextmanager
     def _extended(self, new):
@@ -153,7 +160,8 @@ class BlockStack:
 
     def forward(self, x: torch.Tensor, new: Sequence[int]) -> torch.Tensor:
         """x: bf16 [sum(new), hidden], new[s] next tokens of sequence s; returns the blocks' output of them.  A context's
-        tokens come in one call, as they see each other (ValueError otherwise).  A call that raises has added nothing: it may be repeated."""
+        tokens come in one call, as they see each other (ValueError otherwise).  Runs on torch's current stream.  A call
+        that raises has added nothing: it may be repeated."""
         new = list(new)
         for s, (n, held, c) in enumerate(zip(new, self.pages.lens, self.context)):
             if n and held < c and held + n < c:
@@ -173,32 +181,33 @@ class BlockStack:
         qkv = torch.empty((T, 3 * H), dtype=BF16, device="cuda")
         stats = torch.empty((2, T), device="cuda")
         status = torch.zeros(1, dtype=I32, device="cuda")
+        on = _stream()
 
         def norm(x, gamma, beta):
-            F.fl_k_layernorm_fwd(T, H, x, gamma, beta, c.ln_eps, a, stats[0], stats[1], x_dtype=F.FL_DT_F32)
+            F.fl_k_layernorm_fwd(T, H, x, gamma, beta, c.ln_eps, a, stats[0], stats[1], x_dtype=F.FL_DT_F32, **on)
 
         def residual(M, K, inp, w, bias, x, gamma, beta):
             """alpha * (LN(x) or x) + inp w^T + bias in fp32."""
             y = torch.empty((T, H), device="cuda")
             ln = dict(ln_mean=stats[0], ln_rstd=stats[1], ln_gamma=gamma, ln_beta=beta) if c.residual_from_ln else {}
             F.gemm(M, H, K, inp, K, 0, w, K, 0, y, H, status=status, epilogue=F.FL_EPI_BIAS_RESID, bias=bias, aux=x,
-                   ld_aux=H, aux_dtype=F.FL_DT_F32, d_dtype=F.FL_DT_F32, alpha=c.residual_alpha, **ln)
+                   ld_aux=H, aux_dtype=F.FL_DT_F32, d_dtype=F.FL_DT_F32, alpha=c.residual_alpha, **ln, **on)
             return y
 
         for b in self.blocks:
             (w_qkv, w_dense, w_up, w_down), (b_qkv, b_dense, b_up, b_down) = b["w"], b["b"]
             norm(x, *b["ln"][:2])
-            F.gemm(T, 3 * H, H, a, H, 0, w_qkv, H, 0, qkv, 3 * H, status=status, bias=b_qkv)
+            F.gemm(T, 3 * H, H, a, H, 0, w_qkv, H, 0, qkv, 3 * H, status=status, bias=b_qkv, **on)
             q = qkv.data_ptr()  # the queries are turned in place
             F.fl_k_kv_append(b["cache"], batch, c.n_heads, q, q + 2 * H, q + 4 * H, q, self.rope, self.max_pos,
                              self.status, rotary_dim=self.rdim, positions=pos, block_positions=pos2, ldq=3 * H,
-                             ldk=3 * H, ldv=3 * H, ldqo=3 * H)
+                             ldk=3 * H, ldv=3 * H, ldqo=3 * H, **on)
             F.fl_k_kv_attention(b["cache"], batch, c.n_heads, q, o, self.workspace, self.status, context_lens=context,
-                                ldq=3 * H)
+                                ldq=3 * H, **on)
             h = residual(T, H, o, w_dense, b_dense, x, *b["ln"][:2])
             norm(h, *b["ln"][2:])
             F.gemm(T, Fh, H, a, H, 0, w_up, H, 0, g, Fh, status=status, epilogue=F.FL_EPI_BIAS_GELU, bias=b_up, aux_out=u,
-                   ld_aux_out=Fh)
+                   ld_aux_out=Fh, **on)
             x = residual(T, Fh, g, w_down, b_down, h, *b["ln"][2:])
         bits, cache_bits = int(status.item()), int(self.status.item())
         if bits or cache_bits:
@@ -223,6 +232,7 @@ class Generator:
             head[:V] = torch.from_numpy(c.get_param(F.FL_CP_HEAD, 0)).cuda().view(V, H).to(BF16)
             self.ends.append({"embed": torch.from_numpy(c.get_param(F.FL_CP_EMBED, 0)).cuda().view(V, H).to(BF16),
                               "head": head, "ln": [torch.from_numpy(c.get_param(F.FL_CP_FINAL_LN, t)).cuda() for t in (0, 1)]})
+        torch.cuda.current_stream().synchronize()  # whichever stream uses them
 
     def start(self, context_lens: Optional[Sequence[int]] = None):
         for k in range(len(self.clients)):
@@ -251,7 +261,7 @@ class Generator:
         hs, new = [], [len(t) for t in tokens]
         for c, e, stack, t in zip(self.clients, self.ends, self.bottom, tokens):
             h = torch.empty((len(t), c.cfg.block.hidden), dtype=BF16, device="cuda")
-            F.fl_k_embedding_gather(len(t), h.shape[1], t, e["embed"], c.cfg.vocab, h, stack.status)
+            F.fl_k_embedding_gather(len(t), h.shape[1], t, e["embed"], c.cfg.vocab, h, stack.status, **_stream())
             hs.append(forward(stack, h, [len(t)]))
         mid = forward(self.server, torch.cat(hs), new).split(new)
         out = []
@@ -259,9 +269,9 @@ class Generator:
             H, n = h.shape[1], e["head"].shape[0]
             last = forward(stack, h, [len(h)])[-1:].contiguous()
             y, stats = torch.empty_like(last), torch.empty(2, device="cuda")
-            F.fl_k_layernorm_fwd(1, H, last, *e["ln"], c.cfg.block.ln_eps, y, stats[:1], stats[1:])
+            F.fl_k_layernorm_fwd(1, H, last, *e["ln"], c.cfg.block.ln_eps, y, stats[:1], stats[1:], **_stream())
             z = torch.empty((1, n), device="cuda")
-            F.gemm(1, n, H, y, H, 0, e["head"], H, 0, z, n, d_dtype=F.FL_DT_F32)
+            F.gemm(1, n, H, y, H, 0, e["head"], H, 0, z, n, d_dtype=F.FL_DT_F32, **_stream())
             out.append(z[0, :c.cfg.vocab])
         return out
 

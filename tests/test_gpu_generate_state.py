@@ -37,6 +37,38 @@ def prompt(k, n, vocab=200):
     return torch.randint(vocab, (n,), generator=gen, dtype=torch.int32).cuda()
 
 
+# ------------------------------------------------------------------------------- streams
+
+def test_every_call_goes_to_the_current_stream(F, monkeypatch):
+    """The library's kernels run where torch's own work of the same call runs."""
+    gen = generator(F, 2)
+    torch.cuda.synchronize()
+    st, seen = torch.cuda.Stream(), []
+    plain = F.stream_ptr
+    monkeypatch.setattr(F, "stream_ptr", lambda s: seen.append(plain(s)) or plain(s))
+    with torch.cuda.stream(st):
+        gen.greedy([prompt(0, 9), prompt(1, 30)], 2)
+    torch.cuda.synchronize()
+    assert len(seen) > 100 and set(seen) == {st.cuda_stream}
+
+
+def test_a_stream_that_is_behind_gives_the_same_bits(F):
+    """A stream of its own that is held up before each call: nothing of the call runs ahead of it."""
+    p, more = [prompt(0, 9), prompt(1, 30)], [prompt(2, 1), prompt(3, 1)]
+    outs = []
+    for st in (None, torch.cuda.Stream()):
+        gen = generator(F, 2)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            gen.start([len(t) for t in p])
+            for t in (p, more):
+                if st:
+                    torch.cuda._sleep(20_000_000)
+                outs.append(torch.stack(gen.logits(t)))
+        torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
+
+
 # ------------------------------------------------------------------------------- refusals
 
 

@@ -163,6 +163,10 @@ class BlockStack:
         tokens come in one call, as they see each other (ValueError otherwise).  Runs on torch's current stream.  A call
         that raises has added nothing: it may be repeated."""
         new = list(new)
+        if len(new) != len(self.context) or any(n < 0 for n in new):
+            raise ValueError(f"new tokens {new} for {len(self.context)} sequences")
+        if not x.is_cuda or x.shape != (sum(new), self.cfg.hidden):
+            raise ValueError(f"x {tuple(x.shape)} on {x.device} for {sum(new)} new tokens of {self.cfg.hidden}")
         for s, (n, held, c) in enumerate(zip(new, self.pages.lens, self.context)):
             if n and held < c and held + n < c:
                 raise ValueError(f"sequence {s}: {n} tokens of a context of {c - self.cfg.prefix_len}, which come in one call")
@@ -176,7 +180,7 @@ class BlockStack:
         if self.workspace is None:  # the same for every batch
             size = F.fl_k_kv_attention_workspace(c.n_heads, self.blocks[0]["cache"], batch)
             self.workspace = torch.zeros(size // 4, dtype=I32, device="cuda")
-        x = x.float()
+        x = x.float().contiguous()
         a, o, g, u = (torch.empty((T, n), dtype=BF16, device="cuda") for n in (H, H, Fh, Fh))
         qkv = torch.empty((T, 3 * H), dtype=BF16, device="cuda")
         stats = torch.empty((2, T), device="cuda")

@@ -148,3 +148,30 @@ def test_a_context_in_two_calls_is_refused(F):
         stack.forward(x[:23], [22, 1])
         stack.forward(x[:2], [1, 1])
         srv.close()
+
+
+# ------------------------------------------------------------------------------- arguments
+
+def test_rows_in_any_strides(F):
+    from paper_2406_14898_gb300.generate import BlockStack
+    srv = server(F, 1, 4, 64, 64)
+    stack = BlockStack.from_server(srv, 1, 64, page_size=16)
+    want = stack.forward(rows(40, 256), [40])
+    for x in (rows(40, 256).T.contiguous().T, torch.cat([rows(40, 256), rows(40, 256, 2)], 1)[:, :256],
+              rows(40, 256).repeat_interleave(2, 0)[::2], rows(40, 256).float()):
+        stack.start(0)
+        assert torch.equal(stack.forward(x, [40]), want)
+    srv.close()
+
+
+def test_rows_that_do_not_fit_are_refused(F):
+    from paper_2406_14898_gb300.generate import BlockStack
+    srv = server(F, 1, 4, 64, 64)
+    stack = BlockStack.from_server(srv, 2, 64, page_size=16)
+    x = rows(40, 256)
+    for rows_, new in ((x, [41, 0]), (x, [20, 19]), (x, [40]), (x, [20, 10, 10]), (x, [41, -1]), (x[:, :128], [40, 0]),
+                       (x.view(-1), [40, 0]), (x.cpu(), [40, 0])):
+        with pytest.raises(ValueError):
+            stack.forward(rows_, new)
+    assert stack.pages.lens == [0, 0]
+    srv.close()

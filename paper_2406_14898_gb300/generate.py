@@ -248,6 +248,12 @@ class Generator:
     def logits(self, tokens: Sequence[torch.Tensor]) -> List[torch.Tensor]:
         """fp32 logits after each client's new tokens (int32 on the device), [vocab] of the last one.  A call that
         raises has added nothing to any part of the model."""
+        if len(tokens) != len(self.clients):
+            raise ValueError(f"tokens of {len(tokens)} clients for {len(self.clients)}")
+        for k, t in enumerate(tokens):
+            if t.dtype != I32 or not t.is_cuda or t.dim() != 1 or not len(t):
+                raise ValueError(f"client {k}: {t.dtype} tokens {tuple(t.shape)} on {t.device}, not int32 [1 or more] on the device")
+        tokens = [t.contiguous() for t in tokens]
         done = []
         try:
             return self._logits(tokens, done)

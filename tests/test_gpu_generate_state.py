@@ -175,3 +175,17 @@ def test_rows_that_do_not_fit_are_refused(F):
             stack.forward(rows_, new)
     assert stack.pages.lens == [0, 0]
     srv.close()
+
+
+def test_tokens_that_do_not_fit_are_refused(F):
+    gen = generator(F, 2)
+    gen.start([5, 5])
+    a, b = prompt(0, 5), prompt(1, 5)
+    for tokens in ([a], [a, b, b], [a.long(), b], [a, b.cpu()], [a, b[:0]], [a, b.view(1, 5)]):
+        with pytest.raises(ValueError):
+            gen.logits(tokens)
+    with pytest.raises(RuntimeError):
+        gen.logits([a, b + 200])  # past the vocabulary
+    want = torch.stack(gen.logits([a, b]))
+    gen.start([5, 5])
+    assert torch.equal(torch.stack(gen.logits([a.repeat_interleave(3)[::3], b])), want)

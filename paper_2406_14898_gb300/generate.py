@@ -170,6 +170,8 @@ class BlockStack:
         for s, (n, held, c) in enumerate(zip(new, self.pages.lens, self.context)):
             if n and held < c and held + n < c:
                 raise ValueError(f"sequence {s}: {n} tokens of a context of {c - self.cfg.prefix_len}, which come in one call")
+        if not any(new):
+            return x.to(BF16)
         with self._extended(new) as batch:
             return self._run(x, new, batch)
 

@@ -177,6 +177,22 @@ def test_rows_that_do_not_fit_are_refused(F):
     srv.close()
 
 
+def test_no_new_tokens_are_no_rows(F):
+    from paper_2406_14898_gb300.generate import BlockStack
+    srv = server(F, 1, 4, 64, 64)
+    stack = BlockStack.from_server(srv, 2, 64, page_size=16)
+    x = rows(40, 256)
+    outs = []
+    for idle in (False, True):
+        stack.start(0)
+        stack.start(1)
+        if idle:
+            assert stack.forward(x[:0], [0, 0]).shape == (0, 256)
+        outs.append(stack.forward(x, [40, 0]))
+    assert torch.equal(*outs)
+    srv.close()
+
+
 def test_tokens_that_do_not_fit_are_refused(F):
     gen = generator(F, 2)
     gen.start([5, 5])

@@ -77,7 +77,7 @@ class BlockStack:
     def __init__(self, cfg: "F.fl_server_cfg", blocks, n_seqs: int, max_tokens: int, page_size: int = 64,
                  n_pages: Optional[int] = None):
         """cfg: the shapes (of ``make_cfg``); blocks: for each a function tensor id -> fp32 numpy values
-        (``FL_T_*``); max_tokens: most tokens of a sequence, its prefix included."""
+        (``FL_T_*``); max_tokens: most tokens of a sequence, its prefix included (in whole pages)."""
         c = self.cfg = cfg
         H, Fh, P = c.hidden, c.ffn_hidden, c.prefix_len
         self.rdim = c.rotary_dim or c.head_dim // 2
@@ -100,7 +100,7 @@ class BlockStack:
                         for _ in "kv"]}
             b["cache"] = F.kv_cache(b["kv"][0], b["kv"][1], self.n_pages, page_size, c.n_heads, c.head_dim)
             self.blocks.append(b)
-        self.max_pos = max_tokens + 1
+        self.max_pos = width * page_size + 1  # of any token that its table row has room for
         self.rope = torch.empty((self.max_pos, self.rdim // 2, 2), device="cuda")
         F.fl_k_rotary_table(self.max_pos, self.rdim, c.rope_base, self.rope, **_stream())
         self.status = torch.zeros(1, dtype=I32, device="cuda")

@@ -205,3 +205,19 @@ def test_tokens_that_do_not_fit_are_refused(F):
     want = torch.stack(gen.logits([a, b]))
     gen.start([5, 5])
     assert torch.equal(torch.stack(gen.logits([a.repeat_interleave(3)[::3], b])), want)
+
+
+# ------------------------------------------------------------------------------- positions
+
+def test_a_sequence_may_fill_its_last_page(F):
+    from paper_2406_14898_gb300.generate import BlockStack
+    srv = server(F, 1, 4, 64, 64)
+    x = rows(48, 256)
+    outs = []
+    for most in (48, 40):  # three pages either way
+        stack = BlockStack.from_server(srv, 1, most, page_size=16)
+        outs.append(torch.cat([stack.forward(x[:39], [39]), stack.forward(x[39:], [9])]))
+        with pytest.raises(ValueError):
+            stack.forward(x[:1], [1])
+    assert torch.equal(*outs)
+    srv.close()

@@ -121,8 +121,10 @@ class BlockStack:
     def start(self, s: int, context_len: int = 0, mask_pos: Optional[int] = None):
         """A new sequence in place s: its first context_len tokens see each other (GLM blank infilling, §4.1.1, the
         mask token at mask_pos or last among them) and the rest follow causally."""
-        self.pages.drop(s)
         P = self.cfg.prefix_len
+        if context_len < 0 or (context_len and mask_pos is not None and not 0 <= mask_pos < context_len):
+            raise ValueError(f"a context of {context_len} tokens with its mask at {mask_pos}")
+        self.pages.drop(s)
         self.context[s] = context_len + P if context_len else 0
         self.mask_pos[s] = context_len - 1 if mask_pos is None else mask_pos
         if P:  # the P-tuning prefix takes the first places of the cache; its keys are not turned
@@ -168,6 +170,8 @@ class BlockStack:
         if not x.is_cuda or x.shape != (sum(new), self.cfg.hidden):
             raise ValueError(f"x {tuple(x.shape)} on {x.device} for {sum(new)} new tokens of {self.cfg.hidden}")
         for s, (n, held, c) in enumerate(zip(new, self.pages.lens, self.context)):
+            if n and held < self.cfg.prefix_len:
+                raise ValueError(f"sequence {s} has not been started: its prefix is not there")
             if n and held < c and held + n < c:
                 raise ValueError(f"sequence {s}: {n} tokens of a context of {c - self.cfg.prefix_len}, which come in one call")
         if not any(new):

@@ -221,3 +221,21 @@ def test_a_sequence_may_fill_its_last_page(F):
             stack.forward(x[:1], [1])
     assert torch.equal(*outs)
     srv.close()
+
+
+def test_positions_that_do_not_exist_are_refused(F):
+    from paper_2406_14898_gb300.generate import BlockStack
+    srv = server(F, 1, 4, 64, 64, 7)
+    stack = BlockStack.from_server(srv, 2, 64, page_size=16)
+    x = rows(20, 256)
+    with pytest.raises(ValueError):
+        stack.forward(x, [20, 0])  # its prefix is not there yet
+    stack.start(0, 20, 19)
+    want = stack.forward(x, [20, 0])
+    for context, mask in ((-1, None), (20, 20), (20, -1), (20, 2 ** 30)):
+        with pytest.raises(ValueError):
+            stack.start(0, context, mask)
+    assert stack.pages.lens == [27, 0] and stack.context[0] == 27 and stack.mask_pos[0] == 19
+    stack.start(0, 20)
+    assert torch.equal(stack.forward(x, [20, 0]), want)
+    srv.close()

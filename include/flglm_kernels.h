@@ -248,7 +248,8 @@ int fl_k_colsum(int32_t T, int32_t N, const void* x, float* out, void* stream);
 /* ---------------------------------------------------------------- answering with a model
  * A model answers token by token: the keys and values of the tokens before stay in a paged cache, and a
  * block is given a chunk of new tokens (a whole prompt, a part of one, or the one token chosen last).
- * For each block: the QKV projection (fl_k_gemm, FL_EPI_STORE), fl_k_kv_append, fl_k_kv_attention.
+ * For each block: the QKV projection (fl_k_gemm with FL_EPI_BIAS_ROPE and an append without rotation, which rounds
+ * queries and keys once; or FL_EPI_STORE and an append that turns them), fl_k_kv_append, fl_k_kv_attention.
  * The lengths and the page table are read on the device when the kernels run: no call copies or synchronises,
  * and a captured graph may be replayed after they changed.
  *

@@ -7,8 +7,8 @@ new tokens: a whole prompt, a part of one, or the one token chosen last.
 
 ``BlockStack`` is one part: blocks of a ``Server`` or of a ``Client`` as ``forward`` over packed new
 tokens, from the library's entry points (``fl_k_layernorm_fwd``, ``fl_k_gemm``, ``fl_k_kv_append``,
-``fl_k_kv_attention``).  Its arithmetic is that of ``fl_server_forward``, except that queries and keys are
-rounded to bf16 before their rotation and not only after it.
+``fl_k_kv_attention``).  Its arithmetic is that of ``fl_server_forward``: queries and keys are turned in the
+projection's epilogue, before their one rounding.
 
     python -m paper_2406_14898_gb300.generate --tokens 16
 
@@ -207,11 +207,12 @@ class BlockStack:
         for b in self.blocks:
             (w_qkv, w_dense, w_up, w_down), (b_qkv, b_dense, b_up, b_down) = b["w"], b["b"]
             norm(x, *b["ln"][:2])
-            F.gemm(T, 3 * H, H, a, H, 0, w_qkv, H, 0, qkv, 3 * H, status=status, bias=b_qkv, **on)
-            q = qkv.data_ptr()  # the queries are turned in place
-            F.fl_k_kv_append(b["cache"], batch, c.n_heads, q, q + 2 * H, q + 4 * H, q, self.rope, self.max_pos,
-                             self.status, rotary_dim=self.rdim, positions=pos, block_positions=pos2, ldq=3 * H,
-                             ldk=3 * H, ldv=3 * H, ldqo=3 * H, **on)
+            F.gemm(T, 3 * H, H, a, H, 0, w_qkv, H, 0, qkv, 3 * H, status=status, epilogue=F.FL_EPI_BIAS_ROPE, bias=b_qkv,
+                   pos=pos, pos2=pos2, rope_tab=self.rope, n_heads=c.n_heads, head_dim=c.head_dim,
+                   rotary_dim=self.rdim, **on)
+            q = qkv.data_ptr()
+            F.fl_k_kv_append(b["cache"], batch, c.n_heads, None, q + 2 * H, q + 4 * H, None, None, 0, self.status,
+                             ldk=3 * H, ldv=3 * H, **on)
             F.fl_k_kv_attention(b["cache"], batch, c.n_heads, q, o, self.workspace, self.status, context_lens=context,
                                 ldq=3 * H, **on)
             h = residual(T, H, o, w_dense, b_dense, x, *b["ln"][:2])

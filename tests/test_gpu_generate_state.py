@@ -239,3 +239,43 @@ def test_positions_that_do_not_exist_are_refused(F):
     stack.start(0, 20)
     assert torch.equal(stack.forward(x, [20, 0]), want)
     srv.close()
+
+
+# ------------------------------------------------------------------------------- roundings
+
+@pytest.mark.parametrize("head_dim,glm", [(64, False), (128, True)])
+def test_cached_keys_are_rounded_once(F, head_dim, glm):
+    """Keys of the first block against their definition in 64 bits from the same 16-bit operands.  Tolerance:
+    half an ulp of the key, and of each pair's sums of `hidden` products in 32 bits (in any order) at most
+    hidden 2^-24 sum |a w|, 4 ulps of 32 bits for the turn."""
+    from paper_2406_14898_gb300.generate import BlockStack
+    heads, T = 2, 90
+    H = heads * head_dim
+    H = 256 * -(-H // 256)
+    heads = H // head_dim
+    srv = server(F, 1, heads, head_dim, T)
+    stack = BlockStack.from_server(srv, 1, T, page_size=16)
+    c = 60 if glm else 0
+    stack.start(0, c, 33 if glm else None)
+    x = rows(T, H)
+    stack.forward(x, [T])
+    b = stack.blocks[0]
+    a = torch.empty_like(x)
+    stats = torch.empty((2, T), device="cuda")
+    F.fl_k_layernorm_fwd(T, H, x, *b["ln"][:2], stack.cfg.ln_eps, a, stats[0], stats[1])
+    w = b["w"][0][H:2 * H].double()
+    k = (a.double() @ w.T + b["b"][0][H:2 * H].double()).view(T, heads, head_dim)
+    size = (a.double().abs() @ w.abs().T + b["b"][0][H:2 * H].double().abs()).view(T, heads, head_dim)
+    i = torch.arange(T, device="cuda")
+    first = torch.where(i < c, i, torch.tensor(33, device="cuda")) if glm else i
+    rd = head_dim // 2
+    turn64(k, stack.rope, first, "half", 0, rd)
+    if glm:
+        turn64(k, stack.rope, (i - c + 1).clamp(min=0), "half", rd, rd)
+    at = stack.pages.table[0].long().cuda()
+    got = b["kv"][0][at].transpose(1, 2).flatten(0, 1)[:T].double()  # [token, head, dim]
+    wide = size.amax(-1, keepdim=True)
+    tol = 1.001 * UNIT["bf16"] * k.abs() + 2 * (H + 4) * 2.0 ** -24 * wide
+    worst = ((got - k).abs() / tol).amax()
+    assert float(worst) <= 1, float(worst)
+    srv.close()

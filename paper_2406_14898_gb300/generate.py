@@ -110,8 +110,14 @@ class BlockStack:
         torch.cuda.current_stream().synchronize()  # whichever stream uses them
 
     @classmethod
-    def from_server(cls, srv: "F.Server", n_seqs: int, max_tokens: int, **kw):
-        return cls(srv.cfg, [lambda t, b=b: srv.get_param(b, t) for b in range(srv.cfg.n_blocks)], n_seqs, max_tokens, **kw)
+    def from_server(cls, srv: "F.Server", n_seqs: int, max_tokens: int, replica: Optional[int] = None, **kw):
+        """replica: which one of a handle that holds several (required there: they differ until they are averaged)."""
+        if replica is None:
+            if srv.cfg.n_replicas > 1:
+                raise ValueError(f"the server holds {srv.cfg.n_replicas} replicas: which one answers?")
+            replica = 0
+        return cls(srv.cfg, [lambda t, b=b: srv.get_replica_param(replica, b, t) for b in range(srv.cfg.n_blocks)], n_seqs,
+                   max_tokens, **kw)
 
     @classmethod
     def from_client(cls, client: "F.Client", part: int, n_seqs: int, max_tokens: int, **kw):
@@ -231,9 +237,10 @@ class BlockStack:
 class Generator:
     """Clients that answer together: each has its own ends of the model, the server serves all in one call."""
 
-    def __init__(self, clients: Sequence["F.Client"], server: "F.Server", max_tokens: int):
+    def __init__(self, clients: Sequence["F.Client"], server: "F.Server", max_tokens: int, replica: Optional[int] = None):
+        """replica: as in ``BlockStack.from_server``."""
         self.clients, n = list(clients), len(clients)
-        self.server = BlockStack.from_server(server, n, max_tokens)
+        self.server = BlockStack.from_server(server, n, max_tokens, replica)
         self.bottom = [BlockStack.from_client(c, F.FL_CP_BOTTOM, 1, max_tokens) for c in clients]
         self.top = [BlockStack.from_client(c, F.FL_CP_TOP, 1, max_tokens) for c in clients]
         self.ends = []

@@ -279,3 +279,31 @@ def test_cached_keys_are_rounded_once(F, head_dim, glm):
     worst = ((got - k).abs() / tol).amax()
     assert float(worst) <= 1, float(worst)
     srv.close()
+
+
+# ------------------------------------------------------------------------------- replicas
+
+def test_a_handle_of_replicas_is_asked_for_one(F):
+    """Two replicas that trained on different groups of clients differ; each answers as its own forward does."""
+    from paper_2406_14898_gb300.generate import BlockStack
+    cfg = F.fl_server_cfg()
+    F.lib().fl_server_cfg_default(cfg)
+    cfg.n_blocks, cfg.hidden, cfg.n_heads, cfg.head_dim, cfg.rotary_dim = 1, 256, 4, 64, 0
+    cfg.ffn_hidden, cfg.residual_alpha, cfg.max_tokens, cfg.n_replicas, cfg.init_std = 1024, 2.0, 64, 2, 0.05
+    srv = F.Server(cfg, 5)
+    x = [rows(32, 256, s).view(1, 32, 256) for s in (1, 2)]
+    y, g = ([torch.empty_like(v) for v in x] for _ in "yg")
+    torch.cuda.synchronize()
+    srv.forward(x, [32, 32], y)
+    srv.backward(y, g)
+    srv.step(0.05)
+    srv.forward(x, [32, 32], y)
+    srv.sync()
+    with pytest.raises(ValueError):
+        BlockStack.from_server(srv, 1, 32)
+    outs = [BlockStack.from_server(srv, 1, 32, replica=r).forward(x[r][0], [32]) for r in (0, 1)]
+    for r in (0, 1):
+        assert rel_inf(outs[r].double().cpu().numpy(), y[r][0].double().cpu().numpy()) < TOL
+    other = BlockStack.from_server(srv, 1, 32, replica=0).forward(x[1][0], [32])
+    assert rel_inf(other.double().cpu().numpy(), y[1][0].double().cpu().numpy()) > 10 * TOL
+    srv.close()

@@ -288,15 +288,17 @@ class Generator:
             F.fl_k_embedding_gather(len(t), h.shape[1], t, e["embed"], c.cfg.vocab, h, stack.status, **_stream())
             hs.append(forward(stack, h, [len(t)]))
         mid = forward(self.server, torch.cat(hs), new).split(new)
-        out = []
+        out, status = [], torch.zeros(1, dtype=I32, device="cuda")
         for c, e, stack, h in zip(self.clients, self.ends, self.top, mid):
             H, n = h.shape[1], e["head"].shape[0]
             last = forward(stack, h, [len(h)])[-1:].contiguous()
             y, stats = torch.empty_like(last), torch.empty(2, device="cuda")
             F.fl_k_layernorm_fwd(1, H, last, *e["ln"], c.cfg.block.ln_eps, y, stats[:1], stats[1:], **_stream())
             z = torch.empty((1, n), device="cuda")
-            F.gemm(1, n, H, y, H, 0, e["head"], H, 0, z, n, d_dtype=F.FL_DT_F32, **_stream())
+            F.gemm(1, n, H, y, H, 0, e["head"], H, 0, z, n, status=status, d_dtype=F.FL_DT_F32, **_stream())
             out.append(z[0, :c.cfg.vocab])
+        if bits := int(status.item()):
+            raise RuntimeError(f"generation: device status {bits} of the LM heads")
         return out
 
     def greedy(self, prompts: Sequence[torch.Tensor], count: int) -> List[List[int]]:

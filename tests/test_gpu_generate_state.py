@@ -127,6 +127,30 @@ def test_clients_are_not_ahead_of_a_server_that_refused(F):
     assert torch.equal(*outs)
 
 
+def test_every_product_has_its_status_looked_at(F, monkeypatch):
+    """A wait that gave up, set by the test in each product's status in turn, is an error, and nothing is added."""
+    gen = generator(F, 1, blocks=1)
+    plain, calls, spoiled = F.gemm, [], 0
+
+    def gemm(*args, status=None, **kw):
+        plain(*args, status=status, **kw)
+        calls.append(status)
+        if len(calls) == spoiled:
+            status.fill_(1)
+
+    monkeypatch.setattr(F, "gemm", gemm)
+    gen.start([5])
+    gen.logits([prompt(0, 5)])
+    n = len(calls)
+    assert n == 3 * 4 + 1
+    for spoiled in range(n + 1, 2 * n + 1):
+        del calls[n:]
+        with pytest.raises(RuntimeError):
+            gen.logits([prompt(1, 1)])
+            pytest.fail(f"product {spoiled - n} of {n}")
+        assert [x.pages.lens[0] for x in (gen.server, gen.bottom[0], gen.top[0])] == [5, 5, 5]
+
+
 # ------------------------------------------------------------------------------- contexts
 
 def test_a_context_in_two_calls_is_refused(F):

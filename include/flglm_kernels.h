@@ -313,7 +313,7 @@ typedef struct {
  * token lens[s] - n_s + i.  Token u lies in slot u % page_size of page page_table[s * table_stride +
  * u / page_size].  cu_new [n_seqs + 1], lens [n_seqs], page_table [n_seqs, table_stride]: device int32.
  * max_new: at least the largest n_s, 1 or more where there are tokens (it chooses the kernel; a larger n_s is still
- * computed). */
+ * computed).  n_seqs, n_tokens and table_stride * page_size at most 2^31 - 1024 (CAPACITY). */
 typedef struct {
   int32_t n_seqs, n_tokens, max_new, table_stride;
   const int32_t *cu_new, *lens, *page_table;

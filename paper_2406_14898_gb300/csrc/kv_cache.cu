@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(BLOCK) append_kernel(AppendArgs<T> p, KvBatchD
     if (!(t < bt.S && __ldg(bt.cu + t) <= t && __ldg(bt.cu + t + 1) > t)) {
       int lo = 0, hi = bt.S;  // cu[lo] <= t < cu[hi] (assumed of the ends, checked below)
       while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
+        const int mid = lo + ((hi - lo) >> 1);
         if (__ldg(bt.cu + mid) <= t) lo = mid; else hi = mid;
       }
       s = lo;
@@ -322,8 +322,10 @@ int fl_kv_check(const char* who, const fl_kv_cache* c, const fl_kv_batch* b, int
     return fl_internal_error(FL_ERR_INVALID_ARG, "%s: alignment", who);
   int lg = 4;
   while ((1 << lg) < ps) ++lg;
-  if (((int64_t)b->table_stride << lg) > 0x7fffffff)
-    return fl_internal_error(FL_ERR_CAPACITY, "%s: more than 2^31 - 1 tokens in a page table row", who);
+  // what the kernels count in 32 bits goes up to a few hundred past these: tokens of tiles and key blocks that end late
+  constexpr int64_t most = (1ll << 31) - 1024;
+  if (((int64_t)b->table_stride << lg) > most || b->n_tokens > most || b->n_seqs > most)
+    return fl_internal_error(FL_ERR_CAPACITY, "%s: more than 2^31 - 1024 sequences, new tokens or tokens in a page table row", who);
   *out = KvBatchDev{b->cu_new, b->lens, b->page_table, nullptr, b->n_seqs, b->n_tokens, b->table_stride, lg, c->n_pages,
                     nullptr};
   return FL_OK;

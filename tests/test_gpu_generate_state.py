@@ -331,3 +331,23 @@ def test_a_handle_of_replicas_is_asked_for_one(F):
     other = BlockStack.from_server(srv, 1, 32, replica=0).forward(x[1][0], [32])
     assert rel_inf(other.double().cpu().numpy(), y[1][0].double().cpu().numpy()) > 10 * TOL
     srv.close()
+
+
+# ------------------------------------------------------------------------------- clients
+
+def test_a_clients_logits_do_not_depend_on_the_others(F):
+    lens = [40, 9, 130]
+    prompts = [prompt(k, n) for k, n in enumerate(lens)]
+    steps = [[prompt(10 * j + k, 1) for k in range(3)] for j in range(3)]
+    together = generator(F, 3)
+    together.start(lens)
+    want = [together.logits(t) for t in [prompts] + steps]
+    for k in range(3):
+        alone = generator(F, 1, which=[k])
+        alone.start(lens[k:k + 1])
+        for t, w in zip([prompts] + steps, want):
+            z = alone.logits(t[k:k + 1])[0]
+            assert rel_inf(z.double().cpu().numpy(), w[k].double().cpu().numpy()) < TOL
+        for other in range(3):  # and the bound tells clients apart
+            if other != k:
+                assert rel_inf(want[0][other].double().cpu().numpy(), want[0][k].double().cpu().numpy()) > 10 * TOL

@@ -287,7 +287,7 @@ int fl_k_rotary_table(int32_t max_pos, int32_t rotary_dim, float base, int32_t s
  * rounded once.  backward = 1 applies the transpose, (a c + b s, b c - a s): x is then the gradient of the
  * turned rows, y that of the rows before.  dtype FL_DT_BF16, FL_DT_F16 or FL_DT_F32.  Row t, head h starts at
  * x + t ldx + h x_head_stride elements; y may be x with the same strides, else they do not overlap.
- * A position outside [0, max_pos) gives a row of zeros and sets FL_KV_BAD_POSITION.
+ * A position outside [0, max_pos) gives zeros in the dims that it turns and sets FL_KV_BAD_POSITION.
  * Requirements (UNSUPPORTED): head_dim a multiple of 16 up to 256, rotary_dim a multiple of 16, the turned dims
  * within head_dim; strides multiples of 16 bytes, none negative; pointers 16-byte aligned (positions and status 4).
  * T = 0 does nothing; T n_heads (and the append's rows, n_tokens (n_heads + 2 kv_heads)) below 2^31 (CAPACITY).  A

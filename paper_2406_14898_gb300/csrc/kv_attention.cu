@@ -14,8 +14,8 @@
 // inside a contraction and of the dims of O^T are free: they are chosen so that each lane reads 16
 // consecutive bytes.
 // One new token in each of 32 sequences of 64 to 4096 tokens, 32 key heads of 128: 984 MB read, each key and value once, in
-// 147 us (6.7 TB/s); four sequences of 40001 to 65536, four key heads: 453 MB in 78 us (5.8 TB/s; the launch, the plan and
-// the join of each unit's parts are the rest).  A sequence of 300 takes 9.6 us, the latencies of the plan, the page table,
+// 147 to 149 us (6.6 TB/s); four sequences of 40001 to 65536, four key heads: 453 MB in 78 us (5.8 TB/s; the launch, plan and
+// the join of each unit's parts are the rest).  A sequence of 300 takes 8.4 us, the latencies of the plan, the page table,
 // the keys and the join one after another.
 // P is rounded to 16 bits for its product, the sums take it unrounded: an error of half an ulp of the output's type per
 // weight, independent of one another.
@@ -35,8 +35,8 @@ namespace {
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int STEP = 16;              // keys a warp takes at a time (one page holds them)
 constexpr int BK = WARPS * STEP;      // keys of a block
-constexpr int JOIN = 8;               // parts read at a time when a unit is joined: 453 MB in 80.3 us, one by one 82.9
-constexpr int MIN_COST = 1;           // blocks that are worth a CTA: one token over 5 MB in 9.6 us, 10.5 with 2, 14.8 with 4
+constexpr int JOIN = 8;               // parts read at a time when a unit is joined: when chosen, 453 MB in 80.3 us, one by one 82.9
+constexpr int MIN_COST = 1;           // blocks that are worth a CTA: when chosen, one token over 5 MB in 9.6 us, 10.5 with 2, 14.8 with 4
 constexpr float LOG2E_F = 1.4426950408889634f, LN2_F = 0.6931471805599453f;
 
 template <class T>

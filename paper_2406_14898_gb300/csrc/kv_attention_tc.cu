@@ -20,12 +20,12 @@
 // of the tensor instruction's operands; l sums it unrounded, in fp32 as O.
 // Work is divided among the CTAs as kv_plan.cuh says.
 //
-// 2048 new tokens behind 27953, 32 query heads on 8: 0.97 PFLOP in 655 us (1.48 PFLOP/s, the tensor pipe busy six tenths of
-// the time); 16 prompts of 72 to 979 tokens, 32 heads each with its own keys, 158 us (0.68); 8 chunks of 256 tokens after up
-// to 2044, 70 us.  What bounds it is a stream's chain: scores, weights (two passes over 128 scores, an exponential each),
+// 2048 new tokens behind 27953, 32 query heads on 8: 0.97 TFLOP in 705 us (1.38 PFLOP/s; single calls 655, 1.48, before the
+// card is at its power limit, the tensor pipe busy 62% of the time); 16 prompts of 72 to 979 tokens, 32 heads each with its
+// own keys, 157 us (0.68 PFLOP/s); 8 chunks of 256 tokens after up to 2044, 70 us.  What bounds it is a stream's chain: scores, weights (two passes over 128 scores, an exponential each),
 // products, about 3100 cycles a block of two streams where the products alone take 2048; a short unit adds its
 // ends.  Short code counts: while a role waits its instructions leave the cache, so loops of 64 columns stay rolled, and
-// what is rare is marked as unlikely to keep it out of their lines (776 to 767 us).
+// what is rare is marked as unlikely to keep it out of their lines (776 to 767 us when that was done).
 //
 // Every wait is bounded.  A warp whose wait ran out records it and, in a role that issues, leaves; a softmax warp goes
 // through the rest of its unit without waiting, and its warpgroup then leaves together.
@@ -47,7 +47,7 @@ constexpr int THREADS = 384, W_TMA = 8, W_MMA = 9, W_FIX = 11;
 // with 5, 159 with 4; before the streams took turns 162.5 with 4, 187 with 1, 165 with 8, and 8 chunks of 256 tokens 75.9, 84.7
 // and 78.
 constexpr int ENDS = 5;
-constexpr int MIN_COST = 4;  // worth a CTA: 12 small sequences in 26.9 us, with 10 in 29.2, with 1 as with 4
+constexpr int MIN_COST = 4;  // worth a CTA: when chosen, 12 small sequences in 26.9 us, with 10 in 29.2, with 1 as with 4
 constexpr float LN2_F = 0.6931471805599453f;
 
 template <int HD>
@@ -149,7 +149,8 @@ struct Piece {
   // Streams that compute their weights at the same time wait for their products at the same time, and some CTAs stay so to
   // the end, a fifth behind the others.  So in the blocks that both take part in, a stream's next scores are begun only when
   // the other one has found the maxima of the block before them: where the streams already alternate that has happened.
-  // 2048 tokens behind 27953 in 655 us, without turns 767; turns told before the maxima 721, behind the first weights 900.
+  // 2048 tokens behind 27953, single calls: 655 us, without turns 767; turns told before the maxima 721, behind the first
+  // weights 900.
   FL_DEV int turns() const { return two ? na[0] : 0; }
 };
 constexpr int PIECES = 4;  // told ahead

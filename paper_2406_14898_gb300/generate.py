@@ -235,7 +235,8 @@ class BlockStack:
 
 
 class Generator:
-    """Clients that answer together: each has its own ends of the model, the server serves all in one call."""
+    """Clients that answer together: each has its own ends of the model, the server serves all in one call.  The weights
+    are those of the handles when it is made; one that trains on needs a new generator."""
 
     def __init__(self, clients: Sequence["F.Client"], server: "F.Server", max_tokens: int, replica: Optional[int] = None):
         """replica: as in ``BlockStack.from_server``."""

@@ -215,7 +215,9 @@ def _prepare_trace(case, gen, st):
     S, B, T = case["clients"], case["beams"], case["steps"]
     st["state"] = _search_state(S, B, T, gen)
     st["state"]["steps"] += (torch.rand(S, generator=gen, device="cuda") < 0.5).int()
-    st["state"]["done"] = (torch.rand(S, generator=gen, device="cuda") < 0.3).int()
+    st["state"]["steps"].clamp_(min=1)
+    ended = st["state"]["end_scores"][:, 0] > -math.inf
+    st["state"]["done"] = (ended & (torch.rand(S, generator=gen, device="cuda") < 0.3)).int()
     st["trace_tokens"] = torch.randint(130528, (S, T, B), generator=gen, device="cuda", dtype=torch.int32)
     a, b = (torch.randint(B, (S, T, B), generator=gen, device="cuda", dtype=torch.int32) for _ in "ab")
     st["trace_parents"] = torch.minimum(a, b)

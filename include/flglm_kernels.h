@@ -354,6 +354,107 @@ int fl_k_kv_attention(const fl_kv_cache* cache, const fl_kv_batch* batch, int32_
                       float scale, const int32_t* context_lens, void* o, int64_t ldo, float* lse, void* workspace,
                       int* status, void* stream);
 
+/* ---------------------------------------------------------------- sequences that share pages
+ * A page of a cache may serve several sequences: those that continue one prompt have its whole pages in common.
+ * table [n_seqs, table_stride] and lens [n_seqs] are those of fl_kv_batch; refs [n_pages] counts who has each page: the
+ * sequences' table rows that name it (their first ceil(lens / page_size) entries) and holders outside of the table (a caller that
+ * keeps a prompt's pages for later adds one to each, and takes it off again).  A page with refs 0 is free.  All device
+ * int32.  What a call changes goes to the arrays of a second fl_kv_pages (`to`) of the same sizes, which takes the
+ * first one's place afterwards: none of the arrays may be the same.  page_size as in fl_kv_cache; n_seqs *
+ * table_stride and table_stride * page_size at most 2^31 - 1024, n_seqs at most 2^20 (CAPACITY). */
+typedef struct {
+  int32_t n_seqs, n_pages, page_size, table_stride;
+  int32_t *lens, *table, *refs;
+} fl_kv_pages;
+
+/* More bits of *status. */
+enum {
+  FL_KV_NO_ROOM = 16,   /* too few pages are free, or a sequence outgrows its table row: nothing was changed */
+  FL_KV_BAD_PARENT = 32 /* a parent outside [-1, n_seqs): nothing was changed */
+};
+#define FL_KV_MAX_CACHES 64 /* caches of one call */
+
+/* Every sequence s of `to` continues sequence parents[s] of `from` (NULL: itself; -1: none, it starts empty), with
+ * room for new_tokens[s] tokens more (NULL: none; negative: so many are taken off its end, at most all): the step of a
+ * beam search, new sequences beside old ones, sequences that leave (-1).  With it to->lens is what fl_kv_batch wants
+ * for an append of the new tokens.  Whole pages are shared.  Whoever is about to write (new_tokens > 0) into a
+ * partly filled last page that other sequences or holders have too gets a page of its own, into which the page's
+ * tokens of its sequence are copied in every cache; where all who have the page write, the first of them keeps it.
+ * New pages are the lowest-numbered free ones, handed out in the order of the sequences, each one's copy first; pages that the
+ * call itself frees count as free.  Entries of to->table behind a sequence's pages are -1.
+ * caches [n_caches] (host array, 1 to FL_KV_MAX_CACHES): the caches that the table serves (every block's), alike but for
+ * k and v, with n_pages and page_size those of `from`.  parents, new_tokens: device int32 [n_seqs].
+ * A call that cannot be done as a whole (FL_KV_NO_ROOM, FL_KV_BAD_PARENT) makes `to` what `from` is.  Lengths outside of their row
+ * are brought into it, and entries that name no page are passed on but not copied (FL_KV_BAD_PAGE).
+ * workspace: fl_k_kv_pages_workspace bytes, 16-byte aligned, ZERO before its first use; calls one after another on a
+ * stream, of this kind and the next, may share it as long as n_seqs, n_pages and table_stride stay; calls that may
+ * overlap need one each.  Arrays 4-byte aligned, n_seqs = 0 does nothing. */
+size_t fl_k_kv_pages_workspace(const fl_kv_pages* pages);
+int fl_k_kv_fork(const fl_kv_cache* caches, int32_t n_caches, const fl_kv_pages* from, const fl_kv_pages* to,
+                 const int32_t* parents, const int32_t* new_tokens, void* workspace, int* status, void* stream);
+
+/* Moves the pages in use (refs > 0) to the front: with n of them, those from n on go, in ascending order, to the free ones
+ * below n, in ascending order, in every cache; their old places keep what they held, and are free.  to->table names the new places
+ * (-1 behind a sequence's pages, and where an entry names no page in use: FL_KV_BAD_PAGE), to->refs counts there,
+ * to->lens is from->lens.  moved (device int32 [n_pages]): the new place of each page in use, -1 of the
+ * others; used (device int32): n.  Caches, workspace and limits as in fl_k_kv_fork; n_seqs = 0 is a cache that
+ * only holders outside of the table have. */
+int fl_k_kv_compact(const fl_kv_cache* caches, int32_t n_caches, const fl_kv_pages* from, const fl_kv_pages* to,
+                    int32_t* moved, int32_t* used, void* workspace, int* status, void* stream);
+
+/* ---------------------------------------------------------------- beam search
+ * n_seqs searches of `beams` beams each (1 to FL_BEAM_MAX), over tokens [0, vocab) (1 to 2^19), of at most max_steps tokens.
+ * Beam b of search s is row s * beams + b of the logits, and of the sequences of a cache.  eos: the token that ends a
+ * hypothesis, -1: none.  A search is done when no beam is live, or when `beams` hypotheses have
+ * ended and (early = 1) at once, (early = 0) the best live beam, as long as it is now, does not score more than the worst of them.  A hypothesis of n tokens (eos among them)
+ * with the summed log-probability c scores c / n^length_penalty.  n_seqs at most 16384 (CAPACITY). */
+#define FL_BEAM_MAX 16
+typedef struct {
+  int32_t n_seqs, beams, vocab, max_steps, eos, early;
+  double length_penalty;
+} fl_beam_search;
+
+/* Where the searches stand (device arrays).  A search begins with scores 0, -inf, -inf ...: all of its beams would say the
+ * same; steps and done 0, end_scores -inf, end_steps and end_beams 0. */
+typedef struct {
+  float* scores;      /* [n_seqs, beams] summed log-probabilities of the live beams, descending; -inf: no beam */
+  int32_t* steps;     /* [n_seqs] tokens chosen */
+  int32_t* done;      /* [n_seqs] 1: the search is over */
+  float* end_scores;  /* [n_seqs, beams] scores of the best hypotheses that have ended, descending; -inf: none */
+  int32_t* end_steps; /* [n_seqs, beams] tokens before its eos */
+  int32_t* end_beams; /* [n_seqs, beams] the beam that it ended */
+} fl_beam_state;
+
+/* Bits of *status: a live beam has a logit that is NaN or +infinity, or such a score (the beam is given up); an index of the
+ * back-pointers or the state is out of its range (it counts as 0). */
+enum { FL_BEAM_BAD_LOGITS = 64, FL_BEAM_BAD_TRACE = 128 };
+
+/* One step of every search that is not over (done, or max_steps tokens): with c(b, v) = scores[b] + logits[b, v] - logsumexp(logits[b]) and
+ * candidates ordered by c (then the lower beam, the higher logit, the lower token; -inf is no candidate), the next
+ * beams are the best candidates other than eos, and an eos among the best `beams` of all candidates ends a
+ * hypothesis.  `to` receives the new state (it may be `from`; else no array of the two may be the same).  Each search's new
+ * tokens and the beams (0 .. beams - 1) that they follow are also written into row steps[s] of trace_tokens and trace_parents (int32
+ * [n_seqs, max_steps, beams]).  tokens, parents (int32 [n_seqs, beams]): the same for the model's next
+ * call, parents as rows s * beams + b for fl_k_kv_fork.  A beam that is not live (too few candidates, or the search is
+ * over) has token eos (0 without one) and parent -1, and in the trace itself as parent.
+ * logits: dtype FL_DT_F32, FL_DT_BF16 or FL_DT_F16, rows ld elements apart (a multiple of 16 bytes, vocab or
+ * more; what lies behind vocab is not used), 16-byte aligned.  Rows of beams that are not live are not used.  Sums are fp32,
+ * scores are formed in 64 bits and rounded once.
+ * workspace: fl_k_beam_workspace bytes, 16-byte aligned, ZERO before its first use; calls one after another on a
+ * stream may share it, of any searches for which it is large enough; calls that may overlap need one each. */
+size_t fl_k_beam_workspace(const fl_beam_search* search);
+int fl_k_beam_step(const fl_beam_search* search, const fl_beam_state* from, const fl_beam_state* to, int32_t dtype,
+                   const void* logits, int64_t ld, int32_t* trace_tokens, int32_t* trace_parents, int32_t* tokens,
+                   int32_t* parents, void* workspace, int* status, void* stream);
+
+/* The n_best (1 to beams) best hypotheses of each search: those that have ended and, where the search is not done, the
+ * live beams as they are; equal scores in that order.  out_tokens [n_seqs, n_best, max_steps]: their tokens, then `pad`; a
+ * hypothesis that ended has its eos last (without an eos in `search`, `pad`).  out_lens, out_scores [n_seqs, n_best]: 0 and -inf
+ * where there are fewer.  A state that fl_k_beam_step has left is not changed. */
+int fl_k_beam_trace(const fl_beam_search* search, const fl_beam_state* state, const int32_t* trace_tokens,
+                    const int32_t* trace_parents, int32_t n_best, int32_t pad, int32_t* out_tokens, int32_t* out_lens,
+                    float* out_scores, int* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

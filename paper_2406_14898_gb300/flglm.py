@@ -30,7 +30,10 @@ FL_TILE_AUTO, FL_TILE_128x128, FL_TILE_128x256, FL_TILE_256x256_PAIR = range(4)
 FL_GEMM_MAX_BATCH = 4
 PROF_CLASSES = ("gemm", "attention", "layernorm", "adamw", "other")
 FL_DT_BF16, FL_DT_F32, FL_DT_F16 = 0, 1, 2
-FL_KV_BAD_POSITION, FL_KV_BAD_PAGE, FL_KV_TIMEOUT = 1, 2, 8
+FL_KV_BAD_POSITION, FL_KV_BAD_PAGE, FL_KV_TIMEOUT, FL_KV_NO_ROOM, FL_KV_BAD_PARENT = 1, 2, 8, 16, 32
+FL_KV_MAX_CACHES = 64
+FL_BEAM_BAD_LOGITS, FL_BEAM_BAD_TRACE = 64, 128
+FL_BEAM_MAX = 16
 FL_ROPE_HALF, FL_ROPE_INTERLEAVED = 0, 1
 FL_ROPE_SCALE_NONE, FL_ROPE_SCALE_LINEAR, FL_ROPE_SCALE_NTK, FL_ROPE_SCALE_BY_PARTS = range(4)
 
@@ -90,6 +93,21 @@ class fl_kv_batch(C.Structure):
                 ("cu_new", C.c_void_p), ("lens", C.c_void_p), ("page_table", C.c_void_p)]
 
 
+class fl_kv_pages(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("table_stride", C.c_int32),
+                ("lens", C.c_void_p), ("table", C.c_void_p), ("refs", C.c_void_p)]
+
+
+class fl_beam_search(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("beams", C.c_int32), ("vocab", C.c_int32), ("max_steps", C.c_int32),
+                ("eos", C.c_int32), ("early", C.c_int32), ("length_penalty", C.c_double)]
+
+
+class fl_beam_state(C.Structure):
+    _fields_ = [("scores", C.c_void_p), ("steps", C.c_void_p), ("done", C.c_void_p), ("end_scores", C.c_void_p),
+                ("end_steps", C.c_void_p), ("end_beams", C.c_void_p)]
+
+
 _P = C.c_void_p
 _I32 = C.c_int32
 _I64 = C.c_int64
@@ -144,6 +162,16 @@ _SIGS = {
     "fl_k_kv_attention_workspace": (C.c_size_t, [_I32, C.POINTER(fl_kv_cache), C.POINTER(fl_kv_batch)]),
     "fl_k_kv_attention": (C.c_int, [C.POINTER(fl_kv_cache), C.POINTER(fl_kv_batch), _I32, _P, _I64, _F, _P, _P, _I64,
                                     _P, _P, _P, _P]),
+    "fl_k_kv_pages_workspace": (C.c_size_t, [C.POINTER(fl_kv_pages)]),
+    "fl_k_kv_fork": (C.c_int, [C.POINTER(fl_kv_cache), _I32, C.POINTER(fl_kv_pages), C.POINTER(fl_kv_pages), _P, _P, _P,
+                               _P, _P]),
+    "fl_k_kv_compact": (C.c_int, [C.POINTER(fl_kv_cache), _I32, C.POINTER(fl_kv_pages), C.POINTER(fl_kv_pages), _P, _P,
+                                  _P, _P, _P]),
+    "fl_k_beam_workspace": (C.c_size_t, [C.POINTER(fl_beam_search)]),
+    "fl_k_beam_step": (C.c_int, [C.POINTER(fl_beam_search), C.POINTER(fl_beam_state), C.POINTER(fl_beam_state), _I32, _P,
+                                 _I64, _P, _P, _P, _P, _P, _P, _P]),
+    "fl_k_beam_trace": (C.c_int, [C.POINTER(fl_beam_search), C.POINTER(fl_beam_state), _P, _P, _I32, _I32, _P, _P, _P,
+                                  _P, _P]),
     "fl_client_cfg_default": (None, [C.POINTER(fl_client_cfg)]),
     "fl_client_create": (C.c_int, [C.POINTER(fl_client_cfg), C.c_uint64, C.POINTER(_P)]),
     "fl_client_destroy": (C.c_int, [_P]),
@@ -625,3 +653,62 @@ def fl_k_kv_attention(cache: fl_kv_cache, batch: fl_kv_batch, n_heads, q, o, wor
     check(lib().fl_k_kv_attention(cache, batch, n_heads, ptr(q), row if ldq is None else ldq, scale,
                                   ptr(context_lens), ptr(o), row if ldo is None else ldo, ptr(lse), ptr(workspace),
                                   ptr(status), stream_ptr(stream)))
+
+
+def kv_caches(caches: Sequence[fl_kv_cache]):
+    """The caches that one page table serves, as fl_k_kv_fork and fl_k_kv_compact take them."""
+    return (fl_kv_cache * len(caches))(*caches)
+
+
+def kv_pages(n_seqs, n_pages, page_size, table_stride, lens, table, refs) -> fl_kv_pages:
+    """fl_kv_pages over the device int32 arrays, which the caller keeps alive."""
+    return fl_kv_pages(n_seqs, n_pages, page_size, table_stride, ptr(lens), ptr(table), ptr(refs))
+
+
+def fl_k_kv_pages_workspace(pages: fl_kv_pages) -> int:
+    n = int(lib().fl_k_kv_pages_workspace(pages))
+    if n == 0:
+        raise FlError(-1, (lib().fl_server_last_error(None) or b"").decode())
+    return n
+
+
+def fl_k_kv_fork(caches, pages: fl_kv_pages, out: fl_kv_pages, parents, new_tokens, workspace, status, stream=None):
+    """caches: of kv_caches."""
+    check(lib().fl_k_kv_fork(caches, len(caches), pages, out, ptr(parents), ptr(new_tokens), ptr(workspace), ptr(status),
+                             stream_ptr(stream)))
+
+
+def fl_k_kv_compact(caches, pages: fl_kv_pages, out: fl_kv_pages, moved, used, workspace, status, stream=None):
+    """caches: of kv_caches."""
+    check(lib().fl_k_kv_compact(caches, len(caches), pages, out, ptr(moved), ptr(used), ptr(workspace), ptr(status),
+                                stream_ptr(stream)))
+
+
+def beam_search(n_seqs, beams, vocab, max_steps, eos=-1, length_penalty=1.0, early=False) -> fl_beam_search:
+    return fl_beam_search(n_seqs, beams, vocab, max_steps, eos, 1 if early else 0, length_penalty)
+
+
+def beam_state(scores, steps, done, end_scores, end_steps, end_beams) -> fl_beam_state:
+    """fl_beam_state over the device arrays, which the caller keeps alive."""
+    return fl_beam_state(ptr(scores), ptr(steps), ptr(done), ptr(end_scores), ptr(end_steps), ptr(end_beams))
+
+
+def fl_k_beam_workspace(search: fl_beam_search) -> int:
+    n = int(lib().fl_k_beam_workspace(search))
+    if n == 0:
+        raise FlError(-1, (lib().fl_server_last_error(None) or b"").decode())
+    return n
+
+
+def fl_k_beam_step(search: fl_beam_search, state: fl_beam_state, out: fl_beam_state, logits, trace_tokens, trace_parents,
+                   tokens, parents, workspace, status, dtype=FL_DT_F32, ld=None, stream=None):
+    """out: the new state, or `state`.  ld: row stride of the logits in elements (vocab by default)."""
+    check(lib().fl_k_beam_step(search, state, out, dtype, ptr(logits), search.vocab if ld is None else ld,
+                               ptr(trace_tokens), ptr(trace_parents), ptr(tokens), ptr(parents), ptr(workspace),
+                               ptr(status), stream_ptr(stream)))
+
+
+def fl_k_beam_trace(search: fl_beam_search, state: fl_beam_state, trace_tokens, trace_parents, n_best, pad, out_tokens,
+                    out_lens, out_scores, status, stream=None):
+    check(lib().fl_k_beam_trace(search, state, ptr(trace_tokens), ptr(trace_parents), n_best, pad, ptr(out_tokens),
+                                ptr(out_lens), ptr(out_scores), ptr(status), stream_ptr(stream)))

@@ -1,0 +1,310 @@
+"""Beam search's step and back-pointers against their definition in 64 bits (GPU only)."""
+import numpy as np
+import pytest
+import torch
+
+from tests._beam import DTYPES, INF, Searches, begin, check_step, device_state, step64, trace64
+from tests._gpu import flglm, need_gpu
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def F():
+    need_gpu()
+    return flglm()
+
+
+def row_stride(V, dtype, more=0):
+    unit = 4 if dtype == "f32" else 8
+    return -(-V // unit) * unit + more * unit
+
+
+def logits(rng, S, B, V, dtype, more=1, scale=3.0, stale=np.nan):
+    """[S * B, row] on the device, and the values of its first V columns; behind them `stale`."""
+    x = torch.full((S * B, row_stride(V, dtype, more)), stale, dtype=DTYPES[dtype], device="cuda")
+    x[:, :V] = torch.from_numpy(scale * rng.standard_normal((S * B, V)).astype(np.float32)).cuda().to(DTYPES[dtype])
+    return x
+
+
+def values(x, S, B, V):
+    return x[:, :V].float().cpu().numpy().reshape(S, B, V)
+
+
+def under_way(rng, S, B, max_steps):
+    """A state in the middle of a search."""
+    st = begin(S, B)
+    st["scores"] = -np.cumsum(rng.uniform(0.5, 3, (S, B)).astype(np.float32), 1, dtype=np.float32).astype(np.float64)
+    st["steps"] = rng.integers(0, max_steps, S)
+    for s in range(S):
+        n = int(rng.integers(0, B + 1)) if st["steps"][s] else 0
+        st["end_scores"][s, :n] = -np.sort(rng.uniform(0.01, 4, n).astype(np.float32))
+        st["end_steps"][s, :n] = rng.integers(0, st["steps"][s], n) if n else 0
+        st["end_beams"][s, :n] = rng.integers(0, B, n)
+    return st
+
+
+def one_step(F, state, x, S, B, V, dtype, max_steps, eos=-1, penalty=1.0, early=False, in_place=False, bad=False):
+    run = Searches(F, S, B, V, max_steps, eos, penalty, early)
+    now = device_state(state)
+    out = now if in_place else {k: torch.full_like(v, -7) for k, v in now.items()}
+    run.step(now, out, x, dtype, x.shape[1])
+    want, tokens, parents, rows, was_bad = step64(state, values(x, S, B, V), max_steps, eos, penalty, early)
+    check_step(out, run.tokens, run.parents, want, tokens, parents)
+    assert was_bad == bad and int(run.status.item()) == (F.FL_BEAM_BAD_LOGITS if bad else 0)
+    for s in range(S):
+        tt, tp = run.trace_tokens[s].cpu().numpy(), run.trace_parents[s].cpu().numpy()
+        if rows[s] is not None:
+            t = int(state["steps"][s])
+            assert np.array_equal(tt[t], rows[s][0]) and np.array_equal(tp[t], rows[s][1])
+            tt, tp = np.delete(tt, t, 0), np.delete(tp, t, 0)
+        assert (tt == -9).all() and (tp == -9).all()  # other rows of the trace are left alone
+    assert not run.workspace[:16384].any()  # the counts, for the next call
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("S,B,V", [(1, 1, 1), (2, 3, 2), (1, 16, 7), (3, 5, 8), (2, 4, 9), (5, 2, 1003), (1, 4, 33000),
+                                   (2, 16, 5000), (1, 1, 130528), (40, 4, 4099)])
+def test_step(F, S, B, V, dtype):
+    rng = np.random.default_rng(S * 1000 + B * 100 + V)
+    for eos, penalty, early in ((-1, 0.0, False), (V - 1, 1.0, False), (V // 2, 0.6, True)):
+        st = under_way(rng, S, B, 9)
+        st["done"][:S // 4] = 1
+        x = logits(rng, S, B, V, dtype)
+        if eos >= 0:
+            x[:, eos] = x[:, :V].max(-1).values - torch.from_numpy(rng.uniform(-1, 2, S * B)).cuda().to(x.dtype)
+        one_step(F, st, x, S, B, V, dtype, 9, eos, penalty, early)
+
+
+@pytest.mark.parametrize("S,B,V,dtype", [(64, 16, 130528, "bf16"), (32, 4, 130528, "f32"), (3, 7, 524288, "f16"),
+                                         (700, 3, 257, "f32")])
+def test_step_of_large_calls(F, S, B, V, dtype):
+    rng = np.random.default_rng(V + S)
+    x = torch.randn((S * B, row_stride(V, dtype)), generator=torch.Generator(device="cuda").manual_seed(S),
+                    device="cuda").mul_(3).to(DTYPES[dtype])
+    one_step(F, under_way(rng, S, B, 40), x, S, B, V, dtype, 40, eos=5, penalty=0.8)
+
+
+def test_first_step_looks_at_one_beam(F):
+    rng = np.random.default_rng(1)
+    S, B, V = 3, 5, 700
+    x = logits(rng, S, B, V, "f32")
+    x.view(S, B, -1)[:, 1:] = np.nan  # rows of beams that are not live
+    out = one_step(F, begin(S, B), x, S, B, V, "f32", 4)
+    assert (out["scores"] > -INF).all()
+
+
+def test_in_place(F):
+    rng = np.random.default_rng(2)
+    for S, B, V in ((6, 4, 3001), (2, 16, 40000)):
+        st = under_way(rng, S, B, 30)
+        st["done"][1] = 1
+        one_step(F, st, logits(rng, S, B, V, "bf16"), S, B, V, "bf16", 30, eos=17, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_masks(F, dtype):
+    """Tokens at -inf and at the type's lowest value; rows with nothing left, rows of lowest values only."""
+    rng = np.random.default_rng(3)
+    S, B, V = 6, 3, 1501
+    low = torch.finfo(DTYPES[dtype]).min
+    x = logits(rng, S, B, V, dtype)
+    rows = x.view(S, B, -1)
+    rows[0, :, 40:V] = -INF           # few tokens left
+    rows[1, :, 2:V] = -INF            # fewer than beams in each row
+    rows[2, 0, :V] = -INF             # a row with nothing
+    rows[3, :, :V] = -INF             # a search with nothing: over
+    rows[4, :, 1:V] = low             # one token that counts, and then the lowest values in their order
+    rows[5, 1, :V] = low              # all equal
+    one_step(F, under_way(rng, S, B, 9), x, S, B, V, dtype, 9, eos=11)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_that_are_no_numbers_give_a_beam_up(F, dtype):
+    rng = np.random.default_rng(4)
+    S, B, V = 5, 4, 2050
+    for value, at in ((np.nan, 0), (np.nan, V - 1), (INF, 1027)):
+        x = logits(rng, S, B, V, dtype)
+        x.view(S, B, -1)[1, 2, at] = value
+        x.view(S, B, -1)[3, :, at] = value
+        st = under_way(rng, S, B, 9)
+        st["done"][4] = 1
+        x.view(S, B, -1)[4] = np.nan  # of a search that is over
+        one_step(F, st, x, S, B, V, dtype, 9, eos=at, bad=True)
+    st["scores"][0, 1] = np.nan
+    one_step(F, st, logits(rng, S, B, V, dtype), S, B, V, dtype, 9, bad=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_equal_logits_go_by_their_index(F, dtype):
+    """Whole rows of one value, rows of few values, beams that say the same: the lower beam and token first."""
+    rng = np.random.default_rng(5)
+    for S, B, V in ((3, 4, 20000), (2, 16, 9000), (2, 5, 130)):
+        x = logits(rng, S, B, V, dtype)
+        rows = x.view(S, B, -1)[..., :V]
+        rows[0] = 0.5
+        rows[1] = torch.from_numpy(rng.integers(0, 3, (B, V)).astype(np.float32)).cuda()
+        if S > 2:
+            rows[2] = rows[2, :1]
+        st = under_way(rng, S, B, 9)
+        st["scores"][0] = st["scores"][-1] = -1.5
+        one_step(F, st, x, S, B, V, dtype, 9, eos=3)
+
+
+def test_sorted_and_peaked_rows(F):
+    """Every logit larger than all before; one that takes all of the probability."""
+    rng = np.random.default_rng(6)
+    S, B, V = 2, 8, 30000
+    x = logits(rng, S, B, V, "f32")
+    x.view(S, B, -1)[0, :, :V] = torch.arange(V, device="cuda") / 1000
+    x.view(S, B, -1)[1, :, 77] = 5000.0
+    one_step(F, under_way(rng, S, B, 9), x, S, B, V, "f32", 9, eos=77)
+
+
+@pytest.mark.parametrize("V,early", [(61, False), (11, True), (11, False), (2, True)])
+def test_whole_searches(F, V, early):
+    """From the first token until the trace is full, searches that are over among those that go on: states, traces, hypotheses."""
+    rng = np.random.default_rng(7)
+    S, B, T, eos, penalty = 7, 4, 24, min(9, V - 1), 0.7
+    run = Searches(F, S, B, V, T, eos, penalty, early=early)
+    host, now = begin(S, B), device_state(begin(S, B))
+    out = {k: torch.empty_like(v) for k, v in now.items()}
+    tokens, parents = np.full((S, T, B), -9), np.full((S, T, B), -9)
+    for _ in range(T + 2):
+        x = logits(rng, S, B, V, "f32", scale=1.5)
+        run.step(now, out, x, "f32", x.shape[1])
+        t = host["steps"].copy()
+        host, want_tokens, want_parents, rows, _ = step64(host, values(x, S, B, V), T, eos, penalty, early)
+        check_step(out, run.tokens, run.parents, host, want_tokens, want_parents)
+        for s, row in enumerate(rows):
+            if row is not None:
+                tokens[s, t[s]], parents[s, t[s]] = row
+        # go on with the device's scores, so that roundings do not add up
+        host["scores"], host["end_scores"] = (out[k].double().cpu().numpy() for k in ("scores", "end_scores"))
+        now, out = out, now
+    assert np.array_equal(run.trace_tokens.cpu().numpy(), tokens)
+    assert np.array_equal(run.trace_parents.cpu().numpy(), parents)
+    for n in (1, 3, B):
+        got = run.trace(now, n)
+        want = trace64(host, tokens, parents, n, -1, eos, penalty)
+        for a, b in zip(got, want):
+            assert np.allclose(a.cpu().numpy(), b, rtol=2.0 ** -22, atol=0)
+        assert int(run.status.item()) == 0
+    assert (got[1][:, 0] > 0).all() and (V > 11 or host["done"].any())
+
+
+@pytest.mark.parametrize("S,B,T,n,eos,penalty", [(1, 1, 1, 1, -1, 1.0), (3, 4, 31, 2, 2, 0.0), (2, 16, 33, 16, 2, 1.0),
+                                                 (5, 3, 64, 3, -1, 2.0), (2, 5, 2047, 4, 2, 0.6), (2, 16, 2048, 5, 2, 0.6),
+                                                 (3, 2, 2049, 2, 2, 1.0), (2, 7, 6200, 7, 2, 1.0), (300, 2, 70, 1, 2, 1.0)])
+def test_trace(F, S, B, T, n, eos, penalty):
+    rng = np.random.default_rng(T + B)
+    st = under_way(rng, S, B, T + 1)
+    st["done"] = rng.integers(0, 2, S)
+    st["steps"][-1] = T
+    st["steps"][0] = min(T, 2)
+    st["end_steps"][0] = 0
+    if S > 2:
+        st["steps"][1] = 0  # nothing yet
+        st["end_scores"][1] = -INF
+        st["scores"][2, B - 1] = -INF
+    tokens = rng.integers(0, 50, (S, T, B))
+    parents = rng.integers(0, B, (S, T, B))
+    for s in range(S):  # rows that no step has written
+        used = max(st["steps"][s], st["end_steps"][s].max() + 1)
+        tokens[s, used:], parents[s, used:] = -5, 10 ** 9
+    run = Searches(F, S, B, 50, T, eos, penalty)
+    run.trace_tokens.copy_(torch.from_numpy(tokens))
+    run.trace_parents.copy_(torch.from_numpy(parents))
+    got = run.trace(device_state(st), n, pad=-3)
+    out, lens, scores = trace64(st, tokens, parents, n, -3, eos, penalty)
+    assert np.array_equal(got[0].cpu().numpy(), out) and np.array_equal(got[1].cpu().numpy(), lens)
+    x = got[2].double().cpu().numpy()  # live beams' scores are formed in 64 bits on both sides and rounded once
+    assert np.array_equal(x == -INF, scores == -INF)
+    fine = scores > -INF
+    assert (np.abs(x[fine] - scores[fine]) <= 2.0 ** -23 * np.abs(scores[fine])).all()
+    assert int(run.status.item()) == 0
+
+
+def test_traces_of_all_sizes_in_turn(F):
+    """A large call after a small one after a large one: what a launch needs is set up for all of them."""
+    for B, T in ((16, 2048), (2, 5), (16, 2048), (4, 700), (16, 4096), (1, 1), (16, 2048)):
+        st = begin(1, B)
+        st["scores"][:], st["steps"][:] = -np.arange(1, B + 1), T
+        run = Searches(F, 1, B, 50, T)
+        run.trace_tokens.copy_(torch.arange(T * B).view(1, T, B))
+        run.trace_parents.copy_(torch.arange(B).expand(1, T, B))
+        out, lens, _ = run.trace(device_state(st), B)
+        assert lens.tolist() == [[T] * B]
+        assert torch.equal(out[0].cpu(), torch.arange(T * B, dtype=torch.int32).view(T, B).T)
+
+
+def test_trace_of_indices_out_of_range(F):
+    """They count as 0 and are told; nothing outside of the buffers is touched."""
+    S, B, T = 1, 3, 40
+    st = begin(S, B)
+    st["scores"][:], st["steps"][:] = -1, T
+    run = Searches(F, S, B, 50, T)
+    run.trace_tokens.copy_(torch.arange(T * B).view(S, T, B))
+    run.trace_parents.zero_()
+    run.trace_parents[0, 20, 1] = 3
+    run.trace_parents[0, 30, 1] = -1
+    out, lens, _ = run.trace(device_state(st), 3)
+    assert int(run.status.item()) == F.FL_BEAM_BAD_TRACE and lens.tolist() == [[T] * 3]
+    assert out[0, :, :T - 1].tolist() == [[t * B for t in range(T - 1)]] * 3
+    for name, value in (("steps", T + 5), ("steps", -4), ("end_steps", T), ("end_steps", -1), ("end_beams", B), ("end_beams", -2)):
+        st = begin(S, B)
+        st["steps"][:], st["end_scores"][0, 0] = 3, -1
+        st[name][0] = value
+        run.status.zero_()
+        run.trace_parents.zero_()
+        run.trace(device_state(st), 2)
+        assert int(run.status.item()) == F.FL_BEAM_BAD_TRACE, name
+
+
+def test_one_workspace_for_many_shapes_and_a_graph(F):
+    """Calls one after another share a workspace; a captured step is replayed with other logits and state."""
+    rng = np.random.default_rng(8)
+    big = F.beam_search(9, 16, 60000, 8)
+    work = torch.zeros(F.fl_k_beam_workspace(big) // 4, dtype=torch.int32, device="cuda")
+    shapes = [(9, 16, 60000, "f32"), (3, 2, 100, "bf16"), (1, 5, 60000, "f16"), (9, 4, 5000, "f32")]
+    for S, B, V, dtype in shapes + shapes[::-1]:
+        run = Searches(F, S, B, V, 8, 1, workspace=work)
+        st = under_way(rng, S, B, 8)
+        x = logits(rng, S, B, V, dtype)
+        now = device_state(st)
+        out = {k: torch.empty_like(v) for k, v in now.items()}
+        run.step(now, out, x, dtype, x.shape[1])
+        want, tokens, parents, _, _ = step64(st, values(x, S, B, V), 8, 1, 1.0, False)
+        check_step(out, run.tokens, run.parents, want, tokens, parents)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run.step(now, out, x, dtype, x.shape[1], stream=side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run.step(now, out, x, dtype, x.shape[1], stream=torch.cuda.current_stream())
+    for _ in range(3):
+        st = under_way(rng, S, B, 8)
+        for k, v in device_state(st).items():
+            now[k].copy_(v)
+        x.copy_(logits(rng, S, B, V, dtype))
+        graph.replay()
+        want, tokens, parents, _, _ = step64(st, values(x, S, B, V), 8, 1, 1.0, False)
+        check_step(out, run.tokens, run.parents, want, tokens, parents)
+
+
+def test_same_bits_every_time(F):
+    rng = np.random.default_rng(9)
+    S, B, V = 8, 8, 50000
+    x = logits(rng, S, B, V, "bf16")
+    now = device_state(under_way(rng, S, B, 9))
+    first = None
+    for _ in range(20):
+        run = Searches(F, S, B, V, 9, 4)
+        out = {k: torch.empty_like(v) for k, v in now.items()}
+        run.step(now, out, x, "bf16", x.shape[1])
+        got = [out[k].view(torch.int32) for k in sorted(out)] + [run.tokens, run.parents]
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first))

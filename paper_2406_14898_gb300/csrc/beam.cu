@@ -2,12 +2,14 @@
 //
 // Step.  With c(b, v) = score_b + x_bv - lse_b a search wants the best `beams` of beams x vocab candidates.  Within a
 // beam c is ordered as x is, so each row needs only its largest logits and its log-sum-exp: one pass over the logits, which
-// is the bound (HBM; for few rows the latency of a load and two barriers).  A row is cut into slices, a CTA each, which
-// keeps its slice in registers: the maximum of each of 32 groups of threads is taken, and the B-th largest of those bounds
-// the slice's B-th largest logit from below, since B groups hold one that large each.  About B logits reach the
-// bound; they are ranked by counting.  The CTA of a search that comes last joins the slices' sums and lists.
+// is the bound (HBM; for few rows the latency of a load, some barriers and the join).  A row is cut into slices, a CTA each,
+// which goes through its slice in chunks, the next one's loads in flight.  Of the first chunk the B-th largest of 32 groups of
+// threads' maxima bounds the B-th largest logit from below; of what comes later only what exceeds the bound is looked
+// at, about B logits for each time that the slice doubles, and the bound is raised from those now and then.  The CTA of a
+// search that comes last joins the slices' sums and lists.
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/flglm_kernels.h"
@@ -16,7 +18,9 @@
 
 namespace {
 
-constexpr int THREADS = 256, WARPS = THREADS / 32, GROUPS = 32, MAX_SLICES = 32, MAX_HITS = THREADS;
+constexpr int THREADS = 256, WARPS = THREADS / 32, GROUPS = 32, MAX_SLICES = 32;
+constexpr int PIECES = 4, CHUNK_PIECES = PIECES * THREADS;  // 16-byte pieces of a thread and of a CTA in a chunk
+constexpr int MAX_HITS = 512;
 constexpr int MAX_SEARCHES = 16384, MAX_VOCAB = 1 << 19;
 constexpr float LOG2E = 1.4426950408889634f;
 static_assert(FL_BEAM_MAX <= GROUPS && GROUPS == 32 && FL_BEAM_MAX == 2 * WARPS);
@@ -45,14 +49,21 @@ struct Piece;  // 16 bytes of logits
 template <>
 struct Piece<float> {
   static constexpr int N = 4;
-  FL_DEV static void get(const uint4& u, float* f) {
+  static constexpr uint32_t NONE = 0xff800000u;  // -inf
+  FL_DEV static void get(const uint4& u, float (&f)[4]) {
     f[0] = __uint_as_float(u.x), f[1] = __uint_as_float(u.y), f[2] = __uint_as_float(u.z), f[3] = __uint_as_float(u.w);
   }
+  FL_DEV static uint32_t max2(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+  FL_DEV static float top(uint32_t a) { return __uint_as_float(a); }
+  FL_DEV static uint4 without(const uint4& u, int e) {
+    return make_uint4(e == 0 ? NONE : u.x, e == 1 ? NONE : u.y, e == 2 ? NONE : u.z, e == 3 ? NONE : u.w);
+  }
 };
-template <class T>
+template <class T, uint32_t INF2>
 struct Piece16 {
   static constexpr int N = 8;
-  FL_DEV static void get(const uint4& u, float* f) {
+  static constexpr uint32_t NONE = INF2;
+  FL_DEV static void get(const uint4& u, float (&f)[8]) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -60,18 +71,92 @@ struct Piece16 {
       f[2 * i] = y.x, f[2 * i + 1] = y.y;
     }
   }
+  FL_DEV static float top(uint32_t a) {
+    const float2 y = KvIo<T>::unpack(a);
+    return fmaxf(y.x, y.y);
+  }
+  FL_DEV static uint4 without(const uint4& u, int e) {
+    const uint32_t m = e & 1 ? 0xffff0000u : 0xffffu, x = INF2 & m;
+    return make_uint4(e >> 1 == 0 ? (u.x & ~m) | x : u.x, e >> 1 == 1 ? (u.y & ~m) | x : u.y, e >> 1 == 2 ? (u.z & ~m) | x : u.z,
+                      e >> 1 == 3 ? (u.w & ~m) | x : u.w);
+  }
 };
 template <>
-struct Piece<__nv_bfloat16> : Piece16<__nv_bfloat16> {};
+struct Piece<__nv_bfloat16> : Piece16<__nv_bfloat16, 0xff80ff80u> {
+  FL_DEV static uint32_t max2(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 y = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&y);
+  }
+};
 template <>
-struct Piece<__half> : Piece16<__half> {};
+struct Piece<__half> : Piece16<__half, 0xfc00fc00u> {
+  FL_DEV static uint32_t max2(uint32_t a, uint32_t b) {
+    const __half2 y = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&y);
+  }
+};
+
+// Whole numbers in the order of the floats (no NaN); 0 is below all of them.
+FL_DEV uint32_t order32(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+FL_DEV uint64_t order64(double x) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
+  return u >> 63 ? ~u : u | (1ull << 63);
+}
+
+// Two floats as one operand of the packed fp32 instructions.
+FL_DEV uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+FL_DEV float2 unpack2(uint64_t x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+FL_DEV uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+FL_DEV uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// sum of exp(x - ref) over what a thread has seen.  x - ref is taken before the product with log2(e): rounding the product of x itself
+// would be off by the same for every x near ref.
+struct Sum {
+  float ref = -INFINITY;
+  uint64_t minus = 0, sum = 0;  // (-ref, -ref), or zeros where there is no ref yet; sums of every other element
+  FL_DEV void add(float x, float y) {
+    const float2 u = unpack2(mul2(add2(pack2(x, y), minus), pack2(LOG2E, LOG2E)));
+    sum = add2(sum, pack2(exp2_hw(u.x), exp2_hw(u.y)));
+  }
+  FL_DEV float total() const { return unpack2(sum).x + unpack2(sum).y; }
+  // room for x: sums of up to 2^19 exponentials of 16 and less are far from overflow
+  FL_DEV void see(float x) {
+    if (x > ref + 16.f) {
+      const float f = ref == -INFINITY ? 1.f : exp2_hw((ref - x) * LOG2E);  // (1: nothing so far, or a NaN that stays)
+      sum = mul2(sum, pack2(f, f));
+      ref = x;
+      minus = pack2(-x, -x);
+    }
+  }
+};
 
 struct Join {  // shared memory of the CTA that joins a search
   Cand lists[WARPS][MAX_SLICES * FL_BEAM_MAX];
   Cand best[FL_BEAM_MAX][FL_BEAM_MAX];
-  double c[FL_BEAM_MAX][FL_BEAM_MAX];  // -inf: no candidate
-  double ends[FL_BEAM_MAX], live[FL_BEAM_MAX];
-  float end_x[FL_BEAM_MAX], pool[2 * FL_BEAM_MAX];
+  uint64_t c[FL_BEAM_MAX][FL_BEAM_MAX];  // candidates of each beam, in order64; 0: none
+  uint64_t few[FL_BEAM_MAX * FL_BEAM_MAX];
+  int few_at[FL_BEAM_MAX * FL_BEAM_MAX], few_n;
+  double live[FL_BEAM_MAX], ends[FL_BEAM_MAX], base[FL_BEAM_MAX], length;
+  float m[FL_BEAM_MAX], end_x[FL_BEAM_MAX], pool[2 * FL_BEAM_MAX];
   int pool_step[2 * FL_BEAM_MAX], pool_beam[2 * FL_BEAM_MAX], end_rank[FL_BEAM_MAX];
   int token[FL_BEAM_MAX], parent[FL_BEAM_MAX];
 };
@@ -97,130 +182,147 @@ FL_DEV void rest(const StepArgs& a, int s) {
 
 template <class T>
 FL_DEV void join(const StepArgs& a, int s, int t, Join& j) {
-  const int B = a.p.beams, P = a.slices, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int B = a.p.beams, P = a.slices, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == THREADS - 1) {
+    j.length = pow((double)(t + 1), a.p.length_penalty);
+    j.few_n = 0;
+  }
   // each row's sum and best tokens, a warp a row
   for (int b = warp; b < B; b += WARPS) {
     const int row = s * B + b;
     const float score = a.from.scores[row];
-    double m = -INFINITY, sum = 0;
     const bool reads = score > -INFINITY && score < INFINITY;
-    if (reads) {
-      const float2 mine = lane < P ? __ldcg(a.sums + (int64_t)row * P + lane) : make_float2(-INFINITY, 0.f);
-      float top = mine.x;
-#pragma unroll
-      for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-      sum = mine.x == -INFINITY ? (double)mine.y : mine.y * exp((double)mine.x - top);
-      if (mine.x == INFINITY) sum = NAN;
-#pragma unroll
-      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      m = top;
-    }
-    // x - lse as (x - m) - log(sum): exact for the smallest logits that a type has, too
-    const double part = log(sum);
-    const bool bad = score != score || score == INFINITY || (reads && !(m + part < INFINITY));
-    const bool live = reads && !bad && m > -INFINITY;
-    if (bad && lane == 0) atomicOr(a.status, FL_BEAM_BAD_LOGITS);
+    float m = -INFINITY, sum = 0.f, e = -INFINITY;
     Cand* mine = j.lists[warp];
-    __syncwarp();
-    if (live)
+    if (reads) {
+      const float2 part = lane < P ? __ldcg(a.sums + (int64_t)row * P + lane) : make_float2(-INFINITY, 0.f);
       for (int i = lane; i < P * B; i += 32) {
         const float2 y = __ldcg(reinterpret_cast<const float2*>(a.lists + (int64_t)row * P * B) + i);
         mine[i] = Cand{y.x, __float_as_int(y.y)};
       }
-    __syncwarp();
-    int at = lane * B;
-    for (int k = 0; k < B; ++k) {
-      Cand head{-INFINITY, 0x7fffffff};
-      if (live && lane < P && at < (lane + 1) * B) head = mine[at];
-      Cand top = head;
-#pragma unroll
-      for (int d = 16; d; d >>= 1) {
-        const Cand o{__shfl_xor_sync(0xffffffffu, top.x, d), __shfl_xor_sync(0xffffffffu, top.v, d)};
-        if (better(o, top)) top = o;
-      }
-      if (head.x == top.x && head.v == top.v) ++at;
-      if (lane == 0) {
-        j.best[b][k] = top;
-        j.c[b][k] = top.x > -INFINITY ? (double)score + (((double)top.x - m) - part) : -INFINITY;
-      }
-    }
-    if (lane == 0) {
-      float e = -INFINITY;
-      if (live && a.p.eos >= 0) {
-        uint4 u = *reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld + a.p.eos / Piece<T>::N * Piece<T>::N);
+      if (a.p.eos >= 0) {
         float f[Piece<T>::N];
-        Piece<T>::get(u, f);
+        Piece<T>::get(*reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld + a.p.eos / Piece<T>::N * Piece<T>::N), f);
 #pragma unroll
         for (int i = 0; i < Piece<T>::N; ++i) e = i == a.p.eos % Piece<T>::N ? f[i] : e;
       }
-      j.end_x[b] = e;
-      j.ends[b] = e > -INFINITY ? (double)score + (((double)e - m) - part) : -INFINITY;
+      m = part.x;
+#pragma unroll
+      for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+      sum = part.x == -INFINITY ? part.y : part.y * exp2_hw((part.x - m) * LOG2E);
+      if (part.x == INFINITY) sum = NAN;
+#pragma unroll
+      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    }
+    const bool bad = score != score || score == INFINITY || sum != sum, live = reads && !bad && m > -INFINITY;
+    if (bad && lane == 0) atomicOr(a.status, FL_BEAM_BAD_LOGITS);
+    __syncwarp();
+    int at = lane * B, k = 0;
+    if (live) {
+      const int stop = lane < P ? at + B : at;
+      for (; k < B; ++k) {
+        const Cand head = at < stop ? mine[at] : Cand{-INFINITY, 0};
+        const uint32_t key = head.x > -INFINITY ? order32(head.x) : 0u, top = __reduce_max_sync(0xffffffffu, key);
+        if (top == 0) break;
+        const int v = __reduce_min_sync(0xffffffffu, key == top ? head.v : 0x7fffffff);
+        if (key == top && head.v == v) {
+          j.best[b][k] = head;
+          ++at;
+        }
+      }
+    }
+    __syncwarp();
+    if (lane >= k && lane < B) j.best[b][lane] = Cand{-INFINITY, 0};
+    if (lane == 0) {
+      // c = score + ((x - m) - log(sum)): exact for the smallest logits that a type has, too
+      j.base[b] = live ? log((double)sum) : 0;
+      j.m[b] = m;
+      j.end_x[b] = live ? e : -INFINITY;
       j.token[b] = max(a.p.eos, 0);
       j.parent[b] = -1;
       j.live[b] = -INFINITY;
     }
   }
   __syncthreads();
-  // ranks by counting who comes before: by c, then the lower beam, then the order within the beam
-  for (int i = threadIdx.x; i < B * B; i += THREADS) {
-    const int b = i / B, k = i % B;
-    const double c = j.c[b][k];
-    int rank = k;
-    for (int o = 0; o < B; ++o)
-      if (o != b)
-        for (int n = 0; n < B; ++n) rank += o < b ? j.c[o][n] >= c : j.c[o][n] > c;
-    if (c > -INFINITY && rank < B) {
-      j.token[rank] = j.best[b][k].v;
-      j.parent[rank] = b;
-      j.live[rank] = c;
+  for (int i = tid; i < B * B + B; i += THREADS) {
+    const int b = i < B * B ? i / B : i - B * B, k = i % B;
+    const float x = i < B * B ? j.best[b][k].x : j.end_x[b];
+    const double c = x > -INFINITY ? (double)a.from.scores[s * B + b] + (((double)x - j.m[b]) - j.base[b]) : -INFINITY;
+    if (i < B * B) j.c[b][k] = x > -INFINITY ? order64(c) : 0;
+    else j.ends[b] = c;
+  }
+  __syncthreads();
+  // A row's last candidate bounds the search's last: only what reaches the best of those bounds is ranked, by counting who comes
+  // before: by c, then the lower beam, then the order within the beam.
+  uint64_t bound = 1;
+  for (int b = 0; b < B; ++b) bound = max(bound, j.c[b][B - 1]);
+  for (int i = tid; i < B * B; i += THREADS) {
+    const uint64_t c = j.c[i / B][i % B];
+    if (c >= bound) {
+      const int n = atomicAdd(&j.few_n, 1);
+      j.few[n] = c;
+      j.few_at[n] = i;
     }
   }
-  for (int b = warp; b < B; b += WARPS) {
-    const double c = j.ends[b];
-    const Cand e{j.end_x[b], a.p.eos};
+  __syncthreads();
+  const int n = j.few_n;
+  for (int i = tid; i < n; i += THREADS) {
+    const uint64_t c = j.few[i];
+    const int at = j.few_at[i];
     int rank = 0;
-    if (c > -INFINITY) {
-      for (int i = lane; i < B * B; i += 32) {
-        const int o = i / B;
-        const double x = j.c[o][i % B];
-        rank += o == b ? better(j.best[o][i % B], e) : o < b ? x >= c : x > c;
-      }
-      if (lane < B && lane != b) rank += lane < b ? j.ends[lane] >= c && j.ends[lane] > -INFINITY : j.ends[lane] > c;
+    for (int o = 0; o < n; ++o) rank += j.few[o] > c || (j.few[o] == c && j.few_at[o] < at);
+    if (rank < B) {
+      const int b = at / B, k = at % B;
+      const Cand y = j.best[b][k];
+      j.token[rank] = y.v;
+      j.parent[rank] = b;
+      j.live[rank] = (double)a.from.scores[s * B + b] + (((double)y.x - j.m[b]) - j.base[b]);
     }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, d);
-    if (lane == 0) j.end_rank[b] = c > -INFINITY && rank < B ? rank : -1;
+  }
+  const int b = tid - (THREADS - 32);  // the hypotheses that end
+  if (b >= 0 && b < B) {
+    const double x = j.ends[b];
+    const uint64_t c = x > -INFINITY ? order64(x) : 0;
+    int rank = -1;
+    if (c >= bound) {
+      const Cand e{j.end_x[b], a.p.eos};
+      rank = 0;
+      for (int o = 0; o < n; ++o) {
+        const int ob = j.few_at[o] / B;
+        rank += ob == b ? better(j.best[ob][j.few_at[o] % B], e) : j.few[o] > c || (j.few[o] == c && ob < b);
+      }
+      for (int o = 0; o < B; ++o) {
+        const uint64_t y = j.ends[o] > -INFINITY ? order64(j.ends[o]) : 0;
+        rank += y > c || (y == c && o < b);
+      }
+      if (rank >= B) rank = -1;
+    }
+    j.end_rank[b] = rank;
   }
   __syncthreads();
   // the pool: what had ended, then what ends now in the order of its rank
   if (warp == 0) {
-    const double length = pow((double)(t + 1), a.p.length_penalty);
-    const int b = lane < FL_BEAM_MAX ? lane : lane - FL_BEAM_MAX;
+    const int pb = lane < FL_BEAM_MAX ? lane : lane - FL_BEAM_MAX;
     float x = -INFINITY;
     int step = 0, beam = 0, order = lane;
-    if (b < B) {
+    if (pb < B) {
       if (lane < FL_BEAM_MAX) {
-        x = a.from.end_scores[s * B + b];
-        step = a.from.end_steps[s * B + b];
-        beam = a.from.end_beams[s * B + b];
-      } else if (j.end_rank[b] >= 0) {
-        x = (float)(j.ends[b] / length);
+        x = a.from.end_scores[s * B + pb];
+        step = a.from.end_steps[s * B + pb];
+        beam = a.from.end_beams[s * B + pb];
+      } else if (j.end_rank[pb] >= 0) {
+        x = (float)(j.ends[pb] / j.length);
         step = t;
-        beam = b;
-        order = FL_BEAM_MAX + j.end_rank[b];
+        beam = pb;
+        order = FL_BEAM_MAX + j.end_rank[pb];
       }
     }
-    if (!(x == x)) x = -INFINITY;
+    if (!(x > -INFINITY)) x = -INFINITY, step = beam = 0;
+    const uint64_t key = (uint64_t)order32(x) << 32 | (uint32_t)((63 - order) << 8 | (31 - lane));
     int rank = 0;
-    for (int o = 0; o < 32; ++o) {
-      const float y = __shfl_sync(0xffffffffu, x, o);
-      const int yo = __shfl_sync(0xffffffffu, order, o);
-      rank += o != lane && (y > x || (y == x && (yo < order || (yo == order && o < lane))));
-    }
-    j.pool[lane] = -INFINITY;
-    j.pool_step[lane] = j.pool_beam[lane] = 0;
-    __syncwarp();
-    if (x > -INFINITY && rank < FL_BEAM_MAX) {
+#pragma unroll 4
+    for (int o = 0; o < 32; ++o) rank += __shfl_sync(0xffffffffu, key, o) > key;
+    if (pb < B && rank < B) {  // (the places behind the pool's end are empty ones')
       j.pool[rank] = x;
       j.pool_step[rank] = step;
       j.pool_beam[rank] = beam;
@@ -239,144 +341,180 @@ FL_DEV void join(const StepArgs& a, int s, int t, Join& j) {
     }
     if (lane == 0) {
       const float worst = j.pool[B - 1];
-      const bool over = worst > -INFINITY && (a.p.early || worst >= (float)(j.live[0] / length));
+      const bool over = worst > -INFINITY && (a.p.early || worst >= (float)(j.live[0] / j.length));
       a.to.steps[s] = t + 1;
       a.to.done[s] = over || !(j.live[0] > -INFINITY);
     }
   }
 }
 
-template <class T, int PIECES>
-__global__ void __launch_bounds__(THREADS) beam_step_kernel(StepArgs a) {
+template <class T>
+__global__ void __launch_bounds__(THREADS, 3) beam_step_kernel(StepArgs a) {
   pdl_wait();
   pdl_trigger();
-  constexpr int N = Piece<T>::N;
-  __shared__ float sh_group[GROUPS];
-  __shared__ float sh_sum[WARPS], sh_eos;
-  __shared__ Cand sh_hits[MAX_HITS];
-  __shared__ int sh_count, sh_last;
+  using Io = Piece<T>;
+  constexpr int N = Io::N;
+  __shared__ float sh_group[GROUPS], sh_ref[WARPS], sh_sum[WARPS];
+  __shared__ Cand sh_hits[2][MAX_HITS];
+  __shared__ int sh_count[2], sh_last;
   extern __shared__ __align__(16) char sh_join[];
   const int B = a.p.beams, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int slice = blockIdx.x % (unsigned)a.slices, row = blockIdx.x / (unsigned)a.slices, s = row / B;
+  const int all = (a.p.vocab + N - 1) / N, begin = slice * a.per, end = min(all, begin + a.per);
+  const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld);
+  uint4 cur[PIECES];
+  auto load = [&](int first, uint4 (&u)[PIECES]) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int k = first + i * THREADS + tid;
+      u[i] = k < end ? __ldcs(x + k) : make_uint4(Io::NONE, Io::NONE, Io::NONE, Io::NONE);
+    }
+  };
+  load(begin, cur);  // before it is known whether the beam is live: one latency less
   const int t = a.from.steps[s];  // (no read-only loads of the state: `to` may be the same memory)
   const bool active = a.from.done[s] == 0 && t >= 0 && t < a.p.max_steps;
   const float score = a.from.scores[row];
   if (active && score > -INFINITY && score < INFINITY) {
-    const int all = (a.p.vocab + N - 1) / N, begin = slice * a.per, end = min(all, begin + a.per);
-    const T* x = (const T*)a.x + (int64_t)row * a.ld;
-    uint4 raw[PIECES];
-    float f[PIECES * N];
+    Sum z;
+    float bound = -INFINITY;
+    int side = 0, since = begin, kept = 0;  // the list in use; the first piece that came after it was ranked, what it had then
+    if (tid == 0) sh_count[0] = 0;
+    for (int first = begin, chunk = 0; first < end; first += CHUNK_PIECES, ++chunk) {
+      uint4 next[PIECES];
+      const bool last = first + CHUNK_PIECES >= end;
+      if (!last) load(first + CHUNK_PIECES, next);
+      // tokens behind the vocabulary; the eos, which is summed but no candidate to go on with
+      const int lo = first * N, hi = (first + CHUNK_PIECES) * N;
+      if (hi > a.p.vocab || (a.p.eos >= lo && a.p.eos < hi)) {
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int k = begin + i * THREADS + tid;
-      if (k < end) raw[i] = __ldcs(reinterpret_cast<const uint4*>(x) + k);
-    }
-    if (tid == 0) {
-      sh_count = 0;
-      sh_eos = -INFINITY;
-    }
+        for (int i = 0; i < PIECES; ++i) {
+          const int v = (first + i * THREADS + tid) * N;
+          if (a.p.eos >= v && a.p.eos < v + N) {
+            float f[N], e = -INFINITY;
+            Io::get(cur[i], f);
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int k = begin + i * THREADS + tid;
-      Piece<T>::get(raw[i], f + i * N);
-      if (k >= end)
-#pragma unroll
-        for (int e = 0; e < N; ++e) f[i * N + e] = -INFINITY;
-    }
-    // tokens behind the vocabulary, and the eos, which is no candidate to go on with
-    if (end == all && all * N != a.p.vocab) {
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-          if ((begin + i * THREADS + tid) * N + e >= a.p.vocab) f[i * N + e] = -INFINITY;
-    }
-    __syncthreads();
-    if (a.p.eos >= begin * N && a.p.eos < end * N) {
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-          if ((begin + i * THREADS + tid) * N + e == a.p.eos) {
-            sh_eos = f[i * N + e];
-            f[i * N + e] = -INFINITY;
+            for (int k = 0; k < N; ++k) e = k == a.p.eos - v ? f[k] : e;
+            z.see(e);
+            z.add(e, -INFINITY);
+            cur[i] = Io::without(cur[i], a.p.eos - v);
           }
-    }
-    float top = f[0];
-#pragma unroll
-    for (int i = 1; i < PIECES * N; ++i) top = fmaxf(top, f[i]);
-    float g = top;
-#pragma unroll
-    for (int d = 1; d < THREADS / GROUPS; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
-    if (tid % (THREADS / GROUPS) == 0) sh_group[tid / (THREADS / GROUPS)] = g;
-    __syncthreads();
-    // the B-th largest of the groups' maxima, and the largest
-    g = sh_group[lane];
-    int rank = 0;
-#pragma unroll
-    for (int o = 0; o < GROUPS; ++o) {
-      const float y = sh_group[o];
-      rank += y > g || (y == g && o < lane);
-    }
-    const float bound = __shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == B - 1)) - 1);
-    const float m = fmaxf(__shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == 0)) - 1), sh_eos);
-    // x - m first: rounding the product of x itself would be off by the same for every x near m
-    float sum = 0.f;
-    const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int i = 0; i < PIECES * N; ++i) sum += exp2_hw((f[i] - base) * LOG2E);
-    if (tid == 0) sum += exp2_hw((sh_eos - base) * LOG2E);
-    if (top >= bound && top > -INFINITY) {
-#pragma unroll
-      for (int i = 0; i < PIECES * N; ++i)
-        if (f[i] >= bound && f[i] > -INFINITY) {
-          const int n = atomicAdd(&sh_count, 1);
-          if (n < MAX_HITS) sh_hits[n] = Cand{f[i], (begin + i / N * THREADS + tid) * N + i % N};
+          if (v < a.p.vocab && v + N > a.p.vocab)
+            for (int k = a.p.vocab - v; k < N; ++k) cur[i] = Io::without(cur[i], k);
         }
+      }
+      uint32_t most = Io::NONE;
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i)
+        most = Io::max2(most, Io::max2(Io::max2(cur[i].x, cur[i].y), Io::max2(cur[i].z, cur[i].w)));
+      const float top = Io::top(most);
+      bool look = top > bound;
+      if (chunk == 0) {
+        float g = top;
+#pragma unroll
+        for (int d = 1; d < THREADS / GROUPS; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
+        if (tid % (THREADS / GROUPS) == 0) sh_group[tid / (THREADS / GROUPS)] = g;
+        __syncthreads();
+        // the B-th largest of the groups' maxima, and the largest
+        g = sh_group[lane];
+        int rank = 0;
+#pragma unroll
+        for (int o = 0; o < GROUPS; ++o) {
+          const float y = sh_group[o];
+          rank += y > g || (y == g && o < lane);
+        }
+        bound = __shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == B - 1)) - 1);
+        z.see(__shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == 0)) - 1));
+        look = top >= bound && top > -INFINITY;
+      } else if (look) {
+        z.see(top);
+      }
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        float f[N];
+        Io::get(cur[i], f);
+#pragma unroll
+        for (int k = 0; k < N; k += 2) z.add(f[k], f[k + 1]);
+      }
+      if (look) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          float f[N];
+          Io::get(cur[i], f);
+#pragma unroll
+          for (int k = 0; k < N; ++k)
+            if (f[k] > bound || (chunk == 0 && f[k] == bound && f[k] > -INFINITY)) {
+              const int n = atomicAdd(&sh_count[side], 1);
+              if (n < MAX_HITS) sh_hits[side][n] = Cand{f[k], (first + i * THREADS + tid) * N + k};
+            }
+        }
+      }
+      if (last || chunk == 3 || chunk == 15) {
+        // the best so far, ranked by counting, raise the bound
+        __syncthreads();
+        const int n = sh_count[side];
+        Cand* to = sh_hits[side ^ 1];
+        if (tid == 0) sh_count[side ^ 1] = min(n, B);
+        if (n <= MAX_HITS) {
+          for (int i = tid; i < n; i += THREADS) {
+            const Cand mine = sh_hits[side][i];
+            int r = 0;
+            for (int o = 0; o < n; ++o) r += better(sh_hits[side][o], mine);
+            if (r < B) to[r] = mine;
+          }
+        } else {
+          // more than the list holds (logits that ascend, many equal ones): the best one behind the last found, B times
+          Cand found{INFINITY, -1};
+          for (int r = 0; r < B; ++r) {
+            Cand mine{-INFINITY, 0x7fffffff};
+            if (tid < kept && better(found, sh_hits[side][tid])) mine = sh_hits[side][tid];
+            for (int k = since + tid; k < min(end, first + CHUNK_PIECES); k += THREADS) {
+              float f[N];
+              Io::get(x[k], f);
+              for (int e = 0; e < N; ++e) {
+                const Cand y{f[e], k * N + e};
+                if (y.v < a.p.vocab && y.v != a.p.eos && better(found, y) && better(y, mine)) mine = y;
+              }
+            }
+#pragma unroll
+            for (int d = 16; d; d >>= 1) {
+              const Cand o{__shfl_xor_sync(0xffffffffu, mine.x, d), __shfl_xor_sync(0xffffffffu, mine.v, d)};
+              if (better(o, mine)) mine = o;
+            }
+            if (lane == 0) to[MAX_HITS - WARPS + warp] = mine;
+            __syncthreads();
+            for (int i = 0; i < WARPS; ++i)
+              if (better(to[MAX_HITS - WARPS + i], mine)) mine = to[MAX_HITS - WARPS + i];
+            __syncthreads();
+            if (tid == 0) to[r] = mine;
+            found = mine;
+          }
+        }
+        __syncthreads();
+        side ^= 1;
+        since = first + CHUNK_PIECES;
+        kept = min(n, B);
+        if (n >= B) bound = to[B - 1].x;
+        if (n > 0) z.see(to[0].x);
+      }
+      if (!last)
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) cur[i] = next[i];
     }
+    // the slice's sum and list
+    float ref = z.ref;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, d));
+    float sum = z.ref == -INFINITY ? z.total() : z.total() * exp2_hw((z.ref - ref) * LOG2E);
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (lane == 0) sh_sum[warp] = sum;
+    if (lane == 0) sh_ref[warp] = ref, sh_sum[warp] = sum;
+    if (tid < B) a.lists[(int64_t)blockIdx.x * B + tid] = tid < sh_count[side] ? sh_hits[side][tid] : Cand{-INFINITY, 0};
     __syncthreads();
-    Cand* list = a.lists + (int64_t)blockIdx.x * B;
-    const int hits = sh_count;
     if (tid == 0) {
-      float z = 0.f;
-      for (int i = 0; i < WARPS; ++i) z += sh_sum[i];
-      a.sums[blockIdx.x] = make_float2(m, z);
-    }
-    if (hits <= MAX_HITS) {
-      if (tid < hits) {
-        const Cand mine = sh_hits[tid];
-        int r = 0;
-        for (int o = 0; o < hits; ++o) r += better(sh_hits[o], mine);
-        if (r < B) list[r] = mine;
-      }
-      if (tid >= hits && tid < B) list[tid] = Cand{-INFINITY, 0};
-    } else {
-      // many equal logits: the best one behind the last found, B times
-      __syncthreads();
-      Cand last{INFINITY, -1};
-      for (int r = 0; r < B; ++r) {
-        Cand mine{-INFINITY, 0x7fffffff};
-#pragma unroll
-        for (int i = 0; i < PIECES * N; ++i) {
-          const Cand y{f[i], (begin + i / N * THREADS + tid) * N + i % N};
-          if (better(last, y) && better(y, mine)) mine = y;
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-          const Cand o{__shfl_xor_sync(0xffffffffu, mine.x, d), __shfl_xor_sync(0xffffffffu, mine.v, d)};
-          if (better(o, mine)) mine = o;
-        }
-        if (lane == 0) sh_hits[warp] = mine;
-        __syncthreads();
-        for (int i = 0; i < WARPS; ++i)
-          if (better(sh_hits[i], mine)) mine = sh_hits[i];
-        __syncthreads();
-        if (tid == 0) list[r] = mine;
-        last = mine;
-      }
+      float m = sh_ref[0], q = 0.f;
+      for (int i = 1; i < WARPS; ++i) m = fmaxf(m, sh_ref[i]);
+      for (int i = 0; i < WARPS; ++i) q += sh_ref[i] == -INFINITY ? sh_sum[i] : sh_sum[i] * exp2_hw((sh_ref[i] - m) * LOG2E);
+      a.sums[blockIdx.x] = make_float2(m, q);
     }
   }
   __syncthreads();
@@ -415,33 +553,20 @@ bool state_ok(const fl_beam_state* s) {
   return true;
 }
 
-template <class T, int PIECES>
-int launch_step(const StepArgs& a, cudaStream_t st) {
-  auto kern = beam_step_kernel<T, PIECES>;
-  FL_CUDA_TRY(fl_func_smem((const void*)kern, sizeof(Join)));
-  FL_CUDA_TRY(fl_launch(kern, dim3((unsigned)(a.p.n_seqs * a.p.beams * a.slices)), dim3(THREADS), sizeof(Join), st, a));
-  return FL_OK;
-}
-
-// Slices of a row: as long as a CTA's registers hold (16 pieces of 4, 8 of 8 logits a thread), shorter where the GPU
-// would not be full with those.
+// Slices of a row: enough for some CTAs per SM and wave, of a thread's piece at least.
 template <class T>
-int launch_typed(StepArgs& a, cudaStream_t st) {
-  constexpr int N = Piece<T>::N, MOST = 64 / N;
+int launch_step(StepArgs& a, cudaStream_t st) {
+  constexpr int N = Piece<T>::N;
   const int pieces = (a.p.vocab + N - 1) / N;
   const int64_t rows = (int64_t)a.p.n_seqs * a.p.beams;
-  int slices = (pieces + THREADS * MOST - 1) / (THREADS * MOST);
-  while (slices < MAX_SLICES && rows * slices < 2 * fl_sm_count() && (slices + 1) * THREADS <= pieces) ++slices;
-  a.slices = slices;
+  const int64_t want = (16 * fl_sm_count() + rows - 1) / rows, most = (pieces + THREADS - 1) / THREADS;
+  const int slices = (int)std::min<int64_t>(std::min<int64_t>(want, most), MAX_SLICES);
   a.per = (pieces + slices - 1) / slices;
   a.slices = (pieces + a.per - 1) / a.per;
-  const int each = (a.per + THREADS - 1) / THREADS;
-  if (each <= 1) return launch_step<T, 1>(a, st);
-  if (each <= 2) return launch_step<T, 2>(a, st);
-  if (each <= 4) return launch_step<T, 4>(a, st);
-  if constexpr (MOST > 8)
-    if (each > 8) return launch_step<T, 16>(a, st);
-  return launch_step<T, 8>(a, st);
+  auto kern = beam_step_kernel<T>;
+  FL_CUDA_TRY(fl_func_smem((const void*)kern, sizeof(Join)));
+  FL_CUDA_TRY(fl_launch(kern, dim3((unsigned)(rows * a.slices)), dim3(THREADS), sizeof(Join), st, a));
+  return FL_OK;
 }
 
 // ------------------------------------------------------------------------------- back-pointers
@@ -609,8 +734,8 @@ extern "C" int fl_k_beam_step(const fl_beam_search* search, const fl_beam_state*
   a.sums = (float2*)((char*)workspace + MAX_SEARCHES * sizeof(unsigned));
   a.lists = (Cand*)(a.sums + (int64_t)search->n_seqs * search->beams * MAX_SLICES);
   const cudaStream_t st = (cudaStream_t)stream;
-  return dtype == FL_DT_F32 ? launch_typed<float>(a, st)
-                            : dtype == FL_DT_F16 ? launch_typed<__half>(a, st) : launch_typed<__nv_bfloat16>(a, st);
+  return dtype == FL_DT_F32 ? launch_step<float>(a, st)
+                            : dtype == FL_DT_F16 ? launch_step<__half>(a, st) : launch_step<__nv_bfloat16>(a, st);
 }
 
 extern "C" int fl_k_beam_trace(const fl_beam_search* search, const fl_beam_state* state, const int32_t* trace_tokens,

@@ -5,8 +5,9 @@
 // is the bound (HBM; for few rows the latency of a load, some barriers and the join).  A row is cut into slices, a CTA each,
 // which goes through its slice in chunks, the next one's loads in flight.  Of the first chunk the B-th largest of 32 groups of
 // threads' maxima bounds the B-th largest logit from below; of what comes later only what exceeds the bound is looked
-// at, about B logits for each time that the slice doubles, and the bound is raised from those now and then.  The CTA of a
-// search that comes last joins the slices' sums and lists.
+// at, about B logits for each time that the slice doubles, and the bound is raised now and then.  A second kernel, a
+// CTA a search, joins the slices' sums and lists.  (With the join in the CTA that comes last, CTAs that joined came late
+// for their next slices and so joined again: 64 x 16 rows of 130528 bf16 157 us.)
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -18,9 +19,11 @@
 
 namespace {
 
+constexpr int JOIN_THREADS = 32 * FL_BEAM_MAX;
 constexpr int THREADS = 256, WARPS = THREADS / 32, GROUPS = 32, MAX_SLICES = 32;
-constexpr int PIECES = 4, CHUNK_PIECES = PIECES * THREADS;  // 16-byte pieces of a thread and of a CTA in a chunk
-constexpr int MAX_HITS = 512;
+constexpr int PIECES = 8, CHUNK_PIECES = PIECES * THREADS;  // 16-byte pieces of a thread and of a CTA in a chunk
+constexpr int STAGES = 2, CTAS = 3;                          // chunks on their way or in use, CTAs of an SM
+constexpr int MAX_HITS = 512, MAX_UNITS = 1024;              // of a CTA
 constexpr int MAX_SEARCHES = 16384, MAX_VOCAB = 1 << 19;
 constexpr float LOG2E = 1.4426950408889634f;
 static_assert(FL_BEAM_MAX <= GROUPS && GROUPS == 32 && FL_BEAM_MAX == 2 * WARPS);
@@ -36,9 +39,9 @@ struct StepArgs {
   fl_beam_state from, to;
   const void* x;
   int64_t ld;
-  int slices, per;  // slices of a row, 16-byte pieces of a slice
+  int slices, per, units;  // slices of a row, 16-byte pieces of a slice, slices in all
+  float penalty_hi, penalty_lo;
   int32_t *trace_tokens, *trace_parents, *tokens, *parents;
-  unsigned* counters;
   float2* sums;  // [row][slice] (largest logit, sum of exp(x - it))
   Cand* lists;   // [row][slice][beam], best first; x = -inf: none
   int* status;
@@ -53,11 +56,15 @@ struct Piece<float> {
   FL_DEV static void get(const uint4& u, float (&f)[4]) {
     f[0] = __uint_as_float(u.x), f[1] = __uint_as_float(u.y), f[2] = __uint_as_float(u.z), f[3] = __uint_as_float(u.w);
   }
+  FL_DEV static uint32_t max4(const uint4& u) {
+    float f[4], m;
+    get(u, f);
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(f[0]), "f"(f[1]), "f"(f[2]));
+    return __float_as_uint(fmaxf(m, f[3]));
+  }
   FL_DEV static uint32_t max2(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
   FL_DEV static float top(uint32_t a) { return __uint_as_float(a); }
-  FL_DEV static uint4 without(const uint4& u, int e) {
-    return make_uint4(e == 0 ? NONE : u.x, e == 1 ? NONE : u.y, e == 2 ? NONE : u.z, e == 3 ? NONE : u.w);
-  }
+  FL_DEV static float one(float x) { return x; }
 };
 template <class T, uint32_t INF2>
 struct Piece16 {
@@ -75,11 +82,7 @@ struct Piece16 {
     const float2 y = KvIo<T>::unpack(a);
     return fmaxf(y.x, y.y);
   }
-  FL_DEV static uint4 without(const uint4& u, int e) {
-    const uint32_t m = e & 1 ? 0xffff0000u : 0xffffu, x = INF2 & m;
-    return make_uint4(e >> 1 == 0 ? (u.x & ~m) | x : u.x, e >> 1 == 1 ? (u.y & ~m) | x : u.y, e >> 1 == 2 ? (u.z & ~m) | x : u.z,
-                      e >> 1 == 3 ? (u.w & ~m) | x : u.w);
-  }
+  FL_DEV static float one(T x) { return (float)x; }
 };
 template <>
 struct Piece<__nv_bfloat16> : Piece16<__nv_bfloat16, 0xff80ff80u> {
@@ -87,6 +90,7 @@ struct Piece<__nv_bfloat16> : Piece16<__nv_bfloat16, 0xff80ff80u> {
     const __nv_bfloat162 y = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&y);
   }
+  FL_DEV static uint32_t max4(const uint4& u) { return max2(max2(u.x, u.y), max2(u.z, u.w)); }
 };
 template <>
 struct Piece<__half> : Piece16<__half, 0xfc00fc00u> {
@@ -94,6 +98,7 @@ struct Piece<__half> : Piece16<__half, 0xfc00fc00u> {
     const __half2 y = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&y);
   }
+  FL_DEV static uint32_t max4(const uint4& u) { return max2(max2(u.x, u.y), max2(u.z, u.w)); }
 };
 
 // Whole numbers in the order of the floats (no NaN); 0 is below all of them.
@@ -101,9 +106,68 @@ FL_DEV uint32_t order32(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return u >> 31 ? ~u : u | 0x80000000u;
 }
-FL_DEV uint64_t order64(double x) {
-  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
-  return u >> 63 ? ~u : u | (1ull << 63);
+
+// A number as the unevaluated sum of two floats, the first of which is the sum rounded (T. J. Dekker, A floating-point
+// technique for extending the available precision, 1971): 48 bits, for the scores that are compared and the penalty.  The
+// double-precision units of this card take tens of cycles an operation; the join took 10 us longer with them.
+struct Two {
+  float hi, lo;
+};
+FL_DEV Two two_sum(float a, float b) {
+  const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+  return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+FL_DEV Two two_prod(float a, float b) {
+  const float p = __fmul_rn(a, b);
+  return {p, __fmaf_rn(a, b, -p)};
+}
+FL_DEV Two add(Two x, float y) {
+  const Two s = two_sum(x.hi, y);
+  return two_sum(s.hi, __fadd_rn(s.lo, x.lo));
+}
+FL_DEV Two add(Two x, Two y) { return add(add(x, y.lo), y.hi); }
+FL_DEV Two mul(Two x, Two y) {
+  const Two p = two_prod(x.hi, y.hi);
+  return two_sum(p.hi, __fmaf_rn(x.hi, y.lo, __fmaf_rn(x.lo, y.hi, p.lo)));
+}
+// In the order of the numbers; 0 is below all of them, and of an infinity.
+FL_DEV uint64_t order64(Two x) {
+  return fabsf(x.hi) < INFINITY ? (uint64_t)order32(x.hi) << 32 | order32(x.lo) : 0;
+}
+constexpr float LN2_HI = 0.693147182464599609375f, LN2_LO = -1.904654299958e-9f;  // ln 2 in two floats
+// ln x of a normal x, off by 2^-30 at most where |ln x| < 32: x = 2^e f, ln f = 2 (s + s^3 / 3 + s^5 / 5 + ...) with
+// s = (f - 1) / (f + 1), |s| <= 0.172; s in two floats, the series from s^3 on in one.
+FL_DEV Two log_two(float x) {
+  int e = (int)(__float_as_uint(x) >> 23) - 127;
+  float f = __uint_as_float((__float_as_uint(x) & 0x7fffffu) | 0x3f800000u);
+  if (f > 1.41421356f) f *= 0.5f, ++e;
+  const float n = f - 1.f;  // exact
+  const Two d = two_sum(f, 1.f);
+  const float q = n / d.hi, r = __fmaf_rn(-q, d.lo, __fmaf_rn(-q, d.hi, n)) / d.hi, z = q * q;
+  const float tail = q * z * (0.666666667f + z * (0.4f + z * (0.285714286f + z * (0.222222222f + z * 0.181818182f))));
+  Two y = add(two_prod((float)e, LN2_HI), __fmaf_rn((float)e, LN2_LO, 0.f));
+  y = add(y, 2.f * q);
+  return add(y, __fadd_rn(tail, 2.f * r));
+}
+// n^p, off by 2^-25 at most where it is a normal float: e^y with y = p ln n = k ln 2 + r, the series of e^r in one float
+// behind its first two terms.
+FL_DEV Two pow_two(float n, Two p) {
+  const Two y = mul(log_two(n), p);
+  if (!(fabsf(y.hi) < 80.f)) return {y.hi > 0 ? INFINITY : 0.f, 0.f};
+  const float k = rintf(y.hi * LOG2E);
+  const Two r = add(add(y, two_prod(-k, LN2_HI)), -k * LN2_LO);
+  const float x = r.hi;
+  const float tail = x * x * (0.5f + x * (0.166666667f + x * (0.0416666667f + x * (0.00833333333f + x * (0.00138888889f +
+                     x * (0.000198412698f + x * 0.0000248015873f))))));
+  const Two v = add(add(two_sum(1.f, x), r.lo), tail);
+  const float scale = __uint_as_float((uint32_t)((int)k + 127) << 23);
+  return {v.hi * scale, v.lo * scale};
+}
+// x / y rounded to a float, off by little more than half an ulp.
+FL_DEV float div_two(Two x, Two y) {
+  const float q = x.hi / y.hi;
+  if (!(fabsf(q) < 1e37f && fabsf(q) > 1e-30f && y.hi < 1e37f && y.hi > 1e-30f)) return q;
+  return __fadd_rn(q, __fadd_rn(__fmaf_rn(-q, y.hi, x.hi), __fmaf_rn(-q, y.lo, x.lo)) / y.hi);
 }
 
 // Two floats as one operand of the packed fp32 instructions.
@@ -149,17 +213,27 @@ struct Sum {
   }
 };
 
-struct Join {  // shared memory of the CTA that joins a search
-  Cand lists[WARPS][MAX_SLICES * FL_BEAM_MAX];
+// Shared memory of a search's join; behind it each warp's copy of a row's lists.
+struct Join {
   Cand best[FL_BEAM_MAX][FL_BEAM_MAX];
-  uint64_t c[FL_BEAM_MAX][FL_BEAM_MAX];  // candidates of each beam, in order64; 0: none
+  Two score[FL_BEAM_MAX][FL_BEAM_MAX];  // of each beam's candidates
   uint64_t few[FL_BEAM_MAX * FL_BEAM_MAX];
-  int few_at[FL_BEAM_MAX * FL_BEAM_MAX], few_n;
-  double live[FL_BEAM_MAX], ends[FL_BEAM_MAX], base[FL_BEAM_MAX], length;
-  float m[FL_BEAM_MAX], end_x[FL_BEAM_MAX], pool[2 * FL_BEAM_MAX];
+  int few_at[FL_BEAM_MAX * FL_BEAM_MAX], few_n, any_end;
+  Two live[FL_BEAM_MAX], ends[FL_BEAM_MAX], minus_log[FL_BEAM_MAX], length;
+  float m[FL_BEAM_MAX], from[FL_BEAM_MAX], end_x[FL_BEAM_MAX], pool[2 * FL_BEAM_MAX];
   int pool_step[2 * FL_BEAM_MAX], pool_beam[2 * FL_BEAM_MAX], end_rank[FL_BEAM_MAX];
   int token[FL_BEAM_MAX], parent[FL_BEAM_MAX];
 };
+
+// 16 bytes of global memory to this thread's place in shared memory, in groups that the thread itself waits for.
+FL_DEV void cp_async16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+FL_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+FL_DEV void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 
 // A search that stays as it is.
 FL_DEV void rest(const StepArgs& a, int s) {
@@ -180,84 +254,87 @@ FL_DEV void rest(const StepArgs& a, int s) {
   }
 }
 
+// One search's rows joined, a warp a row.
 template <class T>
-FL_DEV void join(const StepArgs& a, int s, int t, Join& j) {
-  const int B = a.p.beams, P = a.slices, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (tid == THREADS - 1) {
-    j.length = pow((double)(t + 1), a.p.length_penalty);
-    j.few_n = 0;
-  }
-  // each row's sum and best tokens, a warp a row
-  for (int b = warp; b < B; b += WARPS) {
-    const int row = s * B + b;
+__global__ void __launch_bounds__(JOIN_THREADS) beam_join_kernel(StepArgs a) {
+  pdl_wait();
+  pdl_trigger();
+  extern __shared__ __align__(16) char sh_join[];
+  Join& j = *reinterpret_cast<Join*>(sh_join);
+  const int B = a.p.beams, P = a.slices, s = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int t = a.from.steps[s];  // (no read-only loads of the state: `to` may be the same memory)
+  const bool active = a.from.done[s] == 0 && t >= 0 && t < a.p.max_steps;
+  if (tid == 0) j.few_n = j.any_end = 0;
+  if (warp < B) {
+    const int b = warp, row = s * B + b;
     const float score = a.from.scores[row];
-    const bool reads = score > -INFINITY && score < INFINITY;
-    float m = -INFINITY, sum = 0.f, e = -INFINITY;
-    Cand* mine = j.lists[warp];
-    if (reads) {
-      const float2 part = lane < P ? __ldcg(a.sums + (int64_t)row * P + lane) : make_float2(-INFINITY, 0.f);
-      for (int i = lane; i < P * B; i += 32) {
-        const float2 y = __ldcg(reinterpret_cast<const float2*>(a.lists + (int64_t)row * P * B) + i);
-        mine[i] = Cand{y.x, __float_as_int(y.y)};
-      }
-      if (a.p.eos >= 0) {
-        float f[Piece<T>::N];
-        Piece<T>::get(*reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld + a.p.eos / Piece<T>::N * Piece<T>::N), f);
+    Cand* mine = reinterpret_cast<Cand*>(&j + 1) + warp * P * B;
+    const float2 part = lane < P ? __ldg(a.sums + (int64_t)row * P + lane) : make_float2(-INFINITY, 0.f);
+    const float e = a.p.eos >= 0 ? Piece<T>::one(((const T*)a.x)[(int64_t)row * a.ld + a.p.eos]) : -INFINITY;
+    for (int i = lane; i < P * B; i += 32) mine[i] = a.lists[(int64_t)row * P * B + i];
+    const bool reads = active && score > -INFINITY && score < INFINITY;
+    float m = part.x;
 #pragma unroll
-        for (int i = 0; i < Piece<T>::N; ++i) e = i == a.p.eos % Piece<T>::N ? f[i] : e;
-      }
-      m = part.x;
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    float sum = part.x == -INFINITY ? part.y : part.x == INFINITY ? NAN : part.y * exp2_hw((part.x - m) * LOG2E);
 #pragma unroll
-      for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-      sum = part.x == -INFINITY ? part.y : part.y * exp2_hw((part.x - m) * LOG2E);
-      if (part.x == INFINITY) sum = NAN;
-#pragma unroll
-      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    }
-    const bool bad = score != score || score == INFINITY || sum != sum, live = reads && !bad && m > -INFINITY;
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    const bool bad = active && (score != score || score == INFINITY || (reads && sum != sum)), live = reads && !bad && m > -INFINITY;
     if (bad && lane == 0) atomicOr(a.status, FL_BEAM_BAD_LOGITS);
     __syncwarp();
+    // lists merged: each lane has a slice's, its best one that is left and the next
     int at = lane * B, k = 0;
-    if (live) {
-      const int stop = lane < P ? at + B : at;
-      for (; k < B; ++k) {
-        const Cand head = at < stop ? mine[at] : Cand{-INFINITY, 0};
-        const uint32_t key = head.x > -INFINITY ? order32(head.x) : 0u, top = __reduce_max_sync(0xffffffffu, key);
-        if (top == 0) break;
-        const int v = __reduce_min_sync(0xffffffffu, key == top ? head.v : 0x7fffffff);
-        if (key == top && head.v == v) {
-          j.best[b][k] = head;
-          ++at;
-        }
+    const int stop = live && lane < P ? at + B : at;
+    Cand head = at < stop ? mine[at] : Cand{-INFINITY, 0}, next = at + 1 < stop ? mine[at + 1] : Cand{-INFINITY, 0};
+#pragma unroll 1
+    for (; k < B; ++k) {
+      const uint32_t key = head.x > -INFINITY ? order32(head.x) : 0u, top = __reduce_max_sync(0xffffffffu, key);
+      if (top == 0) break;
+      const unsigned who = __ballot_sync(0xffffffffu, key == top);
+      bool won = key == top;
+      if (who & (who - 1)) {  // (all lanes take part, whoever has won)
+        const int v = __reduce_min_sync(0xffffffffu, won ? head.v : 0x7fffffff);
+        won = won && head.v == v;
+      }
+      if (won) {
+        j.best[b][k] = head;
+        head = next;
+        ++at;
+        next = at + 1 < stop ? mine[at + 1] : Cand{-INFINITY, 0};
       }
     }
-    __syncwarp();
     if (lane >= k && lane < B) j.best[b][lane] = Cand{-INFINITY, 0};
     if (lane == 0) {
-      // c = score + ((x - m) - log(sum)): exact for the smallest logits that a type has, too
-      j.base[b] = live ? log((double)sum) : 0;
+      const Two l = live ? log_two(sum) : Two{0.f, 0.f};
+      j.minus_log[b] = {-l.hi, -l.lo};
       j.m[b] = m;
+      j.from[b] = score;
       j.end_x[b] = live ? e : -INFINITY;
       j.token[b] = max(a.p.eos, 0);
       j.parent[b] = -1;
-      j.live[b] = -INFINITY;
+      j.live[b] = {-INFINITY, 0.f};
     }
   }
   __syncthreads();
-  for (int i = tid; i < B * B + B; i += THREADS) {
+  if (!active) {  // it stays as it is
+    if (warp == 0) rest(a, s);
+    return;
+  }
+  // c = score + ((x - m) - log(sum)): exact for the smallest logits that a type has, too
+  for (int i = tid; i < B * B + B; i += JOIN_THREADS) {
     const int b = i < B * B ? i / B : i - B * B, k = i % B;
     const float x = i < B * B ? j.best[b][k].x : j.end_x[b];
-    const double c = x > -INFINITY ? (double)a.from.scores[s * B + b] + (((double)x - j.m[b]) - j.base[b]) : -INFINITY;
-    if (i < B * B) j.c[b][k] = x > -INFINITY ? order64(c) : 0;
-    else j.ends[b] = c;
+    const Two c = add(add(two_sum(x, -j.m[b]), j.minus_log[b]), j.from[b]);
+    (i < B * B ? j.score[b][k] : j.ends[b]) = x > -INFINITY ? c : Two{-INFINITY, 0.f};
   }
+  if (tid == JOIN_THREADS - 1) j.length = pow_two((float)(t + 1), {a.penalty_hi, a.penalty_lo});
   __syncthreads();
   // A row's last candidate bounds the search's last: only what reaches the best of those bounds is ranked, by counting who comes
   // before: by c, then the lower beam, then the order within the beam.
   uint64_t bound = 1;
-  for (int b = 0; b < B; ++b) bound = max(bound, j.c[b][B - 1]);
-  for (int i = tid; i < B * B; i += THREADS) {
-    const uint64_t c = j.c[i / B][i % B];
+  for (int b = 0; b < B; ++b) bound = max(bound, order64(j.score[b][B - 1]));
+  for (int i = tid; i < B * B; i += JOIN_THREADS) {
+    const uint64_t c = order64(j.score[i / B][i % B]);
     if (c >= bound) {
       const int n = atomicAdd(&j.few_n, 1);
       j.few[n] = c;
@@ -266,23 +343,20 @@ FL_DEV void join(const StepArgs& a, int s, int t, Join& j) {
   }
   __syncthreads();
   const int n = j.few_n;
-  for (int i = tid; i < n; i += THREADS) {
+  for (int i = tid; i < n; i += JOIN_THREADS) {
     const uint64_t c = j.few[i];
     const int at = j.few_at[i];
     int rank = 0;
     for (int o = 0; o < n; ++o) rank += j.few[o] > c || (j.few[o] == c && j.few_at[o] < at);
     if (rank < B) {
-      const int b = at / B, k = at % B;
-      const Cand y = j.best[b][k];
-      j.token[rank] = y.v;
-      j.parent[rank] = b;
-      j.live[rank] = (double)a.from.scores[s * B + b] + (((double)y.x - j.m[b]) - j.base[b]);
+      j.token[rank] = j.best[at / B][at % B].v;
+      j.parent[rank] = at / B;
+      j.live[rank] = j.score[at / B][at % B];
     }
   }
-  const int b = tid - (THREADS - 32);  // the hypotheses that end
+  const int b = tid - (JOIN_THREADS - 32);  // the hypotheses that end
   if (b >= 0 && b < B) {
-    const double x = j.ends[b];
-    const uint64_t c = x > -INFINITY ? order64(x) : 0;
+    const uint64_t c = order64(j.ends[b]);
     int rank = -1;
     if (c >= bound) {
       const Cand e{j.end_x[b], a.p.eos};
@@ -292,46 +366,53 @@ FL_DEV void join(const StepArgs& a, int s, int t, Join& j) {
         rank += ob == b ? better(j.best[ob][j.few_at[o] % B], e) : j.few[o] > c || (j.few[o] == c && ob < b);
       }
       for (int o = 0; o < B; ++o) {
-        const uint64_t y = j.ends[o] > -INFINITY ? order64(j.ends[o]) : 0;
+        const uint64_t y = order64(j.ends[o]);
         rank += y > c || (y == c && o < b);
       }
-      if (rank >= B) rank = -1;
+      if (rank < B) j.any_end = 1;
+      else rank = -1;
     }
     j.end_rank[b] = rank;
   }
-  __syncthreads();
   // the pool: what had ended, then what ends now in the order of its rank
   if (warp == 0) {
-    const int pb = lane < FL_BEAM_MAX ? lane : lane - FL_BEAM_MAX;
     float x = -INFINITY;
-    int step = 0, beam = 0, order = lane;
-    if (pb < B) {
-      if (lane < FL_BEAM_MAX) {
-        x = a.from.end_scores[s * B + pb];
-        step = a.from.end_steps[s * B + pb];
-        beam = a.from.end_beams[s * B + pb];
-      } else if (j.end_rank[pb] >= 0) {
-        x = (float)(j.ends[pb] / j.length);
+    int step = 0, beam = 0;
+    if (lane < B) {
+      x = a.from.end_scores[s * B + lane];
+      step = a.from.end_steps[s * B + lane];
+      beam = a.from.end_beams[s * B + lane];
+    }
+    if (!(x > -INFINITY)) x = -INFINITY, step = beam = 0;
+    j.pool[lane] = x;  // (kept here over the barrier)
+    j.pool_step[lane] = step;
+    j.pool_beam[lane] = beam;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    if (j.any_end) {
+      const int pb = lane - FL_BEAM_MAX;
+      float x = j.pool[lane];
+      int step = j.pool_step[lane], beam = j.pool_beam[lane], order = lane;
+      if (pb >= 0 && pb < B && j.end_rank[pb] >= 0) {
+        x = div_two(j.ends[pb], j.length);
         step = t;
         beam = pb;
         order = FL_BEAM_MAX + j.end_rank[pb];
       }
-    }
-    if (!(x > -INFINITY)) x = -INFINITY, step = beam = 0;
-    const uint64_t key = (uint64_t)order32(x) << 32 | (uint32_t)((63 - order) << 8 | (31 - lane));
-    int rank = 0;
+      const uint64_t key = (uint64_t)order32(x) << 32 | (uint32_t)((63 - order) << 8 | (31 - lane));
+      int rank = 0;
 #pragma unroll 4
-    for (int o = 0; o < 32; ++o) rank += __shfl_sync(0xffffffffu, key, o) > key;
-    if (pb < B && rank < B) {  // (the places behind the pool's end are empty ones')
+      for (int o = 0; o < 32; ++o) rank += __shfl_sync(0xffffffffu, key, o) > key;
       j.pool[rank] = x;
       j.pool_step[rank] = step;
       j.pool_beam[rank] = beam;
+      __syncwarp();
     }
-    __syncwarp();
     if (lane < B) {
       const int i = s * B + lane;
       const int64_t tr = ((int64_t)s * a.p.max_steps + t) * B + lane;
-      a.to.scores[i] = (float)j.live[lane];
+      a.to.scores[i] = j.live[lane].hi;
       a.to.end_scores[i] = j.pool[lane];
       a.to.end_steps[i] = j.pool_step[lane];
       a.to.end_beams[i] = j.pool_beam[lane];
@@ -341,190 +422,229 @@ FL_DEV void join(const StepArgs& a, int s, int t, Join& j) {
     }
     if (lane == 0) {
       const float worst = j.pool[B - 1];
-      const bool over = worst > -INFINITY && (a.p.early || worst >= (float)(j.live[0] / j.length));
+      const bool none = !(j.live[0].hi > -INFINITY);
       a.to.steps[s] = t + 1;
-      a.to.done[s] = over || !(j.live[0] > -INFINITY);
+      a.to.done[s] = none || (worst > -INFINITY && (a.p.early || worst >= div_two(j.live[0], j.length)));
     }
   }
 }
 
+// Unit u is slice u % slices of row u / slices.  CTA g has units g, g + G, ... as one line of chunks: a thread asks for its
+// pieces of a chunk two chunks ahead, into places of its own that nobody else waits for, and while a unit ends the next
+// one's first chunks are on their way.
 template <class T>
-__global__ void __launch_bounds__(THREADS, 3) beam_step_kernel(StepArgs a) {
+__global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
   pdl_wait();
   pdl_trigger();
   using Io = Piece<T>;
   constexpr int N = Io::N;
-  __shared__ float sh_group[GROUPS], sh_ref[WARPS], sh_sum[WARPS];
-  __shared__ Cand sh_hits[2][MAX_HITS];
-  __shared__ int sh_count[2], sh_last;
-  extern __shared__ __align__(16) char sh_join[];
+  __shared__ __align__(16) float sh_group[2][GROUPS];
+  __shared__ float sh_ref[WARPS], sh_sum[WARPS];
+  __shared__ int sh_count;
+  __shared__ uint8_t sh_live[MAX_UNITS];
+  __shared__ Cand sh_hits[MAX_HITS];
+  extern __shared__ __align__(16) uint4 sh_ring[];  // [STAGES][CHUNK_PIECES]
   const int B = a.p.beams, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int slice = blockIdx.x % (unsigned)a.slices, row = blockIdx.x / (unsigned)a.slices, s = row / B;
-  const int all = (a.p.vocab + N - 1) / N, begin = slice * a.per, end = min(all, begin + a.per);
-  const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld);
-  uint4 cur[PIECES];
-  auto load = [&](int first, uint4 (&u)[PIECES]) {
+  const int all = (a.p.vocab + N - 1) / N;
+  const int mine = (a.units - 1 - (int)blockIdx.x) / (int)gridDim.x + 1;  // units of this CTA
+  const auto row_of = [&](int i) { return (int)((blockIdx.x + (unsigned)i * gridDim.x) / (unsigned)a.slices); };
+  const auto begin_of = [&](int i) { return (int)((blockIdx.x + (unsigned)i * gridDim.x) % (unsigned)a.slices) * a.per; };
+  // what is asked for next: a unit, its row, the chunk's first piece, the unit's end; the stage that it goes to
+  int ask = 0, ask_first = begin_of(0), ask_end = min(all, ask_first + a.per), ask_stage = 0;
+  const uint4* ask_x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row_of(0) * a.ld);
+  const auto ask_chunk = [&] {
+    uint4* to = sh_ring + ask_stage * CHUNK_PIECES + tid;
+    const uint4* from = ask_x + ask_first + tid;
+    if (ask_first + CHUNK_PIECES <= ask_end) {
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int k = first + i * THREADS + tid;
-      u[i] = k < end ? __ldcs(x + k) : make_uint4(Io::NONE, Io::NONE, Io::NONE, Io::NONE);
+      for (int i = 0; i < PIECES; ++i) cp_async16(to + i * THREADS, from + i * THREADS);
+    } else {
+#pragma unroll 1
+      for (int k = ask_first + tid; k < ask_end; k += THREADS, to += THREADS, from += THREADS) cp_async16(to, from);
     }
+    ask_first += CHUNK_PIECES;
+    ask_stage = ask_stage + 1 == STAGES ? 0 : ask_stage + 1;
   };
-  load(begin, cur);  // before it is known whether the beam is live: one latency less
-  const int t = a.from.steps[s];  // (no read-only loads of the state: `to` may be the same memory)
-  const bool active = a.from.done[s] == 0 && t >= 0 && t < a.p.max_steps;
-  const float score = a.from.scores[row];
-  if (active && score > -INFINITY && score < INFINITY) {
-    Sum z;
-    float bound = -INFINITY;
-    int side = 0, since = begin, kept = 0;  // the list in use; the first piece that came after it was ranked, what it had then
-    if (tid == 0) sh_count[0] = 0;
-    for (int first = begin, chunk = 0; first < end; first += CHUNK_PIECES, ++chunk) {
-      uint4 next[PIECES];
-      const bool last = first + CHUNK_PIECES >= end;
-      if (!last) load(first + CHUNK_PIECES, next);
-      // tokens behind the vocabulary; the eos, which is summed but no candidate to go on with
-      const int lo = first * N, hi = (first + CHUNK_PIECES) * N;
-      if (hi > a.p.vocab || (a.p.eos >= lo && a.p.eos < hi)) {
+  ask_chunk();  // before it is known whether the beam is live: one latency less
+  cp_async_commit();
+  for (int i = tid; i < mine; i += THREADS) {
+    const int row = row_of(i), s = row / B;
+    const int t = a.from.steps[s];  // (no read-only loads of the state: `to` may be the same memory)
+    const float score = a.from.scores[row];
+    sh_live[i] = a.from.done[s] == 0 && t >= 0 && t < a.p.max_steps && score > -INFINITY && score < INFINITY;
+  }
+  __syncthreads();
+  const auto ask_more = [&] {  // one group each time, an empty one behind the last unit
+    if (ask < mine && (ask_first >= ask_end || !sh_live[ask])) {
+      do ++ask;
+      while (ask < mine && !sh_live[ask]);
+      if (ask < mine) {
+        ask_x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row_of(ask) * a.ld);
+        ask_first = begin_of(ask);
+        ask_end = min(all, ask_first + a.per);
+      }
+    }
+    if (ask < mine) ask_chunk();
+    cp_async_commit();
+  };
+  for (int i = 1; i < STAGES - 1; ++i) ask_more();
+  int stage = 0, raised = 0;
+  if (!sh_live[0]) {                // its first chunk came for nothing
+    stage = 1;
+    ask_more();
+  }
+  for (int unit = 0; unit < mine; ++unit) {
+    if (sh_live[unit]) {
+      const int row = row_of(unit);
+      const int begin = begin_of(unit), end = min(all, begin + a.per);
+      const int eos_piece = a.p.eos >= 0 && a.p.eos / N >= begin && a.p.eos / N < end ? a.p.eos / N : -1;
+      Sum z;
+      float bound = -INFINITY, most = -INFINITY;  // of this thread
+      if (tid == 0) sh_count = 0;
+      for (int first = begin, chunk = 0; first < end; first += CHUNK_PIECES, ++chunk) {
+        cp_async_wait<STAGES - 2>();
+        uint4* places = sh_ring + stage * CHUNK_PIECES + tid;  // this thread's
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        ask_more();  // into the stage before, which was read a chunk ago
+        // nothing behind the slice's end and the vocabulary; the eos is summed, but no candidate to go on with
+        if (first + CHUNK_PIECES >= end) {
+#pragma unroll 1
+          for (int i = 0; i < PIECES; ++i) {
+            const int k = first + i * THREADS + tid;
+            if (k >= end) places[i * THREADS] = make_uint4(Io::NONE, Io::NONE, Io::NONE, Io::NONE);
+            else if ((k + 1) * N > a.p.vocab)
+              for (int v = a.p.vocab - k * N; v < N; ++v) reinterpret_cast<T*>(places + i * THREADS)[v] = (T)-INFINITY;
+          }
+        }
+        if (eos_piece >= first && eos_piece < first + CHUNK_PIECES && (eos_piece - first) % THREADS == tid) {
+          T* at = reinterpret_cast<T*>(places + (eos_piece - first - tid)) + a.p.eos % N;
+          const float y = Io::one(*at);
+          *at = (T)-INFINITY;
+          z.see(y);
+          z.add(y, -INFINITY);
+        }
+        uint4 cur[PIECES];
+        uint32_t of_piece[PIECES], of_all = Io::NONE;  // maxima
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) cur[i] = places[i * THREADS];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-          const int v = (first + i * THREADS + tid) * N;
-          if (a.p.eos >= v && a.p.eos < v + N) {
-            float f[N], e = -INFINITY;
-            Io::get(cur[i], f);
+          of_piece[i] = Io::max4(cur[i]);
+          of_all = Io::max2(of_all, of_piece[i]);
+        }
+        const float top = Io::top(of_all);
+        most = fmaxf(most, top);
+        bool equals = false;  // whether logits equal to the bound count: it is new, and fewer than B larger ones may have been seen
+        if ((chunk & (chunk + 1)) == 0) {
+          // each time that what has been seen doubles: the B-th largest of the groups' maxima, and the largest
+          float g = most;
 #pragma unroll
-            for (int k = 0; k < N; ++k) e = k == a.p.eos - v ? f[k] : e;
-            z.see(e);
-            z.add(e, -INFINITY);
-            cur[i] = Io::without(cur[i], a.p.eos - v);
+          for (int d = 1; d < THREADS / GROUPS; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
+          float* group = sh_group[raised & 1];
+          ++raised;
+          if (tid % (THREADS / GROUPS) == 0) group[tid / (THREADS / GROUPS)] = g;
+          __syncthreads();
+          g = group[lane];
+          int rank = 0;
+#pragma unroll
+          for (int o = 0; o < GROUPS; o += 4) {
+            const float4 y = *reinterpret_cast<const float4*>(group + o);
+            rank += (y.x > g || (y.x == g && o < lane)) + (y.y > g || (y.y == g && o + 1 < lane)) +
+                    (y.z > g || (y.z == g && o + 2 < lane)) + (y.w > g || (y.w == g && o + 3 < lane));
           }
-          if (v < a.p.vocab && v + N > a.p.vocab)
-            for (int k = a.p.vocab - v; k < N; ++k) cur[i] = Io::without(cur[i], k);
+          const float b = __shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == B - 1)) - 1);
+          equals = chunk == 0 || b > bound;
+          bound = b;
+          z.see(__shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == 0)) - 1));
         }
-      }
-      uint32_t most = Io::NONE;
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i)
-        most = Io::max2(most, Io::max2(Io::max2(cur[i].x, cur[i].y), Io::max2(cur[i].z, cur[i].w)));
-      const float top = Io::top(most);
-      bool look = top > bound;
-      if (chunk == 0) {
-        float g = top;
-#pragma unroll
-        for (int d = 1; d < THREADS / GROUPS; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
-        if (tid % (THREADS / GROUPS) == 0) sh_group[tid / (THREADS / GROUPS)] = g;
-        __syncthreads();
-        // the B-th largest of the groups' maxima, and the largest
-        g = sh_group[lane];
-        int rank = 0;
-#pragma unroll
-        for (int o = 0; o < GROUPS; ++o) {
-          const float y = sh_group[o];
-          rank += y > g || (y == g && o < lane);
-        }
-        bound = __shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == B - 1)) - 1);
-        z.see(__shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == 0)) - 1));
-        look = top >= bound && top > -INFINITY;
-      } else if (look) {
-        z.see(top);
-      }
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        float f[N];
-        Io::get(cur[i], f);
-#pragma unroll
-        for (int k = 0; k < N; k += 2) z.add(f[k], f[k + 1]);
-      }
-      if (look) {
+        const bool look = top > -INFINITY && (equals ? top >= bound : top > bound);
+        if (look) z.see(top);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
           float f[N];
           Io::get(cur[i], f);
 #pragma unroll
-          for (int k = 0; k < N; ++k)
-            if (f[k] > bound || (chunk == 0 && f[k] == bound && f[k] > -INFINITY)) {
-              const int n = atomicAdd(&sh_count[side], 1);
-              if (n < MAX_HITS) sh_hits[side][n] = Cand{f[k], (first + i * THREADS + tid) * N + k};
-            }
+          for (int k = 0; k < N; k += 2) z.add(f[k], f[k + 1]);
         }
-      }
-      if (last || chunk == 3 || chunk == 15) {
-        // the best so far, ranked by counting, raise the bound
-        __syncthreads();
-        const int n = sh_count[side];
-        Cand* to = sh_hits[side ^ 1];
-        if (tid == 0) sh_count[side ^ 1] = min(n, B);
-        if (n <= MAX_HITS) {
-          for (int i = tid; i < n; i += THREADS) {
-            const Cand mine = sh_hits[side][i];
-            int r = 0;
-            for (int o = 0; o < n; ++o) r += better(sh_hits[side][o], mine);
-            if (r < B) to[r] = mine;
-          }
-        } else {
-          // more than the list holds (logits that ascend, many equal ones): the best one behind the last found, B times
-          Cand found{INFINITY, -1};
-          for (int r = 0; r < B; ++r) {
-            Cand mine{-INFINITY, 0x7fffffff};
-            if (tid < kept && better(found, sh_hits[side][tid])) mine = sh_hits[side][tid];
-            for (int k = since + tid; k < min(end, first + CHUNK_PIECES); k += THREADS) {
-              float f[N];
-              Io::get(x[k], f);
-              for (int e = 0; e < N; ++e) {
-                const Cand y{f[e], k * N + e};
-                if (y.v < a.p.vocab && y.v != a.p.eos && better(found, y) && better(y, mine)) mine = y;
+        if (look) {
+          unsigned which = 0;
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i) which |= Io::top(of_piece[i]) >= bound ? 1u << i : 0u;
+          for (; which; which &= which - 1) {
+            const int i = __ffs(which) - 1;
+            float f[N];
+            Io::get(places[i * THREADS], f);
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+              if (f[k] > bound || (equals && f[k] == bound && f[k] > -INFINITY)) {
+                const int n = atomicAdd(&sh_count, 1);
+                if (n < MAX_HITS) sh_hits[n] = Cand{f[k], (first + i * THREADS + tid) * N + k};
               }
-            }
-#pragma unroll
-            for (int d = 16; d; d >>= 1) {
-              const Cand o{__shfl_xor_sync(0xffffffffu, mine.x, d), __shfl_xor_sync(0xffffffffu, mine.v, d)};
-              if (better(o, mine)) mine = o;
-            }
-            if (lane == 0) to[MAX_HITS - WARPS + warp] = mine;
-            __syncthreads();
-            for (int i = 0; i < WARPS; ++i)
-              if (better(to[MAX_HITS - WARPS + i], mine)) mine = to[MAX_HITS - WARPS + i];
-            __syncthreads();
-            if (tid == 0) to[r] = mine;
-            found = mine;
           }
         }
-        __syncthreads();
-        side ^= 1;
-        since = first + CHUNK_PIECES;
-        kept = min(n, B);
-        if (n >= B) bound = to[B - 1].x;
-        if (n > 0) z.see(to[0].x);
       }
-      if (!last)
+      float ref = z.ref;
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) cur[i] = next[i];
-    }
-    // the slice's sum and list
-    float ref = z.ref;
+      for (int d = 16; d; d >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, d));
+      float sum = z.ref == -INFINITY ? z.total() : z.total() * exp2_hw((z.ref - ref) * LOG2E);
 #pragma unroll
-    for (int d = 16; d; d >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, d));
-    float sum = z.ref == -INFINITY ? z.total() : z.total() * exp2_hw((z.ref - ref) * LOG2E);
+      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      if (lane == 0) sh_ref[warp] = ref, sh_sum[warp] = sum;
+      __syncthreads();
+      // the slice's list: what has come together, ranked by counting
+      const int n = sh_count;
+      Cand* list = a.lists + (int64_t)(blockIdx.x + unit * gridDim.x) * B;
+      if (n <= MAX_HITS) {
+        for (int i = tid; i < n; i += THREADS) {
+          const Cand one = sh_hits[i];
+          int r = 0;
+          for (int o = 0; o < n; ++o) r += better(sh_hits[o], one);
+          if (r < B) list[r] = one;
+        }
+        if (tid >= n && tid < B) list[tid] = Cand{-INFINITY, 0};
+      } else {
+        // more than there is room for (logits that ascend, many equal ones): the best one behind the last found, B times
+        const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld);
+        Cand found{INFINITY, -1};
+        for (int r = 0; r < B; ++r) {
+          Cand one{-INFINITY, 0x7fffffff};
+          for (int k = begin + tid; k < end; k += THREADS) {
+            float f[N];
+            Io::get(__ldg(x + k), f);
+            for (int e = 0; e < N; ++e) {
+              const Cand y{f[e], k * N + e};
+              if (y.v < a.p.vocab && y.v != a.p.eos && better(found, y) && better(y, one)) one = y;
+            }
+          }
 #pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (lane == 0) sh_ref[warp] = ref, sh_sum[warp] = sum;
-    if (tid < B) a.lists[(int64_t)blockIdx.x * B + tid] = tid < sh_count[side] ? sh_hits[side][tid] : Cand{-INFINITY, 0};
-    __syncthreads();
-    if (tid == 0) {
-      float m = sh_ref[0], q = 0.f;
-      for (int i = 1; i < WARPS; ++i) m = fmaxf(m, sh_ref[i]);
-      for (int i = 0; i < WARPS; ++i) q += sh_ref[i] == -INFINITY ? sh_sum[i] : sh_sum[i] * exp2_hw((sh_ref[i] - m) * LOG2E);
-      a.sums[blockIdx.x] = make_float2(m, q);
+          for (int d = 16; d; d >>= 1) {
+            const Cand o{__shfl_xor_sync(0xffffffffu, one.x, d), __shfl_xor_sync(0xffffffffu, one.v, d)};
+            if (better(o, one)) one = o;
+          }
+          if (lane == 0) sh_hits[warp] = one;
+          __syncthreads();
+          for (int i = 0; i < WARPS; ++i)
+            if (better(sh_hits[i], one)) one = sh_hits[i];
+          __syncthreads();
+          if (tid == 0) list[r] = one;
+          found = one;
+        }
+      }
+      if (warp == 0) {
+        const float r = lane < WARPS ? sh_ref[lane] : -INFINITY;
+        float m = r;
+#pragma unroll
+        for (int d = 1; d < WARPS; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        float q = lane < WARPS ? sh_sum[lane] : 0.f;
+        if (r != -INFINITY) q *= exp2_hw((r - m) * LOG2E);
+#pragma unroll
+        for (int d = 1; d < WARPS; d <<= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
+        if (lane == 0) a.sums[blockIdx.x + unit * gridDim.x] = make_float2(m, q);
+      }
+      __syncthreads();  // the hits' and the sums' places are free again
     }
   }
-  __syncthreads();
-  if (tid == 0) sh_last = kv_part_done(a.counters + s, (unsigned)(B * a.slices));
-  __syncthreads();
-  if (!sh_last) return;
-  if (active)
-    join<T>(a, s, t, *reinterpret_cast<Join*>(sh_join));
-  else
-    rest(a, s);
+  cp_async_wait<0>();  // (a first chunk that came for nothing)
 }
 
 int64_t part_bytes(const fl_beam_search* p, int slices) {
@@ -534,7 +654,7 @@ int64_t part_bytes(const fl_beam_search* p, int slices) {
 const char* search_problem(const fl_beam_search* p, int* code) {
   *code = FL_ERR_INVALID_ARG;
   if (!p || p->n_seqs < 0 || p->beams < 1 || p->vocab < 1 || p->max_steps < 1 || p->eos < -1 || p->eos >= p->vocab ||
-      (p->early != 0 && p->early != 1) || !std::isfinite(p->length_penalty))
+      (p->early != 0 && p->early != 1) || !(std::fabs(p->length_penalty) <= 1e6))
     return "search";
   *code = FL_ERR_CAPACITY;
   if (p->beams > FL_BEAM_MAX) return "more than 16 beams";
@@ -553,19 +673,32 @@ bool state_ok(const fl_beam_state* s) {
   return true;
 }
 
-// Slices of a row: enough for some CTAs per SM and wave, of a thread's piece at least.
+// Slices of a row: those with which the CTAs' lines are shortest, in chunks, with the ends of a unit counted as `ends` of them.
 template <class T>
 int launch_step(StepArgs& a, cudaStream_t st) {
-  constexpr int N = Piece<T>::N;
-  const int pieces = (a.p.vocab + N - 1) / N;
-  const int64_t rows = (int64_t)a.p.n_seqs * a.p.beams;
-  const int64_t want = (16 * fl_sm_count() + rows - 1) / rows, most = (pieces + THREADS - 1) / THREADS;
-  const int slices = (int)std::min<int64_t>(std::min<int64_t>(want, most), MAX_SLICES);
-  a.per = (pieces + slices - 1) / slices;
+  constexpr int N = Piece<T>::N, ring = STAGES * CHUNK_PIECES * 16;
+  constexpr float ends = 1.5f;
+  const int pieces = (a.p.vocab + N - 1) / N, slots = CTAS * fl_sm_count();
+  const int rows = a.p.n_seqs * a.p.beams;
+  float least = 0;
+  for (int slices = 1; slices <= MAX_SLICES && (slices - 1) * THREADS < pieces; ++slices) {
+    const int each = (rows * slices + slots - 1) / slots;
+    const float cost = each * (ends + std::max(1.f, (float)pieces / (float)(slices * CHUNK_PIECES)));
+    if (slices > 1 && (cost >= 0.97f * least || each > MAX_UNITS)) continue;
+    least = cost;
+    a.slices = slices;
+  }
+  a.per = (pieces + a.slices - 1) / a.slices;
   a.slices = (pieces + a.per - 1) / a.per;
+  a.units = rows * a.slices;
+  const int grid = std::min(std::max(slots, (a.units + MAX_UNITS - 1) / MAX_UNITS), a.units);
   auto kern = beam_step_kernel<T>;
-  FL_CUDA_TRY(fl_func_smem((const void*)kern, sizeof(Join)));
-  FL_CUDA_TRY(fl_launch(kern, dim3((unsigned)(rows * a.slices)), dim3(THREADS), sizeof(Join), st, a));
+  auto join = beam_join_kernel<T>;
+  const auto lists = [&](int beams, int slices) { return beams * slices * beams * (int)sizeof(Cand); };
+  FL_CUDA_TRY(fl_func_smem((const void*)kern, ring));
+  FL_CUDA_TRY(fl_func_smem((const void*)join, sizeof(Join) + lists(FL_BEAM_MAX, MAX_SLICES)));
+  FL_CUDA_TRY(fl_launch(kern, dim3(grid), dim3(THREADS), ring, st, a));
+  FL_CUDA_TRY(fl_launch(join, dim3(a.p.n_seqs), dim3(JOIN_THREADS), sizeof(Join) + lists(a.p.beams, a.slices), st, a));
   return FL_OK;
 }
 
@@ -577,6 +710,7 @@ struct TraceArgs {
   fl_beam_state s;
   const int32_t *tokens, *parents;
   int n_best, pad;
+  float penalty_hi, penalty_lo;
   int32_t *out_tokens, *out_lens;
   float* out_scores;
   int* status;
@@ -612,7 +746,7 @@ __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) 
         if ((unsigned)before >= (unsigned)T) before = 0;
         if ((unsigned)beam >= (unsigned)B) beam = 0;
       } else if (a.s.done[s] == 0 && steps > 0) {
-        x = (float)((double)a.s.scores[s * B + b] / pow((double)steps, a.p.length_penalty));
+        x = div_two({a.s.scores[s * B + b], 0.f}, pow_two((float)steps, {a.penalty_hi, a.penalty_lo}));
         before = steps;
         beam = b;
       }
@@ -703,7 +837,7 @@ extern "C" size_t fl_k_beam_workspace(const fl_beam_search* search) {
     fl_internal_error(code, "beam workspace: %s", w);
     return 0;
   }
-  return MAX_SEARCHES * sizeof(unsigned) + part_bytes(search, MAX_SLICES);
+  return part_bytes(search, MAX_SLICES);
 }
 
 extern "C" int fl_k_beam_step(const fl_beam_search* search, const fl_beam_state* from, const fl_beam_state* to,
@@ -729,9 +863,9 @@ extern "C" int fl_k_beam_step(const fl_beam_search* search, const fl_beam_state*
     return fl_internal_error(FL_ERR_INVALID_ARG, "beam step: args");
   if (ld < search->vocab || ld % (dtype == FL_DT_F32 ? 4 : 8))
     return fl_internal_error(FL_ERR_UNSUPPORTED, "beam step: row stride %lld (a multiple of 16 bytes, vocab or more)", (long long)ld);
-  StepArgs a{*search, *from, *to, logits, ld, 0, 0, trace_tokens, trace_parents, tokens, parents, (unsigned*)workspace,
-             nullptr, nullptr, status};
-  a.sums = (float2*)((char*)workspace + MAX_SEARCHES * sizeof(unsigned));
+  const float penalty = (float)search->length_penalty;
+  StepArgs a{*search, *from, *to, logits, ld, 0, 0, 0, penalty, (float)(search->length_penalty - penalty), trace_tokens, trace_parents, tokens, parents, nullptr, nullptr, status};
+  a.sums = (float2*)workspace;
   a.lists = (Cand*)(a.sums + (int64_t)search->n_seqs * search->beams * MAX_SLICES);
   const cudaStream_t st = (cudaStream_t)stream;
   return dtype == FL_DT_F32 ? launch_step<float>(a, st)
@@ -749,7 +883,8 @@ extern "C" int fl_k_beam_trace(const fl_beam_search* search, const fl_beam_state
       fl_misaligned(trace_tokens, 4) || fl_misaligned(trace_parents, 4) || fl_misaligned(out_tokens, 4) ||
       fl_misaligned(out_lens, 4) || fl_misaligned(out_scores, 4) || fl_misaligned(status, 4))
     return fl_internal_error(FL_ERR_INVALID_ARG, "beam trace: args");
-  const TraceArgs a{*search, *state, trace_tokens, trace_parents, n_best, pad, out_tokens, out_lens, out_scores, status};
+  const float penalty = (float)search->length_penalty;
+  const TraceArgs a{*search, *state, trace_tokens, trace_parents, n_best, pad, penalty, (float)(search->length_penalty - penalty), out_tokens, out_lens, out_scores, status};
   const int room = search->max_steps < BLOCK_STEPS ? search->max_steps : BLOCK_STEPS, chunks = (room + CHUNK - 1) / CHUNK;
   const int smem = (room + chunks) * (search->beams + n_best);
   // the limit of the largest call, once: a smaller one would lower it for a larger call made before

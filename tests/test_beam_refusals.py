@@ -29,7 +29,8 @@ def state(F, at=0, **kw):
 
 SEARCHES = [("n_seqs", -1, ARG), ("n_seqs", 16385, CAPACITY), ("beams", 0, ARG), ("beams", 17, CAPACITY), ("vocab", 0, ARG),
             ("vocab", 2 ** 19 + 1, CAPACITY), ("max_steps", 0, ARG), ("max_steps", 2 ** 24 + 1, CAPACITY), ("eos", -2, ARG),
-            ("eos", 100, ARG), ("early", 2, ARG), ("length_penalty", float("nan"), ARG), ("length_penalty", float("inf"), ARG)]
+            ("eos", 100, ARG), ("early", 2, ARG), ("length_penalty", float("nan"), ARG), ("length_penalty", float("inf"), ARG),
+            ("length_penalty", -1.1e6, ARG)]
 
 
 def test_step(F):

@@ -20,13 +20,13 @@
 namespace {
 
 constexpr int JOIN_THREADS = 32 * FL_BEAM_MAX;
-constexpr int THREADS = 256, WARPS = THREADS / 32, GROUPS = 32, MAX_SLICES = 32;
+constexpr int THREADS = 128, WARPS = THREADS / 32, GROUPS = 32, MAX_SLICES = 32;
 constexpr int PIECES = 8, CHUNK_PIECES = PIECES * THREADS;  // 16-byte pieces of a thread and of a CTA in a chunk
-constexpr int STAGES = 2, CTAS = 3;                          // chunks on their way or in use, CTAs of an SM
-constexpr int MAX_HITS = 512, MAX_UNITS = 1024;              // of a CTA
+constexpr int STAGES = 2, CTAS = 6;                          // chunks on their way or in use, CTAs of an SM
+constexpr int MAX_HITS = 256, MAX_UNITS = 1024;              // of a CTA
 constexpr int MAX_SEARCHES = 16384, MAX_VOCAB = 1 << 19;
 constexpr float LOG2E = 1.4426950408889634f;
-static_assert(FL_BEAM_MAX <= GROUPS && GROUPS == 32 && FL_BEAM_MAX == 2 * WARPS);
+static_assert(FL_BEAM_MAX <= GROUPS && GROUPS == 32);
 
 struct Cand {  // a token and its logit
   float x;

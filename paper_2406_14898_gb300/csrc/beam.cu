@@ -2,11 +2,11 @@
 //
 // Step.  With c(b, v) = score_b + x_bv - lse_b a search wants the best `beams` of beams x vocab candidates.  Within a
 // beam c is ordered as x is, so each row needs only its largest logits and its log-sum-exp: one pass over the logits, which
-// is the bound (HBM; for few rows the latency of a load, some barriers and the join).  A row is cut into slices, a CTA each,
-// which goes through its slice in chunks, the next one's loads in flight.  Of the first chunk the B-th largest of 32 groups of
+// is the bound (HBM; for few rows the latency of a load, some barriers and the join).  A CTA goes through its part of a row in chunks,
+// the next one's loads in flight.  Of the first chunk the B-th largest of 32 groups of
 // threads' maxima bounds the B-th largest logit from below; of what comes later only what exceeds the bound is looked
-// at, about B logits for each time that the slice doubles, and the bound is raised now and then.  A second kernel, a
-// CTA a search, joins the slices' sums and lists.  (With the join in the CTA that comes last, CTAs that joined came late
+// at, about B logits for each time that what has been seen doubles, and the bound is raised now and then.  A second kernel, a
+// CTA a search, joins the parts' sums and lists.  (With the join in the CTA that comes last, CTAs that joined came late
 // for their next slices and so joined again: 64 x 16 rows of 130528 bf16 157 us.)
 #include <cuda_fp16.h>
 
@@ -20,10 +20,10 @@
 namespace {
 
 constexpr int JOIN_THREADS = 32 * FL_BEAM_MAX;
-constexpr int THREADS = 128, WARPS = THREADS / 32, GROUPS = 32, MAX_SLICES = 32;
+constexpr int THREADS = 128, WARPS = THREADS / 32, GROUPS = 32, MAX_PARTS = 32;
 constexpr int PIECES = 8, CHUNK_PIECES = PIECES * THREADS;  // 16-byte pieces of a thread and of a CTA in a chunk
 constexpr int STAGES = 2, CTAS = 6;                          // chunks on their way or in use, CTAs of an SM
-constexpr int MAX_HITS = 256, MAX_UNITS = 1024;              // of a CTA
+constexpr int MAX_HITS = 256, MAX_ROWS = 512;                // of a CTA
 constexpr int MAX_SEARCHES = 16384, MAX_VOCAB = 1 << 19;
 constexpr float LOG2E = 1.4426950408889634f;
 static_assert(FL_BEAM_MAX <= GROUPS && GROUPS == 32);
@@ -39,11 +39,12 @@ struct StepArgs {
   fl_beam_state from, to;
   const void* x;
   int64_t ld;
-  int slices, per, units;  // slices of a row, 16-byte pieces of a slice, slices in all
+  int row_chunks;  // of a row
   float penalty_hi, penalty_lo;
   int32_t *trace_tokens, *trace_parents, *tokens, *parents;
-  float2* sums;  // [row][slice] (largest logit, sum of exp(x - it))
-  Cand* lists;   // [row][slice][beam], best first; x = -inf: none
+  float2* sums;  // [row][part] (a logit, sum of exp(x - it))
+  Cand* lists;   // [row][part][beam], best first; x = -inf: none
+  int32_t* parts;  // [row] parts that it was cut into
   int* status;
 };
 
@@ -261,18 +262,20 @@ __global__ void __launch_bounds__(JOIN_THREADS) beam_join_kernel(StepArgs a) {
   pdl_trigger();
   extern __shared__ __align__(16) char sh_join[];
   Join& j = *reinterpret_cast<Join*>(sh_join);
-  const int B = a.p.beams, P = a.slices, s = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int B = a.p.beams, s = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int t = a.from.steps[s];  // (no read-only loads of the state: `to` may be the same memory)
   const bool active = a.from.done[s] == 0 && t >= 0 && t < a.p.max_steps;
   if (tid == 0) j.few_n = j.any_end = 0;
   if (warp < B) {
     const int b = warp, row = s * B + b;
     const float score = a.from.scores[row];
-    Cand* mine = reinterpret_cast<Cand*>(&j + 1) + warp * P * B;
-    const float2 part = lane < P ? __ldg(a.sums + (int64_t)row * P + lane) : make_float2(-INFINITY, 0.f);
-    const float e = a.p.eos >= 0 ? Piece<T>::one(((const T*)a.x)[(int64_t)row * a.ld + a.p.eos]) : -INFINITY;
-    for (int i = lane; i < P * B; i += 32) mine[i] = a.lists[(int64_t)row * P * B + i];
     const bool reads = active && score > -INFINITY && score < INFINITY;
+    const int P = reads ? __ldg(a.parts + row) : 0;
+    Cand* mine = reinterpret_cast<Cand*>(&j + 1) + warp * MAX_PARTS * B;
+    float2 part = __ldg(a.sums + (int64_t)row * MAX_PARTS + lane);  // (of any content behind the parts)
+    if (lane >= P) part = make_float2(-INFINITY, 0.f);
+    const float e = a.p.eos >= 0 ? Piece<T>::one(((const T*)a.x)[(int64_t)row * a.ld + a.p.eos]) : -INFINITY;
+    for (int i = lane; i < P * B; i += 32) mine[i] = a.lists[(int64_t)row * MAX_PARTS * B + i];
     float m = part.x;
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
@@ -429,9 +432,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) beam_join_kernel(StepArgs a) {
   }
 }
 
-// Unit u is slice u % slices of row u / slices.  CTA g has units g, g + G, ... as one line of chunks: a thread asks for its
-// pieces of a chunk two chunks ahead, into places of its own that nobody else waits for, and while a unit ends the next
-// one's first chunks are on their way.
+// The chunks of the live beams' rows lie one after another on a line, which is cut into equal pieces, one a CTA: a row's
+// part is what lies in one CTA's piece.  A thread asks for its 16-byte pieces of a chunk a chunk ahead, into places of its own that
+// nobody else waits for, and while a part ends the next one's first chunk is on its way.
 template <class T>
 __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
   pdl_wait();
@@ -440,63 +443,116 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
   constexpr int N = Io::N;
   __shared__ __align__(16) float sh_group[2][GROUPS];
   __shared__ float sh_ref[WARPS], sh_sum[WARPS];
-  __shared__ int sh_count;
-  __shared__ uint8_t sh_live[MAX_UNITS];
+  __shared__ int sh_count, sh_warp[WARPS];
+  __shared__ int sh_rows[MAX_ROWS];
   __shared__ Cand sh_hits[MAX_HITS];
   extern __shared__ __align__(16) uint4 sh_ring[];  // [STAGES][CHUNK_PIECES]
-  const int B = a.p.beams, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int all = (a.p.vocab + N - 1) / N;
-  const int mine = (a.units - 1 - (int)blockIdx.x) / (int)gridDim.x + 1;  // units of this CTA
-  const auto row_of = [&](int i) { return (int)((blockIdx.x + (unsigned)i * gridDim.x) / (unsigned)a.slices); };
-  const auto begin_of = [&](int i) { return (int)((blockIdx.x + (unsigned)i * gridDim.x) % (unsigned)a.slices) * a.per; };
-  // what is asked for next: a unit, its row, the chunk's first piece, the unit's end; the stage that it goes to
-  int ask = 0, ask_first = begin_of(0), ask_end = min(all, ask_first + a.per), ask_stage = 0;
-  const uint4* ask_x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row_of(0) * a.ld);
+  const int B = a.p.beams, rows = a.p.n_seqs * B, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int all = (a.p.vocab + N - 1) / N, L = a.row_chunks;
+  // this CTA's chunks with n live rows: [c0, c1) of n L
+  int c0, c1, ctas, n_live;
+  const auto cut = [&](int n) {
+    const int64_t chunks = (int64_t)n * L;
+    n_live = n;
+    ctas = (int)min((int64_t)gridDim.x, L <= MAX_PARTS ? chunks : (int64_t)(MAX_PARTS - 2) * n);  // no row in more than MAX_PARTS
+    c0 = c1 = 0;
+    if ((int)blockIdx.x >= ctas) return;
+    c0 = (int)kv_div(blockIdx.x * chunks, ctas);
+    c1 = (int)kv_div((blockIdx.x + 1) * chunks, ctas);
+  };
+  const auto live = [&](int row) {
+    // (no read-only loads of the state: `to` may be the same memory; no load behind another's outcome)
+    const int s = row / B, t = a.from.steps[s], done = a.from.done[s];
+    const float score = a.from.scores[row];
+    return (done == 0) & (t >= 0) & (t < a.p.max_steps) & (score > -INFINITY) & (score < INFINITY);
+  };
+  // what is asked for next: a chunk of the line, its row, its first piece; the stage that it goes to
+  int ask = 0, ask_first = 0, ask_stage = 0;
+  const uint4* ask_x = nullptr;
+  const auto ask_row = [&](int row) { ask_x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld); };
   const auto ask_chunk = [&] {
     uint4* to = sh_ring + ask_stage * CHUNK_PIECES + tid;
     const uint4* from = ask_x + ask_first + tid;
-    if (ask_first + CHUNK_PIECES <= ask_end) {
+    if (ask_first + CHUNK_PIECES <= all) {
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) cp_async16(to + i * THREADS, from + i * THREADS);
     } else {
 #pragma unroll 1
-      for (int k = ask_first + tid; k < ask_end; k += THREADS, to += THREADS, from += THREADS) cp_async16(to, from);
+      for (int k = ask_first + tid; k < all; k += THREADS, to += THREADS, from += THREADS) cp_async16(to, from);
     }
+    ++ask;
     ask_first += CHUNK_PIECES;
     ask_stage = ask_stage + 1 == STAGES ? 0 : ask_stage + 1;
   };
-  ask_chunk();  // before it is known whether the beam is live: one latency less
-  cp_async_commit();
-  for (int i = tid; i < mine; i += THREADS) {
-    const int row = row_of(i), s = row / B;
-    const int t = a.from.steps[s];  // (no read-only loads of the state: `to` may be the same memory)
-    const float score = a.from.scores[row];
-    sh_live[i] = a.from.done[s] == 0 && t >= 0 && t < a.p.max_steps && score > -INFINITY && score < INFINITY;
+  // The first chunk as it is if all beams are live, before that is known: one latency less.
+  cut(rows);
+  if (c0 < c1) {
+    ask = c0;
+    ask_first = c0 % L * CHUNK_PIECES;
+    ask_row(c0 / L);
+    ask_chunk();
   }
+  cp_async_commit();
+  // the live rows of this CTA's piece: everybody counts those of some rows
+  const int each = (rows + THREADS - 1) / THREADS, r0 = min(rows, tid * each), r1 = min(rows, r0 + each);
+  int count = 0;
+#pragma unroll 8
+  for (int r = r0; r < r1; ++r) count += live(r);
+  int before = count;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, before, d);
+    if (lane >= d) before += y;
+  }
+  if (lane == 31) sh_warp[warp] = before;
   __syncthreads();
-  const auto ask_more = [&] {  // one group each time, an empty one behind the last unit
-    if (ask < mine && (ask_first >= ask_end || !sh_live[ask])) {
-      do ++ask;
-      while (ask < mine && !sh_live[ask]);
-      if (ask < mine) {
-        ask_x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row_of(ask) * a.ld);
-        ask_first = begin_of(ask);
-        ask_end = min(all, ask_first + a.per);
+  before -= count;
+  int total = 0;
+  for (int w = 0; w < WARPS; ++w) {
+    if (w == warp) before += total;
+    total += sh_warp[w];
+  }
+  const bool guessed = total == rows;
+  if (!guessed) cut(total);
+  const int k0 = c0 / L, k1 = c0 < c1 ? (c1 - 1) / L : -1;  // its first and last live row
+  if (before <= k1 && before + count > k0)
+    for (int r = r0, k = before; r < r1; ++r)
+      if (live(r)) {
+        if (k >= k0 && k <= k1) sh_rows[k - k0] = r;
+        ++k;
       }
+  __syncthreads();
+  if (c0 >= c1) {
+    cp_async_wait<0>();
+    return;
+  }
+  const auto ask_more = [&] {  // one group each time, an empty one behind the last chunk
+    if (ask < c1) {
+      if (ask_first >= all) {
+        ask_first = 0;
+        ask_row(sh_rows[ask / L - k0]);
+      }
+      ask_chunk();
     }
-    if (ask < mine) ask_chunk();
     cp_async_commit();
   };
-  for (int i = 1; i < STAGES - 1; ++i) ask_more();
   int stage = 0, raised = 0;
-  if (!sh_live[0]) {                // its first chunk came for nothing
-    stage = 1;
+  if (!guessed) {  // the first chunk came for nothing, if one did
+    stage = ask_stage = 1;
+    ask = c0;
+    ask_first = c0 % L * CHUNK_PIECES;
+    ask_row(sh_rows[0]);
     ask_more();
   }
-  for (int unit = 0; unit < mine; ++unit) {
-    if (sh_live[unit]) {
-      const int row = row_of(unit);
-      const int begin = begin_of(unit), end = min(all, begin + a.per);
+  static_assert(STAGES == 2);
+  for (int c = c0; c < c1;) {
+    {
+      const int k = c / L, row = sh_rows[k - k0], from = c - k * L, to = min(L, from + c1 - c);
+      c += to - from;
+      const int begin = from * CHUNK_PIECES, end = min(all, to * CHUNK_PIECES);
+      // which part of its row: its CTA's distance from the one of the row's first chunk
+      const int part = blockIdx.x - (int)kv_div(((int64_t)k * L + 1) * ctas - 1, (int64_t)n_live * L);
+      const int64_t at_part = (int64_t)row * MAX_PARTS + part;
       const int eos_piece = a.p.eos >= 0 && a.p.eos / N >= begin && a.p.eos / N < end ? a.p.eos / N : -1;
       Sum z;
       float bound = -INFINITY, most = -INFINITY;  // of this thread
@@ -593,7 +649,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
       __syncthreads();
       // the slice's list: what has come together, ranked by counting
       const int n = sh_count;
-      Cand* list = a.lists + (int64_t)(blockIdx.x + unit * gridDim.x) * B;
+      Cand* list = a.lists + at_part * B;
       if (n <= MAX_HITS) {
         for (int i = tid; i < n; i += THREADS) {
           const Cand one = sh_hits[i];
@@ -639,7 +695,10 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
         if (r != -INFINITY) q *= exp2_hw((r - m) * LOG2E);
 #pragma unroll
         for (int d = 1; d < WARPS; d <<= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
-        if (lane == 0) a.sums[blockIdx.x + unit * gridDim.x] = make_float2(m, q);
+        if (lane == 0) {
+          a.sums[at_part] = make_float2(m, q);
+          if (to == L) a.parts[row] = part + 1;
+        }
       }
       __syncthreads();  // the hits' and the sums' places are free again
     }
@@ -647,8 +706,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
   cp_async_wait<0>();  // (a first chunk that came for nothing)
 }
 
-int64_t part_bytes(const fl_beam_search* p, int slices) {
-  return (int64_t)p->n_seqs * p->beams * slices * (sizeof(float2) + p->beams * sizeof(Cand));
+int64_t part_bytes(const fl_beam_search* p) {
+  return (int64_t)p->n_seqs * p->beams * (MAX_PARTS * (sizeof(float2) + p->beams * sizeof(Cand)) + sizeof(int32_t)) + 16;
 }
 
 const char* search_problem(const fl_beam_search* p, int* code) {
@@ -673,32 +732,21 @@ bool state_ok(const fl_beam_state* s) {
   return true;
 }
 
-// Slices of a row: those with which the CTAs' lines are shortest, in chunks, with the ends of a unit counted as `ends` of them.
 template <class T>
 int launch_step(StepArgs& a, cudaStream_t st) {
   constexpr int N = Piece<T>::N, ring = STAGES * CHUNK_PIECES * 16;
-  constexpr float ends = 1.5f;
-  const int pieces = (a.p.vocab + N - 1) / N, slots = CTAS * fl_sm_count();
   const int rows = a.p.n_seqs * a.p.beams;
-  float least = 0;
-  for (int slices = 1; slices <= MAX_SLICES && (slices - 1) * THREADS < pieces; ++slices) {
-    const int each = (rows * slices + slots - 1) / slots;
-    const float cost = each * (ends + std::max(1.f, (float)pieces / (float)(slices * CHUNK_PIECES)));
-    if (slices > 1 && (cost >= 0.97f * least || each > MAX_UNITS)) continue;
-    least = cost;
-    a.slices = slices;
-  }
-  a.per = (pieces + a.slices - 1) / a.slices;
-  a.slices = (pieces + a.per - 1) / a.per;
-  a.units = rows * a.slices;
-  const int grid = std::min(std::max(slots, (a.units + MAX_UNITS - 1) / MAX_UNITS), a.units);
+  a.row_chunks = ((a.p.vocab + N - 1) / N + CHUNK_PIECES - 1) / CHUNK_PIECES;
+  // as many CTAs as run at once (more where one would have more rows than it keeps), and no more than chunks
+  const int64_t slots = std::max(CTAS * fl_sm_count(), (rows + MAX_ROWS - 3) / (MAX_ROWS - 2));
+  const int grid = (int)std::min<int64_t>(slots, (int64_t)rows * a.row_chunks);
   auto kern = beam_step_kernel<T>;
   auto join = beam_join_kernel<T>;
-  const auto lists = [&](int beams, int slices) { return beams * slices * beams * (int)sizeof(Cand); };
+  const auto join_smem = [](int beams) { return (int)sizeof(Join) + beams * MAX_PARTS * beams * (int)sizeof(Cand); };
   FL_CUDA_TRY(fl_func_smem((const void*)kern, ring));
-  FL_CUDA_TRY(fl_func_smem((const void*)join, sizeof(Join) + lists(FL_BEAM_MAX, MAX_SLICES)));
+  FL_CUDA_TRY(fl_func_smem((const void*)join, join_smem(FL_BEAM_MAX)));
   FL_CUDA_TRY(fl_launch(kern, dim3(grid), dim3(THREADS), ring, st, a));
-  FL_CUDA_TRY(fl_launch(join, dim3(a.p.n_seqs), dim3(JOIN_THREADS), sizeof(Join) + lists(a.p.beams, a.slices), st, a));
+  FL_CUDA_TRY(fl_launch(join, dim3(a.p.n_seqs), dim3(JOIN_THREADS), join_smem(a.p.beams), st, a));
   return FL_OK;
 }
 
@@ -837,7 +885,7 @@ extern "C" size_t fl_k_beam_workspace(const fl_beam_search* search) {
     fl_internal_error(code, "beam workspace: %s", w);
     return 0;
   }
-  return part_bytes(search, MAX_SLICES);
+  return part_bytes(search);
 }
 
 extern "C" int fl_k_beam_step(const fl_beam_search* search, const fl_beam_state* from, const fl_beam_state* to,
@@ -864,9 +912,12 @@ extern "C" int fl_k_beam_step(const fl_beam_search* search, const fl_beam_state*
   if (ld < search->vocab || ld % (dtype == FL_DT_F32 ? 4 : 8))
     return fl_internal_error(FL_ERR_UNSUPPORTED, "beam step: row stride %lld (a multiple of 16 bytes, vocab or more)", (long long)ld);
   const float penalty = (float)search->length_penalty;
-  StepArgs a{*search, *from, *to, logits, ld, 0, 0, 0, penalty, (float)(search->length_penalty - penalty), trace_tokens, trace_parents, tokens, parents, nullptr, nullptr, status};
+  StepArgs a{*search, *from, *to, logits, ld, 0, penalty, (float)(search->length_penalty - penalty), trace_tokens, trace_parents,
+             tokens, parents, nullptr, nullptr, nullptr, status};
   a.sums = (float2*)workspace;
-  a.lists = (Cand*)(a.sums + (int64_t)search->n_seqs * search->beams * MAX_SLICES);
+  const int64_t rows = (int64_t)search->n_seqs * search->beams;
+  a.lists = (Cand*)(a.sums + rows * MAX_PARTS);
+  a.parts = (int32_t*)(a.lists + rows * MAX_PARTS * search->beams);
   const cudaStream_t st = (cudaStream_t)stream;
   return dtype == FL_DT_F32 ? launch_step<float>(a, st)
                             : dtype == FL_DT_F16 ? launch_step<__half>(a, st) : launch_step<__nv_bfloat16>(a, st);

@@ -19,13 +19,12 @@
 
 namespace {
 
-constexpr int JOIN_THREADS = 32 * FL_BEAM_MAX;
 constexpr int THREADS = 128, WARPS = THREADS / 32, GROUPS = 32, MAX_PARTS = 32;
 constexpr int PIECES = 8, CHUNK_PIECES = PIECES * THREADS;  // 16-byte pieces of a thread and of a CTA in a chunk
 constexpr int STAGES = 2, CTAS = 6;                          // chunks on their way or in use, CTAs of an SM
-constexpr int MAX_HITS = 256, MAX_ROWS = 512;                // of a CTA
+constexpr int MAX_HITS = 256, MAX_ROWS = 256;                // of a CTA
 constexpr int MAX_SEARCHES = 16384, MAX_VOCAB = 1 << 19;
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 static_assert(FL_BEAM_MAX <= GROUPS && GROUPS == 32);
 
 struct Cand {  // a token and its logit
@@ -39,7 +38,8 @@ struct StepArgs {
   fl_beam_state from, to;
   const void* x;
   int64_t ld;
-  int row_chunks;  // of a row
+  int crowded;  // more than a CTA per SM
+  int row_chunks, usual_parts;  // of a row; parts that a row is cut into at most where all beams are live
   float penalty_hi, penalty_lo;
   int32_t *trace_tokens, *trace_parents, *tokens, *parents;
   float2* sums;  // [row][part] (a logit, sum of exp(x - it))
@@ -132,6 +132,7 @@ FL_DEV Two mul(Two x, Two y) {
   return two_sum(p.hi, __fmaf_rn(x.hi, y.lo, __fmaf_rn(x.lo, y.hi, p.lo)));
 }
 // In the order of the numbers; 0 is below all of them, and of an infinity.
+FL_DEV float unorder32(uint32_t u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
 FL_DEV uint64_t order64(Two x) {
   return fabsf(x.hi) < INFINITY ? (uint64_t)order32(x.hi) << 32 | order32(x.lo) : 0;
 }
@@ -187,29 +188,40 @@ FL_DEV uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-FL_DEV uint64_t mul2(uint64_t a, uint64_t b) {
+FL_DEV uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
 
-// sum of exp(x - ref) over what a thread has seen.  x - ref is taken before the product with log2(e): rounding the product of x itself
-// would be off by the same for every x near ref.
+// sum of exp(x - ref) over what a thread has seen.  The exponents are x log2(e) - c, c = ref log2(e) rounded, one fused
+// operation each; what the rounding of c took (the same factor for all) is given back when ref changes and in the end.  Where ref is so
+// large that this is no small factor, x - ref is taken first.
 struct Sum {
   float ref = -INFINITY;
-  uint64_t minus = 0, sum = 0;  // (-ref, -ref), or zeros where there is no ref yet; sums of every other element
+  uint64_t minus = 0, sum = 0;  // (-c, -c), or (-ref, -ref) where ref is far; sums of every other element
+  FL_DEV bool far() const { return fabsf(ref) > 4096.f; }  // (-inf, before the first x: so that nothing is a NaN)
   FL_DEV void add(float x, float y) {
-    const float2 u = unpack2(mul2(add2(pack2(x, y), minus), pack2(LOG2E, LOG2E)));
+    const float2 u = unpack2(fma2(pack2(x, y), pack2(LOG2E, LOG2E), minus));
     sum = add2(sum, pack2(exp2_hw(u.x), exp2_hw(u.y)));
   }
-  FL_DEV float total() const { return unpack2(sum).x + unpack2(sum).y; }
+  FL_DEV void add_far(float x) {
+    sum = add2(sum, pack2(exp2_hw((x - (ref == -INFINITY ? 0.f : ref)) * LOG2E), 0.f));
+  }
+  FL_DEV float total() const {
+    const float2 u = unpack2(sum);
+    if (far()) return u.x + u.y;
+    const float d = LN2 * fmaf(ref, LOG2E, unpack2(minus).x);  // 2^-12 at most: e^-d from its first terms
+    return (u.x + u.y) * (1.f - d + 0.5f * d * d);
+  }
   // room for x: sums of up to 2^19 exponentials of 16 and less are far from overflow
   FL_DEV void see(float x) {
     if (x > ref + 16.f) {
-      const float f = ref == -INFINITY ? 1.f : exp2_hw((ref - x) * LOG2E);  // (1: nothing so far, or a NaN that stays)
-      sum = mul2(sum, pack2(f, f));
+      const float s = ref == -INFINITY ? total() : total() * exp2_hw((ref - x) * LOG2E);  // (0, or a NaN that stays)
       ref = x;
-      minus = pack2(-x, -x);
+      const float c = far() ? x : x * LOG2E, d = far() ? 0.f : LN2 * fmaf(ref, LOG2E, -c);
+      minus = pack2(-c, -c);
+      sum = pack2(s + s * (d + 0.5f * d * d), 0.f);
     }
   }
 };
@@ -255,27 +267,30 @@ FL_DEV void rest(const StepArgs& a, int s) {
   }
 }
 
-// One search's rows joined, a warp a row.
+// One search's rows joined, a warp a row.  What it reads is asked for at once, before it is known which of it counts.
 template <class T>
-__global__ void __launch_bounds__(JOIN_THREADS) beam_join_kernel(StepArgs a) {
+__global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a) {
   pdl_wait();
   pdl_trigger();
   extern __shared__ __align__(16) char sh_join[];
   Join& j = *reinterpret_cast<Join*>(sh_join);
-  const int B = a.p.beams, s = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int B = a.p.beams, threads = blockDim.x, s = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int t = a.from.steps[s];  // (no read-only loads of the state: `to` may be the same memory)
   const bool active = a.from.done[s] == 0 && t >= 0 && t < a.p.max_steps;
   if (tid == 0) j.few_n = j.any_end = 0;
   if (warp < B) {
     const int b = warp, row = s * B + b;
     const float score = a.from.scores[row];
-    const bool reads = active && score > -INFINITY && score < INFINITY;
-    const int P = reads ? __ldg(a.parts + row) : 0;
+    const int said = __ldg(a.parts + row);
     Cand* mine = reinterpret_cast<Cand*>(&j + 1) + warp * MAX_PARTS * B;
+    const Cand* lists = a.lists + (int64_t)row * MAX_PARTS * B;
     float2 part = __ldg(a.sums + (int64_t)row * MAX_PARTS + lane);  // (of any content behind the parts)
-    if (lane >= P) part = make_float2(-INFINITY, 0.f);
     const float e = a.p.eos >= 0 ? Piece<T>::one(((const T*)a.x)[(int64_t)row * a.ld + a.p.eos]) : -INFINITY;
-    for (int i = lane; i < P * B; i += 32) mine[i] = a.lists[(int64_t)row * MAX_PARTS * B + i];
+    for (int i = lane; i < a.usual_parts * B; i += 32) mine[i] = lists[i];
+    const bool reads = active && score > -INFINITY && score < INFINITY;
+    const int P = reads ? said : 0;
+    for (int i = a.usual_parts * B + lane; i < P * B; i += 32) mine[i] = lists[i];
+    if (lane >= P) part = make_float2(-INFINITY, 0.f);
     float m = part.x;
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
@@ -324,19 +339,19 @@ __global__ void __launch_bounds__(JOIN_THREADS) beam_join_kernel(StepArgs a) {
     return;
   }
   // c = score + ((x - m) - log(sum)): exact for the smallest logits that a type has, too
-  for (int i = tid; i < B * B + B; i += JOIN_THREADS) {
+  for (int i = tid; i < B * B + B; i += threads) {
     const int b = i < B * B ? i / B : i - B * B, k = i % B;
     const float x = i < B * B ? j.best[b][k].x : j.end_x[b];
     const Two c = add(add(two_sum(x, -j.m[b]), j.minus_log[b]), j.from[b]);
     (i < B * B ? j.score[b][k] : j.ends[b]) = x > -INFINITY ? c : Two{-INFINITY, 0.f};
   }
-  if (tid == JOIN_THREADS - 1) j.length = pow_two((float)(t + 1), {a.penalty_hi, a.penalty_lo});
+  if (tid == threads - 1) j.length = pow_two((float)(t + 1), {a.penalty_hi, a.penalty_lo});
   __syncthreads();
   // A row's last candidate bounds the search's last: only what reaches the best of those bounds is ranked, by counting who comes
   // before: by c, then the lower beam, then the order within the beam.
   uint64_t bound = 1;
   for (int b = 0; b < B; ++b) bound = max(bound, order64(j.score[b][B - 1]));
-  for (int i = tid; i < B * B; i += JOIN_THREADS) {
+  for (int i = tid; i < B * B; i += threads) {
     const uint64_t c = order64(j.score[i / B][i % B]);
     if (c >= bound) {
       const int n = atomicAdd(&j.few_n, 1);
@@ -346,7 +361,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) beam_join_kernel(StepArgs a) {
   }
   __syncthreads();
   const int n = j.few_n;
-  for (int i = tid; i < n; i += JOIN_THREADS) {
+  for (int i = tid; i < n; i += threads) {
     const uint64_t c = j.few[i];
     const int at = j.few_at[i];
     int rank = 0;
@@ -357,7 +372,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) beam_join_kernel(StepArgs a) {
       j.live[rank] = j.score[at / B][at % B];
     }
   }
-  const int b = tid - (JOIN_THREADS - 32);  // the hypotheses that end
+  const int b = tid - (threads - 32);  // the hypotheses that end
   if (b >= 0 && b < B) {
     const uint64_t c = order64(j.ends[b]);
     int rank = -1;
@@ -438,12 +453,18 @@ __global__ void __launch_bounds__(JOIN_THREADS) beam_join_kernel(StepArgs a) {
 template <class T>
 __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
   pdl_wait();
-  pdl_trigger();
+  // The join's CTAs may come while this kernel runs only where they find room beside it: else those that finish first would take
+  // them all (1024 x 1 rows of bf16 70 us instead of 62).
+  if (!a.crowded) pdl_trigger();
   using Io = Piece<T>;
   constexpr int N = Io::N;
-  __shared__ __align__(16) float sh_group[2][GROUPS];
+  constexpr int RING = STAGES * CHUNK_PIECES * 16;
+  static_assert(CTAS * (RING + MAX_HITS * sizeof(Cand) + MAX_ROWS * 4 + THREADS * 4 + 4 * GROUPS * 4 + 128 + 1024) <= 228 * 1024,
+                "so many CTAs fit an SM, which keeps 1 KB of each");
+  __shared__ __align__(16) uint32_t sh_group[2][GROUPS], sh_key[2][GROUPS];
   __shared__ float sh_ref[WARPS], sh_sum[WARPS];
   __shared__ int sh_count, sh_warp[WARPS];
+  __shared__ uint32_t sh_bits[THREADS];
   __shared__ int sh_rows[MAX_ROWS];
   __shared__ Cand sh_hits[MAX_HITS];
   extern __shared__ __align__(16) uint4 sh_ring[];  // [STAGES][CHUNK_PIECES]
@@ -493,34 +514,56 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
     ask_chunk();
   }
   cp_async_commit();
-  // the live rows of this CTA's piece: everybody counts those of some rows
-  const int each = (rows + THREADS - 1) / THREADS, r0 = min(rows, tid * each), r1 = min(rows, r0 + each);
-  int count = 0;
+  // which rows are live, a bit each, 32 x THREADS of them at a time; how many, and those of this CTA's piece
+  const auto bits = [&](int base) {
 #pragma unroll 8
-  for (int r = r0; r < r1; ++r) count += live(r);
-  int before = count;
+    for (int r = base + tid; r < min(rows + 31 & ~31, base + 32 * THREADS); r += THREADS) {
+      const bool x = r < rows && live(r);
+      const uint32_t m = __ballot_sync(0xffffffffu, x);
+      if (lane == 0) sh_bits[(r - base) / 32] = m;
+    }
+    __syncthreads();
+  };
+  const int words = min(THREADS, (rows + 31) / 32);
+  int total = 0, before = 0;  // live rows before this thread's 32
+  const auto count = [&](int base) {
+    const int n = base + 32 * tid < rows && tid < words ? __popc(sh_bits[tid]) : 0;
+    before = n;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, before, d);
-    if (lane >= d) before += y;
-  }
-  if (lane == 31) sh_warp[warp] = before;
-  __syncthreads();
-  before -= count;
-  int total = 0;
-  for (int w = 0; w < WARPS; ++w) {
-    if (w == warp) before += total;
-    total += sh_warp[w];
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, before, d);
+      if (lane >= d) before += y;
+    }
+    if (lane == 31) sh_warp[warp] = before;
+    __syncthreads();
+    before += total - n;
+    for (int w = 0; w < WARPS; ++w) {
+      if (w < warp) before += sh_warp[w];
+      total += sh_warp[w];
+    }
+  };
+  for (int base = 0; base < rows; base += 32 * THREADS) {
+    if (base) __syncthreads();
+    bits(base);
+    count(base);
   }
   const bool guessed = total == rows;
   if (!guessed) cut(total);
   const int k0 = c0 / L, k1 = c0 < c1 ? (c1 - 1) / L : -1;  // its first and last live row
-  if (before <= k1 && before + count > k0)
-    for (int r = r0, k = before; r < r1; ++r)
-      if (live(r)) {
-        if (k >= k0 && k <= k1) sh_rows[k - k0] = r;
-        ++k;
-      }
+  const bool again = rows > 32 * THREADS;                   // the bits and counts are those of the last rows only
+  if (again) total = 0;
+  for (int base = 0; base < rows; base += 32 * THREADS) {
+    if (again) {
+      __syncthreads();
+      bits(base);
+      count(base);
+    }
+    if (base + 32 * tid < rows && tid < words) {
+      int k = before;
+      for (uint32_t m = k <= k1 ? sh_bits[tid] : 0; m; m &= m - 1, ++k)
+        if (k >= k0 && k <= k1) sh_rows[k - k0] = base + 32 * tid + __ffs(m) - 1;
+    }
+  }
   __syncthreads();
   if (c0 >= c1) {
     cp_async_wait<0>();
@@ -537,6 +580,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
     cp_async_commit();
   };
   int stage = 0, raised = 0;
+  // with few beams little comes between two raises, so that each costs more than it saves
+  const int often = B > 4 ? ~0 : 0x55555555;
   if (!guessed) {  // the first chunk came for nothing, if one did
     stage = ask_stage = 1;
     ask = c0;
@@ -577,7 +622,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
           const float y = Io::one(*at);
           *at = (T)-INFINITY;
           z.see(y);
-          z.add(y, -INFINITY);
+          if (z.far()) z.add_far(y);
+          else z.add(y, -INFINITY);
         }
         uint4 cur[PIECES];
         uint32_t of_piece[PIECES], of_all = Io::NONE;  // maxima
@@ -591,36 +637,48 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
         const float top = Io::top(of_all);
         most = fmaxf(most, top);
         bool equals = false;  // whether logits equal to the bound count: it is new, and fewer than B larger ones may have been seen
-        if ((chunk & (chunk + 1)) == 0) {
-          // each time that what has been seen doubles: the B-th largest of the groups' maxima, and the largest
+        const int seen = chunk + 1;
+        if ((seen & chunk) == 0 && (seen & often)) {
+          // each time that what has been seen doubles (quadruples): the B-th largest of the groups' maxima, and the largest
           float g = most;
 #pragma unroll
           for (int d = 1; d < THREADS / GROUPS; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
-          float* group = sh_group[raised & 1];
-          ++raised;
-          if (tid % (THREADS / GROUPS) == 0) group[tid / (THREADS / GROUPS)] = g;
+          uint32_t* keys = sh_key[raised & 1];
+          if (tid % (THREADS / GROUPS) == 0) {
+            const int i = tid / (THREADS / GROUPS);
+            sh_group[raised & 1][i] = order32(g);
+            keys[i] = (order32(g) & ~31u) | (31 - i);
+          }
           __syncthreads();
-          g = group[lane];
+          // (numbers that agree in all but their last bits count as equal, the lower group first: the B groups that are taken have
+          // maxima of the bound and more whichever they are)
+          const uint32_t key = keys[lane], ordered = sh_group[raised & 1][lane];
+          ++raised;
           int rank = 0;
 #pragma unroll
           for (int o = 0; o < GROUPS; o += 4) {
-            const float4 y = *reinterpret_cast<const float4*>(group + o);
-            rank += (y.x > g || (y.x == g && o < lane)) + (y.y > g || (y.y == g && o + 1 < lane)) +
-                    (y.z > g || (y.z == g && o + 2 < lane)) + (y.w > g || (y.w == g && o + 3 < lane));
+            const uint4 y = *reinterpret_cast<const uint4*>(keys + o);
+            rank += (y.x > key) + (y.y > key) + (y.z > key) + (y.w > key);
           }
-          const float b = __shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == B - 1)) - 1);
+          const uint32_t low = __reduce_min_sync(0xffffffffu, rank < B ? ordered : 0xffffffffu);
+          const float b = unorder32(low);
           equals = chunk == 0 || b > bound;
           bound = b;
-          z.see(__shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, rank == 0)) - 1));
+          z.see(unorder32(__reduce_max_sync(0xffffffffu, ordered)));
         }
         const bool look = top > -INFINITY && (equals ? top >= bound : top > bound);
         if (look) z.see(top);
+        if (!z.far()) {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-          float f[N];
-          Io::get(cur[i], f);
+          for (int i = 0; i < PIECES; ++i) {
+            float f[N];
+            Io::get(cur[i], f);
 #pragma unroll
-          for (int k = 0; k < N; k += 2) z.add(f[k], f[k + 1]);
+            for (int k = 0; k < N; k += 2) z.add(f[k], f[k + 1]);
+          }
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < PIECES * N; ++i) z.add_far(Io::one(reinterpret_cast<const T*>(places + i / N * THREADS)[i % N]));
         }
         if (look) {
           unsigned which = 0;
@@ -704,6 +762,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
     }
   }
   cp_async_wait<0>();  // (a first chunk that came for nothing)
+  if (a.crowded) pdl_trigger();
 }
 
 int64_t part_bytes(const fl_beam_search* p) {
@@ -740,13 +799,16 @@ int launch_step(StepArgs& a, cudaStream_t st) {
   // as many CTAs as run at once (more where one would have more rows than it keeps), and no more than chunks
   const int64_t slots = std::max(CTAS * fl_sm_count(), (rows + MAX_ROWS - 3) / (MAX_ROWS - 2));
   const int grid = (int)std::min<int64_t>(slots, (int64_t)rows * a.row_chunks);
+  a.crowded = grid > fl_sm_count();
+  a.usual_parts = std::min({MAX_PARTS, a.row_chunks, grid / rows + 2});
   auto kern = beam_step_kernel<T>;
   auto join = beam_join_kernel<T>;
   const auto join_smem = [](int beams) { return (int)sizeof(Join) + beams * MAX_PARTS * beams * (int)sizeof(Cand); };
   FL_CUDA_TRY(fl_func_smem((const void*)kern, ring));
   FL_CUDA_TRY(fl_func_smem((const void*)join, join_smem(FL_BEAM_MAX)));
   FL_CUDA_TRY(fl_launch(kern, dim3(grid), dim3(THREADS), ring, st, a));
-  FL_CUDA_TRY(fl_launch(join, dim3(a.p.n_seqs), dim3(JOIN_THREADS), join_smem(a.p.beams), st, a));
+  // four warps at least: the work behind the rows' is divided among all (1024 x 1 rows of bf16 with one warp 70 us, with four 57, with sixteen 61)
+  FL_CUDA_TRY(fl_launch(join, dim3(a.p.n_seqs), dim3(32 * std::max(4, a.p.beams)), join_smem(a.p.beams), st, a));
   return FL_OK;
 }
 
@@ -912,7 +974,7 @@ extern "C" int fl_k_beam_step(const fl_beam_search* search, const fl_beam_state*
   if (ld < search->vocab || ld % (dtype == FL_DT_F32 ? 4 : 8))
     return fl_internal_error(FL_ERR_UNSUPPORTED, "beam step: row stride %lld (a multiple of 16 bytes, vocab or more)", (long long)ld);
   const float penalty = (float)search->length_penalty;
-  StepArgs a{*search, *from, *to, logits, ld, 0, penalty, (float)(search->length_penalty - penalty), trace_tokens, trace_parents,
+  StepArgs a{*search, *from, *to, logits, ld, 0, 0, 0, penalty, (float)(search->length_penalty - penalty), trace_tokens, trace_parents,
              tokens, parents, nullptr, nullptr, nullptr, status};
   a.sums = (float2*)workspace;
   const int64_t rows = (int64_t)search->n_seqs * search->beams;

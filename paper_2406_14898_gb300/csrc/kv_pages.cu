@@ -1,8 +1,9 @@
 // Sequences that share the pages of a cache: fork (continue, share, copy on write, extend, shorten, leave) and compact.
 //
 // A call is two launches.  The plan is integer work on a few arrays: who has each page after the call, which are free, who
-// gets which.  One CTA does it, or one cluster where the arrays are long, with a barrier between its phases.  The second
-// launch, over the whole GPU, writes the table and copies the pages' tokens in every cache.
+// gets which; it is bound by latency, loads one behind another and barriers.  One CTA does it with its counts in shared memory,
+// or one cluster where the arrays are long, with its counts in global memory.  The second launch, over the whole GPU, writes the table
+// and copies the pages' tokens in every cache.
 #include "../../include/flglm_kernels.h"
 #include "kv_plan.cuh"
 #include "ptx.cuh"
@@ -10,8 +11,10 @@
 namespace {
 
 constexpr int PLAN_THREADS = 1024, MAX_PLAN_CTAS = 8;
-constexpr int COPY_THREADS = 256;
-constexpr int COPY_PIECES = 2048;  // 16-byte pieces of a unit of copying
+constexpr int COPY_WARPS = 4, COPY_THREADS = 32 * COPY_WARPS, COPY_CTAS = 2;  // a CTA, CTAs of an SM
+constexpr int STAGES = 3, BLOCK_BYTES = 8192;  // of a warp: blocks on their way through shared memory
+constexpr int COPY_SMEM = COPY_WARPS * STAGES * BLOCK_BYTES;
+constexpr int UNIT_BYTES = 16384;              // of a whole page that a warp copies at a time
 
 struct PagesDev {
   const int32_t *lens, *table, *refs;
@@ -19,14 +22,15 @@ struct PagesDev {
   int S, n_pages, ps_log2, W;
 };
 
-// A workspace: what the plan tells the second launch, and counts of each page that are zero between calls.
+// A workspace: what the plan tells the second launch, and the cluster's counts of each page, which are zero between calls.
 struct Ws {
-  int32_t* head;                        // copies, refused
-  int4* totals;                         // of each CTA of the plan: pages wanted, copies, free pages, refused
-  int32_t *delta, *writers, *lowest;    // zero between calls: holders more or less, sequences about to write, S - the first
-  int32_t *wanted, *first;              // of each sequence: 2 pages wanted + copied, place of its first in `list`
-  int32_t* list;                        // new pages in the order of their users (fork), free places (compact)
-  int4* copies;                         // page, place of its new page in `list`, tokens
+  int32_t* head;                      // copies, refused
+  int4* totals;                       // of each CTA of the plan: pages wanted, copies, free pages, refused
+  int32_t *delta, *writers, *lowest;  // zero between calls: holders more or less, sequences about to write, S - the first
+  int4* rows;                         // of each sequence: parent, pages shared with it, place of its first new page, pages
+  int32_t* first;                     // of each sequence: its first new page's place in `list`
+  int32_t* list;                      // new pages in the order of their users (fork), free places (compact)
+  int4* copies;                       // page, place of its new page in `list`, tokens
 };
 int64_t align4(int64_t n) { return (n + 3) & ~int64_t(3); }
 int64_t ws_layout(int32_t* base, int64_t S, int64_t n_pages, Ws* w) {
@@ -37,18 +41,13 @@ int64_t ws_layout(int32_t* base, int64_t S, int64_t n_pages, Ws* w) {
   w->lowest = take(n_pages);
   w->head = take(4);
   w->totals = (int4*)take(4 * MAX_PLAN_CTAS);
-  w->wanted = take(S);
+  w->rows = (int4*)take(4 * S);
   w->first = take(S);
   w->list = take(n_pages);
   w->copies = (int4*)take(4 * (S > n_pages ? S : n_pages));
   return at;
 }
 
-// What a call makes of sequence s.
-struct Row {
-  int p, L, L2, held, want;  // parent (-1: none), tokens before and after, their pages
-  int refuse;
-};
 FL_DEV int len_of(const PagesDev& a, int s, int* status) {
   const int64_t cap = (int64_t)a.W << a.ps_log2;
   const int len = __ldg(a.lens + s);
@@ -57,8 +56,15 @@ FL_DEV int len_of(const PagesDev& a, int s, int* status) {
   return L;
 }
 FL_DEV int pages_of(const PagesDev& a, int L) { return (int)(((int64_t)L + (1 << a.ps_log2) - 1) >> a.ps_log2); }
+
+// What a call makes of sequence s.
+struct Row {
+  int p, L, L2, held, want, had;  // parent (-1: none), tokens before and after, their pages; pages that s itself had
+  int refuse, last;               // last: the partly filled page that it is about to write, -1: none
+};
 FL_DEV Row row_of(const PagesDev& a, const int32_t* parents, const int32_t* grow, int s, int* status) {
   Row r;
+  const int own = len_of(a, s, nullptr), more = grow ? __ldg(grow + s) : 0;
   r.p = parents ? __ldg(parents + s) : s;
   r.refuse = 0;
   if (r.p < -1 || r.p >= a.S) {
@@ -66,11 +72,18 @@ FL_DEV Row row_of(const PagesDev& a, const int32_t* parents, const int32_t* grow
     r.p = -1;
   }
   r.L = r.p >= 0 ? len_of(a, r.p, status) : 0;
-  const int64_t L2 = max((int64_t)0, (int64_t)r.L + (grow ? __ldg(grow + s) : 0));
+  const int64_t L2 = max((int64_t)0, (int64_t)r.L + more);
   if (L2 > ((int64_t)a.W << a.ps_log2)) r.refuse |= FL_KV_NO_ROOM;
   r.L2 = (int)min(L2, (int64_t)a.W << a.ps_log2);
   r.held = pages_of(a, r.L);
   r.want = pages_of(a, r.L2);
+  r.had = pages_of(a, own);
+  r.last = -1;
+  if (r.L2 > r.L && (r.L & ((1 << a.ps_log2) - 1))) {
+    const int q = __ldg(a.table + (int64_t)r.p * a.W + r.held - 1);
+    if ((unsigned)q < (unsigned)a.n_pages) r.last = q;
+    else if (status) atomicOr(status, FL_KV_BAD_PAGE);
+  }
   return r;
 }
 
@@ -79,109 +92,144 @@ FL_DEV uint32_t cluster_nctarank() {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
-
 // Exclusive prefix sum of x over the block's threads, and the block's sum.
-template <class T>
-FL_DEV T block_scan(T x, T* sh, T* total) {
+FL_DEV uint64_t block_scan(uint64_t x, uint64_t* sh, uint64_t* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  T v = x;
+  uint64_t v = x;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const T y = __shfl_up_sync(0xffffffffu, v, d);
+    const uint64_t y = __shfl_up_sync(0xffffffffu, v, d);
     if (lane >= d) v += y;
   }
   if (lane == 31) sh[warp] = v;
   __syncthreads();
-  if (warp == 0) {
-    T w = lane < (int)(blockDim.x >> 5) ? sh[lane] : T(0), u = w;
+  uint64_t u = sh[lane], w = u;  // (PLAN_THREADS / 32 = 32 warps: every warp scans their sums)
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const T y = __shfl_up_sync(0xffffffffu, u, d);
-      if (lane >= d) u += y;
-    }
-    sh[lane] = u - w;
-    if (lane == 31) sh[32] = u;
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint64_t y = __shfl_up_sync(0xffffffffu, u, d);
+    if (lane >= d) u += y;
   }
-  __syncthreads();
-  const T before = sh[warp] + v - x;
-  *total = sh[32];
+  *total = __shfl_sync(0xffffffffu, u, 31);
+  const uint64_t before = __shfl_sync(0xffffffffu, u - w, warp) + v - x;
   __syncthreads();
   return before;
 }
 
+// Counts of each page: of the one CTA in shared memory, of a cluster in the workspace.  `have`: holders after the call, but for
+// what new and copied pages change.
+template <bool ONE>
+struct Counts {
+  const PagesDev& a;
+  const Ws& w;
+  int32_t *have, *writing, *lowest;
+  FL_DEV Counts(const PagesDev& a_, const Ws& w_, int32_t* sh) : a(a_), w(w_) {
+    have = ONE ? sh : w.delta;
+    writing = ONE ? sh + a.n_pages : w.writers;
+    lowest = ONE ? sh + 2 * a.n_pages : w.lowest;
+    if (ONE) {
+      for (int q = threadIdx.x; q < a.n_pages; q += PLAN_THREADS) {
+        have[q] = __ldg(a.refs + q);
+        writing[q] = lowest[q] = 0;
+      }
+    }
+  }
+  FL_DEV int holders(int q) const { return ONE ? have[q] : __ldg(a.refs + q) + __ldcg(have + q); }
+  FL_DEV int writers(int q) const { return ONE ? writing[q] : __ldcg(writing + q); }
+  FL_DEV int first_writer(int q) const { return a.S - (ONE ? lowest[q] : __ldcg(lowest + q)); }
+  FL_DEV void clear(int q) const {
+    if (!ONE) have[q] = writing[q] = lowest[q] = 0;
+  }
+};
+
+template <bool ONE>
 __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, const int32_t* parents, const int32_t* grow,
                                                                  Ws w, int* status) {
   pdl_wait();
   pdl_trigger();
-  __shared__ uint64_t sh[33];
-  const int rank = cluster_ctarank(), ctas = cluster_nctarank(), tid = threadIdx.x, lane = tid & 31;
-  const int ps = 1 << a.ps_log2;
+  __shared__ uint64_t sh[32];
+  __shared__ int sh_p[PLAN_THREADS], sh_keep[PLAN_THREADS], sh_had[PLAN_THREADS];
+  extern __shared__ int32_t sh_counts[];
+  const int rank = ONE ? 0 : cluster_ctarank(), ctas = ONE ? 1 : cluster_nctarank(), tid = threadIdx.x, lane = tid & 31;
+  const Counts<ONE> of(a, w, sh_counts);
   // Holders: old rows' pages lose one, new rows' gain one; where both are the same page nothing happens, which is
-  // most of a beam search's rows.
-  for (int s = rank * (PLAN_THREADS / 32) + (tid >> 5); s < a.S; s += ctas * (PLAN_THREADS / 32)) {
-    const Row r = row_of(a, parents, grow, s, nullptr);
-    const int had = pages_of(a, len_of(a, s, nullptr)), keep = min(r.held, r.want);
-    const int32_t *mine = a.table + (int64_t)s * a.W, *theirs = a.table + (int64_t)max(r.p, 0) * a.W;
-    for (int i = (r.p == s ? keep : 0) + lane; i < max(had, keep); i += 32) {
-      const int x = i < keep ? __ldg(theirs + i) : -1, y = i < had ? __ldg(mine + i) : -1;
+  // most of a beam search's rows.  1024 sequences at a time, their entries divided among all threads (or such tiles among the
+  // CTAs, where there are enough).
+  const int tiles = (a.S + PLAN_THREADS - 1) / PLAN_THREADS;
+  const bool share = tiles < ctas;
+  Row mine;  // of sequence tid, kept where there are no more than threads
+  for (int tile = share ? 0 : rank; tile < tiles; tile += share ? 1 : ctas) {
+    const int s0 = tile * PLAN_THREADS, n = min(PLAN_THREADS, a.S - s0);
+    int longest = 0;
+    if (tid < n) {
+      mine = row_of(a, parents, grow, s0 + tid, nullptr);
+      sh_p[tid] = mine.p;
+      sh_keep[tid] = min(mine.held, mine.want);
+      sh_had[tid] = mine.had;
+      longest = mine.p == s0 + tid && sh_keep[tid] == mine.had ? 0 : max(mine.had, sh_keep[tid]);
+    }
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    if (lane == 0) sh[tid >> 5] = longest;
+    __syncthreads();  // (the counts in shared memory are set, too)
+    longest = __reduce_max_sync(0xffffffffu, (int)sh[lane]);
+    if (tid < n && mine.last >= 0 && (!share || rank == 0)) {
+      atomicAdd(of.writing + mine.last, 1);
+      atomicMax(of.lowest + mine.last, a.S - (s0 + tid));
+    }
+    const int64_t all = (int64_t)n * longest;
+    const int step = share ? ctas * PLAN_THREADS : PLAN_THREADS;
+#pragma unroll 4
+    for (int64_t e = (share ? rank * PLAN_THREADS : 0) + tid; e < all; e += step) {
+      const int r = (int)kv_div(e, longest), i = (int)(e - (int64_t)r * longest), p = sh_p[r], keep = sh_keep[r];
+      if (p == s0 + r && i < keep) continue;
+      const int x = i < keep ? __ldg(a.table + (int64_t)p * a.W + i) : -1;
+      const int y = i < sh_had[r] ? __ldg(a.table + (int64_t)(s0 + r) * a.W + i) : -1;
       if (x != y) {
-        if ((unsigned)x < (unsigned)a.n_pages) atomicAdd(w.delta + x, 1);
-        if ((unsigned)y < (unsigned)a.n_pages) atomicSub(w.delta + y, 1);
+        if ((unsigned)x < (unsigned)a.n_pages) atomicAdd(of.have + x, 1);
+        if ((unsigned)y < (unsigned)a.n_pages) atomicSub(of.have + y, 1);
       }
     }
-    if (lane == 0 && r.L2 > r.L && (r.L & (ps - 1))) {
-      const int q = __ldg(theirs + r.held - 1);
-      if ((unsigned)q < (unsigned)a.n_pages) {
-        atomicAdd(w.writers + q, 1);
-        atomicMax(w.lowest + q, a.S - s);
-      }
-    }
+    __syncthreads();
   }
-  cluster_sync();
-  // What each sequence wants, and what is free: this CTA's part of both.
+  if (tiles == 0) __syncthreads();
+  if (!ONE) cluster_sync();
+  // What each sequence wants, and what is free: this CTA's part of both, a warp's pages one after another.
   const int per = (a.S + ctas - 1) / ctas, s0 = min(a.S, rank * per), s1 = min(a.S, s0 + per);
-  const int pper = (a.n_pages + ctas - 1) / ctas, q0 = min(a.n_pages, rank * pper), q1 = min(a.n_pages, q0 + pper);
-  uint64_t sum = 0;  // pages wanted << 32 | copies
+  const int wper = (a.n_pages + ctas * 32 - 1) / (ctas * 32), q0 = min(a.n_pages, (rank * 32 + (tid >> 5)) * wper),
+            q1 = min(a.n_pages, q0 + wper);
+  const auto row = [&](int s) { return ONE && a.S <= PLAN_THREADS ? mine : row_of(a, parents, grow, s, nullptr); };
+  const auto copied = [&](const Row& r, int s) {
+    return r.last >= 0 && !(of.holders(r.last) == of.writers(r.last) && of.first_writer(r.last) == s);
+  };
+  uint64_t sum = 0, total;  // pages wanted << 32 | copies
   int refuse = 0, nfree = 0;
   for (int s = s0 + tid; s < s1; s += PLAN_THREADS) {
-    const Row r = row_of(a, parents, grow, s, status);
+    const Row r = row(s);
     refuse |= r.refuse;
-    int copied = 0;
-    if (r.L2 > r.L && (r.L & (ps - 1))) {
-      const int q = __ldg(a.table + (int64_t)r.p * a.W + r.held - 1);
-      if ((unsigned)q < (unsigned)a.n_pages)
-        copied = !(__ldg(a.refs + q) + __ldcg(w.delta + q) == __ldcg(w.writers + q) && __ldcg(w.lowest + q) == a.S - s);
-      else
-        atomicOr(status, FL_KV_BAD_PAGE);
-    }
-    const int wanted = max(0, r.want - r.held) + copied;
-    w.wanted[s] = 2 * wanted + copied;
-    sum += ((uint64_t)wanted << 32) | copied;
+    const int c = copied(r, s);
+    sum += ((uint64_t)(max(0, r.want - r.held) + c) << 32) | c;
   }
-  for (int q = q0 + tid; q < q1; q += PLAN_THREADS) nfree += __ldg(a.refs + q) + __ldcg(w.delta + q) == 0;
-  uint64_t total, total2;
-  block_scan<uint64_t>(sum, sh, &total);
-  block_scan<uint64_t>(nfree, sh, &total2);
-  refuse = __syncthreads_or(refuse & FL_KV_NO_ROOM) ? FL_KV_NO_ROOM : 0;
-  int bad = 0;
-  for (int s = s0 + tid; s < s1; s += PLAN_THREADS)
-    if (parents) {
-      const int p = __ldg(parents + s);
-      bad |= p < -1 || p >= a.S;
+  for (int q = q0; q < q1; q += 32) nfree += __popc(__ballot_sync(0xffffffffu, q + lane < q1 && of.holders(min(q + lane, a.n_pages - 1)) == 0));
+  const uint64_t rows_before = block_scan(sum, sh, &total);
+  const int my_rows_total_copies = (int)(uint32_t)total;
+  const int64_t my_rows_total = (int64_t)(total >> 32);
+  uint64_t free_total;
+  const uint64_t free_before = block_scan(lane == 0 ? nfree : 0, sh, &free_total);  // (of this warp's first lane)
+  const int no_room = __syncthreads_or(refuse & FL_KV_NO_ROOM), bad_parent = __syncthreads_or(refuse & FL_KV_BAD_PARENT);
+  refuse = (no_room ? FL_KV_NO_ROOM : 0) | (bad_parent ? FL_KV_BAD_PARENT : 0);
+  int64_t all_wanted = my_rows_total, all_free = (int64_t)free_total, wanted0 = 0, free0 = 0;
+  int copies = my_rows_total_copies, copies0 = 0;
+  if (!ONE) {
+    if (tid == 0) __stcg(w.totals + rank, make_int4((int)my_rows_total, my_rows_total_copies, (int)free_total, refuse));
+    cluster_sync();
+    all_wanted = all_free = refuse = copies = 0;
+    for (int c = 0; c < ctas; ++c) {
+      const int4 t = __ldcg(w.totals + c);
+      if (c == rank) wanted0 = all_wanted, free0 = all_free, copies0 = copies;
+      all_wanted += t.x;
+      all_free += t.z;
+      copies += t.y;
+      refuse |= t.w;
     }
-  if (__syncthreads_or(bad)) refuse |= FL_KV_BAD_PARENT;
-  if (tid == 0) __stcg(w.totals + rank, make_int4((int)(total >> 32), (int)(uint32_t)total, (int)total2, refuse));
-  cluster_sync();
-  int64_t all_wanted = 0, all_free = 0, wanted0 = 0, free0 = 0;
-  int copies = 0, copies0 = 0;
-  refuse = 0;
-  for (int c = 0; c < ctas; ++c) {
-    const int4 t = __ldcg(w.totals + c);
-    if (c == rank) wanted0 = all_wanted, free0 = all_free, copies0 = copies;
-    all_wanted += t.x;
-    all_free += t.z;
-    copies += t.y;
-    refuse |= t.w;
   }
   if (all_wanted > all_free) refuse |= FL_KV_NO_ROOM;
   if (rank == 0 && tid == 0) {
@@ -191,83 +239,102 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, con
   }
   for (int base = s0; base < s1; base += PLAN_THREADS) {
     const int s = base + tid;
-    const int x = s < s1 ? w.wanted[s] : 0;
-    const uint64_t before = block_scan<uint64_t>(((uint64_t)(x >> 1) << 32) | (x & 1), sh, &total);
+    Row r;
+    int c = 0;
+    uint64_t x = 0, before = rows_before;
     if (s < s1) {
-      const Row r = row_of(a, parents, grow, s, nullptr);
+      r = row(s);
+      c = copied(r, s);
+      x = ((uint64_t)(max(0, r.want - r.held) + c) << 32) | c;
+    }
+    total = 0;
+    if (s1 - s0 > PLAN_THREADS) before = block_scan(x, sh, &total);  // (else the sums above are these)
+    if (s < s1) {
+      if (r.last < 0 && r.L2 > r.L && (r.L & ((1 << a.ps_log2) - 1))) atomicOr(status, FL_KV_BAD_PAGE);
+      if (r.p >= 0) len_of(a, r.p, status);
       const int at = (int)(wanted0 + (int64_t)(before >> 32));
       w.first[s] = at;
+      w.rows[s] = make_int4(r.p, min(r.held, r.want), r.held - c, r.want);
       a.lens_to[s] = refuse ? __ldg(a.lens + s) : r.L2;
-      if (x & 1)
-        w.copies[copies0 + (int)(uint32_t)before] =
-            make_int4(__ldg(a.table + (int64_t)r.p * a.W + r.held - 1), at, r.L & (ps - 1), 0);
+      if (c) w.copies[copies0 + (int)(uint32_t)before] = make_int4(r.last, at, r.L & ((1 << a.ps_log2) - 1), 0);
     }
     wanted0 += (int64_t)(total >> 32);
     copies0 += (int)(uint32_t)total;
   }
-  for (int base = q0; base < q1; base += PLAN_THREADS) {
-    const int q = base + tid;
-    int pre = -1, writers = 0;
-    if (q < q1) {
-      pre = __ldg(a.refs + q) + __ldcg(w.delta + q);
-      writers = __ldcg(w.writers + q);
+  int64_t at = free0 + (int64_t)__shfl_sync(0xffffffffu, free_before, 0);
+  for (int q = q0; q < q1; q += 32) {
+    const bool in = q + lane < q1;
+    const int x = min(q + lane, a.n_pages - 1), have = of.holders(x), writers = of.writers(x);
+    const unsigned m = __ballot_sync(0xffffffffu, in && have == 0);
+    if (in) {
+      const int64_t mine_at = at + __popc(m & ((1u << lane) - 1));
+      const bool taken = have == 0 && mine_at < all_wanted;
+      if (taken && !refuse) w.list[mine_at] = x;
+      const int leave = writers == 0 ? 0 : have == writers ? writers - 1 : writers;
+      a.refs_to[x] = refuse ? __ldg(a.refs + x) : taken ? 1 : have - leave;
     }
-    const uint64_t before = block_scan<uint64_t>(pre == 0, sh, &total);
-    if (q < q1) {
-      const int64_t at = free0 + (int64_t)before;
-      const bool taken = pre == 0 && at < all_wanted;
-      if (taken && !refuse) w.list[at] = q;
-      const int leave = writers == 0 ? 0 : pre == writers ? writers - 1 : writers;
-      a.refs_to[q] = refuse ? __ldg(a.refs + q) : taken ? 1 : pre - leave;
-      w.delta[q] = w.writers[q] = w.lowest[q] = 0;
-    }
-    free0 += (int64_t)total;
+    at += __popc(m);
+  }
+  if (!ONE) {
+    cluster_sync();  // nobody looks at the counts any more
+    for (int q = q0 + lane; q < q1; q += 32) of.clear(q);
   }
 }
 
+template <bool ONE>
 __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, int32_t* moved, int32_t* used, Ws w) {
   pdl_wait();
   pdl_trigger();
-  __shared__ uint64_t sh[33];
-  const int rank = cluster_ctarank(), ctas = cluster_nctarank(), tid = threadIdx.x;
-  const int pper = (a.n_pages + ctas - 1) / ctas, q0 = min(a.n_pages, rank * pper), q1 = min(a.n_pages, q0 + pper);
-  uint64_t total, n = 0;
-  for (int q = q0 + tid; q < q1; q += PLAN_THREADS) n += __ldg(a.refs + q) > 0;
-  block_scan<uint64_t>(n, sh, &total);
-  if (tid == 0) __stcg(&w.totals[rank].x, (int)total);
-  cluster_sync();
-  int all = 0, before0 = 0;
-  for (int c = 0; c < ctas; ++c) {
-    if (c == rank) before0 = all;
-    all += __ldcg(&w.totals[c].x);
+  __shared__ uint64_t sh[32];
+  const int rank = ONE ? 0 : cluster_ctarank(), ctas = ONE ? 1 : cluster_nctarank(), tid = threadIdx.x, lane = tid & 31;
+  // a warp's pages one after another
+  const int wper = (a.n_pages + ctas * 32 - 1) / (ctas * 32), q0 = min(a.n_pages, (rank * 32 + (tid >> 5)) * wper),
+            q1 = min(a.n_pages, q0 + wper);
+  const auto busy = [&](int q) { return __ballot_sync(0xffffffffu, q + lane < q1 && __ldg(a.refs + min(q + lane, a.n_pages - 1)) > 0); };
+  uint64_t total;
+  int n = 0;
+  for (int q = q0; q < q1; q += 32) n += __popc(busy(q));
+  int before = (int)block_scan(lane == 0 ? n : 0, sh, &total), all = (int)total;
+  before = __shfl_sync(0xffffffffu, before, 0);
+  if (!ONE) {
+    if (tid == 0) __stcg(&w.totals[rank].x, (int)total);
+    cluster_sync();
+    all = 0;
+    for (int c = 0; c < ctas; ++c) {
+      if (c == rank) before += all;
+      all += __ldcg(&w.totals[c].x);
+    }
   }
-  // pages in use among the first `all`: those that stay
-  const int edge = pper > 0 ? min(ctas - 1, all / pper) : 0;
-  int stay = 0;
-  for (int c = 0; c < edge; ++c) stay += __ldcg(&w.totals[c].x);
+  // the pages in use among the first `all` stay
   n = 0;
-  for (int q = edge * pper + tid; q < all; q += PLAN_THREADS) n += __ldg(a.refs + q) > 0;
-  block_scan<uint64_t>(n, sh, &total);
-  stay += (int)total;
+  for (int q = q0; q < min(q1, all); q += 32) n += __popc(busy(q) & (all - q >= 32 ? ~0u : (1u << (all - q)) - 1));
+  block_scan(lane == 0 ? n : 0, sh, &total);
+  int stay = (int)total;
+  if (!ONE) {
+    if (tid == 0) __stcg(&w.totals[rank].y, stay);
+    cluster_sync();
+    stay = 0;
+    for (int c = 0; c < ctas; ++c) stay += __ldcg(&w.totals[c].y);
+  }
   const int moves = all - stay;
   if (rank == 0 && tid == 0) {
     w.head[0] = moves;
     w.head[1] = 0;
     *used = all;
   }
-  for (int base = q0; base < q1; base += PLAN_THREADS) {
-    const int q = base + tid;
-    const bool busy = q < q1 && __ldg(a.refs + q) > 0;
-    const int before = before0 + (int)block_scan<uint64_t>(busy, sh, &total);
-    if (q < q1) {
-      if (q < all && !busy) w.list[q - before] = q;
-      if (q >= all && busy) w.copies[before - stay] = make_int4(q, before - stay, 1 << a.ps_log2, 0);
+  for (int q = q0; q < q1; q += 32) {
+    const unsigned m = busy(q), bit = 1u << lane;
+    const int x = q + lane, ahead = before + __popc(m & (bit - 1));
+    if (x < q1) {
+      if (x < all && !(m & bit)) __stcg(w.list + (x - ahead), x);
+      if (x >= all && (m & bit)) __stcg(w.copies + (ahead - stay), make_int4(x, ahead - stay, 1 << a.ps_log2, 0));
     }
-    before0 += (int)total;
+    before += __popc(m);
   }
   for (int s = rank * PLAN_THREADS + tid; s < a.S; s += ctas * PLAN_THREADS) a.lens_to[s] = __ldg(a.lens + s);
-  cluster_sync();
-  for (int q = q0 + tid; q < q1; q += PLAN_THREADS) {
+  if (ONE) __syncthreads();
+  else cluster_sync();
+  for (int q = q0 + lane; q < q1; q += 32) {
     const int refs = __ldg(a.refs + q);
     if (refs > 0 && q < all) {
       moved[q] = q;
@@ -287,78 +354,141 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, 
 }
 
 struct Caches {
-  uint4* at[2 * FL_KV_MAX_CACHES];  // keys and values of each
-  int n, heads, row;                // arrays, heads, 16-byte pieces of a row
-  int64_t page_stride, head_stride, token_stride;  // in pieces
+  char* at[2 * FL_KV_MAX_CACHES];  // keys and values of each
+  int n, units;                    // arrays; units of a page
+  int heads, row, by_token;        // bytes of a token's head; whether a token's heads lie next to each other
+  int64_t page_stride, head_stride, token_stride;  // in bytes
 };
+FL_DEV int64_t shfl64(int64_t x, int lane) { return __shfl_sync(0xffffffffu, x, lane); }
 
-FL_DEV void copy_pages(const Caches& c, const Ws& w, int ps_log2) {
-  const int copies = __ldcg(w.head);
-  const int row_log2 = 31 - __clz(c.row);
-  const int units = (int)((((int64_t)c.heads * c.row << ps_log2) + COPY_PIECES - 1) / COPY_PIECES);  // of a whole page
-  const bool heads_outer = c.head_stride >= c.token_stride;
-  const int64_t all = (int64_t)copies * c.n * units;
-  for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
-    const int part = (int)(u % units);
-    const int64_t x = u / units;
-    const int4 job = __ldcg(w.copies + x / c.n);
-    uint4* base = c.at[x % c.n];
-    const int dst = __ldcg(w.list + job.y), pieces = job.z * c.heads * c.row;
-    const uint4* from = base + job.x * c.page_stride;
-    uint4* to = base + dst * c.page_stride;
-    const int inner = heads_outer ? job.z : c.heads;
-    uint4 v[COPY_PIECES / COPY_THREADS];
-    int64_t off[COPY_PIECES / COPY_THREADS];
-#pragma unroll
-    for (int i = 0; i < COPY_PIECES / COPY_THREADS; ++i) {
-      const int k = part * COPY_PIECES + i * COPY_THREADS + threadIdx.x;
-      off[i] = -1;
-      if (k < pieces) {
-        const unsigned r = (unsigned)k >> row_log2, o = r / (unsigned)inner, j = r % (unsigned)inner;
-        off[i] = (int64_t)o * (heads_outer ? c.head_stride : c.token_stride) +
-                 (int64_t)j * (heads_outer ? c.token_stride : c.head_stride) + (k & (c.row - 1));
-        v[i] = __ldcs(from + off[i]);
+// The copies, a warp a unit: from global memory into the warp's shared memory and from there to the new page, in
+// blocks of 8 KB by bulk copies that one lane asks for, two loads ahead of a store.  What a page holds of its sequence is
+// `runs` stretches of memory; each of its units has an equal part of their bytes, so that all are as long.
+// HBM is the bound: TODO.
+FL_DEV void copy_pages(const Caches& c, const Ws& w, int ps_log2, char* ring, uint64_t* full, int* status) {
+  const int lane = threadIdx.x & 31, warps = gridDim.x * COPY_WARPS;
+  const int64_t all = (int64_t)__ldcg(w.head) * c.n * c.units;
+  int issued = 0, stored = 0;  // blocks
+  bool ok = true;
+  static_assert(STAGES == 3);
+  int64_t to0 = 0, to1 = 0;  // of the blocks on their way, the first and the second
+  int bytes0 = 0, bytes1 = 0;
+  const auto store = [&] {  // the first block on its way
+    const int st = stored % STAGES;
+    ok = mbar_wait(full + st, stored / STAGES & 1);
+    if (!ok) return;
+    bulk_store((char*)to0, ring + st * BLOCK_BYTES, bytes0);
+    bulk_commit();
+    ++stored;
+    to0 = to1, bytes0 = bytes1;
+  };
+  for (int64_t u0 = (int64_t)threadIdx.x / 32 * gridDim.x + blockIdx.x; u0 < all; u0 += 32ll * warps) {
+    // 32 units at once, one a lane: where from, where to, how much
+    const int64_t u = u0 + (int64_t)lane * warps;
+    int64_t from = 0, to = 0;
+    int begin = 0, end = 0, run = 1, inner = 1;  // the unit's part of the runs' bytes; bytes of a run, runs of an inner row of them
+    if (u < all) {
+      const int64_t x = kv_div(u, c.units), job_at = kv_div(x, c.n);
+      const int part = (int)(u - x * c.units);
+      const int4 job = __ldcg(w.copies + job_at);
+      const int64_t base = (int64_t)c.at[x - job_at * c.n];
+      from = base + job.x * c.page_stride;
+      to = base + (int64_t)__ldcg(w.list + job.y) * c.page_stride;
+      const int bytes = job.z * c.heads * c.row;
+      if (c.by_token) {  // a token's heads lie next to each other, or a head's tokens do, or neither
+        run = c.token_stride == (int64_t)c.heads * c.row ? bytes : c.heads * c.row;
+      } else if (c.token_stride == c.row) {
+        run = job.z == 1 << ps_log2 && c.head_stride == (int64_t)c.row << ps_log2 ? bytes : job.z * c.row;
+      } else {
+        run = c.row;
+        inner = job.z;
+      }
+      begin = (int)((int64_t)bytes / 16 * part / c.units) * 16;
+      end = (int)((int64_t)bytes / 16 * (part + 1) / c.units) * 16;
+    }
+    for (int l = 0; l < 32 && u0 + (int64_t)l * warps < all; ++l) {
+      const int64_t f = shfl64(from, l), t = shfl64(to, l);
+      const int b = __shfl_sync(0xffffffffu, begin, l), e = __shfl_sync(0xffffffffu, end, l), r = __shfl_sync(0xffffffffu, run, l),
+                in = __shfl_sync(0xffffffffu, inner, l);
+      if (lane == 0) {
+        const int64_t outer = c.by_token ? c.token_stride : c.head_stride;
+        int off = b % r, j = b / r % in;
+        int64_t row = (int64_t)(b / r / in) * outer, col = j * c.token_stride;
+        for (int at = b; at < e && ok;) {
+          const int n = min(BLOCK_BYTES, min(r - off, e - at)), st = issued % STAGES;
+          if (issued - stored == STAGES - 1) store();
+          if (!ok) break;
+          if (issued >= STAGES) bulk_wait_read<1>();  // the store before the last one is through with this stage
+          (issued == stored ? to0 : to1) = t + row + col + off;
+          (issued == stored ? bytes0 : bytes1) = n;
+          mbar_arrive_expect_tx(full + st, n);
+          bulk_load(ring + st * BLOCK_BYTES, (const char*)(f + row + col + off), n, full + st);
+          ++issued;
+          at += n;
+          off += n;
+          if (off == r) {
+            off = 0;
+            col += c.token_stride;
+            if (++j == in) j = 0, col = 0, row += outer;
+          }
+        }
       }
     }
-#pragma unroll
-    for (int i = 0; i < COPY_PIECES / COPY_THREADS; ++i)
-      if (off[i] >= 0) to[off[i]] = v[i];
+  }
+  if (lane == 0) {
+    while (ok && stored < issued) store();
+    if (!ok) {
+      atomicOr(status, FL_KV_TIMEOUT);
+      for (int i = stored; i < issued; ++i) mbar_wait(full + i % STAGES, i / STAGES & 1);  // what is still on its way
+    }
+    bulk_wait_all();
   }
 }
 
-// The rows of the new table, in pieces of a block's threads each.
+// The rows of the new table, in pieces of a block's threads each, from the last CTA on: the first ones begin with the copies.
 template <class F>
 FL_DEV void for_entries(const PagesDev& a, F f) {
   const int per = (a.W + COPY_THREADS - 1) / COPY_THREADS;
-  for (int64_t u = blockIdx.x; u < (int64_t)a.S * per; u += gridDim.x) {
-    const int s = (int)(u / per), i = (int)(u % per) * COPY_THREADS + threadIdx.x;
+  for (int64_t u = gridDim.x - 1 - blockIdx.x; u < (int64_t)a.S * per; u += gridDim.x) {
+    const int s = (int)kv_div(u, per), i = (int)(u - (int64_t)s * per) * COPY_THREADS + threadIdx.x;
     if (i < a.W) f(s, i);
   }
 }
 
-__global__ void __launch_bounds__(COPY_THREADS) fork_kernel(PagesDev a, const int32_t* parents, const int32_t* grow, Ws w,
-                                                            const __grid_constant__ Caches c, int* status) {
+// Every warp's ring and barriers.
+FL_DEV void copy_all(const Caches& c, const Ws& w, int ps_log2, int* status) {
+  extern __shared__ __align__(128) char ring[];
+  __shared__ uint64_t full[COPY_WARPS][STAGES];
+  const int warp = threadIdx.x >> 5;
+  if ((threadIdx.x & 31) == 0) {
+    for (int i = 0; i < STAGES; ++i) mbar_init(&full[warp][i], 1);
+    fence_mbar_init();
+    fence_proxy_async_smem();
+  }
+  __syncwarp();
+  copy_pages(c, w, ps_log2, ring + warp * STAGES * BLOCK_BYTES, full[warp], status);
+}
+
+__global__ void __launch_bounds__(COPY_THREADS) fork_kernel(PagesDev a, Ws w, const __grid_constant__ Caches c, int* status) {
   pdl_wait();
   pdl_trigger();
   const bool refused = __ldcg(w.head + 1) != 0;
   for_entries(a, [&](int s, int i) {
     const int64_t e = (int64_t)s * a.W + i;
-    if (refused) {
-      a.table_to[e] = __ldg(a.table + e);
-      return;
-    }
-    const Row r = row_of(a, parents, grow, s, nullptr);
-    const int start = r.held - (__ldcg(w.wanted + s) & 1);
+    const int4 r = __ldcg(w.rows + s);
+    const int first = __ldcg(w.first + s);
     int page = -1;
-    if (i >= start && i < r.want) {
-      page = __ldcg(w.list + __ldcg(w.first + s) + i - start);
-    } else if (i < min(r.held, r.want)) {
-      page = __ldg(a.table + (int64_t)r.p * a.W + i);
+    if (refused) {
+      page = __ldg(a.table + e);
+    } else if (i >= r.z && i < r.w) {
+      page = __ldcg(w.list + first + i - r.z);
+    } else if (i < r.y) {
+      page = __ldg(a.table + (int64_t)r.x * a.W + i);
       if ((unsigned)page >= (unsigned)a.n_pages) atomicOr(status, FL_KV_BAD_PAGE);
     }
     a.table_to[e] = page;
   });
-  copy_pages(c, w, a.ps_log2);
+  copy_all(c, w, a.ps_log2, status);
 }
 
 __global__ void __launch_bounds__(COPY_THREADS) compact_kernel(PagesDev a, const int32_t* moved, Ws w,
@@ -375,7 +505,7 @@ __global__ void __launch_bounds__(COPY_THREADS) compact_kernel(PagesDev a, const
     }
     a.table_to[e] = page;
   });
-  copy_pages(c, w, a.ps_log2);
+  copy_all(c, w, a.ps_log2, status);
 }
 
 int check_pages(const char* who, const fl_kv_pages* p, PagesDev* out) {
@@ -419,17 +549,19 @@ int check_call(const char* who, const fl_kv_cache* caches, int n, const fl_kv_pa
     if (x.dtype != y.dtype || x.kv_heads != y.kv_heads || x.head_dim != y.head_dim || x.page_stride != y.page_stride ||
         x.head_stride != y.head_stride || x.token_stride != y.token_stride)
       return fl_internal_error(FL_ERR_INVALID_ARG, "%s: caches 0 and %d are not alike", who, i);
-    c->at[2 * i] = (uint4*)x.k;
-    c->at[2 * i + 1] = (uint4*)x.v;
+    c->at[2 * i] = (char*)x.k;
+    c->at[2 * i + 1] = (char*)x.v;
   }
   c->n = 2 * n;
   c->heads = caches[0].kv_heads;
-  c->row = caches[0].head_dim / 8;
-  if (((int64_t)c->heads * c->row << a->ps_log2) >= 1ll << 31)
-    return fl_internal_error(FL_ERR_CAPACITY, "%s: a page of %d heads", who, c->heads);
-  c->page_stride = caches[0].page_stride / 8;
-  c->head_stride = caches[0].head_stride / 8;
-  c->token_stride = caches[0].token_stride / 8;
+  c->row = caches[0].head_dim * 2;
+  const int64_t page = (int64_t)c->heads * c->row << a->ps_log2;
+  if (page >= 1ll << 31) return fl_internal_error(FL_ERR_CAPACITY, "%s: a page of %d heads", who, c->heads);
+  c->units = (int)((page + UNIT_BYTES - 1) / UNIT_BYTES);
+  c->page_stride = caches[0].page_stride * 2;
+  c->head_stride = caches[0].head_stride * 2;
+  c->token_stride = caches[0].token_stride * 2;
+  c->by_token = c->token_stride != c->row && c->head_stride == c->row;
   a->lens_to = to->lens;
   a->table_to = to->table;
   a->refs_to = to->refs;
@@ -438,7 +570,7 @@ int check_call(const char* who, const fl_kv_cache* caches, int n, const fl_kv_pa
 }
 
 template <typename... KArgs, typename... Args>
-cudaError_t launch_plan(void (*kern)(KArgs...), int ctas, cudaStream_t st, Args&&... args) {
+cudaError_t launch_plan(void (*kern)(KArgs...), int ctas, int smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see pdl_wait
@@ -448,13 +580,15 @@ cudaError_t launch_plan(void (*kern)(KArgs...), int ctas, cudaStream_t st, Args&
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(PLAN_THREADS);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
-int plan_ctas(const PagesDev& a) { return (int64_t)a.S * a.W + a.n_pages > 16384 ? MAX_PLAN_CTAS : 1; }
+// One CTA as long as what it goes through is short.
+bool small_plan(const PagesDev& a) { return a.n_pages <= 16384 && (int64_t)a.S * a.W <= 65536 && a.S <= PLAN_THREADS; }
 
 }  // namespace
 
@@ -473,8 +607,14 @@ extern "C" int fl_k_kv_fork(const fl_kv_cache* caches, int32_t n_caches, const f
   if (int rc = check_call("kv fork", caches, n_caches, from, to, workspace, status, &a, &c, &w)) return rc;
   if (fl_misaligned(parents, 4) || fl_misaligned(new_tokens, 4)) return fl_internal_error(FL_ERR_INVALID_ARG, "kv fork: alignment");
   const cudaStream_t st = (cudaStream_t)stream;
-  FL_CUDA_TRY(launch_plan(fork_plan_kernel, plan_ctas(a), st, a, parents, new_tokens, w, status));
-  FL_CUDA_TRY(fl_launch(fork_kernel, dim3(4 * fl_sm_count()), dim3(COPY_THREADS), 0, st, a, parents, new_tokens, w, c, status));
+  if (small_plan(a)) {
+    FL_CUDA_TRY(fl_func_smem((const void*)fork_plan_kernel<true>, 3 * 16384 * 4));
+    FL_CUDA_TRY(launch_plan(fork_plan_kernel<true>, 1, 12 * a.n_pages, st, a, parents, new_tokens, w, status));
+  } else {
+    FL_CUDA_TRY(launch_plan(fork_plan_kernel<false>, MAX_PLAN_CTAS, 0, st, a, parents, new_tokens, w, status));
+  }
+  FL_CUDA_TRY(fl_func_smem((const void*)fork_kernel, COPY_SMEM));
+  FL_CUDA_TRY(fl_launch(fork_kernel, dim3(COPY_CTAS * fl_sm_count()), dim3(COPY_THREADS), COPY_SMEM, st, a, w, c, status));
   return FL_OK;
 }
 
@@ -487,7 +627,11 @@ extern "C" int fl_k_kv_compact(const fl_kv_cache* caches, int32_t n_caches, cons
   if (!moved || !used || fl_misaligned(moved, 4) || fl_misaligned(used, 4))
     return fl_internal_error(FL_ERR_INVALID_ARG, "kv compact: args");
   const cudaStream_t st = (cudaStream_t)stream;
-  FL_CUDA_TRY(launch_plan(compact_plan_kernel, plan_ctas(a), st, a, moved, used, w));
-  FL_CUDA_TRY(fl_launch(compact_kernel, dim3(4 * fl_sm_count()), dim3(COPY_THREADS), 0, st, a, moved, w, c, status));
+  if (a.n_pages <= 16384)
+    FL_CUDA_TRY(launch_plan(compact_plan_kernel<true>, 1, 0, st, a, moved, used, w));
+  else
+    FL_CUDA_TRY(launch_plan(compact_plan_kernel<false>, MAX_PLAN_CTAS, 0, st, a, moved, used, w));
+  FL_CUDA_TRY(fl_func_smem((const void*)compact_kernel, COPY_SMEM));
+  FL_CUDA_TRY(fl_launch(compact_kernel, dim3(COPY_CTAS * fl_sm_count()), dim3(COPY_THREADS), COPY_SMEM, st, a, moved, w, c, status));
   return FL_OK;
 }

@@ -97,6 +97,13 @@ FL_DEV void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar)
       : "memory");
 }
 
+// Untiled bulk copy of `bytes` from this CTA's shared memory to global (bulk-group completion); the same alignment.
+FL_DEV void bulk_store(void* dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(reinterpret_cast<uint64_t>(dst)),
+               "r"(smem_u32(src)), "r"(bytes)
+               : "memory");
+}
+
 // ------------------------------------------------------------------ tcgen05
 FL_DEV void tmem_alloc(uint32_t* dst, uint32_t ncols) {
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)),

@@ -54,8 +54,8 @@ def test_a_place_is_read_before_it_is_asked_for_again():
 def test_plan_phases_are_divided_by_the_clusters_barrier():
     src = _code("kv_pages.cu")
     fork = src[src.index("fork_plan_kernel("):src.index("compact_plan_kernel(")]
-    _in_order(fork, "atomicMax(w.lowest", "cluster_sync()", "__ldcg(w.lowest + q)", "__stcg(w.totals", "cluster_sync()",
-              "__ldcg(w.totals", "w.delta[q] = w.writers[q] = w.lowest[q] = 0")
+    _in_order(fork, "atomicMax(of.lowest", "cluster_sync()", "of.first_writer(r.last)", "__stcg(w.totals", "cluster_sync()",
+              "__ldcg(w.totals", "cluster_sync()", "of.clear(q)")
     compact = src[src.index("compact_plan_kernel("):src.index("struct Caches")]
-    _in_order(compact, "__stcg(&w.totals", "cluster_sync()", "__ldcg(&w.totals", "w.list[q - before] = q", "cluster_sync()",
-              "__ldcg(w.list + i)")
+    _in_order(compact, "__stcg(&w.totals[rank].x", "cluster_sync()", "__ldcg(&w.totals[c].x", "__stcg(&w.totals[rank].y", "cluster_sync()",
+              "__ldcg(&w.totals[c].y", "__stcg(w.list", "cluster_sync()", "__ldcg(w.list + i)")

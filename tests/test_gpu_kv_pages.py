@@ -200,6 +200,48 @@ def test_compact(F, n_pages, busy, page, heads, hd, dtype, token_major):
     assert pool.get(0) == pool.get(1)
 
 
+@pytest.mark.parametrize("heads,hd,page,pad_heads,pad_tokens,token_major", [(3, 64, 16, 8, 0, False), (2, 128, 64, 0, 8, False),
+                                                                             (4, 64, 32, 0, 16, True), (5, 128, 16, 8, 24, True)])
+def test_caches_with_gaps(F, heads, hd, page, pad_heads, pad_tokens, token_major):
+    """Heads and tokens that do not lie next to each other; what lies between them is left alone."""
+    rng = random.Random(heads)
+    S, n_pages, W = 6, 30, 4
+    pool = Pool(F, S, n_pages, page, W, 1, heads, hd)
+    if token_major:
+        head, token = hd + pad_heads, heads * (hd + pad_heads) + pad_tokens
+        each = -(-page * token // head) * head
+    else:
+        token = hd + pad_tokens
+        head = page * token + pad_heads
+        each = heads * head
+    raw = [torch.randint(-30000, 30000, (n_pages * each,), device="cuda", dtype=torch.int16) for _ in "kv"]
+    pool.caches = F.kv_caches([F.kv_cache(*raw, n_pages, page, heads, hd, page_stride=each, head_stride=head, token_stride=token)])
+    views = [x.as_strided((n_pages, page, heads, hd), (each, token, head, 1)) for x in raw]
+    pool.fork(None, [3 * page - 2, 5, 0, 0, page, 1])
+    side = 1
+    for t in range(6):
+        parents = [rng.randrange(S) for _ in range(S)]
+        lens, table, refs = pool.get(side)
+        want = fork(lens, table, refs, page, parents, [1] * S)
+        before = [x.clone() for x in raw]
+        pool.fork(parents, [1] * S, side)
+        side = 1 - side
+        for x, v, b in zip(raw, views, before):
+            expect = b.as_strided(v.shape, v.stride())
+            for a, d, n in want[3]:
+                expect[d, :n] = v[a, :n]
+            assert torch.equal(x, b)
+        assert pool.get(side) == list(want[:3]) and int(pool.status.item()) == 0
+    lens, table, refs = pool.get(side)
+    before = [x.clone() for x in raw]
+    pool.compact(side=side)
+    for x, v, b in zip(raw, views, before):
+        expect = b.as_strided(v.shape, v.stride())
+        for a, d, n in compact(lens, table, refs, page)[4]:
+            expect[d] = v[a]
+        assert torch.equal(x, b)
+
+
 def test_no_sequences(F):
     pool = Pool(F, 0, 5, 16, 2)
     pool.sides[0]["refs"].copy_(torch.tensor([0, 1, 0, 0, 2]))

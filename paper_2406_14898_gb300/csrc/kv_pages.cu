@@ -48,11 +48,9 @@ int64_t ws_layout(int32_t* base, int64_t S, int64_t n_pages, Ws* w) {
   return at;
 }
 
-FL_DEV int len_of(const PagesDev& a, int s, int* status) {
-  const int64_t cap = (int64_t)a.W << a.ps_log2;
-  const int len = __ldg(a.lens + s);
-  const int L = (int)min((int64_t)max(len, 0), cap);
-  if (L != len && status) atomicOr(status, FL_KV_BAD_PAGE);
+FL_DEV int len_of(const PagesDev& a, int s, bool* bad = nullptr) {
+  const int len = __ldg(a.lens + s), L = (int)min((int64_t)max(len, 0), (int64_t)a.W << a.ps_log2);
+  if (L != len && bad) *bad = true;
   return L;
 }
 FL_DEV int pages_of(const PagesDev& a, int L) { return (int)(((int64_t)L + (1 << a.ps_log2) - 1) >> a.ps_log2); }
@@ -61,17 +59,19 @@ FL_DEV int pages_of(const PagesDev& a, int L) { return (int)(((int64_t)L + (1 <<
 struct Row {
   int p, L, L2, held, want, had;  // parent (-1: none), tokens before and after, their pages; pages that s itself had
   int refuse, last;               // last: the partly filled page that it is about to write, -1: none
+  bool bad;                       // a length or that page out of range
 };
-FL_DEV Row row_of(const PagesDev& a, const int32_t* parents, const int32_t* grow, int s, int* status) {
+FL_DEV Row row_of(const PagesDev& a, const int32_t* parents, const int32_t* grow, int s) {
   Row r;
-  const int own = len_of(a, s, nullptr), more = grow ? __ldg(grow + s) : 0;
+  const int own = len_of(a, s), more = grow ? __ldg(grow + s) : 0;
   r.p = parents ? __ldg(parents + s) : s;
   r.refuse = 0;
+  r.bad = false;
   if (r.p < -1 || r.p >= a.S) {
     r.refuse = FL_KV_BAD_PARENT;
     r.p = -1;
   }
-  r.L = r.p >= 0 ? len_of(a, r.p, status) : 0;
+  r.L = r.p >= 0 ? len_of(a, r.p, &r.bad) : 0;
   const int64_t L2 = max((int64_t)0, (int64_t)r.L + more);
   if (L2 > ((int64_t)a.W << a.ps_log2)) r.refuse |= FL_KV_NO_ROOM;
   r.L2 = (int)min(L2, (int64_t)a.W << a.ps_log2);
@@ -82,7 +82,7 @@ FL_DEV Row row_of(const PagesDev& a, const int32_t* parents, const int32_t* grow
   if (r.L2 > r.L && (r.L & ((1 << a.ps_log2) - 1))) {
     const int q = __ldg(a.table + (int64_t)r.p * a.W + r.held - 1);
     if ((unsigned)q < (unsigned)a.n_pages) r.last = q;
-    else if (status) atomicOr(status, FL_KV_BAD_PAGE);
+    else r.bad = true;
   }
   return r;
 }
@@ -92,25 +92,32 @@ FL_DEV uint32_t cluster_nctarank() {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
-// Exclusive prefix sum of x over the block's threads, and the block's sum.
-FL_DEV uint64_t block_scan(uint64_t x, uint64_t* sh, uint64_t* total) {
+// Exclusive prefix sums of x and y over the block's threads, and the block's sums.
+struct Pair {
+  uint64_t x;
+  uint32_t y;
+};
+FL_DEV Pair block_scan(Pair v, Pair* sh, Pair* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint64_t v = x;
+  const auto scan = [&](Pair& u) {
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const uint64_t y = __shfl_up_sync(0xffffffffu, v, d);
-    if (lane >= d) v += y;
-  }
-  if (lane == 31) sh[warp] = v;
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint64_t x = __shfl_up_sync(0xffffffffu, u.x, d);
+      const uint32_t y = __shfl_up_sync(0xffffffffu, u.y, d);
+      if (lane >= d) u.x += x, u.y += y;
+    }
+  };
+  Pair up = v;
+  scan(up);
+  if (lane == 31) sh[warp] = up;
   __syncthreads();
-  uint64_t u = sh[lane], w = u;  // (PLAN_THREADS / 32 = 32 warps: every warp scans their sums)
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const uint64_t y = __shfl_up_sync(0xffffffffu, u, d);
-    if (lane >= d) u += y;
-  }
-  *total = __shfl_sync(0xffffffffu, u, 31);
-  const uint64_t before = __shfl_sync(0xffffffffu, u - w, warp) + v - x;
+  Pair all = sh[lane];  // (PLAN_THREADS / 32 = 32 warps: every warp scans their sums)
+  const Pair mine = sh[warp];
+  scan(all);
+  total->x = __shfl_sync(0xffffffffu, all.x, 31);
+  total->y = __shfl_sync(0xffffffffu, all.y, 31);
+  const Pair before{__shfl_sync(0xffffffffu, all.x, warp) - mine.x + up.x - v.x,
+                    __shfl_sync(0xffffffffu, all.y, warp) - mine.y + up.y - v.y};
   __syncthreads();
   return before;
 }
@@ -146,80 +153,99 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, con
                                                                  Ws w, int* status) {
   pdl_wait();
   pdl_trigger();
-  __shared__ uint64_t sh[32];
-  __shared__ int sh_p[PLAN_THREADS], sh_keep[PLAN_THREADS], sh_had[PLAN_THREADS];
+  __shared__ Pair sh[32];
+  __shared__ int4 sh_changed[PLAN_THREADS];  // sequence, parent, pages shared with it, pages that the sequence had
+  __shared__ int sh_n, sh_longest, sh_refuse;
   extern __shared__ int32_t sh_counts[];
   const int rank = ONE ? 0 : cluster_ctarank(), ctas = ONE ? 1 : cluster_nctarank(), tid = threadIdx.x, lane = tid & 31;
   const Counts<ONE> of(a, w, sh_counts);
+  if (tid == 0) sh_n = sh_longest = sh_refuse = 0;
+  __syncthreads();
   // Holders: old rows' pages lose one, new rows' gain one; where both are the same page nothing happens, which is
-  // most of a beam search's rows.  1024 sequences at a time, their entries divided among all threads (or such tiles among the
-  // CTAs, where there are enough).
+  // most of a beam search's rows.  1024 sequences at a time, the entries of those that change divided among all threads (or
+  // such tiles among the CTAs, where there are enough).
   const int tiles = (a.S + PLAN_THREADS - 1) / PLAN_THREADS;
   const bool share = tiles < ctas;
   Row mine;  // of sequence tid, kept where there are no more than threads
   for (int tile = share ? 0 : rank; tile < tiles; tile += share ? 1 : ctas) {
-    const int s0 = tile * PLAN_THREADS, n = min(PLAN_THREADS, a.S - s0);
-    int longest = 0;
-    if (tid < n) {
-      mine = row_of(a, parents, grow, s0 + tid, nullptr);
-      sh_p[tid] = mine.p;
-      sh_keep[tid] = min(mine.held, mine.want);
-      sh_had[tid] = mine.had;
-      longest = mine.p == s0 + tid && sh_keep[tid] == mine.had ? 0 : max(mine.had, sh_keep[tid]);
+    const int s = tile * PLAN_THREADS + tid;
+    int keep = 0;
+    bool changes = false;
+    if (s < a.S) {
+      mine = row_of(a, parents, grow, s);
+      keep = min(mine.held, mine.want);
+      changes = mine.p != s || keep != mine.had;
     }
-    longest = __reduce_max_sync(0xffffffffu, longest);
-    if (lane == 0) sh[tid >> 5] = longest;
-    __syncthreads();  // (the counts in shared memory are set, too)
-    longest = __reduce_max_sync(0xffffffffu, (int)sh[lane]);
-    if (tid < n && mine.last >= 0 && (!share || rank == 0)) {
-      atomicAdd(of.writing + mine.last, 1);
-      atomicMax(of.lowest + mine.last, a.S - (s0 + tid));
+    int place = 0;
+    if (share) {  // in the sequences' order: the CTAs of a cluster divide one list
+      Pair n;
+      place = (int)block_scan(Pair{0, changes}, sh, &n).y;
+      if (tid == 0) sh_n = (int)n.y;
+    } else if (changes) {
+      place = atomicAdd(&sh_n, 1);
     }
-    const int64_t all = (int64_t)n * longest;
-    const int step = share ? ctas * PLAN_THREADS : PLAN_THREADS;
-#pragma unroll 4
-    for (int64_t e = (share ? rank * PLAN_THREADS : 0) + tid; e < all; e += step) {
-      const int r = (int)kv_div(e, longest), i = (int)(e - (int64_t)r * longest), p = sh_p[r], keep = sh_keep[r];
-      if (p == s0 + r && i < keep) continue;
-      const int x = i < keep ? __ldg(a.table + (int64_t)p * a.W + i) : -1;
-      const int y = i < sh_had[r] ? __ldg(a.table + (int64_t)(s0 + r) * a.W + i) : -1;
-      if (x != y) {
-        if ((unsigned)x < (unsigned)a.n_pages) atomicAdd(of.have + x, 1);
-        if ((unsigned)y < (unsigned)a.n_pages) atomicSub(of.have + y, 1);
+    if (changes) {
+      atomicMax(&sh_longest, max(mine.had, keep));
+      sh_changed[place] = make_int4(s, mine.p, keep, mine.had);
+    }
+    if (s < a.S) {
+      if (mine.last >= 0 && (!share || rank == 0)) {
+        atomicAdd(of.writing + mine.last, 1);
+        atomicMax(of.lowest + mine.last, a.S - s);
       }
     }
     __syncthreads();
+    const int longest = sh_longest, step = (share ? ctas : 1) * PLAN_THREADS;
+    const int64_t all = (int64_t)sh_n * longest;
+    constexpr int BATCH = 4;
+    for (int64_t e0 = (share ? rank * PLAN_THREADS : 0) + tid; e0 < all; e0 += BATCH * step) {
+      int x[BATCH], y[BATCH];
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        x[k] = y[k] = -1;
+        const int64_t e = e0 + (int64_t)k * step;
+        if (e < all) {
+          const int at = (int)kv_div(e, longest), i = (int)(e - (int64_t)at * longest);
+          const int4 r = sh_changed[at];
+          if (i < r.z && !(r.x == r.y && i < r.w)) x[k] = __ldg(a.table + (int64_t)r.y * a.W + i);
+          if (i < r.w && !(r.x == r.y && i < r.z)) y[k] = __ldg(a.table + (int64_t)r.x * a.W + i);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k)
+        if (x[k] != y[k]) {
+          if ((unsigned)x[k] < (unsigned)a.n_pages) atomicAdd(of.have + x[k], 1);
+          if ((unsigned)y[k] < (unsigned)a.n_pages) atomicSub(of.have + y[k], 1);
+        }
+    }
+    __syncthreads();
+    if (tid == 0) sh_n = sh_longest = 0;
+    if (tiles > 1) __syncthreads();
   }
-  if (tiles == 0) __syncthreads();
   if (!ONE) cluster_sync();
   // What each sequence wants, and what is free: this CTA's part of both, a warp's pages one after another.
   const int per = (a.S + ctas - 1) / ctas, s0 = min(a.S, rank * per), s1 = min(a.S, s0 + per);
   const int wper = (a.n_pages + ctas * 32 - 1) / (ctas * 32), q0 = min(a.n_pages, (rank * 32 + (tid >> 5)) * wper),
             q1 = min(a.n_pages, q0 + wper);
-  const auto row = [&](int s) { return ONE && a.S <= PLAN_THREADS ? mine : row_of(a, parents, grow, s, nullptr); };
+  const auto row = [&](int s) { return ONE ? mine : row_of(a, parents, grow, s); };
   const auto copied = [&](const Row& r, int s) {
     return r.last >= 0 && !(of.holders(r.last) == of.writers(r.last) && of.first_writer(r.last) == s);
   };
-  uint64_t sum = 0, total;  // pages wanted << 32 | copies
-  int refuse = 0, nfree = 0;
+  Pair sum{0, 0}, total;  // pages wanted << 32 | copies; free pages
   for (int s = s0 + tid; s < s1; s += PLAN_THREADS) {
     const Row r = row(s);
-    refuse |= r.refuse;
+    if (r.refuse) atomicOr(&sh_refuse, r.refuse);
     const int c = copied(r, s);
-    sum += ((uint64_t)(max(0, r.want - r.held) + c) << 32) | c;
+    sum.x += ((uint64_t)(max(0, r.want - r.held) + c) << 32) | c;
   }
+  uint32_t nfree = 0;
   for (int q = q0; q < q1; q += 32) nfree += __popc(__ballot_sync(0xffffffffu, q + lane < q1 && of.holders(min(q + lane, a.n_pages - 1)) == 0));
-  const uint64_t rows_before = block_scan(sum, sh, &total);
-  const int my_rows_total_copies = (int)(uint32_t)total;
-  const int64_t my_rows_total = (int64_t)(total >> 32);
-  uint64_t free_total;
-  const uint64_t free_before = block_scan(lane == 0 ? nfree : 0, sh, &free_total);  // (of this warp's first lane)
-  const int no_room = __syncthreads_or(refuse & FL_KV_NO_ROOM), bad_parent = __syncthreads_or(refuse & FL_KV_BAD_PARENT);
-  refuse = (no_room ? FL_KV_NO_ROOM : 0) | (bad_parent ? FL_KV_BAD_PARENT : 0);
-  int64_t all_wanted = my_rows_total, all_free = (int64_t)free_total, wanted0 = 0, free0 = 0;
-  int copies = my_rows_total_copies, copies0 = 0;
+  if (lane == 0) sum.y = nfree;
+  const Pair before = block_scan(sum, sh, &total);  // (the free ones: of this warp's first lane)
+  int64_t all_wanted = (int64_t)(total.x >> 32), all_free = total.y, wanted0 = 0, free0 = 0;
+  int copies = (int)(uint32_t)total.x, copies0 = 0, refuse = sh_refuse;
   if (!ONE) {
-    if (tid == 0) __stcg(w.totals + rank, make_int4((int)my_rows_total, my_rows_total_copies, (int)free_total, refuse));
+    if (tid == 0) __stcg(w.totals + rank, make_int4((int)all_wanted, copies, (int)all_free, refuse));
     cluster_sync();
     all_wanted = all_free = refuse = copies = 0;
     for (int c = 0; c < ctas; ++c) {
@@ -241,27 +267,26 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, con
     const int s = base + tid;
     Row r;
     int c = 0;
-    uint64_t x = 0, before = rows_before;
+    Pair x{0, 0}, ahead = before;
     if (s < s1) {
       r = row(s);
       c = copied(r, s);
-      x = ((uint64_t)(max(0, r.want - r.held) + c) << 32) | c;
+      x.x = ((uint64_t)(max(0, r.want - r.held) + c) << 32) | c;
     }
-    total = 0;
-    if (s1 - s0 > PLAN_THREADS) before = block_scan(x, sh, &total);  // (else the sums above are these)
+    total = Pair{0, 0};
+    if (s1 - s0 > PLAN_THREADS) ahead = block_scan(x, sh, &total);  // (else the sums above are these)
     if (s < s1) {
-      if (r.last < 0 && r.L2 > r.L && (r.L & ((1 << a.ps_log2) - 1))) atomicOr(status, FL_KV_BAD_PAGE);
-      if (r.p >= 0) len_of(a, r.p, status);
-      const int at = (int)(wanted0 + (int64_t)(before >> 32));
+      if (r.bad) atomicOr(status, FL_KV_BAD_PAGE);
+      const int at = (int)(wanted0 + (int64_t)(ahead.x >> 32));
       w.first[s] = at;
       w.rows[s] = make_int4(r.p, min(r.held, r.want), r.held - c, r.want);
       a.lens_to[s] = refuse ? __ldg(a.lens + s) : r.L2;
-      if (c) w.copies[copies0 + (int)(uint32_t)before] = make_int4(r.last, at, r.L & ((1 << a.ps_log2) - 1), 0);
+      if (c) w.copies[copies0 + (int)(uint32_t)ahead.x] = make_int4(r.last, at, r.L & ((1 << a.ps_log2) - 1), 0);
     }
-    wanted0 += (int64_t)(total >> 32);
-    copies0 += (int)(uint32_t)total;
+    wanted0 += (int64_t)(total.x >> 32);
+    copies0 += (int)(uint32_t)total.x;
   }
-  int64_t at = free0 + (int64_t)__shfl_sync(0xffffffffu, free_before, 0);
+  int64_t at = free0 + __shfl_sync(0xffffffffu, before.y, 0);
   for (int q = q0; q < q1; q += 32) {
     const bool in = q + lane < q1;
     const int x = min(q + lane, a.n_pages - 1), have = of.holders(x), writers = of.writers(x);
@@ -285,19 +310,18 @@ template <bool ONE>
 __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, int32_t* moved, int32_t* used, Ws w) {
   pdl_wait();
   pdl_trigger();
-  __shared__ uint64_t sh[32];
+  __shared__ Pair sh[32];
   const int rank = ONE ? 0 : cluster_ctarank(), ctas = ONE ? 1 : cluster_nctarank(), tid = threadIdx.x, lane = tid & 31;
   // a warp's pages one after another
   const int wper = (a.n_pages + ctas * 32 - 1) / (ctas * 32), q0 = min(a.n_pages, (rank * 32 + (tid >> 5)) * wper),
             q1 = min(a.n_pages, q0 + wper);
   const auto busy = [&](int q) { return __ballot_sync(0xffffffffu, q + lane < q1 && __ldg(a.refs + min(q + lane, a.n_pages - 1)) > 0); };
-  uint64_t total;
-  int n = 0;
+  Pair total;
+  uint32_t n = 0;
   for (int q = q0; q < q1; q += 32) n += __popc(busy(q));
-  int before = (int)block_scan(lane == 0 ? n : 0, sh, &total), all = (int)total;
-  before = __shfl_sync(0xffffffffu, before, 0);
+  int before = (int)__shfl_sync(0xffffffffu, block_scan(Pair{0, lane == 0 ? n : 0}, sh, &total).y, 0), all = (int)total.y;
   if (!ONE) {
-    if (tid == 0) __stcg(&w.totals[rank].x, (int)total);
+    if (tid == 0) __stcg(&w.totals[rank].x, all);
     cluster_sync();
     all = 0;
     for (int c = 0; c < ctas; ++c) {
@@ -308,8 +332,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, 
   // the pages in use among the first `all` stay
   n = 0;
   for (int q = q0; q < min(q1, all); q += 32) n += __popc(busy(q) & (all - q >= 32 ? ~0u : (1u << (all - q)) - 1));
-  block_scan(lane == 0 ? n : 0, sh, &total);
-  int stay = (int)total;
+  block_scan(Pair{0, lane == 0 ? n : 0}, sh, &total);
+  int stay = (int)total.y;
   if (!ONE) {
     if (tid == 0) __stcg(&w.totals[rank].y, stay);
     cluster_sync();
@@ -498,11 +522,13 @@ __global__ void __launch_bounds__(COPY_THREADS) compact_kernel(PagesDev a, const
   for_entries(a, [&](int s, int i) {
     const int64_t e = (int64_t)s * a.W + i;
     int page = -1;
-    if (i < pages_of(a, len_of(a, s, status))) {
+    bool bad = false;
+    if (i < pages_of(a, len_of(a, s, &bad))) {
       const int x = __ldg(a.table + e);
       if ((unsigned)x < (unsigned)a.n_pages) page = __ldcg(moved + x);
-      if (page < 0) atomicOr(status, FL_KV_BAD_PAGE);
+      bad |= page < 0;
     }
+    if (bad) atomicOr(status, FL_KV_BAD_PAGE);
     a.table_to[e] = page;
   });
   copy_all(c, w, a.ps_log2, status);

@@ -813,7 +813,7 @@ int launch_step(StepArgs& a, cudaStream_t st) {
 }
 
 // ------------------------------------------------------------------------------- back-pointers
-constexpr int TRACE_THREADS = 512, CHUNK = 32, BLOCK_STEPS = 2048;
+constexpr int TRACE_THREADS = 256, CHUNK = 16, MAX_STEPS = 2048, MAX_TRACE_CTAS = 8;  // steps of a CTA, CTAs of a search
 
 struct TraceArgs {
   fl_beam_search p;
@@ -821,26 +821,37 @@ struct TraceArgs {
   const int32_t *tokens, *parents;
   int n_best, pad;
   float penalty_hi, penalty_lo;
+  int block;  // steps of a CTA, CHUNK at least
   int32_t *out_tokens, *out_lens;
   float* out_scores;
   int* status;
 };
 
+FL_DEV uint32_t ld_cluster_u8(const void* p, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u8 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(p), rank)) : "memory");
+  return v;
+}
+
 // Beams after each step, from the last step to the first: b(t - 1) = parent[t][b(t)].  Following one pointer after
-// another costs a load's latency a step; here each chunk of 32 steps becomes one map from the beams behind it to
-// those before it, all chunks at once from shared memory, the hypotheses jump from chunk to chunk, and then all chunks
-// are walked at once for the beams in between.
+// another costs a load's latency a step.  Here a cluster has a search and each of its CTAs some of the steps, of which each chunk
+// of 16 becomes one map from the beams behind it to those before it, all at once from shared memory; those together give
+// the CTA's map, the CTAs learn each other's, the hypotheses jump from CTA to CTA and from chunk to chunk, and then all
+// chunks are walked at once for the beams in between.  Latency is the bound.  TODO
 __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) {
   pdl_wait();
   pdl_trigger();
   extern __shared__ __align__(16) uint8_t sh[];
-  const int B = a.p.beams, T = a.p.max_steps, n = a.n_best, s = blockIdx.x, tid = threadIdx.x;
-  const int room = min(T, BLOCK_STEPS), chunks = (room + CHUNK - 1) / CHUNK;
-  uint8_t* par = sh;                       // [step][beam]
-  uint8_t* map = par + room * B;           // [chunk][beam]
-  uint8_t* entry = map + chunks * B;       // [chunk][hypothesis]: its beam after the chunk's last step that it has
-  uint8_t* chain = entry + chunks * n;     // [hypothesis][step]
-  __shared__ int h_steps[FL_BEAM_MAX], h_ended[FL_BEAM_MAX], h_beam[FL_BEAM_MAX];
+  const int B = a.p.beams, T = a.p.max_steps, n = a.n_best, block = a.block, tid = threadIdx.x;
+  const int rank = cluster_ctarank(), ctas = cluster_nctarank(), s = blockIdx.x / ctas;
+  const int chunks = (block + CHUNK - 1) / CHUNK;
+  uint8_t* par = sh;                    // [step][beam]
+  uint8_t* map = par + block * B;       // [chunk][beam]
+  uint8_t* entry = map + chunks * B;    // [chunk][hypothesis]: its beam after the chunk's last step that it has
+  uint8_t* chain = entry + chunks * n;  // [hypothesis][step]
+  uint8_t* behind = chain + block * n;  // [chunk][beam]: the beam after the chunk's last step, by the beam behind the block
+  __shared__ int h_steps[FL_BEAM_MAX], h_ended[FL_BEAM_MAX], h_beam[FL_BEAM_MAX], h_from[FL_BEAM_MAX], h_after[FL_BEAM_MAX];
+  __shared__ uint8_t of_block[FL_BEAM_MAX], of_part[FL_BEAM_MAX];  // beams before the block: by the beam behind it; of hypotheses that end in it
   if (tid < 32) {
     const int b = tid < FL_BEAM_MAX ? tid : tid - FL_BEAM_MAX;
     const int raw = a.s.steps[s], steps = min(max(raw, 0), T);
@@ -863,27 +874,30 @@ __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) 
     }
     if (!(x == x)) x = -INFINITY;
     if (bad) atomicOr(a.status, FL_BEAM_BAD_TRACE);
-    int rank = 0;
-    for (int o = 0; o < 32; ++o) {
-      const float y = __shfl_sync(0xffffffffu, x, o);
-      rank += y > x || (y == x && o < tid);
-    }
-    if (rank < n) {
+    const uint64_t key = (uint64_t)order32(x) << 32 | (31 - tid);
+    int place = 0;
+#pragma unroll 8
+    for (int o = 0; o < 32; ++o) place += __shfl_sync(0xffffffffu, key, o) > key;
+    if (place < n) {
       const bool some = x > -INFINITY;
-      h_steps[rank] = some ? before : 0;
-      h_ended[rank] = some && tid < FL_BEAM_MAX;
-      h_beam[rank] = beam;
-      a.out_scores[s * n + rank] = x;
-      a.out_lens[s * n + rank] = some ? before + (tid < FL_BEAM_MAX) : 0;
+      h_steps[place] = some ? before : 0;
+      h_ended[place] = some && tid < FL_BEAM_MAX;
+      h_beam[place] = beam;
+      if (rank == 0) {
+        a.out_scores[s * n + place] = x;
+        a.out_lens[s * n + place] = some ? before + (tid < FL_BEAM_MAX) : 0;
+      }
     }
   }
   __syncthreads();
-  for (int t1 = T; t1 > 0;) {
-    const int t0 = (t1 - 1) / BLOCK_STEPS * BLOCK_STEPS, len = t1 - t0, nc = (len + CHUNK - 1) / CHUNK;
-    const int64_t first = ((int64_t)s * T + t0) * B;
-    int longest = 0;
-    for (int h = 0; h < n; ++h) longest = max(longest, h_steps[h]);
+  int longest = 0;
+  for (int h = 0; h < n; ++h) longest = max(longest, h_steps[h]);
+  const int row = block * ctas;  // steps of the cluster at a time
+  for (int base = (T - 1) / row * row; base >= 0; base -= row) {
+    const int t0 = base + rank * block, len = max(0, min(block, T - t0)), nc = (len + CHUNK - 1) / CHUNK;
     const int have = min(max(longest - t0, 0), len);  // steps that some hypothesis has
+    const int64_t first = ((int64_t)s * T + t0) * B;
+#pragma unroll 4
     for (int i = tid; i < have * B; i += TRACE_THREADS) {
       int p = __ldg(a.parents + first + i);
       if ((unsigned)p >= (unsigned)B) {
@@ -894,48 +908,67 @@ __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) 
     }
     __syncthreads();
     for (int i = tid; i < nc * B; i += TRACE_THREADS) {
-      const int c = i / B, lo = c * CHUNK, hi = min(lo + CHUNK, have);
+      const int c = i / B, lo = c * CHUNK;
       int b = i % B;
-      for (int t = hi - 1; t >= lo; --t) b = par[t * B + b];
+      for (int t = min(lo + CHUNK, have) - 1; t >= lo; --t) b = par[t * B + b];
       map[i] = (uint8_t)b;
     }
     __syncthreads();
-    if (tid < n) {
-      int b = h_beam[tid];
-      const int mine = min(max(h_steps[tid] - t0, 0), len);  // its steps in this block
+    // The block from behind, chunk by chunk: for each beam that may be there, and for the hypotheses whose steps end in it.
+    if (tid < B || (tid >= 32 && tid < 32 + n)) {
+      const bool full = tid < B;
+      const int i = full ? tid : tid - 32, mine = full ? have : min(max(h_steps[i] - t0, 0), len);
+      uint8_t* told = full ? behind + i : entry + i;
+      int b = full ? tid : h_beam[i];
       for (int c = nc - 1; c >= 0; --c) {
         const int lo = c * CHUNK;
-        entry[c * n + tid] = (uint8_t)b;
-        if (mine <= lo) continue;
+        told[c * (full ? B : n)] = (uint8_t)b;
         if (mine >= min(lo + CHUNK, have))
           b = map[c * B + b];
         else
           for (int t = mine - 1; t >= lo; --t) b = par[t * B + b];
       }
-      h_beam[tid] = b;
+      (full ? of_block : of_part)[i] = (uint8_t)b;
     }
     __syncthreads();
+    if (ctas > 1) cluster_sync();
+    if (tid < n) {  // the beam after the block's last step, if the hypothesis has that; the one before the row
+      int b = h_beam[tid], after = b;
+      for (int r = ctas - 1; r >= 0; --r) {
+        if (r == rank) b = after;
+        const int begin = base + r * block, end = min(begin + block, T), has = h_steps[tid];
+        if (ctas == 1) break;
+        if (has >= end && has > begin) after = (int)ld_cluster_u8(of_block + after, r);
+        else if (has > begin) after = (int)ld_cluster_u8(of_part + tid, r);
+      }
+      if (ctas == 1) after = h_steps[tid] >= min(base + block, T) ? of_block[after] : of_part[tid];
+      h_from[tid] = b;
+      h_after[tid] = after;
+    }
+    if (ctas > 1) cluster_sync();  // (everybody has read the others' maps)
+    else __syncthreads();
+    if (tid < n) h_beam[tid] = h_after[tid];
     for (int i = tid; i < nc * n; i += TRACE_THREADS) {
-      const int c = i / n, h = i % n, lo = c * CHUNK;
-      int b = entry[i];
-      for (int t = min(lo + CHUNK, min(h_steps[h] - t0, len)) - 1; t >= lo; --t) {
-        chain[h * room + t] = (uint8_t)b;
-        b = par[t * B + b];
+      const int c = i / n, h = i % n, lo = c * CHUNK, has = min(h_steps[h] - t0, len);
+      int beam = has == len ? behind[c * B + h_from[h]] : entry[i];
+      for (int t = min(lo + CHUNK, has) - 1; t >= lo; --t) {
+        chain[h * block + t] = (uint8_t)beam;
+        beam = par[t * B + beam];
       }
     }
     __syncthreads();
-    for (int h = 0; h < n; ++h) {
-      int32_t* out = a.out_tokens + ((int64_t)s * n + h) * T + t0;
-      const int mine = h_steps[h] - t0;
-      for (int t = tid; t < len; t += TRACE_THREADS) {
-        int v = a.pad;
-        if (t < mine) v = __ldg(a.tokens + first + (int64_t)t * B + chain[h * room + t]);
-        else if (t == mine && h_ended[h] && a.p.eos >= 0) v = a.p.eos;
-        out[t] = v;
-      }
+    // 32 steps of a hypothesis a warp
+    const int pieces = (len + 31) / 32, lane = tid & 31;
+#pragma unroll 4
+    for (int i = tid >> 5; i < n * pieces; i += TRACE_THREADS / 32) {
+      const int h = i / pieces, t = i % pieces * 32 + lane, has = h_steps[h] - t0;
+      if (t >= len) continue;
+      int v = a.pad;
+      if (t < has) v = __ldg(a.tokens + first + (int64_t)t * B + chain[h * block + t]);
+      else if (t == has && h_ended[h] && a.p.eos >= 0) v = a.p.eos;
+      a.out_tokens[((int64_t)s * n + h) * T + t0 + t] = v;
     }
     __syncthreads();
-    t1 = t0;
   }
 }
 
@@ -997,11 +1030,28 @@ extern "C" int fl_k_beam_trace(const fl_beam_search* search, const fl_beam_state
       fl_misaligned(out_lens, 4) || fl_misaligned(out_scores, 4) || fl_misaligned(status, 4))
     return fl_internal_error(FL_ERR_INVALID_ARG, "beam trace: args");
   const float penalty = (float)search->length_penalty;
-  const TraceArgs a{*search, *state, trace_tokens, trace_parents, n_best, pad, penalty, (float)(search->length_penalty - penalty), out_tokens, out_lens, out_scores, status};
-  const int room = search->max_steps < BLOCK_STEPS ? search->max_steps : BLOCK_STEPS, chunks = (room + CHUNK - 1) / CHUNK;
-  const int smem = (room + chunks) * (search->beams + n_best);
+  // CTAs of 256 steps, as many as a cluster has; longer ones where those are too few
+  const int T = search->max_steps;
+  int ctas = 1;
+  while (ctas < MAX_TRACE_CTAS && T > ctas * 256) ctas *= 2;
+  const int block = std::min(MAX_STEPS, std::max(CHUNK, (T + ctas - 1) / ctas)), chunks = (block + CHUNK - 1) / CHUNK;
+  const TraceArgs a{*search,    *state, trace_tokens, trace_parents, n_best, pad, penalty, (float)(search->length_penalty - penalty), block,
+                    out_tokens, out_lens, out_scores, status};
   // the limit of the largest call, once: a smaller one would lower it for a larger call made before
-  FL_CUDA_TRY(fl_func_smem((const void*)beam_trace_kernel, (BLOCK_STEPS + BLOCK_STEPS / CHUNK) * 2 * FL_BEAM_MAX));
-  FL_CUDA_TRY(fl_launch(beam_trace_kernel, dim3(search->n_seqs), dim3(TRACE_THREADS), smem, (cudaStream_t)stream, a));
+  FL_CUDA_TRY(fl_func_smem((const void*)beam_trace_kernel, (MAX_STEPS * 2 + MAX_STEPS / CHUNK * 3) * FL_BEAM_MAX));
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see pdl_wait
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(search->n_seqs * ctas);
+  cfg.blockDim = dim3(TRACE_THREADS);
+  cfg.dynamicSmemBytes = (block + chunks) * (search->beams + n_best) + chunks * search->beams;
+  cfg.stream = (cudaStream_t)stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = ctas > 1 ? 2 : 1;
+  FL_CUDA_TRY(cudaLaunchKernelEx(&cfg, beam_trace_kernel, a));
   return FL_OK;
 }

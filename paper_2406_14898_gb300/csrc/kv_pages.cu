@@ -87,11 +87,6 @@ FL_DEV Row row_of(const PagesDev& a, const int32_t* parents, const int32_t* grow
   return r;
 }
 
-FL_DEV uint32_t cluster_nctarank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
 // Exclusive prefix sums of x and y over the block's threads, and the block's sums.
 struct Pair {
   uint64_t x;
@@ -609,7 +604,7 @@ cudaError_t launch_plan(void (*kern)(KArgs...), int ctas, int smem, cudaStream_t
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = ctas > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 

@@ -250,6 +250,11 @@ FL_DEV uint32_t cluster_ctarank() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
+FL_DEV uint32_t cluster_nctarank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
 // All threads of both CTAs; orders shared-memory and barrier operations across the pair.
 // (Not .aligned: the threads of a warp may arrive from divergent paths.)
 FL_DEV void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }

@@ -242,6 +242,9 @@ struct Join {
 FL_DEV void cp_async16(void* to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
 }
+FL_DEV void cp_async4(void* to, const void* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
 FL_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 FL_DEV void cp_async_wait() {
@@ -841,15 +844,15 @@ FL_DEV uint32_t ld_cluster_u8(const void* p, uint32_t rank) {
 __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) {
   pdl_wait();
   pdl_trigger();
-  extern __shared__ __align__(16) uint8_t sh[];
-  const int B = a.p.beams, T = a.p.max_steps, n = a.n_best, block = a.block, tid = threadIdx.x;
+  extern __shared__ __align__(16) int32_t token[];  // [step][beam], a step's row from another bank than the next one's; then bytes
+  const int B = a.p.beams, T = a.p.max_steps, n = a.n_best, block = a.block, line = block + 4, odd = B | 1, tid = threadIdx.x;
   const int rank = cluster_ctarank(), ctas = cluster_nctarank(), s = blockIdx.x / ctas;
   const int chunks = (block + CHUNK - 1) / CHUNK;
-  uint8_t* par = sh;                    // [step][beam]
+  uint8_t* par = reinterpret_cast<uint8_t*>(token + block * odd);  // [step][beam]
   uint8_t* map = par + block * B;       // [chunk][beam]
   uint8_t* entry = map + chunks * B;    // [chunk][hypothesis]: its beam after the chunk's last step that it has
-  uint8_t* chain = entry + chunks * n;  // [hypothesis][step]
-  uint8_t* behind = chain + block * n;  // [chunk][beam]: the beam after the chunk's last step, by the beam behind the block
+  uint8_t* chain = entry + chunks * n;  // [hypothesis][step], a hypothesis's line from another bank than the next one's
+  uint8_t* behind = chain + line * n;  // [chunk][beam]: the beam after the chunk's last step, by the beam behind the block
   __shared__ int h_steps[FL_BEAM_MAX], h_ended[FL_BEAM_MAX], h_beam[FL_BEAM_MAX], h_from[FL_BEAM_MAX], h_after[FL_BEAM_MAX];
   __shared__ uint8_t of_block[FL_BEAM_MAX], of_part[FL_BEAM_MAX];  // beams before the block: by the beam behind it; of hypotheses that end in it
   if (tid < 32) {
@@ -897,6 +900,8 @@ __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) 
     const int t0 = base + rank * block, len = max(0, min(block, T - t0)), nc = (len + CHUNK - 1) / CHUNK;
     const int have = min(max(longest - t0, 0), len);  // steps that some hypothesis has
     const int64_t first = ((int64_t)s * T + t0) * B;
+    for (int i = tid; i < have * B; i += TRACE_THREADS) cp_async4(token + i / B * odd + i % B, a.tokens + first + i);
+    cp_async_commit();
 #pragma unroll 4
     for (int i = tid; i < have * B; i += TRACE_THREADS) {
       int p = __ldg(a.parents + first + i);
@@ -952,10 +957,11 @@ __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) 
       const int c = i / n, h = i % n, lo = c * CHUNK, has = min(h_steps[h] - t0, len);
       int beam = has == len ? behind[c * B + h_from[h]] : entry[i];
       for (int t = min(lo + CHUNK, has) - 1; t >= lo; --t) {
-        chain[h * block + t] = (uint8_t)beam;
+        chain[h * line + t] = (uint8_t)beam;
         beam = par[t * B + beam];
       }
     }
+    cp_async_wait<0>();
     __syncthreads();
     // 32 steps of a hypothesis a warp
     const int pieces = (len + 31) / 32, lane = tid & 31;
@@ -964,7 +970,7 @@ __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) 
       const int h = i / pieces, t = i % pieces * 32 + lane, has = h_steps[h] - t0;
       if (t >= len) continue;
       int v = a.pad;
-      if (t < has) v = __ldg(a.tokens + first + (int64_t)t * B + chain[h * block + t]);
+      if (t < has) v = token[t * odd + chain[h * line + t]];
       else if (t == has && h_ended[h] && a.p.eos >= 0) v = a.p.eos;
       a.out_tokens[((int64_t)s * n + h) * T + t0 + t] = v;
     }
@@ -1038,7 +1044,7 @@ extern "C" int fl_k_beam_trace(const fl_beam_search* search, const fl_beam_state
   const TraceArgs a{*search,    *state, trace_tokens, trace_parents, n_best, pad, penalty, (float)(search->length_penalty - penalty), block,
                     out_tokens, out_lens, out_scores, status};
   // the limit of the largest call, once: a smaller one would lower it for a larger call made before
-  FL_CUDA_TRY(fl_func_smem((const void*)beam_trace_kernel, (MAX_STEPS * 2 + MAX_STEPS / CHUNK * 3) * FL_BEAM_MAX));
+  FL_CUDA_TRY(fl_func_smem((const void*)beam_trace_kernel, MAX_STEPS * 4 * (FL_BEAM_MAX + 1) + (MAX_STEPS * 2 + 4 + MAX_STEPS / CHUNK * 3) * FL_BEAM_MAX));
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see pdl_wait
@@ -1048,7 +1054,7 @@ extern "C" int fl_k_beam_trace(const fl_beam_search* search, const fl_beam_state
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3(search->n_seqs * ctas);
   cfg.blockDim = dim3(TRACE_THREADS);
-  cfg.dynamicSmemBytes = (block + chunks) * (search->beams + n_best) + chunks * search->beams;
+  cfg.dynamicSmemBytes = block * (4 * (search->beams | 1) + search->beams) + (block + 4) * n_best + chunks * (2 * search->beams + n_best);
   cfg.stream = (cudaStream_t)stream;
   cfg.attrs = attr;
   cfg.numAttrs = ctas > 1 ? 2 : 1;

@@ -13,12 +13,14 @@ projection's epilogue, before their one rounding.
     python -m paper_2406_14898_gb300.generate --tokens 16
 
 runs a small split model with randomly initialised weights: three clients with prompts of different
-lengths answer together.
+lengths answer together; with ``--beams 4`` each keeps its four likeliest answers under way (``Generator.beam_search``), whose
+sequences share the pages of what they have in common.
 """
 from __future__ import annotations
 
 import argparse
 import contextlib
+import copy
 from typing import List, Optional, Sequence
 
 import torch
@@ -71,6 +73,34 @@ class Pages:
         self.table[s] = -1
 
 
+class SharedPages:
+    """The pages of a stack whose sequences share them, from a ``Pages`` on: which, how long and how many have each stays on the
+    device (``fl_k_kv_fork``), before and after the last step in turn."""
+
+    def __init__(self, pages: Pages, caches: Sequence["F.fl_kv_cache"]):
+        n, width = pages.table.shape
+        self.n_pages = len(pages.free) + sum(len(h) for h in pages.held)
+        refs = torch.zeros(self.n_pages, dtype=I32)
+        for h in pages.held:
+            refs[h] += 1
+        now = {"lens": torch.tensor(pages.lens, dtype=I32).cuda(), "table": pages.table.cuda(), "refs": refs.cuda()}
+        self.sides = [now, {k: torch.empty_like(v) for k, v in now.items()}]
+        self.structs = [F.kv_pages(n, self.n_pages, pages.page_size, width, **side) for side in self.sides]
+        self.caches = F.kv_caches(caches)
+        self.workspace = torch.zeros(F.fl_k_kv_pages_workspace(self.structs[0]) // 4, dtype=I32, device="cuda")
+        self.cu = torch.arange(n + 1, dtype=I32, device="cuda")
+        self.one = torch.ones(n, dtype=I32, device="cuda")
+
+    def step(self, parents: torch.Tensor, status: torch.Tensor) -> "F.fl_kv_batch":
+        """Every sequence follows its parent (device int32, -1: none) and gets room for a token: the batch of those."""
+        F.fl_k_kv_fork(self.caches, *self.structs, parents, self.one, self.workspace, status, **_stream())
+        self.sides.reverse()
+        self.structs.reverse()
+        now = self.sides[0]
+        n, width = now["table"].shape
+        return F.kv_batch(n, n, 1, self.cu, now["lens"], now["table"], width)
+
+
 class BlockStack:
     """The blocks of one part of the model, with a key / value cache each, on the current CUDA device."""
 
@@ -81,9 +111,6 @@ class BlockStack:
         c = self.cfg = cfg
         H, Fh, P = c.hidden, c.ffn_hidden, c.prefix_len
         self.rdim = c.rotary_dim or c.head_dim // 2
-        width = -(-max_tokens // page_size)
-        self.n_pages = n_seqs * width if n_pages is None else n_pages
-        self.pages = Pages(self.n_pages, page_size, n_seqs, max_tokens)
 
         def dev(x, *shape):
             return torch.from_numpy(x).cuda().view(*shape)
@@ -94,12 +121,19 @@ class BlockStack:
                                                              (F.FL_T_WUP, (Fh, H)), (F.FL_T_WDOWN, (H, Fh)))],
                  "b": [dev(get(t), -1) for t in (F.FL_T_BQKV, F.FL_T_BDENSE, F.FL_T_BUP, F.FL_T_BDOWN)],
                  "ln": [dev(get(t), H) for t in (F.FL_T_LN1_G, F.FL_T_LN1_B, F.FL_T_LN2_G, F.FL_T_LN2_B)],
-                 "prefix": [dev(get(t), P, H).to(BF16) for t in (F.FL_T_PREFIX_K, F.FL_T_PREFIX_V)] if P else None,
-                 # handed out uncleared
-                 "kv": [torch.empty((self.n_pages, c.n_heads, page_size, c.head_dim), dtype=BF16, device="cuda")
-                        for _ in "kv"]}
-            b["cache"] = F.kv_cache(b["kv"][0], b["kv"][1], self.n_pages, page_size, c.n_heads, c.head_dim)
+                 "prefix": [dev(get(t), P, H).to(BF16) for t in (F.FL_T_PREFIX_K, F.FL_T_PREFIX_V)] if P else None}
             self.blocks.append(b)
+        self._make_room(n_seqs, max_tokens, page_size, n_pages)
+
+    def _make_room(self, n_seqs, max_tokens, page_size, n_pages):
+        c, width = self.cfg, -(-max_tokens // page_size)
+        self.max_tokens, self.page_size = max_tokens, page_size
+        self.n_pages = n_seqs * width if n_pages is None else n_pages
+        self.pages = Pages(self.n_pages, page_size, n_seqs, max_tokens)
+        self.shared = None
+        for b in self.blocks:  # handed out uncleared
+            b["kv"] = [torch.empty((self.n_pages, c.n_heads, page_size, c.head_dim), dtype=BF16, device="cuda") for _ in "kv"]
+            b["cache"] = F.kv_cache(b["kv"][0], b["kv"][1], self.n_pages, page_size, c.n_heads, c.head_dim)
         self.max_pos = width * page_size + 1  # of any token that its table row has room for
         self.rope = torch.empty((self.max_pos, self.rdim // 2, 2), device="cuda")
         F.fl_k_rotary_table(self.max_pos, self.rdim, c.rope_base, self.rope, **_stream())
@@ -108,6 +142,13 @@ class BlockStack:
         self.context = [0] * n_seqs   # context lengths, prefix included; 0: plainly causal
         self.mask_pos = [0] * n_seqs
         torch.cuda.current_stream().synchronize()  # whichever stream uses them
+
+    def with_sequences(self, n_seqs: int) -> "BlockStack":
+        """A stack of the same weights (not copied) with caches of its own for n_seqs sequences."""
+        other = copy.copy(self)
+        other.blocks = [dict(b) for b in self.blocks]
+        other._make_room(n_seqs, self.max_tokens, self.page_size, None)
+        return other
 
     @classmethod
     def from_server(cls, srv: "F.Server", n_seqs: int, max_tokens: int, replica: Optional[int] = None, **kw):
@@ -130,6 +171,7 @@ class BlockStack:
         P = self.cfg.prefix_len
         if context_len < 0 or (context_len and mask_pos is not None and not 0 <= mask_pos < context_len):
             raise ValueError(f"a context of {context_len} tokens with its mask at {mask_pos}")
+        self._alone()
         self.pages.drop(s)
         self.context[s] = context_len + P if context_len else 0
         self.mask_pos[s] = context_len - 1 if mask_pos is None else mask_pos
@@ -138,6 +180,10 @@ class BlockStack:
                 for b in self.blocks:
                     F.fl_k_kv_append(b["cache"], batch, self.cfg.n_heads, None, *b["prefix"], None, None, 0, self.status,
                                      **_stream())
+
+    def _alone(self):
+        if self.shared is not None:
+            raise ValueError("the sequences share their pages: `follow` goes on with them")
 
     @contextlib.contextmanager
     def _extended(self, new):
@@ -180,14 +226,38 @@ class BlockStack:
                 raise ValueError(f"sequence {s} has not been started: its prefix is not there")
             if n and held < c and held + n < c:
                 raise ValueError(f"sequence {s}: {n} tokens of a context of {c - self.cfg.prefix_len}, which come in one call")
+        self._alone()
         if not any(new):
             return x.to(BF16)
         with self._extended(new) as batch:
-            return self._run(x, new, batch)
+            return self._run(x, batch, *self._positions(new))
 
-    def _run(self, x, new, batch):
-        c, T, H, Fh = self.cfg, sum(new), self.cfg.hidden, self.cfg.ffn_hidden
-        pos, pos2 = self._positions(new)
+    def follow(self, x: torch.Tensor, parents: torch.Tensor) -> torch.Tensor:
+        """x: bf16 [sequences, hidden], one token behind each; sequence s first becomes what sequence parents[s] was (device int32, -1:
+        an empty one), as a step of a beam search picks it.  Whole pages are shared, a partly filled one is copied.  From the
+        first such call on the pages are kept on the device, and ``forward`` is refused.  A call that raises
+        has spoilt the sequences."""
+        n, c = len(self.context), self.cfg
+        if not x.is_cuda or x.shape != (n, c.hidden):
+            raise ValueError(f"x {tuple(x.shape)} on {x.device} for a token of {c.hidden} behind each of {n} sequences")
+        if parents.dtype != I32 or not parents.is_cuda or parents.shape != (n,):
+            raise ValueError(f"{parents.dtype} parents {tuple(parents.shape)} on {parents.device}, not int32 [{n}] on the device")
+        if self.shared is None:
+            self.shared = SharedPages(self.pages, [b["cache"] for b in self.blocks])
+            self.shared.context, self.shared.mask = (torch.tensor(v, dtype=I32).cuda() for v in (self.context, self.mask_pos))
+        batch = self.shared.step(parents.contiguous(), self.status)
+        # as _positions, on the device; a sequence that has just begun has no prefix
+        i = (self.shared.sides[0]["lens"] - 1 - c.prefix_len).clamp(min=0)
+        first, second = i, None
+        if any(self.context):
+            own = (self.shared.context - c.prefix_len).clamp(min=0)
+            span = (own > 0) & (i >= own)
+            first = torch.where(span, self.shared.mask, i)
+            second = torch.where(span, i - own + 1, 0).to(I32)
+        return self._run(x, batch, first.to(I32), second)
+
+    def _run(self, x, batch, pos, pos2):
+        c, T, H, Fh = self.cfg, len(x), self.cfg.hidden, self.cfg.ffn_hidden
         context = torch.tensor(self.context, dtype=I32).cuda() if pos2 is not None else None
         if self.workspace is None:  # the same for every batch
             size = F.fl_k_kv_attention_workspace(c.n_heads, self.blocks[0]["cache"], batch)
@@ -250,7 +320,7 @@ class Generator:
             head = torch.zeros((-(-V // 128) * 128, H), dtype=BF16, device="cuda")  # rows in whole GEMM tiles
             head[:V] = torch.from_numpy(c.get_param(F.FL_CP_HEAD, 0)).cuda().view(V, H).to(BF16)
             self.ends.append({"embed": torch.from_numpy(c.get_param(F.FL_CP_EMBED, 0)).cuda().view(V, H).to(BF16),
-                              "head": head, "ln": [torch.from_numpy(c.get_param(F.FL_CP_FINAL_LN, t)).cuda() for t in (0, 1)]})
+                              "head": head, "eps": c.cfg.block.ln_eps, "ln": [torch.from_numpy(c.get_param(F.FL_CP_FINAL_LN, t)).cuda() for t in (0, 1)]})
         torch.cuda.current_stream().synchronize()  # whichever stream uses them
 
     def start(self, context_lens: Optional[Sequence[int]] = None):
@@ -260,15 +330,17 @@ class Generator:
             self.bottom[k].start(0, c)
             self.top[k].start(0, c)
 
+    def _head(self, e, h: torch.Tensor, z: torch.Tensor, status: torch.Tensor):
+        """fp32 logits of the rows h into z [rows, vocab in whole GEMM tiles]."""
+        T, H = h.shape
+        y, stats = torch.empty_like(h), torch.empty((2, T), device="cuda")
+        F.fl_k_layernorm_fwd(T, H, h, *e["ln"], e["eps"], y, stats[0], stats[1], **_stream())
+        F.gemm(T, z.shape[1], H, y, H, 0, e["head"], H, 0, z, z.shape[1], status=status, d_dtype=F.FL_DT_F32, **_stream())
+
     def logits(self, tokens: Sequence[torch.Tensor]) -> List[torch.Tensor]:
         """fp32 logits after each client's new tokens (int32 on the device), [vocab] of the last one.  A call that
         raises has added nothing to any part of the model."""
-        if len(tokens) != len(self.clients):
-            raise ValueError(f"tokens of {len(tokens)} clients for {len(self.clients)}")
-        for k, t in enumerate(tokens):
-            if t.dtype != I32 or not t.is_cuda or t.dim() != 1 or not len(t):
-                raise ValueError(f"client {k}: {t.dtype} tokens {tuple(t.shape)} on {t.device}, not int32 [1 or more] on the device")
-        tokens = [t.contiguous() for t in tokens]
+        tokens = self._checked(tokens)
         done = []
         try:
             return self._logits(tokens, done)
@@ -276,6 +348,14 @@ class Generator:
             for stack, new in done:
                 stack.pages.shorten(new)
             raise
+
+    def _checked(self, tokens):
+        if len(tokens) != len(self.clients):
+            raise ValueError(f"tokens of {len(tokens)} clients for {len(self.clients)}")
+        for k, t in enumerate(tokens):
+            if t.dtype != I32 or not t.is_cuda or t.dim() != 1 or not len(t):
+                raise ValueError(f"client {k}: {t.dtype} tokens {tuple(t.shape)} on {t.device}, not int32 [1 or more] on the device")
+        return [t.contiguous() for t in tokens]
 
     def _logits(self, tokens, done):
         def forward(stack, x, new):
@@ -291,12 +371,9 @@ class Generator:
         mid = forward(self.server, torch.cat(hs), new).split(new)
         out, status = [], torch.zeros(1, dtype=I32, device="cuda")
         for c, e, stack, h in zip(self.clients, self.ends, self.top, mid):
-            H, n = h.shape[1], e["head"].shape[0]
             last = forward(stack, h, [len(h)])[-1:].contiguous()
-            y, stats = torch.empty_like(last), torch.empty(2, device="cuda")
-            F.fl_k_layernorm_fwd(1, H, last, *e["ln"], c.cfg.block.ln_eps, y, stats[:1], stats[1:], **_stream())
-            z = torch.empty((1, n), device="cuda")
-            F.gemm(1, n, H, y, H, 0, e["head"], H, 0, z, n, status=status, d_dtype=F.FL_DT_F32, **_stream())
+            z = torch.empty((1, e["head"].shape[0]), device="cuda")
+            self._head(e, last, z, status)
             out.append(z[0, :c.cfg.vocab])
         if bits := int(status.item()):
             raise RuntimeError(f"generation: device status {bits} of the LM heads")
@@ -314,6 +391,93 @@ class Generator:
         return answers
 
 
+    def beam_search(self, prompts: Sequence[torch.Tensor], count: int, beams: int, eos: int = -1, length_penalty: float = 1.0,
+                    early: bool = False) -> List[List[tuple]]:
+        """The `beams` best answers of up to `count` tokens after each prompt (int32 on the device), best first: (tokens, score),
+        the score being the summed log-probability over the tokens' number to the power of length_penalty.  eos: a token that
+        ends an answer (and is its last); early: as in ``fl_beam_search``.  The prompts' sequences of ``logits`` are left as they are."""
+        n, vocab = len(self.clients), self.clients[0].cfg.vocab
+        prompts = self._checked(prompts)
+        if any(c.cfg.vocab != vocab for c in self.clients):
+            raise ValueError("the clients' vocabularies differ")
+        if count < 1 or not 1 <= beams <= F.FL_BEAM_MAX:
+            raise ValueError(f"{count} tokens with {beams} beams (1 to {F.FL_BEAM_MAX})")
+        room = min(x.max_tokens - x.cfg.prefix_len for x in (self.server, *self.bottom, *self.top))
+        if any(len(p) + count - 1 > room for p in prompts):
+            raise ValueError(f"prompts of {[len(p) for p in prompts]} tokens and {count} more in sequences of {room}")
+        # the first sequence of each client's beams has the prompt; the others follow it
+        wide = Generator.__new__(Generator)
+        wide.clients, wide.ends = self.clients, self.ends
+        wide.server = self.server.with_sequences(n * beams)
+        wide.bottom, wide.top = ([x.with_sequences(beams) for x in stacks] for stacks in (self.bottom, self.top))
+        for k, p in enumerate(prompts):
+            for stack, s in ((wide.server, k * beams), (wide.bottom[k], 0), (wide.top[k], 0)):
+                stack.start(s, len(p))
+                for b in range(1, beams):
+                    stack.context[s + b], stack.mask_pos[s + b] = stack.context[s], stack.mask_pos[s]
+        search = F.beam_search(n, beams, vocab, count, eos=eos, length_penalty=length_penalty, early=early)
+        state = {"scores": torch.full((n, beams), -float("inf"), device="cuda"),
+                 "end_scores": torch.full((n, beams), -float("inf"), device="cuda")}
+        state["scores"][:, 0] = 0
+        for name, shape in (("steps", n), ("done", n), ("end_steps", (n, beams)), ("end_beams", (n, beams))):
+            state[name] = torch.zeros(shape, dtype=I32, device="cuda")
+        now = F.beam_state(**state)
+        trace = [torch.empty((n, count, beams), dtype=I32, device="cuda") for _ in range(2)]
+        tokens, parents = (torch.empty((n, beams), dtype=I32, device="cuda") for _ in range(2))
+        workspace = torch.empty(F.fl_k_beam_workspace(search), dtype=torch.uint8, device="cuda")
+        status = torch.zeros(1, dtype=I32, device="cuda")
+        z = torch.zeros((n, beams, self.ends[0]["head"].shape[0]), device="cuda")
+        for k, row in enumerate(wide._prompted(prompts, beams)):
+            z[k, 0, :vocab] = row
+        for t in range(count):
+            F.fl_k_beam_step(search, now, now, z, *trace, tokens, parents, workspace, status, ld=z.shape[2], **_stream())
+            if t + 1 == count or bool(state["done"].all()):
+                break
+            wide._followed(tokens, parents, z, status)
+        out = (torch.empty((n, beams, count), dtype=I32, device="cuda"), torch.empty((n, beams), dtype=I32, device="cuda"),
+               torch.empty((n, beams), device="cuda"))
+        F.fl_k_beam_trace(search, now, *trace, beams, 0, *out, status, **_stream())
+        if bits := int(status.item()):
+            raise RuntimeError(f"beam search: device status {bits}")
+        words, lens, scores = (x.tolist() for x in out)
+        return [[(w[:m], x) for w, m, x in zip(words[k], lens[k], scores[k]) if m] for k in range(n)]
+
+    def _prompted(self, prompts, beams):
+        """Logits after the prompts, each in the first of its client's sequences."""
+        hs, out, status = [], [], torch.zeros(1, dtype=I32, device="cuda")
+        for c, e, stack, t in zip(self.clients, self.ends, self.bottom, prompts):
+            h = torch.empty((len(t), c.cfg.block.hidden), dtype=BF16, device="cuda")
+            F.fl_k_embedding_gather(len(t), h.shape[1], t, e["embed"], c.cfg.vocab, h, stack.status, **_stream())
+            hs.append(stack.forward(h, [len(t)] + [0] * (beams - 1)))
+        new = [n for t in prompts for n in [len(t)] + [0] * (beams - 1)]
+        mid = self.server.forward(torch.cat(hs), new).split([len(t) for t in prompts])
+        for c, e, stack, h in zip(self.clients, self.ends, self.top, mid):
+            last = stack.forward(h, [len(h)] + [0] * (beams - 1))[-1:].contiguous()
+            z = torch.empty((1, e["head"].shape[0]), device="cuda")
+            self._head(e, last, z, status)
+            out.append(z[0, :c.cfg.vocab])
+        if bits := int(status.item()):
+            raise RuntimeError(f"generation: device status {bits} of the LM heads")
+        return out
+
+    def _followed(self, tokens, parents, z, status):
+        """Logits z [clients, beams, row] after tokens [clients, beams] behind the sequences parents [clients, beams] (rows of the
+        server's stack)."""
+        beams = tokens.shape[1]
+        own = torch.where(parents < 0, -1, parents % beams).to(I32)  # rows of a client's stacks
+        hs = []
+        for k, (c, e, stack) in enumerate(zip(self.clients, self.ends, self.bottom)):
+            h = torch.empty((beams, c.cfg.block.hidden), dtype=BF16, device="cuda")
+            F.fl_k_embedding_gather(beams, h.shape[1], tokens[k], e["embed"], c.cfg.vocab, h, stack.status, **_stream())
+            hs.append(stack.follow(h, own[k]))
+        mid = self.server.follow(torch.cat(hs), parents.view(-1)).split(beams)
+        gemm_status = torch.zeros(1, dtype=I32, device="cuda")
+        for k, (e, stack, h) in enumerate(zip(self.ends, self.top, mid)):
+            self._head(e, stack.follow(h, own[k]), z[k], gemm_status)
+        if bits := int(gemm_status.item()):
+            raise RuntimeError(f"generation: device status {bits} of the LM heads")
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
     ap.add_argument("--tokens", type=int, default=16, help="tokens to answer with")
@@ -323,6 +487,8 @@ def main(argv=None):
     ap.add_argument("--blocks", type=int, default=2, help="server blocks")
     ap.add_argument("--vocab", type=int, default=1000)
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--beams", type=int, default=0, help="answers under way of a client (0: the likeliest token each time)")
+    ap.add_argument("--eos", type=int, default=-1, help="with beams: the token that ends an answer")
     a = ap.parse_args(argv)
     room = max(a.prompts) + a.tokens
     cfg, cc = F.fl_server_cfg(), F.fl_client_cfg()
@@ -336,7 +502,14 @@ def main(argv=None):
     clients = [F.Client(cc, a.seed + 1) for _ in a.prompts]  # the same model, as after averaging
     gen = torch.Generator().manual_seed(a.seed)
     prompts = [torch.randint(a.vocab, (n,), generator=gen, dtype=I32).cuda() for n in a.prompts]
-    answers = Generator(clients, F.Server(cfg, a.seed), room).greedy(prompts, a.tokens)
+    generator = Generator(clients, F.Server(cfg, a.seed), room)
+    if a.beams:
+        found = generator.beam_search(prompts, a.tokens, a.beams, a.eos)
+        for k, best in enumerate(found):
+            for tokens, score in best:
+                print(f"client {k} ({a.prompts[k]} tokens), {score:.4f}: {' '.join(map(str, tokens))}")
+        return found
+    answers = generator.greedy(prompts, a.tokens)
     for k, x in enumerate(answers):
         print(f"client {k} ({a.prompts[k]} tokens): {' '.join(map(str, x))}")
     return answers

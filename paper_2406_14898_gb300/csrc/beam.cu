@@ -230,11 +230,10 @@ struct Sum {
 struct Join {
   Cand best[FL_BEAM_MAX][FL_BEAM_MAX];
   Two score[FL_BEAM_MAX][FL_BEAM_MAX];  // of each beam's candidates
-  uint64_t few[FL_BEAM_MAX * FL_BEAM_MAX];
-  int few_at[FL_BEAM_MAX * FL_BEAM_MAX], few_n, any_end;
-  Two live[FL_BEAM_MAX], ends[FL_BEAM_MAX], minus_log[FL_BEAM_MAX], length;
-  float m[FL_BEAM_MAX], from[FL_BEAM_MAX], end_x[FL_BEAM_MAX], pool[2 * FL_BEAM_MAX];
-  int pool_step[2 * FL_BEAM_MAX], pool_beam[2 * FL_BEAM_MAX], end_rank[FL_BEAM_MAX];
+  uint64_t key[FL_BEAM_MAX][FL_BEAM_MAX];  // their order64; 0: none
+  Two live[FL_BEAM_MAX], ends[FL_BEAM_MAX], length;
+  float end_x[FL_BEAM_MAX], pool[2 * FL_BEAM_MAX];
+  int pool_step[2 * FL_BEAM_MAX], pool_beam[2 * FL_BEAM_MAX];
   int token[FL_BEAM_MAX], parent[FL_BEAM_MAX];
 };
 
@@ -280,7 +279,13 @@ __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a)
   const int B = a.p.beams, threads = blockDim.x, s = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int t = a.from.steps[s];  // (no read-only loads of the state: `to` may be the same memory)
   const bool active = a.from.done[s] == 0 && t >= 0 && t < a.p.max_steps;
-  if (tid == 0) j.few_n = j.any_end = 0;
+  float pool_score = -INFINITY;  // what had ended, for the last warp's work
+  int pool_step = 0, pool_beam = 0;
+  if (tid < B) {
+    pool_score = a.from.end_scores[s * B + tid];
+    pool_step = a.from.end_steps[s * B + tid];
+    pool_beam = a.from.end_beams[s * B + tid];
+  }
   if (warp < B) {
     const int b = warp, row = s * B + b;
     const float score = a.from.scores[row];
@@ -324,129 +329,119 @@ __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a)
         next = at + 1 < stop ? mine[at + 1] : Cand{-INFINITY, 0};
       }
     }
-    if (lane >= k && lane < B) j.best[b][lane] = Cand{-INFINITY, 0};
+    __syncwarp();
+    // c = score + ((x - m) - log(sum)): exact for the smallest logits that a type has, too
+    const Two l = live ? log_two(sum) : Two{0.f, 0.f};
+    const auto c_of = [&](float x) {
+      return x > -INFINITY ? add(add(two_sum(x, -m), Two{-l.hi, -l.lo}), score) : Two{-INFINITY, 0.f};
+    };
+    const Cand one = lane < k ? j.best[b][lane] : Cand{-INFINITY, 0};
+    const Two c = c_of(one.x);
+    // a row's candidates stay in their order where their c differ by less than these numbers resolve
+    uint64_t key = order64(c);
+#pragma unroll
+    for (int d = 1; d < FL_BEAM_MAX; d <<= 1) {
+      const uint64_t y = __shfl_up_sync(0xffffffffu, key, d);
+      if (lane >= d) key = min(key, y);
+    }
+    if (lane < B) {
+      j.best[b][lane] = one;
+      j.score[b][lane] = c;
+      j.key[b][lane] = key;
+    }
     if (lane == 0) {
-      const Two l = live ? log_two(sum) : Two{0.f, 0.f};
-      j.minus_log[b] = {-l.hi, -l.lo};
-      j.m[b] = m;
-      j.from[b] = score;
       j.end_x[b] = live ? e : -INFINITY;
+      const Two end = c_of(j.end_x[b]);
+      j.ends[b] = order64(end) ? end : Two{-INFINITY, 0.f};
       j.token[b] = max(a.p.eos, 0);
       j.parent[b] = -1;
       j.live[b] = {-INFINITY, 0.f};
     }
   }
-  __syncthreads();
-  if (!active) {  // it stays as it is
-    if (warp == 0) rest(a, s);
-    return;
-  }
-  // c = score + ((x - m) - log(sum)): exact for the smallest logits that a type has, too
-  for (int i = tid; i < B * B + B; i += threads) {
-    const int b = i < B * B ? i / B : i - B * B, k = i % B;
-    const float x = i < B * B ? j.best[b][k].x : j.end_x[b];
-    const Two c = add(add(two_sum(x, -j.m[b]), j.minus_log[b]), j.from[b]);
-    (i < B * B ? j.score[b][k] : j.ends[b]) = x > -INFINITY ? c : Two{-INFINITY, 0.f};
-  }
   if (tid == threads - 1) j.length = pow_two((float)(t + 1), {a.penalty_hi, a.penalty_lo});
   __syncthreads();
-  // A row's last candidate bounds the search's last: only what reaches the best of those bounds is ranked, by counting who comes
-  // before: by c, then the lower beam, then the order within the beam.
-  uint64_t bound = 1;
-  for (int b = 0; b < B; ++b) bound = max(bound, order64(j.score[b][B - 1]));
-  for (int i = tid; i < B * B; i += threads) {
-    const uint64_t c = order64(j.score[i / B][i % B]);
-    if (c >= bound) {
-      const int n = atomicAdd(&j.few_n, 1);
-      j.few[n] = c;
-      j.few_at[n] = i;
-    }
+  if (warp != 0) return;
+  if (!active) {  // it stays as it is
+    rest(a, s);
+    return;
   }
-  __syncthreads();
-  const int n = j.few_n;
-  for (int i = tid; i < n; i += threads) {
-    const uint64_t c = j.few[i];
-    const int at = j.few_at[i];
-    int rank = 0;
-    for (int o = 0; o < n; ++o) rank += j.few[o] > c || (j.few[o] == c && j.few_at[o] < at);
-    if (rank < B) {
-      j.token[rank] = j.best[at / B][at % B].v;
-      j.parent[rank] = at / B;
-      j.live[rank] = j.score[at / B][at % B];
-    }
+  // The rows' lists merged: lanes 0 to 15 have a beam's list each, the others a beam's eos.  The best one of all comes next, until
+  // there are B that go on; an eos among the first B ends a hypothesis.
+  const int beam = lane % FL_BEAM_MAX;
+  const bool is_eos = lane >= FL_BEAM_MAX;
+  uint64_t key = 0, next = 0;
+  if (beam < B) {
+    key = is_eos ? order64(j.ends[beam]) : j.key[beam][0];
+    if (!is_eos && B > 1) next = j.key[beam][1];
   }
-  const int b = tid - (threads - 32);  // the hypotheses that end
-  if (b >= 0 && b < B) {
-    const uint64_t c = order64(j.ends[b]);
-    int rank = -1;
-    if (c >= bound) {
-      const Cand e{j.end_x[b], a.p.eos};
-      rank = 0;
-      for (int o = 0; o < n; ++o) {
-        const int ob = j.few_at[o] / B;
-        rank += ob == b ? better(j.best[ob][j.few_at[o] % B], e) : j.few[o] > c || (j.few[o] == c && ob < b);
-      }
-      for (int o = 0; o < B; ++o) {
-        const uint64_t y = order64(j.ends[o]);
-        rank += y > c || (y == c && o < b);
-      }
-      if (rank < B) j.any_end = 1;
-      else rank = -1;
+  int at = 0, n_live = 0, end_rank = -1;
+#pragma unroll 1
+  for (int rank = 0; n_live < B; ++rank) {
+    const uint32_t hi = (uint32_t)(key >> 32), top = __reduce_max_sync(0xffffffffu, hi);
+    if (top == 0) break;
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, hi == top ? (uint32_t)key : 0u);
+    const unsigned who = __ballot_sync(0xffffffffu, hi == top && (uint32_t)key == lo);
+    int w = __ffs(who) - 1;
+    if (who & (who - 1)) {  // equal: the lower beam; of one beam the better of the list's and the eos
+      const Cand mine = beam >= B || key == 0 ? Cand{-INFINITY, 0} : is_eos ? Cand{j.end_x[beam], a.p.eos} : j.best[beam][at];
+      const Cand other{__shfl_xor_sync(0xffffffffu, mine.x, FL_BEAM_MAX), __shfl_xor_sync(0xffffffffu, mine.v, FL_BEAM_MAX)};
+      const int order = who >> lane & 1 ? 2 * beam + better(other, mine) : 0x7fffffff;
+      const int first = __reduce_min_sync(0xffffffffu, order);
+      w = __ffs(__ballot_sync(0xffffffffu, order == first)) - 1;
     }
-    j.end_rank[b] = rank;
+    if (lane == w) {
+      if (is_eos) {
+        if (rank < B) end_rank = rank;
+        key = 0;
+      } else {
+        j.token[n_live] = j.best[beam][at].v;
+        j.parent[n_live] = beam;
+        j.live[n_live] = j.score[beam][at];
+        ++at;
+        key = next;
+        next = at + 1 < B ? j.key[beam][at + 1] : 0;
+      }
+    }
+    n_live += w < FL_BEAM_MAX;
   }
   // the pool: what had ended, then what ends now in the order of its rank
-  if (warp == 0) {
-    float x = -INFINITY;
-    int step = 0, beam = 0;
-    if (lane < B) {
-      x = a.from.end_scores[s * B + lane];
-      step = a.from.end_steps[s * B + lane];
-      beam = a.from.end_beams[s * B + lane];
+  float x = pool_score;
+  int step = pool_step, from_beam = pool_beam;
+  if (!(x > -INFINITY)) x = -INFINITY, step = from_beam = 0;
+  if (__any_sync(0xffffffffu, end_rank >= 0)) {
+    if (end_rank >= 0) {
+      x = div_two(j.ends[beam], j.length);
+      step = t;
+      from_beam = beam;
     }
-    if (!(x > -INFINITY)) x = -INFINITY, step = beam = 0;
-    j.pool[lane] = x;  // (kept here over the barrier)
-    j.pool_step[lane] = step;
-    j.pool_beam[lane] = beam;
+    const int order = end_rank >= 0 ? FL_BEAM_MAX + end_rank : lane;
+    const uint64_t place = (uint64_t)order32(x) << 32 | (uint32_t)((63 - order) << 8 | (31 - lane));
+    int rank = 0;
+#pragma unroll 8
+    for (int o = 0; o < 32; ++o) rank += __shfl_sync(0xffffffffu, place, o) > place;
+    j.pool[rank] = x;
+    j.pool_step[rank] = step;
+    j.pool_beam[rank] = from_beam;
+    __syncwarp();
+    x = j.pool[lane], step = j.pool_step[lane], from_beam = j.pool_beam[lane];
   }
-  __syncthreads();
-  if (warp == 0) {
-    if (j.any_end) {
-      const int pb = lane - FL_BEAM_MAX;
-      float x = j.pool[lane];
-      int step = j.pool_step[lane], beam = j.pool_beam[lane], order = lane;
-      if (pb >= 0 && pb < B && j.end_rank[pb] >= 0) {
-        x = div_two(j.ends[pb], j.length);
-        step = t;
-        beam = pb;
-        order = FL_BEAM_MAX + j.end_rank[pb];
-      }
-      const uint64_t key = (uint64_t)order32(x) << 32 | (uint32_t)((63 - order) << 8 | (31 - lane));
-      int rank = 0;
-#pragma unroll 4
-      for (int o = 0; o < 32; ++o) rank += __shfl_sync(0xffffffffu, key, o) > key;
-      j.pool[rank] = x;
-      j.pool_step[rank] = step;
-      j.pool_beam[rank] = beam;
-      __syncwarp();
-    }
-    if (lane < B) {
-      const int i = s * B + lane;
-      const int64_t tr = ((int64_t)s * a.p.max_steps + t) * B + lane;
-      a.to.scores[i] = j.live[lane].hi;
-      a.to.end_scores[i] = j.pool[lane];
-      a.to.end_steps[i] = j.pool_step[lane];
-      a.to.end_beams[i] = j.pool_beam[lane];
-      a.tokens[i] = a.trace_tokens[tr] = j.token[lane];
-      a.trace_parents[tr] = j.parent[lane] < 0 ? lane : j.parent[lane];
-      a.parents[i] = j.parent[lane] < 0 ? -1 : s * B + j.parent[lane];
-    }
-    if (lane == 0) {
-      const float worst = j.pool[B - 1];
-      const bool none = !(j.live[0].hi > -INFINITY);
-      a.to.steps[s] = t + 1;
-      a.to.done[s] = none || (worst > -INFINITY && (a.p.early || worst >= div_two(j.live[0], j.length)));
-    }
+  __syncwarp();
+  const float worst = __shfl_sync(0xffffffffu, x, B - 1);
+  if (lane < B) {
+    const int i = s * B + lane, parent = j.parent[lane], token = j.token[lane];
+    const int64_t tr = ((int64_t)s * a.p.max_steps + t) * B + lane;
+    a.to.scores[i] = j.live[lane].hi;
+    a.to.end_scores[i] = x;
+    a.to.end_steps[i] = step;
+    a.to.end_beams[i] = from_beam;
+    a.tokens[i] = a.trace_tokens[tr] = token;
+    a.trace_parents[tr] = parent < 0 ? lane : parent;
+    a.parents[i] = parent < 0 ? -1 : s * B + parent;
+  }
+  if (lane == 0) {
+    const bool none = !(j.live[0].hi > -INFINITY);
+    a.to.steps[s] = t + 1;
+    a.to.done[s] = none || (worst > -INFINITY && (a.p.early || worst >= div_two(j.live[0], j.length)));
   }
 }
 
@@ -466,7 +461,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
                 "so many CTAs fit an SM, which keeps 1 KB of each");
   __shared__ __align__(16) uint32_t sh_group[2][GROUPS], sh_key[2][GROUPS];
   __shared__ float sh_ref[WARPS], sh_sum[WARPS];
-  __shared__ int sh_count, sh_warp[WARPS];
+  __shared__ int sh_count, sh_few, sh_warp[WARPS];
   __shared__ uint32_t sh_bits[THREADS];
   __shared__ int sh_rows[MAX_ROWS];
   __shared__ Cand sh_hits[MAX_HITS];
@@ -481,15 +476,23 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
     ctas = (int)min((int64_t)gridDim.x, L <= MAX_PARTS ? chunks : (int64_t)(MAX_PARTS - 2) * n);  // no row in more than MAX_PARTS
     c0 = c1 = 0;
     if ((int)blockIdx.x >= ctas) return;
-    c0 = (int)kv_div(blockIdx.x * chunks, ctas);
-    c1 = (int)kv_div((blockIdx.x + 1) * chunks, ctas);
+    const bool one = ctas == chunks;  // a chunk each
+    c0 = one ? (int)blockIdx.x : (int)kv_div(blockIdx.x * chunks, ctas);
+    c1 = one ? c0 + 1 : (int)kv_div((blockIdx.x + 1) * chunks, ctas);
   };
-  const auto live = [&](int row) {
-    // (no read-only loads of the state: `to` may be the same memory; no load behind another's outcome)
-    const int s = row / B, t = a.from.steps[s], done = a.from.done[s];
-    const float score = a.from.scores[row];
+  // (no read-only loads of the state: `to` may be the same memory; no load behind another's outcome)
+  const auto is_live = [&](int t, int done, float score) {
     return (done == 0) & (t >= 0) & (t < a.p.max_steps) & (score > -INFINITY) & (score < INFINITY);
   };
+  // the first rows' states are asked for ahead of the logits
+  constexpr int EARLY = 8;
+  int early_t[EARLY], early_done[EARLY];
+  float early_score[EARLY];
+#pragma unroll
+  for (int i = 0; i < EARLY; ++i) {
+    const int row = tid + i * THREADS, s = row / B;
+    if (row < rows) early_t[i] = a.from.steps[s], early_done[i] = a.from.done[s], early_score[i] = a.from.scores[row];
+  }
   // what is asked for next: a chunk of the line, its row, its first piece; the stage that it goes to
   int ask = 0, ask_first = 0, ask_stage = 0;
   const uint4* ask_x = nullptr;
@@ -508,22 +511,46 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
     ask_first += CHUNK_PIECES;
     ask_stage = ask_stage + 1 == STAGES ? 0 : ask_stage + 1;
   };
-  // The first chunk as it is if all beams are live, before that is known: one latency less.
-  cut(rows);
-  if (c0 < c1) {
+  bool known = false;  // which rows are live; until then, and where all are, the k-th of them is row k
+  int k0 = 0;
+  const auto ask_more = [&] {  // one group each time, an empty one behind the last chunk
+    if (ask < c1) {
+      if (ask_first >= all) {
+        ask_first = 0;
+        ask_row(known ? sh_rows[ask / L - k0] : ask / L);
+      }
+      ask_chunk();
+    }
+    cp_async_commit();
+  };
+  const auto ask_first_ones = [&] {
     ask = c0;
     ask_first = c0 % L * CHUNK_PIECES;
-    ask_row(c0 / L);
-    ask_chunk();
-  }
-  cp_async_commit();
+    ask_stage = 0;
+    ask_row(known ? sh_rows[0] : c0 / L);
+    ask_more();
+    ask_more();
+  };
+  // The first chunks as they are if all beams are live, before that is known.
+  cut(rows);
+  ask_first_ones();
   // which rows are live, a bit each, 32 x THREADS of them at a time; how many, and those of this CTA's piece
+  const auto set_bits = [&](int row, bool x) {
+    const uint32_t m = __ballot_sync(0xffffffffu, x);
+    if (lane == 0) sh_bits[row / 32 % THREADS] = m;
+  };
   const auto bits = [&](int base) {
-#pragma unroll 8
-    for (int r = base + tid; r < min(rows + 31 & ~31, base + 32 * THREADS); r += THREADS) {
-      const bool x = r < rows && live(r);
-      const uint32_t m = __ballot_sync(0xffffffffu, x);
-      if (lane == 0) sh_bits[(r - base) / 32] = m;
+    if (base == 0) {
+#pragma unroll
+      for (int i = 0; i < EARLY; ++i) {
+        const int r = tid + i * THREADS;
+        set_bits(r, r < rows && is_live(early_t[i], early_done[i], early_score[i]));
+      }
+    }
+#pragma unroll 4
+    for (int r = base + (base == 0 ? EARLY * THREADS : 0) + tid; r < min(rows + 31 & ~31, base + 32 * THREADS); r += THREADS) {
+      const int row = min(r, rows - 1), s = row / B;
+      set_bits(r, r < rows && is_live(a.from.steps[s], a.from.done[s], a.from.scores[row]));
     }
     __syncthreads();
   };
@@ -552,7 +579,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
   }
   const bool guessed = total == rows;
   if (!guessed) cut(total);
-  const int k0 = c0 / L, k1 = c0 < c1 ? (c1 - 1) / L : -1;  // its first and last live row
+  k0 = c0 / L;
+  const int k1 = c0 < c1 ? (c1 - 1) / L : -1;  // its first and last live row are k0 and k1
   const bool again = rows > 32 * THREADS;                   // the bits and counts are those of the last rows only
   if (again) total = 0;
   for (int base = 0; base < rows; base += 32 * THREADS) {
@@ -572,26 +600,14 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
     cp_async_wait<0>();
     return;
   }
-  const auto ask_more = [&] {  // one group each time, an empty one behind the last chunk
-    if (ask < c1) {
-      if (ask_first >= all) {
-        ask_first = 0;
-        ask_row(sh_rows[ask / L - k0]);
-      }
-      ask_chunk();
-    }
-    cp_async_commit();
-  };
+  known = true;
+  if (!guessed) {  // the first chunks came for nothing
+    cp_async_wait<0>();
+    ask_first_ones();
+  }
   int stage = 0, raised = 0;
   // with few beams little comes between two raises, so that each costs more than it saves
   const int often = B > 4 ? ~0 : 0x55555555;
-  if (!guessed) {  // the first chunk came for nothing, if one did
-    stage = ask_stage = 1;
-    ask = c0;
-    ask_first = c0 % L * CHUNK_PIECES;
-    ask_row(sh_rows[0]);
-    ask_more();
-  }
   static_assert(STAGES == 2);
   for (int c = c0; c < c1;) {
     {
@@ -599,17 +615,46 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
       c += to - from;
       const int begin = from * CHUNK_PIECES, end = min(all, to * CHUNK_PIECES);
       // which part of its row: its CTA's distance from the one of the row's first chunk
-      const int part = blockIdx.x - (int)kv_div(((int64_t)k * L + 1) * ctas - 1, (int64_t)n_live * L);
+      const int part = ctas == (int64_t)n_live * L ? from : blockIdx.x - (int)kv_div(((int64_t)k * L + 1) * ctas - 1, (int64_t)n_live * L);
       const int64_t at_part = (int64_t)row * MAX_PARTS + part;
       const int eos_piece = a.p.eos >= 0 && a.p.eos / N >= begin && a.p.eos / N < end ? a.p.eos / N : -1;
       Sum z;
       float bound = -INFINITY, most = -INFINITY;  // of this thread
-      if (tid == 0) sh_count = 0;
+      bool settled = false;                       // the bound is that of all that has been seen
+      if (tid == 0) sh_count = sh_few = 0;
+      // the bound raised to the B-th largest of the groups' maxima, with a barrier; true where it is higher now
+      const auto raise = [&] {
+        float g = most;
+#pragma unroll
+        for (int d = 1; d < THREADS / GROUPS; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
+        uint32_t* keys = sh_key[raised & 1];
+        if (tid % (THREADS / GROUPS) == 0) {
+          const int i = tid / (THREADS / GROUPS);
+          sh_group[raised & 1][i] = order32(g);
+          keys[i] = (order32(g) & ~31u) | (31 - i);
+        }
+        __syncthreads();
+        // (numbers that agree in all but their last bits count as equal, the lower group first: the B groups that are taken have
+        // maxima of the bound and more whichever they are)
+        const uint32_t key = keys[lane], ordered = sh_group[raised & 1][lane];
+        ++raised;
+        int rank = 0;
+#pragma unroll
+        for (int o = 0; o < GROUPS; o += 4) {
+          const uint4 y = *reinterpret_cast<const uint4*>(keys + o);
+          rank += (y.x > key) + (y.y > key) + (y.z > key) + (y.w > key);
+        }
+        const float b = unorder32(__reduce_min_sync(0xffffffffu, rank < B ? ordered : 0xffffffffu));
+        z.see(unorder32(__reduce_max_sync(0xffffffffu, ordered)));
+        const bool higher = b > bound;
+        bound = b;
+        settled = true;
+        return higher;
+      };
       for (int first = begin, chunk = 0; first < end; first += CHUNK_PIECES, ++chunk) {
-        cp_async_wait<STAGES - 2>();
+        cp_async_wait<STAGES - 1>();
         uint4* places = sh_ring + stage * CHUNK_PIECES + tid;  // this thread's
         stage = stage + 1 == STAGES ? 0 : stage + 1;
-        ask_more();  // into the stage before, which was read a chunk ago
         // nothing behind the slice's end and the vocabulary; the eos is summed, but no candidate to go on with
         if (first + CHUNK_PIECES >= end) {
 #pragma unroll 1
@@ -641,34 +686,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
         most = fmaxf(most, top);
         bool equals = false;  // whether logits equal to the bound count: it is new, and fewer than B larger ones may have been seen
         const int seen = chunk + 1;
-        if ((seen & chunk) == 0 && (seen & often)) {
-          // each time that what has been seen doubles (quadruples): the B-th largest of the groups' maxima, and the largest
-          float g = most;
-#pragma unroll
-          for (int d = 1; d < THREADS / GROUPS; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
-          uint32_t* keys = sh_key[raised & 1];
-          if (tid % (THREADS / GROUPS) == 0) {
-            const int i = tid / (THREADS / GROUPS);
-            sh_group[raised & 1][i] = order32(g);
-            keys[i] = (order32(g) & ~31u) | (31 - i);
-          }
-          __syncthreads();
-          // (numbers that agree in all but their last bits count as equal, the lower group first: the B groups that are taken have
-          // maxima of the bound and more whichever they are)
-          const uint32_t key = keys[lane], ordered = sh_group[raised & 1][lane];
-          ++raised;
-          int rank = 0;
-#pragma unroll
-          for (int o = 0; o < GROUPS; o += 4) {
-            const uint4 y = *reinterpret_cast<const uint4*>(keys + o);
-            rank += (y.x > key) + (y.y > key) + (y.z > key) + (y.w > key);
-          }
-          const uint32_t low = __reduce_min_sync(0xffffffffu, rank < B ? ordered : 0xffffffffu);
-          const float b = unorder32(low);
-          equals = chunk == 0 || b > bound;
-          bound = b;
-          z.see(unorder32(__reduce_max_sync(0xffffffffu, ordered)));
-        }
+        settled = false;
+        if ((seen & chunk) == 0 && (seen & often)) equals = raise() || chunk == 0;
         const bool look = top > -INFINITY && (equals ? top >= bound : top > bound);
         if (look) z.see(top);
         if (!z.far()) {
@@ -699,6 +718,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
               }
           }
         }
+        ask_more();  // into the stage that has been read
       }
       float ref = z.ref;
 #pragma unroll
@@ -707,9 +727,37 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
 #pragma unroll
       for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
       if (lane == 0) sh_ref[warp] = ref, sh_sum[warp] = sum;
-      __syncthreads();
-      // the slice's list: what has come together, ranked by counting
-      const int n = sh_count;
+      // The part's list: of what has come together, what reaches the bound of the whole part, ranked by counting.
+      const bool early = !settled;
+      if (early) raise();
+      else __syncthreads();
+      int n = sh_count;
+      const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld);
+      if (n > MAX_HITS) {
+        // more than there was room for (logits that ascend): once more through the part, with that bound
+        __syncthreads();
+        if (tid == 0) sh_count = 0;
+        __syncthreads();
+        for (int k = begin + tid; k < end; k += THREADS) {
+          float f[N];
+          Io::get(__ldg(x + k), f);
+          for (int e = 0; e < N; ++e)
+            if (f[e] >= bound && f[e] > -INFINITY && k * N + e < a.p.vocab && k * N + e != a.p.eos) {
+              const int at = atomicAdd(&sh_count, 1);
+              if (at < MAX_HITS) sh_hits[at] = Cand{f[e], k * N + e};
+            }
+        }
+        __syncthreads();
+        n = sh_count;
+      } else if (early && n > 32) {
+        static_assert(MAX_HITS == 2 * THREADS);
+        const Cand h0 = sh_hits[tid], h1 = sh_hits[tid + THREADS];
+        __syncthreads();
+        if (tid < n && h0.x >= bound) sh_hits[atomicAdd(&sh_few, 1)] = h0;
+        if (tid + THREADS < n && h1.x >= bound) sh_hits[atomicAdd(&sh_few, 1)] = h1;
+        __syncthreads();
+        n = sh_few;
+      }
       Cand* list = a.lists + at_part * B;
       if (n <= MAX_HITS) {
         for (int i = tid; i < n; i += THREADS) {
@@ -720,8 +768,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
         }
         if (tid >= n && tid < B) list[tid] = Cand{-INFINITY, 0};
       } else {
-        // more than there is room for (logits that ascend, many equal ones): the best one behind the last found, B times
-        const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld);
+        // many equal logits: the best one behind the last found, B times
         Cand found{INFINITY, -1};
         for (int r = 0; r < B; ++r) {
           Cand one{-INFINITY, 0x7fffffff};

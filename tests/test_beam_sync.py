@@ -39,16 +39,20 @@ def test_a_units_places_are_not_written_before_they_were_read():
     """The hits of a unit lie behind a barrier when they are ranked, and a barrier divides that from the next unit's."""
     src = _code("beam.cu")
     kernel = src[src.index("beam_step_kernel(StepArgs a)"):src.index("int64_t part_bytes(")]
-    _in_order(kernel, "if (tid == 0) sh_count = 0;", "__syncthreads()", "atomicAdd(&sh_count, 1)", "sh_sum[warp] = sum", "__syncthreads()",
-              "const int n = sh_count", "a.sums[", "__syncthreads()")
+    _in_order(kernel, "if (tid == 0) sh_count = sh_few = 0;", "const auto raise =", "__syncthreads()", "equals = raise()", "atomicAdd(&sh_count, 1)",
+              "sh_sum[warp] = sum", "if (early) raise();", "__syncthreads()", "int n = sh_count", "a.sums[", "__syncthreads()")
 
 
 def test_a_place_is_read_before_it_is_asked_for_again():
     """A chunk's group has arrived before its places are read; the next request goes to another stage."""
     src = _code("beam.cu")
-    loop = src[src.index("for (int first = begin, chunk = 0;"):src.index("uint4 cur[PIECES];")]
-    _in_order(loop, "cp_async_wait<STAGES - 2>()", "places = sh_ring + stage * CHUNK_PIECES + tid", "ask_more()")
+    loop = src[src.index("for (int first = begin, chunk = 0;"):src.index("float ref = z.ref;")]
+    _in_order(loop, "cp_async_wait<STAGES - 1>()", "places = sh_ring + stage * CHUNK_PIECES + tid", "cur[i] = places", "Io::get(places[",
+              "ask_more()")
     assert "static_assert(STAGES == 2);" in src
+    first = src[src.index("const auto ask_first_ones"):src.index("cut(rows);")]
+    assert first.count("ask_more();") == 2  # a group for each stage before the loop
+    _in_order(src, "if (!guessed) {", "cp_async_wait<0>()", "ask_first_ones()")
 
 
 def test_plan_phases_are_divided_by_the_clusters_barrier():

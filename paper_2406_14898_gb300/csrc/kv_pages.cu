@@ -25,7 +25,6 @@ struct PagesDev {
 // A workspace: what the plan tells the second launch, and the cluster's counts of each page, which are zero between calls.
 struct Ws {
   int32_t* head;                      // copies, refused
-  int4* totals;                       // of each CTA of the plan: pages wanted, copies, free pages, refused
   int32_t *delta, *writers, *lowest;  // zero between calls: holders more or less, sequences about to write, S - the first
   int4* rows;                         // of each sequence: parent, pages shared with it, place of its first new page, pages
   int32_t* first;                     // of each sequence: its first new page's place in `list`
@@ -40,7 +39,6 @@ int64_t ws_layout(int32_t* base, int64_t S, int64_t n_pages, Ws* w) {
   w->writers = take(n_pages);
   w->lowest = take(n_pages);
   w->head = take(4);
-  w->totals = (int4*)take(4 * MAX_PLAN_CTAS);
   w->rows = (int4*)take(4 * S);
   w->first = take(S);
   w->list = take(n_pages);
@@ -85,6 +83,20 @@ FL_DEV Row row_of(const PagesDev& a, const int32_t* parents, const int32_t* grow
     else r.bad = true;
   }
   return r;
+}
+
+// Four numbers of CTA `rank` of the cluster, from the same place in its shared memory.
+FL_DEV int4 ld_cluster_int4(const int4* p, uint32_t rank) {
+  int4 v;
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(mapa_shared(smem_u32(p), rank))
+               : "memory");
+  return v;
+}
+FL_DEV int4 shfl_int4(int4 v, int lane) {
+  return make_int4(__shfl_sync(0xffffffffu, v.x, lane), __shfl_sync(0xffffffffu, v.y, lane), __shfl_sync(0xffffffffu, v.z, lane),
+                   __shfl_sync(0xffffffffu, v.w, lane));
 }
 
 // Exclusive prefix sums of x and y over the block's threads, and the block's sums.
@@ -151,6 +163,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, con
   __shared__ Pair sh[32];
   __shared__ int4 sh_changed[PLAN_THREADS];  // sequence, parent, pages shared with it, pages that the sequence had
   __shared__ int sh_n, sh_longest, sh_refuse;
+  __shared__ int4 sh_totals;  // of this CTA: pages wanted, copies, free pages, refused
   extern __shared__ int32_t sh_counts[];
   const int rank = ONE ? 0 : cluster_ctarank(), ctas = ONE ? 1 : cluster_nctarank(), tid = threadIdx.x, lane = tid & 31;
   const Counts<ONE> of(a, w, sh_counts);
@@ -219,10 +232,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, con
   }
   if (!ONE) cluster_sync();
   // What each sequence wants, and what is free: this CTA's part of both, a warp's pages one after another.
-  const int per = (a.S + ctas - 1) / ctas, s0 = min(a.S, rank * per), s1 = min(a.S, s0 + per);
+  const bool kept = tiles <= 1;  // every CTA has every sequence's Row: the first one goes on with them
+  const int per = kept ? a.S : (a.S + ctas - 1) / ctas, s0 = min(a.S, rank * per), s1 = min(a.S, s0 + per);
   const int wper = (a.n_pages + ctas * 32 - 1) / (ctas * 32), q0 = min(a.n_pages, (rank * 32 + (tid >> 5)) * wper),
             q1 = min(a.n_pages, q0 + wper);
-  const auto row = [&](int s) { return ONE ? mine : row_of(a, parents, grow, s); };
+  const auto row = [&](int s) { return kept ? mine : row_of(a, parents, grow, s); };
   const auto copied = [&](const Row& r, int s) {
     return r.last >= 0 && !(of.holders(r.last) == of.writers(r.last) && of.first_writer(r.last) == s);
   };
@@ -240,11 +254,12 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, con
   int64_t all_wanted = (int64_t)(total.x >> 32), all_free = total.y, wanted0 = 0, free0 = 0;
   int copies = (int)(uint32_t)total.x, copies0 = 0, refuse = sh_refuse;
   if (!ONE) {
-    if (tid == 0) __stcg(w.totals + rank, make_int4((int)all_wanted, copies, (int)all_free, refuse));
+    if (tid == 0) sh_totals = make_int4((int)all_wanted, copies, (int)all_free, refuse);
     cluster_sync();
+    const int4 totals = ld_cluster_int4(&sh_totals, min(lane, ctas - 1));
     all_wanted = all_free = refuse = copies = 0;
     for (int c = 0; c < ctas; ++c) {
-      const int4 t = __ldcg(w.totals + c);
+      const int4 t = shfl_int4(totals, c);
       if (c == rank) wanted0 = all_wanted, free0 = all_free, copies0 = copies;
       all_wanted += t.x;
       all_free += t.z;
@@ -306,6 +321,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, 
   pdl_wait();
   pdl_trigger();
   __shared__ Pair sh[32];
+  __shared__ int4 sh_all, sh_stay;  // of this CTA
   const int rank = ONE ? 0 : cluster_ctarank(), ctas = ONE ? 1 : cluster_nctarank(), tid = threadIdx.x, lane = tid & 31;
   // a warp's pages one after another
   const int wper = (a.n_pages + ctas * 32 - 1) / (ctas * 32), q0 = min(a.n_pages, (rank * 32 + (tid >> 5)) * wper),
@@ -316,12 +332,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, 
   for (int q = q0; q < q1; q += 32) n += __popc(busy(q));
   int before = (int)__shfl_sync(0xffffffffu, block_scan(Pair{0, lane == 0 ? n : 0}, sh, &total).y, 0), all = (int)total.y;
   if (!ONE) {
-    if (tid == 0) __stcg(&w.totals[rank].x, all);
+    if (tid == 0) sh_all = make_int4(all, 0, 0, 0);
     cluster_sync();
+    const int of = ld_cluster_int4(&sh_all, min(lane, ctas - 1)).x;
     all = 0;
     for (int c = 0; c < ctas; ++c) {
       if (c == rank) before += all;
-      all += __ldcg(&w.totals[c].x);
+      all += __shfl_sync(0xffffffffu, of, c);
     }
   }
   // the pages in use among the first `all` stay
@@ -330,10 +347,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, 
   block_scan(Pair{0, lane == 0 ? n : 0}, sh, &total);
   int stay = (int)total.y;
   if (!ONE) {
-    if (tid == 0) __stcg(&w.totals[rank].y, stay);
+    if (tid == 0) sh_stay = make_int4(stay, 0, 0, 0);
     cluster_sync();
+    const int of = ld_cluster_int4(&sh_stay, min(lane, ctas - 1)).x;
     stay = 0;
-    for (int c = 0; c < ctas; ++c) stay += __ldcg(&w.totals[c].y);
+    for (int c = 0; c < ctas; ++c) stay += __shfl_sync(0xffffffffu, of, c);
   }
   const int moves = all - stay;
   if (rank == 0 && tid == 0) {

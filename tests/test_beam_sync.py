@@ -58,8 +58,8 @@ def test_a_place_is_read_before_it_is_asked_for_again():
 def test_plan_phases_are_divided_by_the_clusters_barrier():
     src = _code("kv_pages.cu")
     fork = src[src.index("fork_plan_kernel("):src.index("compact_plan_kernel(")]
-    _in_order(fork, "atomicMax(of.lowest", "cluster_sync()", "of.first_writer(r.last)", "__stcg(w.totals", "cluster_sync()",
-              "__ldcg(w.totals", "cluster_sync()", "of.clear(q)")
+    _in_order(fork, "atomicMax(of.lowest", "cluster_sync()", "of.first_writer(r.last)", "sh_totals = make_int4", "cluster_sync()",
+              "ld_cluster_int4(&sh_totals", "cluster_sync()", "of.clear(q)")
     compact = src[src.index("compact_plan_kernel("):src.index("struct Caches")]
-    _in_order(compact, "__stcg(&w.totals[rank].x", "cluster_sync()", "__ldcg(&w.totals[c].x", "__stcg(&w.totals[rank].y", "cluster_sync()",
-              "__ldcg(&w.totals[c].y", "__stcg(w.list", "cluster_sync()", "__ldcg(w.list + i)")
+    _in_order(compact, "sh_all = make_int4", "cluster_sync()", "ld_cluster_int4(&sh_all", "sh_stay = make_int4", "cluster_sync()",
+              "ld_cluster_int4(&sh_stay", "__stcg(w.list", "cluster_sync()", "__ldcg(w.list + i)")

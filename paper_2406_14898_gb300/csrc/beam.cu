@@ -491,6 +491,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
 #pragma unroll
   for (int i = 0; i < EARLY; ++i) {
     const int row = tid + i * THREADS, s = row / B;
+    if (i * THREADS >= rows) break;
     if (row < rows) early_t[i] = a.from.steps[s], early_done[i] = a.from.done[s], early_score[i] = a.from.scores[row];
   }
   // what is asked for next: a chunk of the line, its row, its first piece; the stage that it goes to
@@ -544,6 +545,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
 #pragma unroll
       for (int i = 0; i < EARLY; ++i) {
         const int r = tid + i * THREADS;
+        if (i * THREADS >= rows) break;
         set_bits(r, r < rows && is_live(early_t[i], early_done[i], early_score[i]));
       }
     }

@@ -85,6 +85,59 @@ def test_step_of_large_calls(F, S, B, V, dtype):
     one_step(F, under_way(rng, S, B, 40), x, S, B, V, dtype, 40, eos=5, penalty=0.8)
 
 
+@pytest.mark.parametrize("B,dtype", [(16, "f32"), (3, "f32"), (16, "bf16")])
+def test_long_parts(F, B, dtype):
+    """Parts of several chunks: logits that ascend (all of them are better than what came before), descend, are equal, or take
+    few values; most of the others masked; beams and searches that rest among them."""
+    rng = np.random.default_rng(10 + B)
+    S, V = 192 // B, 130528 * (2 if dtype == "bf16" else 1)
+    x = logits(rng, S, B, V, dtype)
+    rows = x.view(S, B, -1)[..., :V]
+    up = torch.linspace(-30, 30, V, device="cuda").to(x.dtype)
+    rows[0], rows[1], rows[2], rows[3] = up, up.flip(0), -2.5, torch.randint(0, 3, (B, V), device="cuda").to(x.dtype)
+    rows[4, :, :V - 2000] = -INF
+    rows[5, :, 100:] = -INF
+    rows[6, 0] = -INF
+    st = under_way(rng, S, B, 9)
+    st["done"][7:9] = 1
+    st["scores"][9:, B - 1] = -INF
+    one_step(F, st, x, S, B, V, dtype, 9, eos=V - 1, penalty=0.5)
+
+
+@pytest.mark.parametrize("S,B,V,dtype", [(300, 16, 5000, "f32"), (9000, 1, 70, "bf16"), (16384, 16, 20, "f16")])
+def test_many_rows(F, S, B, V, dtype):
+    """More rows than are looked at together, up to the most there may be; many of them rest."""
+    rng = np.random.default_rng(S)
+    st = begin(S, B)
+    st["scores"][:] = -np.arange(1, B + 1)
+    st["steps"] = rng.integers(0, 10, S)  # (10: over)
+    st["done"][rng.random(S) < 0.4] = 1
+    st["scores"][rng.random((S, B)) < 0.3] = -INF
+    st["done"][:S // 10] = 1
+    x = logits(rng, S, B, V, dtype)
+    one_step(F, st, x, S, B, V, dtype, 10, eos=3, in_place=True)
+
+
+def test_two_calls_at_once(F):
+    """Two searches on two streams, each with its own workspace."""
+    rng = np.random.default_rng(11)
+    calls = []
+    for S, B, V, dtype in ((64, 8, 60000, "bf16"), (5, 4, 30000, "f32")):
+        st = under_way(rng, S, B, 9)
+        x = logits(rng, S, B, V, dtype)
+        run = Searches(F, S, B, V, 9, 2)
+        now = device_state(st)
+        calls.append((run, now, {k: torch.empty_like(v) for k, v in now.items()}, x, dtype, torch.cuda.Stream(),
+                      step64(st, values(x, S, B, V), 9, 2, 1.0, False)))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for run, now, out, x, dtype, stream, _ in calls:
+            run.step(now, out, x, dtype, x.shape[1], stream=stream)
+    torch.cuda.synchronize()
+    for run, now, out, x, dtype, stream, (want, tokens, parents, _, _) in calls:
+        check_step(out, run.tokens, run.parents, want, tokens, parents)
+
+
 def test_first_step_looks_at_one_beam(F):
     rng = np.random.default_rng(1)
     S, B, V = 3, 5, 700

@@ -57,6 +57,7 @@ struct Piece<float> {
   FL_DEV static void get(const uint4& u, float (&f)[4]) {
     f[0] = __uint_as_float(u.x), f[1] = __uint_as_float(u.y), f[2] = __uint_as_float(u.z), f[3] = __uint_as_float(u.w);
   }
+  FL_DEV static void word(uint32_t u, float (&f)[1]) { f[0] = __uint_as_float(u); }
   FL_DEV static uint32_t max4(const uint4& u) {
     float f[4], m;
     get(u, f);
@@ -78,6 +79,10 @@ struct Piece16 {
       const float2 y = KvIo<T>::unpack(w[i]);
       f[2 * i] = y.x, f[2 * i + 1] = y.y;
     }
+  }
+  FL_DEV static void word(uint32_t u, float (&f)[2]) {
+    const float2 y = KvIo<T>::unpack(u);
+    f[0] = y.x, f[1] = y.y;
   }
   FL_DEV static float top(uint32_t a) {
     const float2 y = KvIo<T>::unpack(a);
@@ -608,9 +613,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
     ask_first_ones();
   }
   int stage = 0, raised = 0;
-  // with few beams little comes between two raises, so that each costs more than it saves
-  const int often = B > 4 ? ~0 : 0x55555555;
-  static_assert(STAGES == 2);
+  static_assert(STAGES == 2 && PIECES * 4 == 32);
   for (int c = c0; c < c1;) {
     {
       const int k = c / L, row = sh_rows[k - k0], from = c - k * L, to = min(L, from + c1 - c);
@@ -676,20 +679,17 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
           else z.add(y, -INFINITY);
         }
         uint4 cur[PIECES];
-        uint32_t of_piece[PIECES], of_all = Io::NONE;  // maxima
+        uint32_t largest = Io::NONE;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) cur[i] = places[i * THREADS];
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-          of_piece[i] = Io::max4(cur[i]);
-          of_all = Io::max2(of_all, of_piece[i]);
-        }
-        const float top = Io::top(of_all);
+        for (int i = 0; i < PIECES; ++i) largest = Io::max2(largest, Io::max4(cur[i]));
+        const float top = Io::top(largest);
         most = fmaxf(most, top);
         bool equals = false;  // whether logits equal to the bound count: it is new, and fewer than B larger ones may have been seen
         const int seen = chunk + 1;
         settled = false;
-        if ((seen & chunk) == 0 && (seen & often)) equals = raise() || chunk == 0;
+        if ((seen & chunk) == 0) equals = raise() || chunk == 0;
         const bool look = top > -INFINITY && (equals ? top >= bound : top > bound);
         if (look) z.see(top);
         if (!z.far()) {
@@ -704,21 +704,23 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
 #pragma unroll 1
           for (int i = 0; i < PIECES * N; ++i) z.add_far(Io::one(reinterpret_cast<const T*>(places + i / N * THREADS)[i % N]));
         }
-        if (look) {
-          unsigned which = 0;
+        // what exceeds the bound, a thread's logits at a time by its whole warp
+        if (unsigned who = __ballot_sync(0xffffffffu, look)) {
+          __syncwarp();  // (a thread's own copies are seen by the others)
+          const uint4* its = places - lane + lane / 4 * THREADS;
+          const int its_first = (first + lane / 4 * THREADS + tid - lane) * N + lane % 4 * (N / 4);
+          for (; who; who &= who - 1) {
+            const int l = __ffs(who) - 1;
+            float f[N / 4];
+            Io::word(reinterpret_cast<const uint32_t*>(its + l)[lane % 4], f);
 #pragma unroll
-          for (int i = 0; i < PIECES; ++i) which |= Io::top(of_piece[i]) >= bound ? 1u << i : 0u;
-          for (; which; which &= which - 1) {
-            const int i = __ffs(which) - 1;
-            float f[N];
-            Io::get(places[i * THREADS], f);
-#pragma unroll
-            for (int k = 0; k < N; ++k)
+            for (int k = 0; k < N / 4; ++k)
               if (f[k] > bound || (equals && f[k] == bound && f[k] > -INFINITY)) {
                 const int n = atomicAdd(&sh_count, 1);
-                if (n < MAX_HITS) sh_hits[n] = Cand{f[k], (first + i * THREADS + tid) * N + k};
+                if (n < MAX_HITS) sh_hits[n] = Cand{f[k], its_first + l * N + k};
               }
           }
+          __syncwarp();  // the places have been read
         }
         ask_more();  // into the stage that has been read
       }

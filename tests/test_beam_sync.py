@@ -47,9 +47,9 @@ def test_a_place_is_read_before_it_is_asked_for_again():
     """A chunk's group has arrived before its places are read; the next request goes to another stage."""
     src = _code("beam.cu")
     loop = src[src.index("for (int first = begin, chunk = 0;"):src.index("float ref = z.ref;")]
-    _in_order(loop, "cp_async_wait<STAGES - 1>()", "places = sh_ring + stage * CHUNK_PIECES + tid", "cur[i] = places", "Io::get(places[",
-              "ask_more()")
-    assert "static_assert(STAGES == 2);" in src
+    _in_order(loop, "cp_async_wait<STAGES - 1>()", "places = sh_ring + stage * CHUNK_PIECES + tid", "cur[i] = places", "__ballot_sync(0xffffffffu, look)",
+              "__syncwarp()", "Io::word(", "__syncwarp()", "ask_more()")
+    assert "static_assert(STAGES == 2 &&" in src
     first = src[src.index("const auto ask_first_ones"):src.index("cut(rows);")]
     assert first.count("ask_more();") == 2  # a group for each stage before the loop
     _in_order(src, "if (!guessed) {", "cp_async_wait<0>()", "ask_first_ones()")

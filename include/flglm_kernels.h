@@ -388,7 +388,9 @@ enum {
  * are brought into it, and entries that name no page are passed on but not copied (FL_KV_BAD_PAGE).
  * workspace: fl_k_kv_pages_workspace bytes, 16-byte aligned, ZERO before its first use; calls one after another on a
  * stream, of this kind and the next, may share it as long as n_seqs, n_pages and table_stride stay; calls that may
- * overlap need one each.  Arrays 4-byte aligned, n_seqs = 0 does nothing. */
+ * overlap need one each.  Arrays 4-byte aligned; n_seqs = 0: lens and table may be NULL, and refs are passed on.  More caches than
+ * FL_KV_MAX_CACHES: more calls with the same from, to, parents and new_tokens, which leave the same `to`.  A copy's waits are
+ * bounded (FL_KV_TIMEOUT: copies are missing). */
 size_t fl_k_kv_pages_workspace(const fl_kv_pages* pages);
 int fl_k_kv_fork(const fl_kv_cache* caches, int32_t n_caches, const fl_kv_pages* from, const fl_kv_pages* to,
                  const int32_t* parents, const int32_t* new_tokens, void* workspace, int* status, void* stream);

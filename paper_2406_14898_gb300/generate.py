@@ -86,14 +86,16 @@ class SharedPages:
         now = {"lens": torch.tensor(pages.lens, dtype=I32).cuda(), "table": pages.table.cuda(), "refs": refs.cuda()}
         self.sides = [now, {k: torch.empty_like(v) for k, v in now.items()}]
         self.structs = [F.kv_pages(n, self.n_pages, pages.page_size, width, **side) for side in self.sides]
-        self.caches = F.kv_caches(caches)
+        # a call takes so many of them; calls from the same sides leave the same pages
+        self.caches = [F.kv_caches(caches[i:i + F.FL_KV_MAX_CACHES]) for i in range(0, len(caches), F.FL_KV_MAX_CACHES)]
         self.workspace = torch.zeros(F.fl_k_kv_pages_workspace(self.structs[0]) // 4, dtype=I32, device="cuda")
         self.cu = torch.arange(n + 1, dtype=I32, device="cuda")
         self.one = torch.ones(n, dtype=I32, device="cuda")
 
     def step(self, parents: torch.Tensor, status: torch.Tensor) -> "F.fl_kv_batch":
         """Every sequence follows its parent (device int32, -1: none) and gets room for a token: the batch of those."""
-        F.fl_k_kv_fork(self.caches, *self.structs, parents, self.one, self.workspace, status, **_stream())
+        for caches in self.caches:
+            F.fl_k_kv_fork(caches, *self.structs, parents, self.one, self.workspace, status, **_stream())
         self.sides.reverse()
         self.structs.reverse()
         now = self.sides[0]

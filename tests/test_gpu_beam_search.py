@@ -88,6 +88,24 @@ def test_follow_refuses_what_does_not_fit(F):
     srv.close()
 
 
+def test_stack_of_more_blocks_than_a_call_copies(F):
+    """66 blocks, a prompt's last page copied in each of them, bit by bit."""
+    from paper_2406_14898_gb300.generate import BlockStack
+    blocks = F.FL_KV_MAX_CACHES + 2
+    srv = server(F, blocks, 4, 64, 32)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    row = lambda n: torch.randn((n, 256), generator=gen, device="cuda").bfloat16()  # noqa: E731
+    stack = BlockStack.from_server(srv, 3, 32, page_size=16)
+    prompt = row(21)
+    stack.forward(prompt, [21, 0, 0])
+    stack.follow(row(3), torch.zeros(3, dtype=torch.int32, device="cuda"))
+    for kv in (b["kv"] for b in stack.blocks):
+        for a in kv:
+            pages = stack.shared.sides[0]["table"][:, 1].long()
+            assert len(set(pages.tolist())) == 3 and all(torch.equal(a[p, :, :5], a[pages[0], :, :5]) for p in pages)
+    srv.close()
+
+
 def generator(F, n, vocab, tokens, hidden=256, blocks=2):
     from paper_2406_14898_gb300.generate import Generator
     cfg, cc = F.fl_server_cfg(), F.fl_client_cfg()

@@ -1,13 +1,16 @@
 // Beam search: the next beams from every beam's logits, and the hypotheses' tokens from the back-pointers.
 //
 // Step.  With c(b, v) = score_b + x_bv - lse_b a search wants the best `beams` of beams x vocab candidates.  Within a
-// beam c is ordered as x is, so each row needs only its largest logits and its log-sum-exp: one pass over the logits, which
-// is the bound (HBM; for few rows the latency of a load, some barriers and the join).  A CTA goes through its part of a row in chunks,
-// the next one's loads in flight.  Of the first chunk the B-th largest of 32 groups of
+// beam c is ordered as x is, so each row needs only its largest logits and its log-sum-exp: one pass over the logits.  A CTA goes
+// through its part of a row in chunks, the next one's loads in flight.  Of the first chunk the B-th largest of 32 groups of
 // threads' maxima bounds the B-th largest logit from below; of what comes later only what exceeds the bound is looked
-// at, about B logits for each time that what has been seen doubles, and the bound is raised now and then.  A second kernel, a
+// at, about B logits for each time that what has been seen doubles, which is when the bound is raised.  A second kernel, a
 // CTA a search, joins the parts' sums and lists.  (With the join in the CTA that comes last, CTAs that joined came late
-// for their next slices and so joined again: 64 x 16 rows of 130528 bf16 157 us.)
+// for their next parts and so joined again: 64 x 16 rows of 130528 bf16 157 us, when two kernels took 92.)
+//
+// Many rows are bound by HBM and the instructions beside it: 1024 x 1 rows of 130528 fp32 92 us (5.8 TB/s), bf16 54 (4.9), 64 x 16
+// rows of bf16 67 (4.0), of which the pass alone takes 49, the hits and lists 8, the join 10.  Few rows are bound by latency: 1 x 4
+// rows of fp32 9.0 us, of which the join takes 4.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -114,8 +117,8 @@ FL_DEV uint32_t order32(float x) {
 }
 
 // A number as the unevaluated sum of two floats, the first of which is the sum rounded (T. J. Dekker, A floating-point
-// technique for extending the available precision, 1971): 48 bits, for the scores that are compared and the penalty.  The
-// double-precision units of this card take tens of cycles an operation; the join took 10 us longer with them.
+// technique for extending the available precision, 1971): 48 bits, for the scores that are compared and the penalty.  (The
+// double-precision units of this card run at a small fraction of these' rate.)
 struct Two {
   float hi, lo;
 };
@@ -274,7 +277,10 @@ FL_DEV void rest(const StepArgs& a, int s) {
   }
 }
 
-// One search's rows joined, a warp a row.  What it reads is asked for at once, before it is known which of it counts.
+// One search's rows joined, a warp a row, then all of them by the first warp: whichever list's best is the best of all comes next.
+// Latency is the bound, 0.14 us a candidate here and 0.18 there.  (Lists merged two and two by exchanges between lanes instead: in
+// registers 64 x 16 rows of bf16 66.1 us for 66.8, but 1 x 4 fp32 11.1 for 9.0, as much code comes from L2; in shared memory, with less
+// code, 68.2 and 12.5.)  What it reads is asked for at once, before it is known which of it counts.
 template <class T>
 __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a) {
   pdl_wait();
@@ -457,7 +463,7 @@ template <class T>
 __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
   pdl_wait();
   // The join's CTAs may come while this kernel runs only where they find room beside it: else those that finish first would take
-  // them all (1024 x 1 rows of bf16 70 us instead of 62).
+  // them all (1024 x 1 rows of bf16 62 us instead of 54).
   if (!a.crowded) pdl_trigger();
   using Io = Piece<T>;
   constexpr int N = Io::N;
@@ -861,7 +867,7 @@ int launch_step(StepArgs& a, cudaStream_t st) {
   FL_CUDA_TRY(fl_func_smem((const void*)kern, ring));
   FL_CUDA_TRY(fl_func_smem((const void*)join, join_smem(FL_BEAM_MAX)));
   FL_CUDA_TRY(fl_launch(kern, dim3(grid), dim3(THREADS), ring, st, a));
-  // four warps at least: the work behind the rows' is divided among all (1024 x 1 rows of bf16 with one warp 70 us, with four 57, with sixteen 61)
+  // four warps at least, and no more than it has work for (1024 x 1 rows of bf16 with one warp 60 us, with four 54, with sixteen 59)
   FL_CUDA_TRY(fl_launch(join, dim3(a.p.n_seqs), dim3(32 * std::max(4, a.p.beams)), join_smem(a.p.beams), st, a));
   return FL_OK;
 }
@@ -891,7 +897,8 @@ FL_DEV uint32_t ld_cluster_u8(const void* p, uint32_t rank) {
 // another costs a load's latency a step.  Here a cluster has a search and each of its CTAs some of the steps, of which each chunk
 // of 16 becomes one map from the beams behind it to those before it, all at once from shared memory; those together give
 // the CTA's map, the CTAs learn each other's, the hypotheses jump from CTA to CTA and from chunk to chunk, and then all
-// chunks are walked at once for the beams in between.  Latency is the bound.  TODO
+// chunks are walked at once for the beams in between.  Latency is the bound: 64 x 16 hypotheses of 2048 steps 16.7 us (a CTA a
+// search 44), the best of 16 x 4 of 256 steps 6.6
 __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) {
   pdl_wait();
   pdl_trigger();

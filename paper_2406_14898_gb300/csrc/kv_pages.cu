@@ -1,6 +1,6 @@
 // Sequences that share the pages of a cache: fork (continue, share, copy on write, extend, shorten, leave) and compact.
 //
-// A call is two launches.  The plan is integer work on a few arrays: who has each page after the call, which are free, who
+// A call is two launches, 6 to 7 us together where there is little to copy.  The plan is integer work on a few arrays: who has each page after the call, which are free, who
 // gets which; it is bound by latency, loads one behind another and barriers.  One CTA does it with its counts in shared memory,
 // or one cluster where the arrays are long, with its counts in global memory.  The second launch, over the whole GPU, writes the table
 // and copies the pages' tokens in every cache.
@@ -401,7 +401,8 @@ FL_DEV int64_t shfl64(int64_t x, int lane) { return __shfl_sync(0xffffffffu, x, 
 // The copies, a warp a unit: from global memory into the warp's shared memory and from there to the new page, in
 // blocks of 8 KB by bulk copies that one lane asks for, two loads ahead of a store.  What a page holds of its sequence is
 // `runs` stretches of memory; each of its units has an equal part of their bytes, so that all are as long.
-// HBM is the bound: TODO.
+// HBM is the bound: 74 pages of 27 MB moved in 26 caches 610 us (6.3 TB/s read and written, with the plan), the copies of a beam
+// search's 64 sequences 100 us (5.9 TB/s).  16-byte loads and stores by all threads took 661 and 118.
 FL_DEV void copy_pages(const Caches& c, const Ws& w, int ps_log2, char* ring, uint64_t* full, int* status) {
   const int lane = threadIdx.x & 31, warps = gridDim.x * COPY_WARPS;
   const int64_t all = (int64_t)__ldcg(w.head) * c.n * c.units;

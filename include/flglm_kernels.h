@@ -410,7 +410,7 @@ int fl_k_kv_compact(const fl_kv_cache* caches, int32_t n_caches, const fl_kv_pag
  * hypothesis, -1: none.  A search is done when no beam is live, or when `beams` hypotheses have
  * ended and (early = 1) at once, (early = 0) the best live beam, as long as it is now, does not score more than the worst of them.  A hypothesis of n tokens (eos among them)
  * with the summed log-probability c scores c / n^length_penalty
- * (length_penalty at most 10^6 either way).  n_seqs at most 16384 (CAPACITY). */
+ * (length_penalty at most 16 either way, and so that max_steps^length_penalty lies within e^-80 and e^80).  n_seqs at most 16384 (CAPACITY). */
 #define FL_BEAM_MAX 16
 typedef struct {
   int32_t n_seqs, beams, vocab, max_steps, eos, early;

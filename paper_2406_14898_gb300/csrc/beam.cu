@@ -832,7 +832,7 @@ int64_t part_bytes(const fl_beam_search* p) {
 const char* search_problem(const fl_beam_search* p, int* code) {
   *code = FL_ERR_INVALID_ARG;
   if (!p || p->n_seqs < 0 || p->beams < 1 || p->vocab < 1 || p->max_steps < 1 || p->eos < -1 || p->eos >= p->vocab ||
-      (p->early != 0 && p->early != 1) || !(std::fabs(p->length_penalty) <= 1e6))
+      (p->early != 0 && p->early != 1) || !(std::fabs(p->length_penalty) <= 16 && std::fabs(p->length_penalty) * std::log((double)p->max_steps) <= 80))
     return "search";
   *code = FL_ERR_CAPACITY;
   if (p->beams > FL_BEAM_MAX) return "more than 16 beams";

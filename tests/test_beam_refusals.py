@@ -30,7 +30,7 @@ def state(F, at=0, **kw):
 SEARCHES = [("n_seqs", -1, ARG), ("n_seqs", 16385, CAPACITY), ("beams", 0, ARG), ("beams", 17, CAPACITY), ("vocab", 0, ARG),
             ("vocab", 2 ** 19 + 1, CAPACITY), ("max_steps", 0, ARG), ("max_steps", 2 ** 24 + 1, CAPACITY), ("eos", -2, ARG),
             ("eos", 100, ARG), ("early", 2, ARG), ("length_penalty", float("nan"), ARG), ("length_penalty", float("inf"), ARG),
-            ("length_penalty", -1.1e6, ARG)]
+            ("length_penalty", -1.1e6, ARG), ("length_penalty", 16.5, ARG)]
 
 
 def test_step(F):
@@ -58,6 +58,8 @@ def test_step(F):
     assert L.fl_k_beam_step(good[0], state(F), state(F), *good[3:]) == CUDA       # in place
     assert L.fl_k_beam_step(good[0], state(F), state(F, 6, steps=A[1]), *good[3:]) == ARG
     assert L.fl_k_beam_step(good[0], state(F), state(F, 6, steps=A[2]), *good[3:]) == ARG
+    assert L.fl_k_beam_step(search(F, max_steps=2 ** 24, length_penalty=-5.0), *good[1:]) == ARG  # 2^120
+    assert L.fl_k_beam_step(search(F, max_steps=2 ** 24, length_penalty=-4.8), *good[1:]) == CUDA
     assert L.fl_k_beam_step(search(F, n_seqs=0), *good[1:]) == 0
     assert L.fl_k_beam_workspace(search(F)) > L.fl_k_beam_workspace(search(F, beams=3)) > 0
     with pytest.raises(F.FlError):

@@ -248,7 +248,7 @@ def test_whole_searches(F, V, early):
 
 @pytest.mark.parametrize("S,B,T,n,eos,penalty", [(1, 1, 1, 1, -1, 1.0), (3, 4, 31, 2, 2, 0.0), (2, 16, 33, 16, 2, 1.0),
                                                  (5, 3, 64, 3, -1, 2.0), (2, 5, 2047, 4, 2, 0.6), (2, 16, 2048, 5, 2, 0.6),
-                                                 (3, 2, 2049, 2, 2, 1.0), (2, 7, 6200, 7, 2, 1.0), (300, 2, 70, 1, 2, 1.0)])
+                                                 (3, 2, 2049, 2, 2, 1.0), (2, 4, 300, 4, 2, 12.0), (2, 4, 300, 4, -1, -3.0), (2, 7, 6200, 7, 2, 1.0), (300, 2, 70, 1, 2, 1.0)])
 def test_trace(F, S, B, T, n, eos, penalty):
     rng = np.random.default_rng(T + B)
     st = under_way(rng, S, B, T + 1)

@@ -401,7 +401,7 @@ FL_DEV int64_t shfl64(int64_t x, int lane) { return __shfl_sync(0xffffffffu, x, 
 // The copies, a warp a unit: from global memory into the warp's shared memory and from there to the new page, in
 // blocks of 8 KB by bulk copies that one lane asks for, two loads ahead of a store.  What a page holds of its sequence is
 // `runs` stretches of memory; each of its units has an equal part of their bytes, so that all are as long.
-// HBM is the bound: 74 pages of 27 MB moved in 26 caches 610 us (6.3 TB/s read and written, with the plan), the copies of a beam
+// HBM is the bound: 71 pages of 27 MB moved in 26 caches 610 us (6.3 TB/s read and written, with the plan), the copies of a beam
 // search's 64 sequences 100 us (5.9 TB/s).  16-byte loads and stores by all threads took 661 and 118.
 FL_DEV void copy_pages(const Caches& c, const Ws& w, int ps_log2, char* ring, uint64_t* full, int* status) {
   const int lane = threadIdx.x & 31, warps = gridDim.x * COPY_WARPS;

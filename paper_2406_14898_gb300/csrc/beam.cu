@@ -238,11 +238,12 @@ struct Sum {
 struct Join {
   Cand best[FL_BEAM_MAX][FL_BEAM_MAX];
   Two score[FL_BEAM_MAX][FL_BEAM_MAX];  // of each beam's candidates
-  uint64_t key[FL_BEAM_MAX][FL_BEAM_MAX];  // their order64; 0: none
-  Two live[FL_BEAM_MAX], ends[FL_BEAM_MAX], length;
-  float end_x[FL_BEAM_MAX], pool[2 * FL_BEAM_MAX];
+  uint64_t key[FL_BEAM_MAX][FL_BEAM_MAX];  // their order64, descending; 0: none
+  Two ends[FL_BEAM_MAX], length;           // of each beam's eos; steps^penalty
+  int end_place[FL_BEAM_MAX];              // candidates of its beam ahead of it
+  int next[FL_BEAM_MAX], end_rank[FL_BEAM_MAX];  // the beams that go on (beam << 8 | place in its list); places of the eos that end; -1: none
+  float pool[2 * FL_BEAM_MAX];
   int pool_step[2 * FL_BEAM_MAX], pool_beam[2 * FL_BEAM_MAX];
-  int token[FL_BEAM_MAX], parent[FL_BEAM_MAX];
 };
 
 // 16 bytes of global memory to this thread's place in shared memory, in groups that the thread itself waits for.
@@ -277,10 +278,11 @@ FL_DEV void rest(const StepArgs& a, int s) {
   }
 }
 
-// One search's rows joined, a warp a row, then all of them by the first warp: whichever list's best is the best of all comes next.
-// Latency is the bound, 0.14 us a candidate here and 0.18 there.  (Lists merged two and two by exchanges between lanes instead: in
-// registers 64 x 16 rows of bf16 66.1 us for 66.8, but 1 x 4 fp32 11.1 for 9.0, as much code comes from L2; in shared memory, with less
-// code, 68.2 and 12.5.)  What it reads is asked for at once, before it is known which of it counts.
+// One search's rows joined, a warp a row: of the parts' lists whichever one's best is the best of all comes next, B times; then each
+// row's candidates are placed among all by searches in the other rows' lists.  Latency is the bound, 0.14 us a candidate of a row.
+// (Rows merged as the parts are, by one warp: 0.18 us a candidate, 1 x 16 rows of bf16 16.6 us for 15.7, 64 x 16 66.8 for 65.5.  Lists
+// merged two and two by exchanges between lanes: in registers 64 x 16 66.1, but 1 x 4 fp32 11.1 for 8.8, as so much code comes
+// from L2; in shared memory, with less code, 68.2 and 12.5.)  What it reads is asked for at once, before it is known which of it counts.
 template <class T>
 __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a) {
   pdl_wait();
@@ -355,66 +357,62 @@ __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a)
       const uint64_t y = __shfl_up_sync(0xffffffffu, key, d);
       if (lane >= d) key = min(key, y);
     }
+    const Cand eos{live ? e : -INFINITY, a.p.eos};
+    const Two end = c_of(eos.x);
+    // (where the eos' c equals a candidate's, the order is that of the logits)
+    const int before = __popc(__ballot_sync(0xffffffffu, lane < B && key != 0 && (key > order64(end) || (key == order64(end) && better(one, eos)))));
+    if (lane < FL_BEAM_MAX) j.key[b][lane] = lane < B ? key : 0;
     if (lane < B) {
       j.best[b][lane] = one;
       j.score[b][lane] = c;
-      j.key[b][lane] = key;
     }
     if (lane == 0) {
-      j.end_x[b] = live ? e : -INFINITY;
-      const Two end = c_of(j.end_x[b]);
-      j.ends[b] = order64(end) ? end : Two{-INFINITY, 0.f};
-      j.token[b] = max(a.p.eos, 0);
-      j.parent[b] = -1;
-      j.live[b] = {-INFINITY, 0.f};
+      j.ends[b] = end;
+      j.end_place[b] = before;
+      j.next[b] = j.end_rank[b] = -1;
     }
   }
   if (tid == threads - 1) j.length = pow_two((float)(t + 1), {a.penalty_hi, a.penalty_lo});
   __syncthreads();
-  if (warp != 0) return;
   if (!active) {  // it stays as it is
-    rest(a, s);
+    if (warp == 0) rest(a, s);
     return;
   }
-  // The rows' lists merged: lanes 0 to 15 have a beam's list each, the others a beam's eos.  The best one of all comes next, until
-  // there are B that go on; an eos among the first B ends a hypothesis.
-  const int beam = lane % FL_BEAM_MAX;
-  const bool is_eos = lane >= FL_BEAM_MAX;
-  uint64_t key = 0, next = 0;
-  if (beam < B) {
-    key = is_eos ? order64(j.ends[beam]) : j.key[beam][0];
-    if (!is_eos && B > 1) next = j.key[beam][1];
-  }
-  int at = 0, n_live = 0, end_rank = -1;
-#pragma unroll 1
-  for (int rank = 0; n_live < B; ++rank) {
-    const uint32_t hi = (uint32_t)(key >> 32), top = __reduce_max_sync(0xffffffffu, hi);
-    if (top == 0) break;
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, hi == top ? (uint32_t)key : 0u);
-    const unsigned who = __ballot_sync(0xffffffffu, hi == top && (uint32_t)key == lo);
-    int w = __ffs(who) - 1;
-    if (who & (who - 1)) {  // equal: the lower beam; of one beam the better of the list's and the eos
-      const Cand mine = beam >= B || key == 0 ? Cand{-INFINITY, 0} : is_eos ? Cand{j.end_x[beam], a.p.eos} : j.best[beam][at];
-      const Cand other{__shfl_xor_sync(0xffffffffu, mine.x, FL_BEAM_MAX), __shfl_xor_sync(0xffffffffu, mine.v, FL_BEAM_MAX)};
-      const int order = who >> lane & 1 ? 2 * beam + better(other, mine) : 0x7fffffff;
-      const int first = __reduce_min_sync(0xffffffffu, order);
-      w = __ffs(__ballot_sync(0xffffffffu, order == first)) - 1;
+  // The rows' lists joined: by c, then the lower beam, then that beam's order, in which its eos has its place.  A candidate's place is
+  // how many are ahead of it in each list.  The first B go on; an eos among the first B of all ends a hypothesis.
+  if (warp < B) {
+    const int b = warp, k = lane % FL_BEAM_MAX;
+    const auto ahead_in = [&](int q, uint64_t key) {  // of another beam's list
+      const uint64_t least = key + (q > b);  // (key is not 0 and no infinity's: no overflow)
+      int n = 0;
+#pragma unroll
+      for (int d = FL_BEAM_MAX / 2; d; d >>= 1) n += j.key[q][n + d - 1] >= least ? d : 0;
+      return n + (j.key[q][n] >= least);
+    };
+    const uint64_t mine = j.key[b][k];
+    int place = 0;
+#pragma unroll 4
+    for (int q = lane / FL_BEAM_MAX; q < B; q += 2) {
+      const int n = ahead_in(q, mine);
+      place += q == b ? k : n;
     }
-    if (lane == w) {
-      if (is_eos) {
-        if (rank < B) end_rank = rank;
-        key = 0;
-      } else {
-        j.token[n_live] = j.best[beam][at].v;
-        j.parent[n_live] = beam;
-        j.live[n_live] = j.score[beam][at];
-        ++at;
-        key = next;
-        next = at + 1 < B ? j.key[beam][at + 1] : 0;
+    place += __shfl_xor_sync(0xffffffffu, place, FL_BEAM_MAX);
+    if (mine != 0 && place < B && lane < FL_BEAM_MAX) j.next[place] = b << 8 | k;
+    const uint64_t end = order64(j.ends[b]);
+    if (end != 0) {
+      int n = 0;
+      if (lane < B) {
+        const uint64_t other = order64(j.ends[lane]);
+        n = lane == b ? j.end_place[b] : ahead_in(lane, end) + (other > end || (other == end && lane < b));
       }
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (lane == 0 && n < B) j.end_rank[b] = n;
     }
-    n_live += w < FL_BEAM_MAX;
   }
+  __syncthreads();
+  if (warp != 0) return;
+  const int beam = lane % FL_BEAM_MAX, next = lane < B ? j.next[lane] : -1;
+  const int end_rank = lane >= FL_BEAM_MAX && beam < B ? j.end_rank[beam] : -1;
   // the pool: what had ended, then what ends now in the order of its rank
   float x = pool_score;
   int step = pool_step, from_beam = pool_beam;
@@ -439,20 +437,20 @@ __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a)
   __syncwarp();
   const float worst = __shfl_sync(0xffffffffu, x, B - 1);
   if (lane < B) {
-    const int i = s * B + lane, parent = j.parent[lane], token = j.token[lane];
+    const int i = s * B + lane, parent = next >> 8, token = next >= 0 ? j.best[parent][next & 255].v : max(a.p.eos, 0);
+    const Two score = next >= 0 ? j.score[parent][next & 255] : Two{-INFINITY, 0.f};
     const int64_t tr = ((int64_t)s * a.p.max_steps + t) * B + lane;
-    a.to.scores[i] = j.live[lane].hi;
+    a.to.scores[i] = score.hi;
     a.to.end_scores[i] = x;
     a.to.end_steps[i] = step;
     a.to.end_beams[i] = from_beam;
     a.tokens[i] = a.trace_tokens[tr] = token;
-    a.trace_parents[tr] = parent < 0 ? lane : parent;
-    a.parents[i] = parent < 0 ? -1 : s * B + parent;
-  }
-  if (lane == 0) {
-    const bool none = !(j.live[0].hi > -INFINITY);
-    a.to.steps[s] = t + 1;
-    a.to.done[s] = none || (worst > -INFINITY && (a.p.early || worst >= div_two(j.live[0], j.length)));
+    a.trace_parents[tr] = next < 0 ? lane : parent;
+    a.parents[i] = next < 0 ? -1 : s * B + parent;
+    if (lane == 0) {
+      a.to.steps[s] = t + 1;
+      a.to.done[s] = next < 0 || (worst > -INFINITY && (a.p.early || worst >= div_two(score, j.length)));
+    }
   }
 }
 

@@ -55,6 +55,14 @@ def test_a_place_is_read_before_it_is_asked_for_again():
     _in_order(src, "if (!guessed) {", "cp_async_wait<0>()", "ask_first_ones()")
 
 
+def test_joined_rows_are_placed_behind_a_barrier():
+    src = _code("beam.cu")
+    join = src[src.index("beam_join_kernel(StepArgs a)"):src.index("beam_step_kernel(StepArgs a)")]
+    _in_order(join, "j.next[b] = j.end_rank[b] = -1", "__syncthreads()", "if (!active)", "ahead_in(q, mine)", "j.next[place] =",
+              "j.end_rank[b] = n", "__syncthreads()", "if (warp != 0) return;", "j.next[lane]")
+    assert join.count("__syncthreads()") == 2 and join.count("return;") == 2
+
+
 def test_plan_phases_are_divided_by_the_clusters_barrier():
     src = _code("kv_pages.cu")
     fork = src[src.index("fork_plan_kernel("):src.index("compact_plan_kernel(")]

@@ -9,8 +9,8 @@
 // for their next parts and so joined again: 64 x 16 rows of 130528 bf16 157 us, when two kernels took 92.)
 //
 // Many rows are bound by HBM and the instructions beside it: 1024 x 1 rows of 130528 fp32 92 us (5.8 TB/s), bf16 54 (4.9), 64 x 16
-// rows of bf16 67 (4.0), of which the pass alone takes 49, the hits and lists 8, the join 10.  Few rows are bound by latency: 1 x 4
-// rows of fp32 9.0 us, of which the join takes 4.
+// rows of bf16 65.5 (4.1), of which the pass alone takes 49, the hits and lists 8, the join 8.  Few rows are bound by latency: 1 x 4
+// rows of fp32 8.8 us, of which the join takes 4.
 #include <cuda_fp16.h>
 
 #include <algorithm>

@@ -407,10 +407,10 @@ int fl_k_kv_compact(const fl_kv_cache* caches, int32_t n_caches, const fl_kv_pag
 /* ---------------------------------------------------------------- beam search
  * n_seqs searches of `beams` beams each (1 to FL_BEAM_MAX), over tokens [0, vocab) (1 to 2^19), of at most max_steps tokens.
  * Beam b of search s is row s * beams + b of the logits, and of the sequences of a cache.  eos: the token that ends a
- * hypothesis, -1: none.  A search is done when no beam is live, or when `beams` hypotheses have
- * ended and (early = 1) at once, (early = 0) the best live beam, as long as it is now, does not score more than the worst of them.  A hypothesis of n tokens (eos among them)
- * with the summed log-probability c scores c / n^length_penalty
- * (length_penalty at most 16 either way, and so that max_steps^length_penalty lies within e^-80 and e^80).  n_seqs at most 16384 (CAPACITY). */
+ * hypothesis, -1: none.  A search is done when no beam is live, or when `beams` hypotheses have ended and (early = 1) at
+ * once, (early = 0) the best live beam, as long as it is now, does not score more than the worst of them.  A hypothesis of
+ * n tokens (eos among them) with the summed log-probability c scores c / n^length_penalty (length_penalty at most 16
+ * either way, and so that max_steps^length_penalty lies within e^-80 and e^80).  n_seqs at most 16384 (CAPACITY). */
 #define FL_BEAM_MAX 16
 typedef struct {
   int32_t n_seqs, beams, vocab, max_steps, eos, early;
@@ -432,8 +432,8 @@ typedef struct {
  * back-pointers or the state is out of its range (it counts as 0). */
 enum { FL_BEAM_BAD_LOGITS = 64, FL_BEAM_BAD_TRACE = 128 };
 
-/* One step of every search that is not over (done, or max_steps tokens): with c(b, v) = scores[b] + logits[b, v] - logsumexp(logits[b]) and
- * candidates ordered by c (then the lower beam, the higher logit, the lower token; -inf is no candidate), the next
+/* One step of every search that is not over (done, or max_steps tokens): with
+ * c(b, v) = scores[b] + logits[b, v] - logsumexp(logits[b]) and candidates ordered by c (then the lower beam, the higher logit, the lower token; -inf is no candidate), the next
  * beams are the best candidates other than eos, and an eos among the best `beams` of all candidates ends a
  * hypothesis.  `to` receives the new state (it may be `from`; else no array of the two may be the same).  Each search's new
  * tokens and the beams (0 .. beams - 1) that they follow are also written into row steps[s] of trace_tokens and trace_parents (int32
@@ -443,7 +443,8 @@ enum { FL_BEAM_BAD_LOGITS = 64, FL_BEAM_BAD_TRACE = 128 };
  * logits: dtype FL_DT_F32, FL_DT_BF16 or FL_DT_F16, rows ld elements apart (a multiple of 16 bytes, vocab or
  * more; what lies behind vocab is not used), 16-byte aligned.  Rows of beams that are not live are not used.  Sums are fp32,
  * scores are formed in 48 bits and rounded once; a candidate whose score is -inf in 32 bits is none.
- * workspace: fl_k_beam_workspace bytes, 16-byte aligned, of any content; calls one after another on a stream may share it, of any searches for which it is large enough; calls that may overlap need one each. */
+ * workspace: fl_k_beam_workspace bytes, 16-byte aligned, of any content; calls one after another on a stream may share
+ * it, of any searches for which it is large enough; calls that may overlap need one each. */
 size_t fl_k_beam_workspace(const fl_beam_search* search);
 int fl_k_beam_step(const fl_beam_search* search, const fl_beam_state* from, const fl_beam_state* to, int32_t dtype,
                    const void* logits, int64_t ld, int32_t* trace_tokens, int32_t* trace_parents, int32_t* tokens,

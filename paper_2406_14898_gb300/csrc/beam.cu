@@ -241,7 +241,8 @@ struct Join {
   uint64_t key[FL_BEAM_MAX][FL_BEAM_MAX];  // their order64, descending; 0: none
   Two ends[FL_BEAM_MAX], length;           // of each beam's eos; steps^penalty
   int end_place[FL_BEAM_MAX];              // candidates of its beam ahead of it
-  int next[FL_BEAM_MAX], end_rank[FL_BEAM_MAX];  // the beams that go on (beam << 8 | place in its list); places of the eos that end; -1: none
+  // the beams that go on (beam << 8 | place in its list); places of the eos that end; -1: none
+  int next[FL_BEAM_MAX], end_rank[FL_BEAM_MAX];
   float pool[2 * FL_BEAM_MAX];
   int pool_step[2 * FL_BEAM_MAX], pool_beam[2 * FL_BEAM_MAX];
 };
@@ -360,7 +361,8 @@ __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a)
     const Cand eos{live ? e : -INFINITY, a.p.eos};
     const Two end = c_of(eos.x);
     // (where the eos' c equals a candidate's, the order is that of the logits)
-    const int before = __popc(__ballot_sync(0xffffffffu, lane < B && key != 0 && (key > order64(end) || (key == order64(end) && better(one, eos)))));
+    const bool is_before = key > order64(end) || (key == order64(end) && better(one, eos));
+    const int before = __popc(__ballot_sync(0xffffffffu, lane < B && key != 0 && is_before));
     if (lane < FL_BEAM_MAX) j.key[b][lane] = lane < B ? key : 0;
     if (lane < B) {
       j.best[b][lane] = one;
@@ -830,8 +832,10 @@ int64_t part_bytes(const fl_beam_search* p) {
 const char* search_problem(const fl_beam_search* p, int* code) {
   *code = FL_ERR_INVALID_ARG;
   if (!p || p->n_seqs < 0 || p->beams < 1 || p->vocab < 1 || p->max_steps < 1 || p->eos < -1 || p->eos >= p->vocab ||
-      (p->early != 0 && p->early != 1) || !(std::fabs(p->length_penalty) <= 16 && std::fabs(p->length_penalty) * std::log((double)p->max_steps) <= 80))
+      (p->early != 0 && p->early != 1))
     return "search";
+  const double penalty = std::fabs(p->length_penalty);
+  if (!(penalty <= 16 && penalty * std::log((double)p->max_steps) <= 80)) return "length_penalty";
   *code = FL_ERR_CAPACITY;
   if (p->beams > FL_BEAM_MAX) return "more than 16 beams";
   if (p->n_seqs > MAX_SEARCHES) return "more than 16384 searches";
@@ -910,7 +914,8 @@ __global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) 
   uint8_t* chain = entry + chunks * n;  // [hypothesis][step], a hypothesis's line from another bank than the next one's
   uint8_t* behind = chain + line * n;  // [chunk][beam]: the beam after the chunk's last step, by the beam behind the block
   __shared__ int h_steps[FL_BEAM_MAX], h_ended[FL_BEAM_MAX], h_beam[FL_BEAM_MAX], h_from[FL_BEAM_MAX], h_after[FL_BEAM_MAX];
-  __shared__ uint8_t of_block[FL_BEAM_MAX], of_part[FL_BEAM_MAX];  // beams before the block: by the beam behind it; of hypotheses that end in it
+  // beams before the block: by the beam behind it; of hypotheses that end in it
+  __shared__ uint8_t of_block[FL_BEAM_MAX], of_part[FL_BEAM_MAX];
   if (tid < 32) {
     const int b = tid < FL_BEAM_MAX ? tid : tid - FL_BEAM_MAX;
     const int raw = a.s.steps[s], steps = min(max(raw, 0), T);
@@ -1100,7 +1105,8 @@ extern "C" int fl_k_beam_trace(const fl_beam_search* search, const fl_beam_state
   const TraceArgs a{*search,    *state, trace_tokens, trace_parents, n_best, pad, penalty, (float)(search->length_penalty - penalty), block,
                     out_tokens, out_lens, out_scores, status};
   // the limit of the largest call, once: a smaller one would lower it for a larger call made before
-  FL_CUDA_TRY(fl_func_smem((const void*)beam_trace_kernel, MAX_STEPS * 4 * (FL_BEAM_MAX + 1) + (MAX_STEPS * 2 + 4 + MAX_STEPS / CHUNK * 3) * FL_BEAM_MAX));
+  constexpr int most = MAX_STEPS * 4 * (FL_BEAM_MAX + 1) + (MAX_STEPS * 2 + 4 + MAX_STEPS / CHUNK * 3) * FL_BEAM_MAX;
+  FL_CUDA_TRY(fl_func_smem((const void*)beam_trace_kernel, most));
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see pdl_wait

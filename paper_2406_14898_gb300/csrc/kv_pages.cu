@@ -1,9 +1,10 @@
 // Sequences that share the pages of a cache: fork (continue, share, copy on write, extend, shorten, leave) and compact.
 //
-// A call is two launches, 6 to 7 us together where there is little to copy.  The plan is integer work on a few arrays: who has each page after the call, which are free, who
-// gets which; it is bound by latency, loads one behind another and barriers.  One CTA does it with its counts in shared memory,
-// or one cluster where the arrays are long, with its counts in global memory.  The second launch, over the whole GPU, writes the table
-// and copies the pages' tokens in every cache.
+// A call is two launches, 6 to 7 us together where there is little to copy.  The plan is integer work on a few arrays:
+// who has each page after the call, which are free, who gets which; it is bound by latency, loads one behind another and
+// barriers.  One CTA does it with its counts in shared memory, or one cluster where the arrays are long, with its counts
+// in global memory.  The second launch, over the whole GPU, writes the table and copies the pages' tokens in every
+// cache.
 #include "../../include/flglm_kernels.h"
 #include "kv_plan.cuh"
 #include "ptx.cuh"

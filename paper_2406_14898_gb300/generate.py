@@ -322,7 +322,8 @@ class Generator:
             head = torch.zeros((-(-V // 128) * 128, H), dtype=BF16, device="cuda")  # rows in whole GEMM tiles
             head[:V] = torch.from_numpy(c.get_param(F.FL_CP_HEAD, 0)).cuda().view(V, H).to(BF16)
             self.ends.append({"embed": torch.from_numpy(c.get_param(F.FL_CP_EMBED, 0)).cuda().view(V, H).to(BF16),
-                              "head": head, "eps": c.cfg.block.ln_eps, "ln": [torch.from_numpy(c.get_param(F.FL_CP_FINAL_LN, t)).cuda() for t in (0, 1)]})
+                              "head": head, "eps": c.cfg.block.ln_eps,
+                              "ln": [torch.from_numpy(c.get_param(F.FL_CP_FINAL_LN, t)).cuda() for t in (0, 1)]})
         torch.cuda.current_stream().synchronize()  # whichever stream uses them
 
     def start(self, context_lens: Optional[Sequence[int]] = None):

@@ -281,3 +281,34 @@ def test_graph_of_two_steps_replayed(F):
         assert pool.get() == lists[:3]
         assert all(torch.equal(a, b) for a, b in zip(before, pool.bits()))
     assert int(pool.status.item()) == 0
+
+
+def test_two_tables_at_once(F):
+    """Two tables on two streams, each with its own workspace; one's counts lie in a CTA's shared memory, the other's in a cluster's."""
+    rng = random.Random(8)
+    calls, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for S, n_pages, W, seed in ((12, 400, 30, 1), (1200, 18000, 12, 2)):
+        pool = Pool(F, S, n_pages, 16, W, blocks=1, heads=1, seed=seed)
+        lens = [rng.randrange(1, 16 * W - 24) for _ in range(S)]
+        table, refs, at = [], [0] * n_pages, 0
+        for n in lens:
+            held = -(-n // 16)
+            table.append(list(range(at, at + held)) + [-1] * (W - held))
+            refs[at:at + held] = [1] * held
+            at += held
+        pool.set(lens, table, refs)
+        parents = [[rng.randrange(S) if rng.random() < 0.3 else s for s in range(S)] for _ in range(6)]
+        calls.append((pool, parents, [torch.tensor(p, dtype=torch.int32, device="cuda") for p in parents],
+                      torch.ones(S, dtype=torch.int32, device="cuda"), lens, table, refs, pool.bits()))
+    torch.cuda.synchronize()
+    for t in range(6):
+        for stream, (pool, _, parents, new, *_) in zip(streams, calls):
+            F.fl_k_kv_fork(pool.caches, pool.pages[t % 2], pool.pages[1 - t % 2], parents[t], new, pool.workspace, pool.status,
+                           stream=stream)
+    torch.cuda.synchronize()
+    for pool, parents, _, _, *lists, bits in calls:
+        for p in parents:
+            lists = list(fork(*lists[:3], 16, p, [1] * len(p)))
+            bits = moved_bits(bits, lists[3])
+        assert pool.get() == lists[:3] and int(pool.status.item()) == 0
+        assert all(torch.equal(a, b) for a, b in zip(bits, pool.bits()))

@@ -900,8 +900,9 @@ FL_DEV uint32_t ld_cluster_u8(const void* p, uint32_t rank) {
 // of 16 becomes one map from the beams behind it to those before it, all at once from shared memory; those together give
 // the CTA's map, the CTAs learn each other's, the hypotheses jump from CTA to CTA and from chunk to chunk, and then all
 // chunks are walked at once for the beams in between.  Latency is the bound: 64 x 16 hypotheses of 2048 steps 16.7 us (a CTA a
-// search 44), the best of 16 x 4 of 256 steps 6.6
-__global__ void __launch_bounds__(TRACE_THREADS) beam_trace_kernel(TraceArgs a) {
+// search 44), the best of 16 x 4 of 256 steps 6.2.  Eight CTAs fit an SM, a call's beside the last one's: with room for
+// four 64 x 16 took 19.7.
+__global__ void __launch_bounds__(TRACE_THREADS, 8) beam_trace_kernel(TraceArgs a) {
   pdl_wait();
   pdl_trigger();
   extern __shared__ __align__(16) int32_t token[];  // [step][beam], a step's row from another bank than the next one's; then bytes
@@ -1097,10 +1098,12 @@ extern "C" int fl_k_beam_trace(const fl_beam_search* search, const fl_beam_state
       fl_misaligned(out_lens, 4) || fl_misaligned(out_scores, 4) || fl_misaligned(status, 4))
     return fl_internal_error(FL_ERR_INVALID_ARG, "beam trace: args");
   const float penalty = (float)search->length_penalty;
-  // CTAs of 256 steps, as many as a cluster has; longer ones where those are too few
+  // CTAs of 64 steps, as many as a cluster has; longer ones where those are too few (the best of 16 x 4 beams of 256 steps with CTAs of
+  // 256 6.7 us)
+  constexpr int CTA_STEPS = 64;
   const int T = search->max_steps;
   int ctas = 1;
-  while (ctas < MAX_TRACE_CTAS && T > ctas * 256) ctas *= 2;
+  while (ctas < MAX_TRACE_CTAS && T > ctas * CTA_STEPS) ctas *= 2;
   const int block = std::min(MAX_STEPS, std::max(CHUNK, (T + ctas - 1) / ctas)), chunks = (block + CHUNK - 1) / CHUNK;
   const TraceArgs a{*search,    *state, trace_tokens, trace_parents, n_best, pad, penalty, (float)(search->length_penalty - penalty), block,
                     out_tokens, out_lens, out_scores, status};

@@ -203,7 +203,7 @@ class BlockStack:
             raise
 
     def _positions(self, new):
-        """The two position streams of the new tokens: (i, 0) in the context, (mask, 1 ..) in the span."""
+        """The two position streams of the new tokens, (i, 0) in the context, (mask, 1 ..) in the span, and the sequences' contexts."""
         first, second = [], []
         for s, n in enumerate(new):
             c = self.context[s] - self.cfg.prefix_len if self.context[s] else 0
@@ -211,8 +211,8 @@ class BlockStack:
                 span = c > 0 and i >= c
                 first.append(self.mask_pos[s] if span else i)
                 second.append(i - c + 1 if span else 0)
-        two = any(self.context)
-        return torch.tensor(first, dtype=I32).cuda(), torch.tensor(second, dtype=I32).cuda() if two else None
+        on = [torch.tensor(v, dtype=I32).cuda() for v in (first, second, self.context)]
+        return on if any(self.context) else (on[0], None, None)
 
     def forward(self, x: torch.Tensor, new: Sequence[int]) -> torch.Tensor:
         """x: bf16 [sum(new), hidden], new[s] next tokens of sequence s; returns the blocks' output of them.  A context's
@@ -236,8 +236,8 @@ class BlockStack:
 
     def follow(self, x: torch.Tensor, parents: torch.Tensor) -> torch.Tensor:
         """x: bf16 [sequences, hidden], one token behind each; sequence s first becomes what sequence parents[s] was (device int32, -1:
-        an empty one), as a step of a beam search picks it.  Whole pages are shared, a partly filled one is copied.  From the
-        first such call on the pages are kept on the device, and ``forward`` is refused.  A call that raises
+        an empty one), with its context and mask, as a step of a beam search picks it.  Whole pages are shared, a partly filled
+        one is copied.  From the first such call on the pages are kept on the device, and ``forward`` is refused.  A call that raises
         has spoilt the sequences."""
         n, c = len(self.context), self.cfg
         if not x.is_cuda or x.shape != (n, c.hidden):
@@ -246,21 +246,21 @@ class BlockStack:
             raise ValueError(f"{parents.dtype} parents {tuple(parents.shape)} on {parents.device}, not int32 [{n}] on the device")
         if self.shared is None:
             self.shared = SharedPages(self.pages, [b["cache"] for b in self.blocks])
-            self.shared.context, self.shared.mask = (torch.tensor(v, dtype=I32).cuda() for v in (self.context, self.mask_pos))
+            self.shared.kept = torch.tensor([self.context, self.mask_pos], dtype=I32).cuda()
         batch = self.shared.step(parents.contiguous(), self.status)
+        # what a sequence has of its parent beside the pages (a parent out of range has been told to the status)
+        self.shared.kept = torch.where(parents >= 0, self.shared.kept[:, parents.clamp(0, n - 1).long()], 0)
+        context, mask = self.shared.kept
         # as _positions, on the device; a sequence that has just begun has no prefix
         i = (self.shared.sides[0]["lens"] - 1 - c.prefix_len).clamp(min=0)
-        first, second = i, None
-        if any(self.context):
-            own = (self.shared.context - c.prefix_len).clamp(min=0)
-            span = (own > 0) & (i >= own)
-            first = torch.where(span, self.shared.mask, i)
-            second = torch.where(span, i - own + 1, 0).to(I32)
-        return self._run(x, batch, first.to(I32), second)
+        if not any(self.context):
+            return self._run(x, batch, i.to(I32), None, None)
+        own = (context - c.prefix_len).clamp(min=0)
+        span = (own > 0) & (i >= own)
+        return self._run(x, batch, torch.where(span, mask, i).to(I32), torch.where(span, i - own + 1, 0).to(I32), context)
 
-    def _run(self, x, batch, pos, pos2):
+    def _run(self, x, batch, pos, pos2, context):
         c, T, H, Fh = self.cfg, len(x), self.cfg.hidden, self.cfg.ffn_hidden
-        context = torch.tensor(self.context, dtype=I32).cuda() if pos2 is not None else None
         if self.workspace is None:  # the same for every batch
             size = F.fl_k_kv_attention_workspace(c.n_heads, self.blocks[0]["cache"], batch)
             self.workspace = torch.zeros(size // 4, dtype=I32, device="cuda")
@@ -416,8 +416,6 @@ class Generator:
         for k, p in enumerate(prompts):
             for stack, s in ((wide.server, k * beams), (wide.bottom[k], 0), (wide.top[k], 0)):
                 stack.start(s, len(p))
-                for b in range(1, beams):
-                    stack.context[s + b], stack.mask_pos[s + b] = stack.context[s], stack.mask_pos[s]
         search = F.beam_search(n, beams, vocab, count, eos=eos, length_penalty=length_penalty, early=early)
         state = {"scores": torch.full((n, beams), -float("inf"), device="cuda"),
                  "end_scores": torch.full((n, beams), -float("inf"), device="cuda")}

@@ -236,9 +236,9 @@ class BlockStack:
 
     def follow(self, x: torch.Tensor, parents: torch.Tensor) -> torch.Tensor:
         """x: bf16 [sequences, hidden], one token behind each; sequence s first becomes what sequence parents[s] was (device int32, -1:
-        an empty one), with its context and mask, as a step of a beam search picks it.  Whole pages are shared, a partly filled
-        one is copied.  From the first such call on the pages are kept on the device, and ``forward`` is refused.  A call that raises
-        has spoilt the sequences."""
+        an empty one, without a prefix), with its context and mask, as a step of a beam search picks it.  Whole pages are shared, a
+        partly filled one is copied.  From the first such call on the pages are kept on the device, and ``forward`` is refused.  A
+        call that raises has spoilt the sequences."""
         n, c = len(self.context), self.cfg
         if not x.is_cuda or x.shape != (n, c.hidden):
             raise ValueError(f"x {tuple(x.shape)} on {x.device} for a token of {c.hidden} behind each of {n} sequences")
@@ -246,16 +246,17 @@ class BlockStack:
             raise ValueError(f"{parents.dtype} parents {tuple(parents.shape)} on {parents.device}, not int32 [{n}] on the device")
         if self.shared is None:
             self.shared = SharedPages(self.pages, [b["cache"] for b in self.blocks])
-            self.shared.kept = torch.tensor([self.context, self.mask_pos], dtype=I32).cuda()
+            prefix = [c.prefix_len if held >= c.prefix_len else 0 for held in self.pages.lens]
+            self.shared.kept = torch.tensor([self.context, self.mask_pos, prefix], dtype=I32).cuda()
         batch = self.shared.step(parents.contiguous(), self.status)
         # what a sequence has of its parent beside the pages (a parent out of range has been told to the status)
         self.shared.kept = torch.where(parents >= 0, self.shared.kept[:, parents.clamp(0, n - 1).long()], 0)
-        context, mask = self.shared.kept
-        # as _positions, on the device; a sequence that has just begun has no prefix
-        i = (self.shared.sides[0]["lens"] - 1 - c.prefix_len).clamp(min=0)
+        context, mask, prefix = self.shared.kept
+        # as _positions, on the device (no tokens: what a refused step leaves of an empty sequence)
+        i = (self.shared.sides[0]["lens"] - 1 - prefix).clamp(min=0)
         if not any(self.context):
             return self._run(x, batch, i.to(I32), None, None)
-        own = (context - c.prefix_len).clamp(min=0)
+        own = context - torch.where(context > 0, prefix, 0)
         span = (own > 0) & (i >= own)
         return self._run(x, batch, torch.where(span, mask, i).to(I32), torch.where(span, i - own + 1, 0).to(I32), context)
 

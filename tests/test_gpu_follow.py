@@ -51,3 +51,31 @@ def test_context_and_mask_come_from_the_parent(F, prefix):
             want = alone(lambda: BlockStack.from_server(srv, 1, 100, page_size=16), tokens, c, m)
             assert rel_inf(y[s:s + 1].double().cpu().numpy(), want.double().cpu().numpy()) < TOL, (t, s)
     srv.close()
+
+
+@pytest.mark.parametrize("glm", [False, True])
+def test_a_sequence_that_begins_anew_has_no_prefix(F, glm):
+    """Parent -1 in a stack with a prefix: what it says is that of the same blocks without a prefix, from position 0 on."""
+    from paper_2406_14898_gb300.generate import BlockStack
+    srv, bare = server(F, 2, 4, 64, 64, 7), server(F, 2, 4, 64, 64)
+    for b in range(2):
+        for t in range(12):
+            bare.set_param(b, t, srv.get_param(b, t))
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    stack = BlockStack.from_server(srv, 3, 60, page_size=16)
+    for s in range(2):  # the third is not even started
+        stack.start(s, 11 if glm else 0)
+    prompt = rows(gen, 11)
+    stack.forward(prompt, [11, 0, 0])
+    have = {0: (srv, 11 if glm else 0, prompt)}
+    parents = [[0, -1, 2], [0, 1, 2], [1, -1, 0], [0, 1, 1]] + [[s, s, s] for s in (0, 1)] + [[0, 1, 2]] * 12
+    for t, p in enumerate(parents):
+        x = rows(gen, 3)
+        y = stack.follow(x, torch.tensor(p, dtype=torch.int32, device="cuda"))
+        have = {s: have.get(q, (bare, 0, prompt[:0])) for s, q in enumerate(p)}
+        have = {s: (w, c, torch.cat([v, x[s:s + 1]])) for s, (w, c, v) in have.items()}
+        for s, (w, c, tokens) in have.items():
+            want = alone(lambda: BlockStack.from_server(w, 1, 60, page_size=16), tokens, c, None)
+            assert rel_inf(y[s:s + 1].double().cpu().numpy(), want.double().cpu().numpy()) < TOL, (t, s)
+    srv.close()
+    bare.close()

@@ -237,8 +237,8 @@ class BlockStack:
     def follow(self, x: torch.Tensor, parents: torch.Tensor) -> torch.Tensor:
         """x: bf16 [sequences, hidden], one token behind each; sequence s first becomes what sequence parents[s] was (device int32, -1:
         an empty one, without a prefix), with its context and mask, as a step of a beam search picks it.  Whole pages are shared, a
-        partly filled one is copied.  From the first such call on the pages are kept on the device, and ``forward`` is refused.  A
-        call that raises has spoilt the sequences."""
+        partly filled one is copied.  A sequence whose context is not there yet is not followed (RuntimeError).  From the first such
+        call on the pages are kept on the device, and ``forward`` is refused.  A call that raises has spoilt the sequences."""
         n, c = len(self.context), self.cfg
         if not x.is_cuda or x.shape != (n, c.hidden):
             raise ValueError(f"x {tuple(x.shape)} on {x.device} for a token of {c.hidden} behind each of {n} sequences")
@@ -252,6 +252,8 @@ class BlockStack:
         # what a sequence has of its parent beside the pages (a parent out of range has been told to the status)
         self.shared.kept = torch.where(parents >= 0, self.shared.kept[:, parents.clamp(0, n - 1).long()], 0)
         context, mask, prefix = self.shared.kept
+        early = (self.shared.sides[0]["lens"] <= context).any()  # a context's tokens see each other: they come before
+        self.status.bitwise_or_(torch.where(early, F.FL_KV_BAD_POSITION, 0).to(I32))
         # as _positions, on the device (no tokens: what a refused step leaves of an empty sequence)
         i = (self.shared.sides[0]["lens"] - 1 - prefix).clamp(min=0)
         if not any(self.context):

@@ -79,3 +79,24 @@ def test_a_sequence_that_begins_anew_has_no_prefix(F, glm):
             assert rel_inf(y[s:s + 1].double().cpu().numpy(), want.double().cpu().numpy()) < TOL, (t, s)
     srv.close()
     bare.close()
+
+
+def test_a_context_that_is_not_there_yet_is_not_followed(F):
+    """As in a call of its own: a context's tokens come together, so none of them follows a sequence that has not got them."""
+    from paper_2406_14898_gb300.generate import BlockStack
+    srv = server(F, 1, 4, 64, 64)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+
+    def stack():
+        st = BlockStack.from_server(srv, 2, 60, page_size=16)
+        for s in range(2):
+            st.start(s, 9)
+        st.forward(rows(gen, 9), [9, 0])
+        return st
+
+    good, bad = stack(), stack()
+    good.follow(rows(gen, 2), torch.tensor([0, -1], dtype=torch.int32, device="cuda"))
+    good.follow(rows(gen, 2), torch.tensor([0, 1], dtype=torch.int32, device="cuda"))
+    with pytest.raises(RuntimeError):
+        bad.follow(rows(gen, 2), torch.tensor([0, 1], dtype=torch.int32, device="cuda"))
+    srv.close()

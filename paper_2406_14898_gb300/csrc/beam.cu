@@ -6,11 +6,13 @@
 // threads' maxima bounds the B-th largest logit from below; of what comes later only what exceeds the bound is looked
 // at, about B logits for each time that what has been seen doubles, which is when the bound is raised.  A second kernel, a
 // CTA a search, joins the parts' sums and lists.  (With the join in the CTA that comes last, CTAs that joined came late
-// for their next parts and so joined again: 64 x 16 rows of 130528 bf16 157 us, when two kernels took 92.)
+// for their next parts and so joined again: 64 x 16 rows of 130528 bf16 157 us, when two kernels took 92.)  Sums are kept for each
+// chunk of a row, whose places do not depend on the cut (a part's sums as one: 64 x 16 rows of bf16 65.4 us for 68.1, but equal
+// rows that were cut otherwise had sums that differed in their last bits).
 //
-// Many rows are bound by HBM and the instructions beside it: 1024 x 1 rows of 130528 fp32 92 us (5.8 TB/s), bf16 54 (4.9), 64 x 16
-// rows of bf16 65.5 (4.1), of which the pass alone takes 49, the hits and lists 8, the join 8.  Few rows are bound by latency: 1 x 4
-// rows of fp32 8.8 us, of which the join takes 4.
+// Many rows are bound by HBM and the instructions beside it: 1024 x 1 rows of 130528 fp32 93 us (5.7 TB/s), bf16 56.5 (4.7), 64 x 16
+// rows of bf16 68 (3.9), of which the hits and lists take 8, the join 8.  Few rows are bound by latency: 1 x 4 rows of fp32 8.8
+// us, of which the join takes 4.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -45,7 +47,7 @@ struct StepArgs {
   int row_chunks, usual_parts;  // of a row; parts that a row is cut into at most where all beams are live
   float penalty_hi, penalty_lo;
   int32_t *trace_tokens, *trace_parents, *tokens, *parents;
-  float2* sums;  // [row][part] (a logit, sum of exp(x - it))
+  float2* sums;  // [row][chunk] (its largest logit, sum of exp(x - it))
   Cand* lists;   // [row][part][beam], best first; x = -inf: none
   int32_t* parts;  // [row] parts that it was cut into
   int* status;
@@ -202,36 +204,43 @@ FL_DEV uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
-// sum of exp(x - ref) over what a thread has seen.  The exponents are x log2(e) - c, c = ref log2(e) rounded, one fused
-// operation each; what the rounding of c took (the same factor for all) is given back when ref changes and in the end.  Where ref is so
-// large that this is no small factor, x - ref is taken first.
+// sum of exp(x - ref) over a thread's logits of a chunk, ref the largest of its warp's: so a chunk's sum depends on nothing but the
+// chunk, wherever the rows are cut and whatever else is in the call, and rows of equal logits have equal sums.  The exponents are
+// x log2(e) - c, c = ref log2(e) rounded, one fused operation each; what the rounding of c took (the same factor for all)
+// is given back in the end.  Where ref is so large that this is no small factor, x - ref is taken first.
 struct Sum {
-  float ref = -INFINITY;
-  uint64_t minus = 0, sum = 0;  // (-c, -c), or (-ref, -ref) where ref is far; sums of every other element
-  FL_DEV bool far() const { return fabsf(ref) > 4096.f; }  // (-inf, before the first x: so that nothing is a NaN)
+  float ref;                // (0 where there is no number)
+  uint64_t minus, sum = 0;  // (-c, -c); sums of every other element
+  FL_DEV explicit Sum(float x) : ref(x == -INFINITY ? 0.f : x), minus(pack2(-ref * LOG2E, -ref * LOG2E)) {}
+  FL_DEV bool far() const { return fabsf(ref) > 4096.f; }
   FL_DEV void add(float x, float y) {
     const float2 u = unpack2(fma2(pack2(x, y), pack2(LOG2E, LOG2E), minus));
     sum = add2(sum, pack2(exp2_hw(u.x), exp2_hw(u.y)));
   }
-  FL_DEV void add_far(float x) {
-    sum = add2(sum, pack2(exp2_hw((x - (ref == -INFINITY ? 0.f : ref)) * LOG2E), 0.f));
-  }
-  FL_DEV float total() const {
+  FL_DEV void add_far(float x) { sum = add2(sum, pack2(exp2_hw((x - ref) * LOG2E), 0.f)); }
+  // The warp's, from all of its lanes.
+  FL_DEV float of_warp() const {
     const float2 u = unpack2(sum);
-    if (far()) return u.x + u.y;
-    const float d = LN2 * fmaf(ref, LOG2E, unpack2(minus).x);  // 2^-12 at most: e^-d from its first terms
-    return (u.x + u.y) * (1.f - d + 0.5f * d * d);
+    float x = u.x + u.y;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    const float e = far() ? 0.f : LN2 * fmaf(ref, LOG2E, unpack2(minus).x);  // 2^-12 at most: e^-e from its first terms
+    return x * (1.f - e + 0.5f * e * e);
   }
-  // room for x: sums of up to 2^19 exponentials of 16 and less are far from overflow
-  FL_DEV void see(float x) {
-    if (x > ref + 16.f) {
-      const float s = ref == -INFINITY ? total() : total() * exp2_hw((ref - x) * LOG2E);  // (0, or a NaN that stays)
-      ref = x;
-      const float c = far() ? x : x * LOG2E, d = far() ? 0.f : LN2 * fmaf(ref, LOG2E, -c);
-      minus = pack2(-c, -c);
-      sum = pack2(s + s * (d + 0.5f * d * d), 0.f);
-    }
-  }
+};
+// (a logit, sum of exp(x - it)): the same sum from a larger one, and two of them as one.
+FL_DEV float scaled(float2 p, float m) {
+  return p.x == -INFINITY ? p.y : p.x == INFINITY ? NAN : p.y * exp2_hw((p.x - m) * LOG2E);
+}
+FL_DEV float2 joined(float2 p, float2 q) {
+  const float m = fmaxf(p.x, q.x);
+  return make_float2(m, scaled(p, m) + scaled(q, m));
+}
+
+// A warp's 32 numbers in shared memory, each lane's own.
+struct Lanes {
+  float at[32];
+  FL_DEV void operator=(float x) { at[threadIdx.x & 31] = x; }
 };
 
 // Shared memory of a search's join; behind it each warp's copy of a row's lists.
@@ -306,17 +315,19 @@ __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a)
     const int said = __ldg(a.parts + row);
     Cand* mine = reinterpret_cast<Cand*>(&j + 1) + warp * MAX_PARTS * B;
     const Cand* lists = a.lists + (int64_t)row * MAX_PARTS * B;
-    float2 part = __ldg(a.sums + (int64_t)row * MAX_PARTS + lane);  // (of any content behind the parts)
+    const float2* sums = a.sums + (int64_t)row * a.row_chunks;
+    float2 part = lane < a.row_chunks ? sums[lane] : make_float2(-INFINITY, 0.f);  // (of any content where the row is not used)
     const float e = a.p.eos >= 0 ? Piece<T>::one(((const T*)a.x)[(int64_t)row * a.ld + a.p.eos]) : -INFINITY;
     for (int i = lane; i < a.usual_parts * B; i += 32) mine[i] = lists[i];
     const bool reads = active && score > -INFINITY && score < INFINITY;
     const int P = reads ? said : 0;
     for (int i = a.usual_parts * B + lane; i < P * B; i += 32) mine[i] = lists[i];
-    if (lane >= P) part = make_float2(-INFINITY, 0.f);
+    if (!reads) part = make_float2(-INFINITY, 0.f);
+    for (int c = lane + 32; reads && c < a.row_chunks; c += 32) part = joined(part, sums[c]);
     float m = part.x;
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    float sum = part.x == -INFINITY ? part.y : part.x == INFINITY ? NAN : part.y * exp2_hw((part.x - m) * LOG2E);
+    float sum = scaled(part, m);
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     const bool bad = active && (score != score || score == INFINITY || (reads && sum != sum)), live = reads && !bad && m > -INFINITY;
@@ -468,12 +479,13 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
   using Io = Piece<T>;
   constexpr int N = Io::N;
   constexpr int RING = STAGES * CHUNK_PIECES * 16;
-  static_assert(CTAS * (RING + MAX_HITS * sizeof(Cand) + MAX_ROWS * 4 + THREADS * 4 + 4 * GROUPS * 4 + 128 + 1024) <= 228 * 1024,
+  static_assert(CTAS * (RING + MAX_HITS * sizeof(Cand) + MAX_ROWS * 4 + 2 * WARPS * sizeof(Lanes) + 4 * GROUPS * 4 + 128 + 1024) <= 228 * 1024,
                 "so many CTAs fit an SM, which keeps 1 KB of each");
   __shared__ __align__(16) uint32_t sh_group[2][GROUPS], sh_key[2][GROUPS];
-  __shared__ float sh_ref[WARPS], sh_sum[WARPS];
+  __shared__ Lanes sh_ref[WARPS], sh_sum[WARPS];  // of a warp's part of up to 32 chunks
   __shared__ int sh_count, sh_few, sh_warp[WARPS];
-  __shared__ uint32_t sh_bits[THREADS];
+  uint32_t* const sh_bits = reinterpret_cast<uint32_t*>(sh_sum);  // [THREADS], before there are sums
+  static_assert(sizeof(sh_sum) == THREADS * sizeof(uint32_t));
   __shared__ int sh_rows[MAX_ROWS];
   __shared__ Cand sh_hits[MAX_HITS];
   extern __shared__ __align__(16) uint4 sh_ring[];  // [STAGES][CHUNK_PIECES]
@@ -624,12 +636,11 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
     {
       const int k = c / L, row = sh_rows[k - k0], from = c - k * L, to = min(L, from + c1 - c);
       c += to - from;
-      const int begin = from * CHUNK_PIECES, end = min(all, to * CHUNK_PIECES);
+      const int part_begin = from * CHUNK_PIECES, part_end = min(all, to * CHUNK_PIECES);
       // which part of its row: its CTA's distance from the one of the row's first chunk
       const int part = ctas == (int64_t)n_live * L ? from : blockIdx.x - (int)kv_div(((int64_t)k * L + 1) * ctas - 1, (int64_t)n_live * L);
       const int64_t at_part = (int64_t)row * MAX_PARTS + part;
-      const int eos_piece = a.p.eos >= 0 && a.p.eos / N >= begin && a.p.eos / N < end ? a.p.eos / N : -1;
-      Sum z;
+      const int eos_piece = a.p.eos >= 0 && a.p.eos / N >= part_begin && a.p.eos / N < part_end ? a.p.eos / N : -1;
       float bound = -INFINITY, most = -INFINITY;  // of this thread
       bool settled = false;                       // the bound is that of all that has been seen
       if (tid == 0) sh_count = sh_few = 0;
@@ -656,177 +667,180 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
           rank += (y.x > key) + (y.y > key) + (y.z > key) + (y.w > key);
         }
         const float b = unorder32(__reduce_min_sync(0xffffffffu, rank < B ? ordered : 0xffffffffu));
-        z.see(unorder32(__reduce_max_sync(0xffffffffu, ordered)));
         const bool higher = b > bound;
         bound = b;
         settled = true;
         return higher;
       };
-      for (int first = begin, chunk = 0; first < end; first += CHUNK_PIECES, ++chunk) {
-        cp_async_wait<STAGES - 1>();
-        uint4* places = sh_ring + stage * CHUNK_PIECES + tid;  // this thread's
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
-        // nothing behind the slice's end and the vocabulary; the eos is summed, but no candidate to go on with
-        if (first + CHUNK_PIECES >= end) {
+      // 32 chunks at a time, lane i of each warp with its part of the i-th one's sum
+      for (int begin = part_begin; begin < part_end; begin += 32 * CHUNK_PIECES) {
+        const int end = min(part_end, begin + 32 * CHUNK_PIECES);
+        struct { float ref, sum; } z{-INFINITY, 0.f};
+        for (int first = begin, chunk = 0; first < end; first += CHUNK_PIECES, ++chunk) {
+          cp_async_wait<STAGES - 1>();
+          uint4* places = sh_ring + stage * CHUNK_PIECES + tid;  // this thread's
+          stage = stage + 1 == STAGES ? 0 : stage + 1;
+          // nothing behind the slice's end and the vocabulary; the eos is summed, but no candidate to go on with
+          if (first + CHUNK_PIECES >= end) {
 #pragma unroll 1
-          for (int i = 0; i < PIECES; ++i) {
-            const int k = first + i * THREADS + tid;
-            if (k >= end) places[i * THREADS] = make_uint4(Io::NONE, Io::NONE, Io::NONE, Io::NONE);
-            else if ((k + 1) * N > a.p.vocab)
-              for (int v = a.p.vocab - k * N; v < N; ++v) reinterpret_cast<T*>(places + i * THREADS)[v] = (T)-INFINITY;
+            for (int i = 0; i < PIECES; ++i) {
+              const int k = first + i * THREADS + tid;
+              if (k >= end) places[i * THREADS] = make_uint4(Io::NONE, Io::NONE, Io::NONE, Io::NONE);
+              else if ((k + 1) * N > a.p.vocab)
+                for (int v = a.p.vocab - k * N; v < N; ++v) reinterpret_cast<T*>(places + i * THREADS)[v] = (T)-INFINITY;
+            }
           }
-        }
-        if (eos_piece >= first && eos_piece < first + CHUNK_PIECES && (eos_piece - first) % THREADS == tid) {
-          T* at = reinterpret_cast<T*>(places + (eos_piece - first - tid)) + a.p.eos % N;
-          const float y = Io::one(*at);
-          *at = (T)-INFINITY;
-          z.see(y);
-          if (z.far()) z.add_far(y);
-          else z.add(y, -INFINITY);
-        }
-        uint4 cur[PIECES];
-        uint32_t largest = Io::NONE;
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) cur[i] = places[i * THREADS];
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) largest = Io::max2(largest, Io::max4(cur[i]));
-        const float top = Io::top(largest);
-        most = fmaxf(most, top);
-        bool equals = false;  // whether logits equal to the bound count: it is new, and fewer than B larger ones may have been seen
-        const int seen = chunk + 1;
-        settled = false;
-        if ((seen & chunk) == 0) equals = raise() || chunk == 0;
-        const bool look = top > -INFINITY && (equals ? top >= bound : top > bound);
-        if (look) z.see(top);
-        if (!z.far()) {
-#pragma unroll
-          for (int i = 0; i < PIECES; ++i) {
-            float f[N];
-            Io::get(cur[i], f);
-#pragma unroll
-            for (int k = 0; k < N; k += 2) z.add(f[k], f[k + 1]);
+          float apart = -INFINITY;
+          if (eos_piece >= first && eos_piece < first + CHUNK_PIECES && (eos_piece - first) % THREADS == tid) {
+            T* at = reinterpret_cast<T*>(places + (eos_piece - first - tid)) + a.p.eos % N;
+            apart = Io::one(*at);
+            *at = (T)-INFINITY;
           }
-        } else {
+          uint4 cur[PIECES];
+          uint32_t largest = Io::NONE;
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i) cur[i] = places[i * THREADS];
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i) largest = Io::max2(largest, Io::max4(cur[i]));
+          const float top = Io::top(largest);
+          most = fmaxf(most, top);
+          bool equals = false;  // whether logits equal to the bound count: it is new, and fewer than B larger ones may have been seen
+          const int seen = chunk + 1;
+          settled = false;
+          if ((seen & chunk) == 0) equals = raise() || chunk == 0;
+          const bool look = top > -INFINITY && (equals ? top >= bound : top > bound);
+          const float ref = unorder32(__reduce_max_sync(0xffffffffu, order32(fmaxf(top, apart))));
+          Sum one(ref);
+          if (!one.far()) {
+            if (apart != -INFINITY) one.add(apart, -INFINITY);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+              float f[N];
+              Io::get(cur[i], f);
+#pragma unroll
+              for (int k = 0; k < N; k += 2) one.add(f[k], f[k + 1]);
+            }
+          } else {
+            if (apart != -INFINITY) one.add_far(apart);
 #pragma unroll 1
-          for (int i = 0; i < PIECES * N; ++i) z.add_far(Io::one(reinterpret_cast<const T*>(places + i / N * THREADS)[i % N]));
-        }
-        // what exceeds the bound, a thread's logits at a time by its whole warp
-        if (unsigned who = __ballot_sync(0xffffffffu, look)) {
-          __syncwarp();  // (a thread's own copies are seen by the others)
-          const uint4* its = places - lane + lane / 4 * THREADS;
-          const int its_first = (first + lane / 4 * THREADS + tid - lane) * N + lane % 4 * (N / 4);
-          for (; who; who &= who - 1) {
-            const int l = __ffs(who) - 1;
-            float f[N / 4];
-            Io::word(reinterpret_cast<const uint32_t*>(its + l)[lane % 4], f);
+            for (int i = 0; i < PIECES * N; ++i) one.add_far(Io::one(reinterpret_cast<const T*>(places + i / N * THREADS)[i % N]));
+          }
+          const float total = one.of_warp();
+          if (lane == chunk) z = {ref, total};
+          // what exceeds the bound, a thread's logits at a time by its whole warp
+          if (unsigned who = __ballot_sync(0xffffffffu, look)) {
+            __syncwarp();  // (a thread's own copies are seen by the others)
+            const uint4* its = places - lane + lane / 4 * THREADS;
+            const int its_first = (first + lane / 4 * THREADS + tid - lane) * N + lane % 4 * (N / 4);
+            for (; who; who &= who - 1) {
+              const int l = __ffs(who) - 1;
+              float f[N / 4];
+              Io::word(reinterpret_cast<const uint32_t*>(its + l)[lane % 4], f);
 #pragma unroll
-            for (int k = 0; k < N / 4; ++k)
-              if (f[k] > bound || (equals && f[k] == bound && f[k] > -INFINITY)) {
-                const int n = atomicAdd(&sh_count, 1);
-                if (n < MAX_HITS) sh_hits[n] = Cand{f[k], its_first + l * N + k};
+              for (int k = 0; k < N / 4; ++k)
+                if (f[k] > bound || (equals && f[k] == bound && f[k] > -INFINITY)) {
+                  const int n = atomicAdd(&sh_count, 1);
+                  if (n < MAX_HITS) sh_hits[n] = Cand{f[k], its_first + l * N + k};
+                }
+            }
+            __syncwarp();  // the places have been read
+          }
+          ask_more();  // into the stage that has been read
+        }
+        const float ref = z.ref;
+        const float sum = z.sum;
+        sh_ref[warp] = ref;
+        sh_sum[warp] = sum;
+        // The part's list: of what has come together, what reaches the bound of the whole part, ranked by counting.
+        const bool early = !settled;
+        if (early) raise();
+        else __syncthreads();
+        int n = sh_count;
+        if (end == part_end) {
+          const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld);
+          if (n > MAX_HITS) {
+            // more than there was room for (logits that ascend): once more through the part, with that bound
+            __syncthreads();
+            if (tid == 0) sh_count = 0;
+            __syncthreads();
+            for (int k = part_begin + tid; k < part_end; k += THREADS) {
+              float f[N];
+              Io::get(__ldg(x + k), f);
+              for (int e = 0; e < N; ++e)
+                if (f[e] >= bound && f[e] > -INFINITY && k * N + e < a.p.vocab && k * N + e != a.p.eos) {
+                  const int at = atomicAdd(&sh_count, 1);
+                  if (at < MAX_HITS) sh_hits[at] = Cand{f[e], k * N + e};
+                }
+            }
+            __syncthreads();
+            n = sh_count;
+          } else if (early && n > 32) {
+            static_assert(MAX_HITS == 2 * THREADS);
+            const Cand h0 = sh_hits[tid], h1 = sh_hits[tid + THREADS];
+            __syncthreads();
+            if (tid < n && h0.x >= bound) sh_hits[atomicAdd(&sh_few, 1)] = h0;
+            if (tid + THREADS < n && h1.x >= bound) sh_hits[atomicAdd(&sh_few, 1)] = h1;
+            __syncthreads();
+            n = sh_few;
+          }
+          Cand* list = a.lists + at_part * B;
+          if (n <= MAX_HITS) {
+            for (int i = tid; i < n; i += THREADS) {
+              const Cand one = sh_hits[i];
+              int r = 0;
+              for (int o = 0; o < n; ++o) r += better(sh_hits[o], one);
+              if (r < B) list[r] = one;
+            }
+            if (tid >= n && tid < B) list[tid] = Cand{-INFINITY, 0};
+          } else {
+            // many equal logits: the best one behind the last found, B times
+            Cand found{INFINITY, -1};
+            for (int r = 0; r < B; ++r) {
+              Cand one{-INFINITY, 0x7fffffff};
+              for (int k = part_begin + tid; k < part_end; k += THREADS) {
+                float f[N];
+                Io::get(__ldg(x + k), f);
+                for (int e = 0; e < N; ++e) {
+                  const Cand y{f[e], k * N + e};
+                  if (y.v < a.p.vocab && y.v != a.p.eos && better(found, y) && better(y, one)) one = y;
+                }
               }
-          }
-          __syncwarp();  // the places have been read
-        }
-        ask_more();  // into the stage that has been read
-      }
-      float ref = z.ref;
 #pragma unroll
-      for (int d = 16; d; d >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, d));
-      float sum = z.ref == -INFINITY ? z.total() : z.total() * exp2_hw((z.ref - ref) * LOG2E);
-#pragma unroll
-      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      if (lane == 0) sh_ref[warp] = ref, sh_sum[warp] = sum;
-      // The part's list: of what has come together, what reaches the bound of the whole part, ranked by counting.
-      const bool early = !settled;
-      if (early) raise();
-      else __syncthreads();
-      int n = sh_count;
-      const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.ld);
-      if (n > MAX_HITS) {
-        // more than there was room for (logits that ascend): once more through the part, with that bound
-        __syncthreads();
-        if (tid == 0) sh_count = 0;
-        __syncthreads();
-        for (int k = begin + tid; k < end; k += THREADS) {
-          float f[N];
-          Io::get(__ldg(x + k), f);
-          for (int e = 0; e < N; ++e)
-            if (f[e] >= bound && f[e] > -INFINITY && k * N + e < a.p.vocab && k * N + e != a.p.eos) {
-              const int at = atomicAdd(&sh_count, 1);
-              if (at < MAX_HITS) sh_hits[at] = Cand{f[e], k * N + e};
-            }
-        }
-        __syncthreads();
-        n = sh_count;
-      } else if (early && n > 32) {
-        static_assert(MAX_HITS == 2 * THREADS);
-        const Cand h0 = sh_hits[tid], h1 = sh_hits[tid + THREADS];
-        __syncthreads();
-        if (tid < n && h0.x >= bound) sh_hits[atomicAdd(&sh_few, 1)] = h0;
-        if (tid + THREADS < n && h1.x >= bound) sh_hits[atomicAdd(&sh_few, 1)] = h1;
-        __syncthreads();
-        n = sh_few;
-      }
-      Cand* list = a.lists + at_part * B;
-      if (n <= MAX_HITS) {
-        for (int i = tid; i < n; i += THREADS) {
-          const Cand one = sh_hits[i];
-          int r = 0;
-          for (int o = 0; o < n; ++o) r += better(sh_hits[o], one);
-          if (r < B) list[r] = one;
-        }
-        if (tid >= n && tid < B) list[tid] = Cand{-INFINITY, 0};
-      } else {
-        // many equal logits: the best one behind the last found, B times
-        Cand found{INFINITY, -1};
-        for (int r = 0; r < B; ++r) {
-          Cand one{-INFINITY, 0x7fffffff};
-          for (int k = begin + tid; k < end; k += THREADS) {
-            float f[N];
-            Io::get(__ldg(x + k), f);
-            for (int e = 0; e < N; ++e) {
-              const Cand y{f[e], k * N + e};
-              if (y.v < a.p.vocab && y.v != a.p.eos && better(found, y) && better(y, one)) one = y;
+              for (int d = 16; d; d >>= 1) {
+                const Cand o{__shfl_xor_sync(0xffffffffu, one.x, d), __shfl_xor_sync(0xffffffffu, one.v, d)};
+                if (better(o, one)) one = o;
+              }
+              if (lane == 0) sh_hits[warp] = one;
+              __syncthreads();
+              for (int i = 0; i < WARPS; ++i)
+                if (better(sh_hits[i], one)) one = sh_hits[i];
+              __syncthreads();
+              if (tid == 0) list[r] = one;
+              found = one;
             }
           }
-#pragma unroll
-          for (int d = 16; d; d >>= 1) {
-            const Cand o{__shfl_xor_sync(0xffffffffu, one.x, d), __shfl_xor_sync(0xffffffffu, one.v, d)};
-            if (better(o, one)) one = o;
-          }
-          if (lane == 0) sh_hits[warp] = one;
-          __syncthreads();
-          for (int i = 0; i < WARPS; ++i)
-            if (better(sh_hits[i], one)) one = sh_hits[i];
-          __syncthreads();
-          if (tid == 0) list[r] = one;
-          found = one;
         }
-      }
-      if (warp == 0) {
-        const float r = lane < WARPS ? sh_ref[lane] : -INFINITY;
-        float m = r;
+        if (tid < (end - begin + CHUNK_PIECES - 1) / CHUNK_PIECES) {  // chunk tid's, the warps' in their order
+          const int at = begin / CHUNK_PIECES + tid;
+          float2 whole = make_float2(sh_ref[0].at[tid], sh_sum[0].at[tid]);
 #pragma unroll
-        for (int d = 1; d < WARPS; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        float q = lane < WARPS ? sh_sum[lane] : 0.f;
-        if (r != -INFINITY) q *= exp2_hw((r - m) * LOG2E);
-#pragma unroll
-        for (int d = 1; d < WARPS; d <<= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
-        if (lane == 0) {
-          a.sums[at_part] = make_float2(m, q);
-          if (to == L) a.parts[row] = part + 1;
+          for (int w = 1; w < WARPS; ++w) whole = joined(whole, make_float2(sh_ref[w].at[tid], sh_sum[w].at[tid]));
+          a.sums[(int64_t)row * L + at] = whole;
+          if (at == L - 1) a.parts[row] = part + 1;
         }
+        __syncthreads();  // the hits' and the sums' places are free again
       }
-      __syncthreads();  // the hits' and the sums' places are free again
     }
   }
   cp_async_wait<0>();  // (a first chunk that came for nothing)
   if (a.crowded) pdl_trigger();
 }
 
-int64_t part_bytes(const fl_beam_search* p) {
-  return (int64_t)p->n_seqs * p->beams * (MAX_PARTS * (sizeof(float2) + p->beams * sizeof(Cand)) + sizeof(int32_t)) + 16;
+// Chunks of a row of 16-byte pieces of N logits.
+int chunks_of(int vocab, int N) { return ((vocab + N - 1) / N + CHUNK_PIECES - 1) / CHUNK_PIECES; }
+
+int64_t part_bytes(const fl_beam_search* p) {  // (chunks of fp32 logits: the most)
+  return (int64_t)p->n_seqs * p->beams * (chunks_of(p->vocab, 4) * sizeof(float2) + MAX_PARTS * p->beams * sizeof(Cand) + sizeof(int32_t)) + 16;
 }
 
 const char* search_problem(const fl_beam_search* p, int* code) {
@@ -857,7 +871,7 @@ template <class T>
 int launch_step(StepArgs& a, cudaStream_t st) {
   constexpr int N = Piece<T>::N, ring = STAGES * CHUNK_PIECES * 16;
   const int rows = a.p.n_seqs * a.p.beams;
-  a.row_chunks = ((a.p.vocab + N - 1) / N + CHUNK_PIECES - 1) / CHUNK_PIECES;
+  a.row_chunks = chunks_of(a.p.vocab, N);
   // as many CTAs as run at once (more where one would have more rows than it keeps), and no more than chunks
   const int64_t slots = std::max(CTAS * fl_sm_count(), (rows + MAX_ROWS - 3) / (MAX_ROWS - 2));
   const int grid = (int)std::min<int64_t>(slots, (int64_t)rows * a.row_chunks);
@@ -1079,7 +1093,7 @@ extern "C" int fl_k_beam_step(const fl_beam_search* search, const fl_beam_state*
              tokens, parents, nullptr, nullptr, nullptr, status};
   a.sums = (float2*)workspace;
   const int64_t rows = (int64_t)search->n_seqs * search->beams;
-  a.lists = (Cand*)(a.sums + rows * MAX_PARTS);
+  a.lists = (Cand*)(a.sums + rows * chunks_of(search->vocab, 4));
   a.parts = (int32_t*)(a.lists + rows * MAX_PARTS * search->beams);
   const cudaStream_t st = (cudaStream_t)stream;
   return dtype == FL_DT_F32 ? launch_step<float>(a, st)

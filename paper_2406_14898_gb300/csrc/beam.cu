@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a)
   if (warp < B) {
     const int b = warp, row = s * B + b;
     const float score = a.from.scores[row];
-    const int said = __ldg(a.parts + row);
+    const int said = a.parts[row];
     Cand* mine = reinterpret_cast<Cand*>(&j + 1) + warp * MAX_PARTS * B;
     const Cand* lists = a.lists + (int64_t)row * MAX_PARTS * B;
     const float2* sums = a.sums + (int64_t)row * a.row_chunks;
@@ -765,7 +765,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
             __syncthreads();
             for (int k = part_begin + tid; k < part_end; k += THREADS) {
               float f[N];
-              Io::get(__ldg(x + k), f);
+              Io::get(x[k], f);
               for (int e = 0; e < N; ++e)
                 if (f[e] >= bound && f[e] > -INFINITY && k * N + e < a.p.vocab && k * N + e != a.p.eos) {
                   const int at = atomicAdd(&sh_count, 1);
@@ -799,7 +799,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) beam_step_kernel(StepArgs a) {
               Cand one{-INFINITY, 0x7fffffff};
               for (int k = part_begin + tid; k < part_end; k += THREADS) {
                 float f[N];
-                Io::get(__ldg(x + k), f);
+                Io::get(x[k], f);
                 for (int e = 0; e < N; ++e) {
                   const Cand y{f[e], k * N + e};
                   if (y.v < a.p.vocab && y.v != a.p.eos && better(found, y) && better(y, one)) one = y;
@@ -978,14 +978,19 @@ __global__ void __launch_bounds__(TRACE_THREADS, 8) beam_trace_kernel(TraceArgs 
     const int64_t first = ((int64_t)s * T + t0) * B;
     for (int i = tid; i < have * B; i += TRACE_THREADS) cp_async4(token + i / B * odd + i % B, a.tokens + first + i);
     cp_async_commit();
-#pragma unroll 4
-    for (int i = tid; i < have * B; i += TRACE_THREADS) {
-      int p = __ldg(a.parents + first + i);
-      if ((unsigned)p >= (unsigned)B) {
-        atomicOr(a.status, FL_BEAM_BAD_TRACE);
-        p = 0;
+    for (int i = tid; i < have * B; i += 4 * TRACE_THREADS) {
+      const int32_t* from = a.parents + first + i;
+      int p[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) p[k] = i + k * TRACE_THREADS < have * B ? from[k * TRACE_THREADS] : 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if ((unsigned)p[k] >= (unsigned)B) {
+          atomicOr(a.status, FL_BEAM_BAD_TRACE);
+          p[k] = 0;
+        }
+        if (i + k * TRACE_THREADS < have * B) par[i + k * TRACE_THREADS] = (uint8_t)p[k];
       }
-      par[i] = (uint8_t)p;
     }
     __syncthreads();
     for (int i = tid; i < nc * B; i += TRACE_THREADS) {

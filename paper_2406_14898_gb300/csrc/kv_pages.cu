@@ -48,7 +48,7 @@ int64_t ws_layout(int32_t* base, int64_t S, int64_t n_pages, Ws* w) {
 }
 
 FL_DEV int len_of(const PagesDev& a, int s, bool* bad = nullptr) {
-  const int len = __ldg(a.lens + s), L = (int)min((int64_t)max(len, 0), (int64_t)a.W << a.ps_log2);
+  const int len = a.lens[s], L = (int)min((int64_t)max(len, 0), (int64_t)a.W << a.ps_log2);
   if (L != len && bad) *bad = true;
   return L;
 }
@@ -62,8 +62,8 @@ struct Row {
 };
 FL_DEV Row row_of(const PagesDev& a, const int32_t* parents, const int32_t* grow, int s) {
   Row r;
-  const int own = len_of(a, s), more = grow ? __ldg(grow + s) : 0;
-  r.p = parents ? __ldg(parents + s) : s;
+  const int own = len_of(a, s), more = grow ? grow[s] : 0;
+  r.p = parents ? parents[s] : s;
   r.refuse = 0;
   r.bad = false;
   if (r.p < -1 || r.p >= a.S) {
@@ -79,7 +79,7 @@ FL_DEV Row row_of(const PagesDev& a, const int32_t* parents, const int32_t* grow
   r.had = pages_of(a, own);
   r.last = -1;
   if (r.L2 > r.L && (r.L & ((1 << a.ps_log2) - 1))) {
-    const int q = __ldg(a.table + (int64_t)r.p * a.W + r.held - 1);
+    const int q = a.table[(int64_t)r.p * a.W + r.held - 1];
     if ((unsigned)q < (unsigned)a.n_pages) r.last = q;
     else r.bad = true;
   }
@@ -143,12 +143,12 @@ struct Counts {
     lowest = ONE ? sh + 2 * a.n_pages : w.lowest;
     if (ONE) {
       for (int q = threadIdx.x; q < a.n_pages; q += PLAN_THREADS) {
-        have[q] = __ldg(a.refs + q);
+        have[q] = a.refs[q];
         writing[q] = lowest[q] = 0;
       }
     }
   }
-  FL_DEV int holders(int q) const { return ONE ? have[q] : __ldg(a.refs + q) + __ldcg(have + q); }
+  FL_DEV int holders(int q) const { return ONE ? have[q] : a.refs[q] + __ldcg(have + q); }
   FL_DEV int writers(int q) const { return ONE ? writing[q] : __ldcg(writing + q); }
   FL_DEV int first_writer(int q) const { return a.S - (ONE ? lowest[q] : __ldcg(lowest + q)); }
   FL_DEV void clear(int q) const {
@@ -216,8 +216,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, con
         if (e < all) {
           const int at = (int)kv_div(e, longest), i = (int)(e - (int64_t)at * longest);
           const int4 r = sh_changed[at];
-          if (i < r.z && !(r.x == r.y && i < r.w)) x[k] = __ldg(a.table + (int64_t)r.y * a.W + i);
-          if (i < r.w && !(r.x == r.y && i < r.z)) y[k] = __ldg(a.table + (int64_t)r.x * a.W + i);
+          if (i < r.z && !(r.x == r.y && i < r.w)) x[k] = a.table[(int64_t)r.y * a.W + i];
+          if (i < r.w && !(r.x == r.y && i < r.z)) y[k] = a.table[(int64_t)r.x * a.W + i];
         }
       }
 #pragma unroll
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, con
       const int at = (int)(wanted0 + (int64_t)(ahead.x >> 32));
       w.first[s] = at;
       w.rows[s] = make_int4(r.p, min(r.held, r.want), r.held - c, r.want);
-      a.lens_to[s] = refuse ? __ldg(a.lens + s) : r.L2;
+      a.lens_to[s] = refuse ? a.lens[s] : r.L2;
       if (c) w.copies[copies0 + (int)(uint32_t)ahead.x] = make_int4(r.last, at, r.L & ((1 << a.ps_log2) - 1), 0);
     }
     wanted0 += (int64_t)(total.x >> 32);
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(PagesDev a, con
       const bool taken = have == 0 && mine_at < all_wanted;
       if (taken && !refuse) w.list[mine_at] = x;
       const int leave = writers == 0 ? 0 : have == writers ? writers - 1 : writers;
-      a.refs_to[x] = refuse ? __ldg(a.refs + x) : taken ? 1 : have - leave;
+      a.refs_to[x] = refuse ? a.refs[x] : taken ? 1 : have - leave;
     }
     at += __popc(m);
   }
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, 
   // a warp's pages one after another
   const int wper = (a.n_pages + ctas * 32 - 1) / (ctas * 32), q0 = min(a.n_pages, (rank * 32 + (tid >> 5)) * wper),
             q1 = min(a.n_pages, q0 + wper);
-  const auto busy = [&](int q) { return __ballot_sync(0xffffffffu, q + lane < q1 && __ldg(a.refs + min(q + lane, a.n_pages - 1)) > 0); };
+  const auto busy = [&](int q) { return __ballot_sync(0xffffffffu, q + lane < q1 && a.refs[min(q + lane, a.n_pages - 1)] > 0); };
   Pair total;
   uint32_t n = 0;
   for (int q = q0; q < q1; q += 32) n += __popc(busy(q));
@@ -369,11 +369,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, 
     }
     before += __popc(m);
   }
-  for (int s = rank * PLAN_THREADS + tid; s < a.S; s += ctas * PLAN_THREADS) a.lens_to[s] = __ldg(a.lens + s);
+  for (int s = rank * PLAN_THREADS + tid; s < a.S; s += ctas * PLAN_THREADS) a.lens_to[s] = a.lens[s];
   if (ONE) __syncthreads();
   else cluster_sync();
   for (int q = q0 + lane; q < q1; q += 32) {
-    const int refs = __ldg(a.refs + q);
+    const int refs = a.refs[q];
     if (refs > 0 && q < all) {
       moved[q] = q;
       a.refs_to[q] = refs;
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(PagesDev a, 
   for (int i = rank * PLAN_THREADS + tid; i < moves; i += ctas * PLAN_THREADS) {
     const int src = __ldcg(&w.copies[i].x), dst = __ldcg(w.list + i);
     moved[src] = dst;
-    a.refs_to[dst] = __ldg(a.refs + src);
+    a.refs_to[dst] = a.refs[src];
   }
 }
 
@@ -518,11 +518,11 @@ __global__ void __launch_bounds__(COPY_THREADS) fork_kernel(PagesDev a, Ws w, co
     const int first = __ldcg(w.first + s);
     int page = -1;
     if (refused) {
-      page = __ldg(a.table + e);
+      page = a.table[e];
     } else if (i >= r.z && i < r.w) {
       page = __ldcg(w.list + first + i - r.z);
     } else if (i < r.y) {
-      page = __ldg(a.table + (int64_t)r.x * a.W + i);
+      page = a.table[(int64_t)r.x * a.W + i];
       if ((unsigned)page >= (unsigned)a.n_pages) atomicOr(status, FL_KV_BAD_PAGE);
     }
     a.table_to[e] = page;
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(COPY_THREADS) compact_kernel(PagesDev a, const
     int page = -1;
     bool bad = false;
     if (i < pages_of(a, len_of(a, s, &bad))) {
-      const int x = __ldg(a.table + e);
+      const int x = a.table[e];
       if ((unsigned)x < (unsigned)a.n_pages) page = __ldcg(moved + x);
       bad |= page < 0;
     }

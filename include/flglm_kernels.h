@@ -442,8 +442,9 @@ enum { FL_BEAM_BAD_LOGITS = 64, FL_BEAM_BAD_TRACE = 128 };
  * over) has token eos (0 without one) and parent -1, and in the trace itself as parent.
  * logits: dtype FL_DT_F32, FL_DT_BF16 or FL_DT_F16, rows ld elements apart (a multiple of 16 bytes, vocab or
  * more; what lies behind vocab is not used), 16-byte aligned.  Rows of beams that are not live are not used.  Sums are fp32,
- * scores are formed in 48 bits and rounded once; a candidate whose score is -inf in 32 bits is none.  A row's log-sum-exp depends
- * on the row alone: rows of equal logits have the same, to the bit, and a search's outcome does not depend on the others of the call.
+ * c is formed from them in 48 bits and rounded once, n^length_penalty is off by 2^-25 at most; a candidate whose score is -inf in 32 bits
+ * is none.  A row's log-sum-exp depends on the row and on eos alone: rows of equal logits have the same, to the bit, and a search's
+ * outcome does not depend on the others of the call.
  * workspace: fl_k_beam_workspace bytes, 16-byte aligned, of any content; calls one after another on a stream may share
  * it, of any searches for which it is large enough; calls that may overlap need one each. */
 size_t fl_k_beam_workspace(const fl_beam_search* search);

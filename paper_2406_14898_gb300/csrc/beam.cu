@@ -119,7 +119,8 @@ FL_DEV uint32_t order32(float x) {
 }
 
 // A number as the unevaluated sum of two floats, the first of which is the sum rounded (T. J. Dekker, A floating-point
-// technique for extending the available precision, 1971): 48 bits, for the scores that are compared and the penalty.  (The
+// technique for extending the available precision, 1971): 48 bits, for the scores that are compared and the penalty, whose series
+// are in one float from their small terms on.  (The
 // double-precision units of this card run at a small fraction of these' rate.)
 struct Two {
   float hi, lo;
@@ -147,7 +148,7 @@ FL_DEV uint64_t order64(Two x) {
   return fabsf(x.hi) < INFINITY ? (uint64_t)order32(x.hi) << 32 | order32(x.lo) : 0;
 }
 constexpr float LN2_HI = 0.693147182464599609375f, LN2_LO = -1.904654299958e-9f;  // ln 2 in two floats
-// ln x of a normal x, off by 2^-30 at most where |ln x| < 32: x = 2^e f, ln f = 2 (s + s^3 / 3 + s^5 / 5 + ...) with
+// ln x of a normal x, off by 2^-29 at most where |ln x| < 32: x = 2^e f, ln f = 2 (s + s^3 / 3 + s^5 / 5 + ...) with
 // s = (f - 1) / (f + 1), |s| <= 0.172; s in two floats, the series from s^3 on in one.
 FL_DEV Two log_two(float x) {
   int e = (int)(__float_as_uint(x) >> 23) - 127;
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(32 * FL_BEAM_MAX) beam_join_kernel(StepArgs a)
   const int B = a.p.beams, threads = blockDim.x, s = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int t = a.from.steps[s];  // (no read-only loads of the state: `to` may be the same memory)
   const bool active = a.from.done[s] == 0 && t >= 0 && t < a.p.max_steps;
-  float pool_score = -INFINITY;  // what had ended, for the last warp's work
+  float pool_score = -INFINITY;  // what had ended, for the first warp's work
   int pool_step = 0, pool_beam = 0;
   if (tid < B) {
     pool_score = a.from.end_scores[s * B + tid];

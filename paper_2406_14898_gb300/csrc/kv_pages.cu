@@ -402,7 +402,7 @@ FL_DEV int64_t shfl64(int64_t x, int lane) { return __shfl_sync(0xffffffffu, x, 
 // The copies, a warp a unit: from global memory into the warp's shared memory and from there to the new page, in
 // blocks of 8 KB by bulk copies that one lane asks for, two loads ahead of a store.  What a page holds of its sequence is
 // `runs` stretches of memory; each of its units has an equal part of their bytes, so that all are as long.
-// HBM is the bound: 71 pages of 27 MB moved in 26 caches 610 us (6.3 TB/s read and written, with the plan), the copies of a beam
+// HBM is the bound: 71 pages of 27 MB moved in 26 caches 616 us (6.3 TB/s read and written, with the plan), the copies of a beam
 // search's 64 sequences 100 us (5.9 TB/s).  16-byte loads and stores by all threads took 661 and 118.
 FL_DEV void copy_pages(const Caches& c, const Ws& w, int ps_log2, char* ring, uint64_t* full, int* status) {
   const int lane = threadIdx.x & 31, warps = gridDim.x * COPY_WARPS;
@@ -628,7 +628,10 @@ cudaError_t launch_plan(void (*kern)(KArgs...), int ctas, int smem, cudaStream_t
   return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
-// One CTA as long as what it goes through is short.
+// One CTA as long as what it goes through is short; tables of more entries take a cluster, whose barriers cost 5 us.  A whole call, one
+// CTA / a cluster, us: beams that all change, 16 x 64 entries 7.8 / 13.4, 16 x 512 11.5 / 13.3, 16 x 1024 15.8 / 14.0, 16 x 4096 38.6 /
+// 18.0, 64 x 1024 43.4 / 17.4; sequences that stay as they are, 192 x 71 8.5 / 11.1, 192 x 341 9.0 / 11.6, 64 x 1022 11.4 / 12.5, 1000 x 65
+// 12.8 / 19.2.  The host does not know which of the two a call is: the bound is for the second kind, a server's calls.
 bool small_plan(const PagesDev& a) { return a.n_pages <= 16384 && (int64_t)a.S * a.W <= 65536 && a.S <= PLAN_THREADS; }
 
 }  // namespace

@@ -437,7 +437,7 @@ class Generator:
             F.fl_k_beam_step(search, now, now, z, *trace, tokens, parents, workspace, status, ld=z.shape[2], **_stream())
             if t + 1 == count or bool(state["done"].all()):
                 break
-            wide._followed(tokens, parents, z, status)
+            wide._followed(tokens, parents, z)
         out = (torch.empty((n, beams, count), dtype=I32, device="cuda"), torch.empty((n, beams), dtype=I32, device="cuda"),
                torch.empty((n, beams), device="cuda"))
         F.fl_k_beam_trace(search, now, *trace, beams, 0, *out, status, **_stream())
@@ -464,7 +464,7 @@ class Generator:
             raise RuntimeError(f"generation: device status {bits} of the LM heads")
         return out
 
-    def _followed(self, tokens, parents, z, status):
+    def _followed(self, tokens, parents, z):
         """Logits z [clients, beams, row] after tokens [clients, beams] behind the sequences parents [clients, beams] (rows of the
         server's stack)."""
         beams = tokens.shape[1]
